@@ -373,6 +373,134 @@ adasum_status_t adasum_device_status(int64_t total_elems, int32_t num_tensors, i
                                      adasum_dtype_t dtype, uint32_t flags, const void* workspace,
                                      void* stream);
 
+/*
+ * ---- producing a worker's gradients in the fused buffer -----------------------------------------
+ *
+ * The calls below are the two ends of a worker's backward pass that the combine needs and that a plain
+ * matrix library does not give: the token embedding with its gradient, and activations kept in 8 bits
+ * with the gradients that are formed from them (the paper has no counterpart; Section 4.3 names memory
+ * as what limits the microbatch).  Gradients are written where the reduce reads them: a destination is
+ * a tensor's place inside a worker's fused buffer, aligned to its element size only, in fp32, fp16 or
+ * bf16, multiplied by `scale` (1 over the number of microbatches, or the scale that
+ * adasum_reduce_scaled divides out).  With accumulate != 0 the scaled gradient is added to what the
+ * destination holds (one rounding to its type per call) instead of replacing it.
+ *
+ * Conventions beyond those at the top of this file: matrices are row-major with contiguous rows; a
+ * stride is the distance between rows in ELEMENTS and at least the row's length; matrices are aligned
+ * to their element size (16-byte aligned rows select the vectorised paths); all arithmetic is fp32
+ * unless stated, with one rounding to the stored type; ADASUM_F64 is refused with ADASUM_ERR_DTYPE;
+ * a call with nothing to write returns ADASUM_OK without a launch; the library keeps no state between
+ * these calls.  They may be captured into a CUDA graph.
+ */
+
+/*
+ * Token embedding with scaling:  out[t] = scale * table[tokens[t]].
+ *
+ *   table         device, num_rows x dim of table_dtype, rows table_stride apart
+ *   tokens        device, num_tokens signed integers of token_bytes (4 or 8) bytes.  A token outside
+ *                 [0, num_rows) (padding) stands for a row of zeros
+ *   out           device, num_tokens x dim of out_dtype, rows out_stride apart
+ */
+adasum_status_t adasum_embedding_forward(const void* table, int64_t table_stride, int64_t num_rows,
+                                         int64_t dim, adasum_dtype_t table_dtype, const void* tokens,
+                                         int32_t token_bytes, int64_t num_tokens, float scale, void* out,
+                                         int64_t out_stride, adasum_dtype_t out_dtype, void* stream);
+
+/*
+ * Its gradient:  grad_table[v] = scale * sum of grad_out[t] over the tokens t with tokens[t] == v, for
+ * every row v (zeros where no token points; with accumulate, such rows are left alone).  The tokens
+ * are sorted (stably, by row) and a row's terms are added in the order of their positions, in fp32 and
+ * in a fixed association, so the result is deterministic.  Tokens outside [0, num_rows) add nothing.
+ *
+ *   grad_out      device, num_tokens x dim of `dtype`, rows grad_out_stride apart
+ *   grad_table    device, num_rows x dim of grad_dtype, contiguous
+ *   workspace     device, adasum_embedding_grad_workspace_bytes(...) bytes, 256-byte aligned; contents
+ *                 on entry are ignored
+ *   limits        num_tokens, num_rows < 2^31, dim <= 2^22 (ADASUM_ERR_ARG)
+ */
+size_t adasum_embedding_grad_workspace_bytes(int64_t num_tokens, int64_t num_rows, int64_t dim);
+adasum_status_t adasum_embedding_grad(const void* grad_out, int64_t grad_out_stride, adasum_dtype_t dtype,
+                                      const void* tokens, int32_t token_bytes, int64_t num_tokens,
+                                      float scale, void* grad_table, int64_t num_rows, int64_t dim,
+                                      adasum_dtype_t grad_dtype, int32_t accumulate, void* workspace,
+                                      size_t workspace_bytes, void* stream);
+
+/*
+ * Activations kept in 8 bits.  A checkpoint keeps a [rows, features] matrix x as one signed byte per
+ * value and one byte per group of 32 consecutive features of a row (the last group is filled up with
+ * zeros).  With E the binary exponent of a group's largest magnitude, the group's step is 2^(E - 6), at
+ * least 2^-126; a code is x / step rounded to the nearest integer, ties to even, limited to +-127; the
+ * value kept is code * step.  (This is the arithmetic of the OCP Microscaling format MXINT8.)  The
+ * error of a kept value is at most step / 2, and at most one step where the limit applies, with step
+ * at most 1/64 of the group's largest magnitude.  A group that holds an Inf or NaN is kept as NaN:
+ * step byte 255 and codes 0.
+ *
+ * Layout: with W = 32 * ceil(features / 32), first rows x W codes, row by row, then rows x W / 32 step
+ * bytes (exponent of the step + 127), row by row.  16-byte aligned.
+ *
+ * A kept value has at most 7 significant bits, so it is exact in fp32 and bf16, and in fp16 if x was
+ * fp16; the step is a power of two for that reason: the tensor cores multiply exactly the values kept.
+ */
+size_t adasum_checkpoint_bytes(int64_t rows, int64_t features);
+
+typedef enum {
+    ADASUM_ACT_NONE = 0,        /* y = x */
+    ADASUM_ACT_RELU = 1,        /* slope 0 at x <= 0 */
+    ADASUM_ACT_GELU = 2,        /* x Phi(x), Phi the normal distribution function */
+    ADASUM_ACT_GELU_TANH = 3,   /* x / 2 (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) */
+    ADASUM_ACT_SILU = 4         /* x / (1 + exp(-x)) */
+} adasum_activation_t;
+
+/*
+ * y = activation(x) (of x itself), and x into `checkpoint`, in one pass.
+ *   x, y          device, rows x features of `dtype`; y may be x itself (same stride), or NULL (only
+ *                 the checkpoint is written); otherwise they must not overlap
+ *   checkpoint    device, adasum_checkpoint_bytes(rows, features) bytes, 16-byte aligned
+ */
+adasum_status_t adasum_checkpoint_save(const void* x, int64_t x_stride, int64_t rows, int64_t features,
+                                       adasum_dtype_t dtype, adasum_activation_t activation, void* y,
+                                       int64_t y_stride, void* checkpoint, void* stream);
+
+/* The values kept, in `dtype` (exact in fp32 and bf16; fp16 rounds values beyond its range or precision). */
+adasum_status_t adasum_checkpoint_load(const void* checkpoint, int64_t rows, int64_t features, void* out,
+                                       int64_t out_stride, adasum_dtype_t dtype, void* stream);
+
+/*
+ * Gradient of an activation from the values kept:  grad_in = grad_out * activation'(kept x).
+ * Both gradients are rows x features of `dtype`; grad_in may be grad_out itself (same stride).
+ */
+adasum_status_t adasum_checkpoint_act_grad(const void* checkpoint, int64_t rows, int64_t features,
+                                           adasum_activation_t activation, const void* grad_out,
+                                           int64_t grad_out_stride, adasum_dtype_t dtype, void* grad_in,
+                                           int64_t grad_in_stride, void* stream);
+
+/*
+ * Gradients of a linear layer y = x w^T + b from the values kept of its input x:
+ *
+ *     grad_weight[n][k] = scale * sum_t grad_out[t][n] * (kept x)[t][k]
+ *     grad_bias[n]      = scale * sum_t grad_out[t][n]                       (if not NULL)
+ *
+ *   grad_out      device, rows x outputs of `dtype`, rows grad_out_stride apart
+ *   grad_weight   device, outputs x features of grad_dtype, contiguous
+ *   grad_bias     device, `outputs` elements of grad_dtype, or NULL
+ *   workspace     device, adasum_checkpoint_weight_grad_workspace_bytes(...) bytes, 256-byte aligned;
+ *                 contents on entry are ignored
+ *   limits        rows, features, outputs < 2^31 - 256 (ADASUM_ERR_ARG)
+ *
+ * Products are exact (fp16 and bf16 gradients multiply the kept values in their own type; fp32
+ * gradients go in as three bf16 terms that add up to them exactly, except bits below 2^-133); sums are
+ * fp32.  With rows == 0 the gradients are zeros.  fp16 gradients round kept values that fp16 cannot
+ * hold (possible only if x was saved from fp32 or bf16).
+ */
+size_t adasum_checkpoint_weight_grad_workspace_bytes(int64_t rows, int64_t features, int64_t outputs,
+                                                     adasum_dtype_t dtype);
+adasum_status_t adasum_checkpoint_weight_grad(const void* checkpoint, int64_t rows, int64_t features,
+                                              const void* grad_out, int64_t grad_out_stride,
+                                              int64_t outputs, adasum_dtype_t dtype, float scale,
+                                              void* grad_weight, void* grad_bias,
+                                              adasum_dtype_t grad_dtype, int32_t accumulate,
+                                              void* workspace, size_t workspace_bytes, void* stream);
+
 /* Static, human-readable name of a status code. */
 const char* adasum_status_string(adasum_status_t status);
 
@@ -399,6 +527,13 @@ const char* adasum_last_error(void);
 #define ADASUM_KERNEL_FUSED_SMALL 4   /* both passes in one cooperative launch (inputs that fit the L2) */
 #define ADASUM_KERNEL_WSUM_GRAM 5     /* second pass of `level` and first pass of level + 1 in one kernel */
 #define ADASUM_KERNEL_SHORT_TENSORS 6 /* the whole tree of the tensors of at most 64 elements, in fp64 */
+#define ADASUM_KERNEL_EMBEDDING 7        /* token lookup */
+#define ADASUM_KERNEL_EMBEDDING_SORT 8   /* tokens sorted by row, gradient table zeroed */
+#define ADASUM_KERNEL_EMBEDDING_SUM 9    /* sums over runs of equal tokens (level 0), sums joined over tiles (level 1) */
+#define ADASUM_KERNEL_CHECKPOINT_SAVE 10
+#define ADASUM_KERNEL_CHECKPOINT_LOAD 11
+#define ADASUM_KERNEL_ACT_GRAD 12
+#define ADASUM_KERNEL_WEIGHT_GRAD 13     /* level 0: gradients re-laid for the product, 1: the product, 2: sums joined */
 
 typedef struct {
     int32_t kernel;

@@ -360,7 +360,8 @@ class _LaunchRecord(ctypes.Structure):
 
 
 KERNEL_NAMES = {0: "gram_partial", 1: "tree_weights", 2: "weighted_sum", 3: "convert", 4: "fused_small",
-                5: "wsum_gram", 6: "short_tensors"}
+                5: "wsum_gram", 6: "short_tensors", 7: "embedding", 8: "embedding_sort", 9: "embedding_sum",
+                10: "checkpoint_save", 11: "checkpoint_load", 12: "act_grad", 13: "weight_grad"}
 
 _lib.adasum_profile_enable.restype = ctypes.c_int
 _lib.adasum_profile_enable.argtypes = [ctypes.c_int32]
@@ -408,3 +409,263 @@ def adasum_pair_noalloc(a, b, tensor_offsets=None, out=None, stream=None):
     if status != ADASUM_OK:
         raise AdasumError(status)
     return out
+
+
+# ---- producing a worker's gradients in the fused buffer ---------------------------------------------
+
+ADASUM_ACT = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+ADASUM_CHECKPOINT_GROUP = 32
+
+_i64, _i32, _vp, _f32 = ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_float
+_lib.adasum_embedding_forward.restype = ctypes.c_int
+_lib.adasum_embedding_forward.argtypes = [_vp, _i64, _i64, _i64, ctypes.c_int, _vp, _i32, _i64, _f32, _vp, _i64,
+                                          ctypes.c_int, _vp]
+_lib.adasum_embedding_grad_workspace_bytes.restype = ctypes.c_size_t
+_lib.adasum_embedding_grad_workspace_bytes.argtypes = [_i64, _i64, _i64]
+_lib.adasum_embedding_grad.restype = ctypes.c_int
+_lib.adasum_embedding_grad.argtypes = [_vp, _i64, ctypes.c_int, _vp, _i32, _i64, _f32, _vp, _i64, _i64, ctypes.c_int,
+                                       _i32, _vp, ctypes.c_size_t, _vp]
+_lib.adasum_checkpoint_bytes.restype = ctypes.c_size_t
+_lib.adasum_checkpoint_bytes.argtypes = [_i64, _i64]
+_lib.adasum_checkpoint_save.restype = ctypes.c_int
+_lib.adasum_checkpoint_save.argtypes = [_vp, _i64, _i64, _i64, ctypes.c_int, ctypes.c_int, _vp, _i64, _vp, _vp]
+_lib.adasum_checkpoint_load.restype = ctypes.c_int
+_lib.adasum_checkpoint_load.argtypes = [_vp, _i64, _i64, _vp, _i64, ctypes.c_int, _vp]
+_lib.adasum_checkpoint_act_grad.restype = ctypes.c_int
+_lib.adasum_checkpoint_act_grad.argtypes = [_vp, _i64, _i64, ctypes.c_int, _vp, _i64, ctypes.c_int, _vp, _i64, _vp]
+_lib.adasum_checkpoint_weight_grad_workspace_bytes.restype = ctypes.c_size_t
+_lib.adasum_checkpoint_weight_grad_workspace_bytes.argtypes = [_i64, _i64, _i64, ctypes.c_int]
+_lib.adasum_checkpoint_weight_grad.restype = ctypes.c_int
+_lib.adasum_checkpoint_weight_grad.argtypes = [_vp, _i64, _i64, _vp, _i64, _i64, ctypes.c_int, _f32, _vp, _vp,
+                                               ctypes.c_int, _i32, _vp, ctypes.c_size_t, _vp]
+
+
+def _matrix(name: str, t, rows=None, cols=None):
+    """Checks a CUDA matrix with contiguous rows; returns its row stride in elements."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA matrix")
+    shape = t.shape
+    if (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
+        raise ValueError(f"{name} is {tuple(shape)}, need ({rows}, {cols})")
+    row_stride, col_stride = t.stride()
+    if col_stride != 1 and shape[1] > 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return row_stride if shape[0] > 1 else max(row_stride, shape[1])
+
+
+def _operator_dtype(name: str, dtype) -> int:
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise TypeError(f"{name} is {dtype}: fp32, fp16 or bf16")
+    return code
+
+
+def _one_device(first, *others):
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError(f"tensors on {first.device} and {t.device}")
+
+
+def _operator_stream(first, stream):
+    """Stream handle for a call on the tensors' device: the given stream, or that device's current one."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(first.device.index)
+    return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _operator_call(first, function, *args):
+    """Calls `function` with the tensors' device current; raises on any status but ADASUM_OK."""
+    index = first.device.index
+    if index == torch.cuda.current_device():
+        status = function(*args)
+    else:
+        with torch.cuda.device(index):
+            status = function(*args)
+    if status != ADASUM_OK:
+        raise AdasumError(status)
+
+
+def _allocate(first, stream, shape, dtype):
+    """A tensor for a call on `stream`: the caching allocator must not hand it on before that stream is done."""
+    t = torch.empty(shape, dtype=dtype, device=first.device)
+    if stream is not None and t.numel() > 0:
+        if not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(int(stream), device=first.device)
+        # the memory may still be in use on the current stream, from which it was handed out
+        stream.wait_stream(torch.cuda.current_stream(first.device))
+        t.record_stream(stream)
+    return t
+
+
+def _operator_workspace(first, stream, workspace, need: int):
+    if workspace is None:
+        workspace = _allocate(first, stream, max(need, 256), torch.uint8)
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    else:
+        _one_device(first, workspace)
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def _tokens(tokens):
+    if tokens.dtype not in (torch.int32, torch.int64) or not tokens.is_cuda:
+        raise TypeError("tokens must be a CUDA tensor of int32 or int64")
+    if not tokens.is_contiguous():
+        raise ValueError("tokens must be contiguous")
+
+
+def adasum_embedding_forward(table, tokens, scale: float = 1.0, out=None, out_dtype=None, stream=None):
+    """``adasum_embedding_forward`` of the C ABI: ``scale * table[tokens]``, zeros for tokens outside the
+    table.  ``tokens`` has any shape; returns ``out`` of shape ``[tokens.numel(), dim]`` (of the table's
+    type unless ``out_dtype`` says otherwise)."""
+    table_stride = _matrix("table", table)
+    _tokens(tokens)
+    count = tokens.numel()
+    num_rows, dim = table.shape
+    if out is None:
+        out = _allocate(table, stream, (count, dim), out_dtype or table.dtype)
+    _one_device(table, tokens, out)
+    _operator_call(table, _lib.adasum_embedding_forward, table.data_ptr(), table_stride, num_rows, dim,
+                   _operator_dtype("table", table.dtype), tokens.data_ptr(), tokens.element_size(), count, scale,
+                   out.data_ptr(), _matrix("out", out, count, dim), _operator_dtype("out", out.dtype),
+                   _operator_stream(table, stream))
+    return out
+
+
+def adasum_embedding_grad_workspace_bytes(num_tokens: int, num_rows: int, dim: int) -> int:
+    return int(_lib.adasum_embedding_grad_workspace_bytes(int(num_tokens), int(num_rows), int(dim)))
+
+
+def adasum_embedding_grad(grad_out, tokens, num_rows=None, grad_table=None, grad_dtype=None, scale: float = 1.0,
+                          accumulate: bool = False, workspace=None, stream=None):
+    """``adasum_embedding_grad`` of the C ABI.  ``grad_out``: ``[tokens.numel(), dim]``.  The gradient goes
+    to ``grad_table`` (``[num_rows, dim]`` or flat, contiguous: a tensor's place in a fused buffer), which
+    is allocated here (fp32 unless ``grad_dtype`` says otherwise) if only ``num_rows`` is given."""
+    _tokens(tokens)
+    count = tokens.numel()
+    stride = _matrix("grad_out", grad_out, count)
+    dim = grad_out.shape[1]
+    if grad_table is None:
+        if num_rows is None or accumulate:
+            raise ValueError("grad_table is missing")
+        grad_table = _allocate(grad_out, stream, (num_rows, dim), grad_dtype or torch.float32)
+    if not grad_table.is_contiguous():
+        raise ValueError("grad_table must be contiguous")
+    if num_rows is None:
+        num_rows = grad_table.shape[0] if grad_table.dim() == 2 else grad_table.numel() // max(dim, 1)
+    if grad_table.numel() != num_rows * dim or (grad_table.dim() == 2 and grad_table.shape[1] != dim):
+        raise ValueError(f"grad_table is {tuple(grad_table.shape)}, need ({num_rows}, {dim})")
+    _one_device(grad_out, tokens, grad_table)
+    workspace, ws_bytes = _operator_workspace(
+        grad_out, stream, workspace, _lib.adasum_embedding_grad_workspace_bytes(count, num_rows, dim))
+    _operator_call(grad_out, _lib.adasum_embedding_grad, grad_out.data_ptr(), stride,
+                   _operator_dtype("grad_out", grad_out.dtype), tokens.data_ptr(), tokens.element_size(), count, scale,
+                   grad_table.data_ptr(), num_rows, dim, _operator_dtype("grad_table", grad_table.dtype),
+                   int(accumulate), workspace.data_ptr(), ws_bytes, _operator_stream(grad_out, stream))
+    return grad_table
+
+
+def adasum_checkpoint_bytes(rows: int, features: int) -> int:
+    return int(_lib.adasum_checkpoint_bytes(int(rows), int(features)))
+
+
+def _checkpoint(first, checkpoint, rows: int, features: int):
+    if checkpoint.dtype != torch.uint8 or not checkpoint.is_contiguous():
+        raise TypeError("checkpoint must be a contiguous tensor of uint8")
+    need = _lib.adasum_checkpoint_bytes(rows, features)
+    if checkpoint.numel() < need:
+        raise ValueError(f"checkpoint has {checkpoint.numel()} bytes, {rows} x {features} needs {need}")
+    _one_device(first, checkpoint)
+    return checkpoint.data_ptr()
+
+
+def adasum_checkpoint_save(x, activation: str = "none", out=None, checkpoint=None, want_out: bool = True, stream=None):
+    """``adasum_checkpoint_save`` of the C ABI: returns ``(activation(x), checkpoint)``; ``out`` may be ``x``
+    itself.  With ``want_out=False`` only the checkpoint is written and the first item is None."""
+    stride = _matrix("x", x)
+    rows, features = x.shape
+    if checkpoint is None:
+        checkpoint = _allocate(x, stream, _lib.adasum_checkpoint_bytes(rows, features), torch.uint8)
+    if out is None and want_out:
+        out = _allocate(x, stream, (rows, features), x.dtype)
+    if out is not None and out.dtype != x.dtype:
+        raise TypeError("out must have the type of x")
+    _one_device(x, out)
+    _operator_call(x, _lib.adasum_checkpoint_save, x.data_ptr(), stride, rows, features,
+                   _operator_dtype("x", x.dtype), ADASUM_ACT[activation], None if out is None else out.data_ptr(),
+                   0 if out is None else _matrix("out", out, rows, features),
+                   _checkpoint(x, checkpoint, rows, features), _operator_stream(x, stream))
+    return out, checkpoint
+
+
+def adasum_checkpoint_load(checkpoint, rows: int, features: int, dtype=None, out=None, stream=None):
+    """``adasum_checkpoint_load`` of the C ABI: the kept values, in ``dtype`` (fp32 by default) or ``out``."""
+    if out is None:
+        out = _allocate(checkpoint, stream, (rows, features), dtype or torch.float32)
+    _operator_call(checkpoint, _lib.adasum_checkpoint_load, _checkpoint(out, checkpoint, rows, features), rows,
+                   features, out.data_ptr(), _matrix("out", out, rows, features), _operator_dtype("out", out.dtype),
+                   _operator_stream(checkpoint, stream))
+    return out
+
+
+def adasum_checkpoint_act_grad(checkpoint, grad_out, activation: str, grad_in=None, stream=None):
+    """``adasum_checkpoint_act_grad`` of the C ABI: ``grad_out * activation'(kept x)``; ``grad_in`` may be
+    ``grad_out`` itself."""
+    stride = _matrix("grad_out", grad_out)
+    rows, features = grad_out.shape
+    if grad_in is None:
+        grad_in = _allocate(grad_out, stream, (rows, features), grad_out.dtype)
+    elif grad_in.dtype != grad_out.dtype:
+        raise TypeError("grad_in must have the type of grad_out")
+    _one_device(grad_out, grad_in)
+    _operator_call(grad_out, _lib.adasum_checkpoint_act_grad, _checkpoint(grad_out, checkpoint, rows, features), rows,
+                   features, ADASUM_ACT[activation], grad_out.data_ptr(), stride,
+                   _operator_dtype("grad_out", grad_out.dtype), grad_in.data_ptr(),
+                   _matrix("grad_in", grad_in, rows, features), _operator_stream(grad_out, stream))
+    return grad_in
+
+
+def adasum_checkpoint_weight_grad_workspace_bytes(rows: int, features: int, outputs: int, dtype) -> int:
+    return int(_lib.adasum_checkpoint_weight_grad_workspace_bytes(int(rows), int(features), int(outputs),
+                                                                  _dtype_code(dtype)))
+
+
+def adasum_checkpoint_weight_grad(checkpoint, grad_out, features=None, grad_weight=None, grad_bias=None,
+                                  want_bias: bool = False, grad_dtype=None, scale: float = 1.0,
+                                  accumulate: bool = False, workspace=None, stream=None):
+    """``adasum_checkpoint_weight_grad`` of the C ABI.  ``grad_out``: ``[rows, outputs]``.  The gradients go to
+    ``grad_weight`` (``[outputs, features]`` or flat) and ``grad_bias`` (``[outputs]``), both contiguous;
+    what is not given is allocated here (fp32 unless ``grad_dtype`` says otherwise; a bias gradient only
+    with ``want_bias``).  Returns ``(grad_weight, grad_bias)``."""
+    stride = _matrix("grad_out", grad_out)
+    rows, outputs = grad_out.shape
+    if grad_weight is None:
+        if features is None or accumulate:
+            raise ValueError("grad_weight is missing")
+        grad_weight = _allocate(grad_out, stream, (outputs, features), grad_dtype or torch.float32)
+    if features is None:
+        features = grad_weight.shape[1] if grad_weight.dim() == 2 else grad_weight.numel() // max(outputs, 1)
+    if not grad_weight.is_contiguous():
+        raise ValueError("grad_weight must be contiguous")
+    if grad_weight.numel() != outputs * features or (grad_weight.dim() == 2 and grad_weight.shape[1] != features):
+        raise ValueError(f"grad_weight is {tuple(grad_weight.shape)}, need ({outputs}, {features})")
+    if grad_bias is None and want_bias:
+        if accumulate:
+            raise ValueError("grad_bias is missing")
+        grad_bias = _allocate(grad_out, stream, (outputs,), grad_weight.dtype)
+    if grad_bias is not None:
+        if grad_bias.dtype != grad_weight.dtype:
+            raise TypeError("grad_bias must have the type of grad_weight")
+        if not grad_bias.is_contiguous() or grad_bias.numel() != outputs:
+            raise ValueError(f"grad_bias must be contiguous and have {outputs} elements")
+    _one_device(grad_out, grad_weight, grad_bias)
+    code = _operator_dtype("grad_out", grad_out.dtype)
+    workspace, ws_bytes = _operator_workspace(
+        grad_out, stream, workspace,
+        _lib.adasum_checkpoint_weight_grad_workspace_bytes(rows, features, outputs, code))
+    _operator_call(grad_out, _lib.adasum_checkpoint_weight_grad, _checkpoint(grad_out, checkpoint, rows, features),
+                   rows, features, grad_out.data_ptr(), stride, outputs, code, scale, grad_weight.data_ptr(),
+                   None if grad_bias is None else grad_bias.data_ptr(),
+                   _operator_dtype("grad_weight", grad_weight.dtype), int(accumulate), workspace.data_ptr(), ws_bytes,
+                   _operator_stream(grad_out, stream))
+    return grad_weight, grad_bias

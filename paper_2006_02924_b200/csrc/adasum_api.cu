@@ -29,6 +29,8 @@ adasum_status_t fail(adasum_status_t status, const char* fmt, ...)
     return status;
 }
 
+void clear_error() { g_error[0] = '\0'; }
+
 namespace {
 
 // ---- optional per-launch timing ---------------------------------------------------------------

@@ -1,0 +1,592 @@
+// Token embedding with scaling, and its gradient by sorted tokens.
+//
+// The gradient of row v is a sum over the tokens that point at v.  Three launches:
+//
+//   embedding_sort_kernel  the first cluster of blocks sorts (row, position) pairs, stably, by row; all
+//                          other blocks write zeros into the whole gradient table meanwhile (the table
+//                          of a large vocabulary is the larger part of the traffic, and most of its rows
+//                          have no token)
+//   embedding_sum_kernel   cuts the sorted list into tiles of equal length, whatever the rows' counts
+//                          are; a block walks its tile once, a row's terms in registers, and writes rows
+//                          that lie inside the tile; the sums of the rows that cross the tile's ends
+//                          go to the workspace
+//   embedding_join_kernel  adds those, tile by tile in order, and writes the rows
+//
+// Every sum has a fixed association, so results are deterministic without atomics.
+#include <cooperative_groups.h>
+
+#include "adasum_operators.cuh"
+
+namespace adasum {
+namespace {
+
+namespace cg = cooperative_groups;
+
+// ---- lookup ------------------------------------------------------------------------------------------
+
+template <typename Id>
+__device__ __forceinline__ int64_t token_row(const Id* tokens, int64_t t, int64_t num_rows)
+{
+    const int64_t id = (int64_t)tokens[t];
+    return id >= 0 && id < num_rows ? id : -1;
+}
+
+constexpr int kLookupBlock = 128;
+constexpr int kLookupVectors = 4;
+
+// One thread: kLookupVectors vectors of eight elements of the output.
+template <typename T, typename Id>
+__global__ void __launch_bounds__(kLookupBlock)
+embedding_forward_kernel(const T* table, int64_t table_stride, bool table_vec, int64_t num_rows, int64_t dim,
+                         const Id* tokens, float scale, void* out, int out_dtype, int64_t out_stride, bool out_vec,
+                         RowDivider divider, uint64_t vectors)
+{
+    const uint64_t first = (uint64_t)blockIdx.x * (kLookupBlock * kLookupVectors) + threadIdx.x;
+    float v[kLookupVectors][8];
+    int64_t token[kLookupVectors], row[kLookupVectors];
+    int count[kLookupVectors];
+    uint32_t at[kLookupVectors];
+#pragma unroll
+    for (int u = 0; u < kLookupVectors; ++u) {
+        const uint64_t n = first + u * kLookupBlock;
+        uint64_t t;
+        divide_row(divider, n, t, at[u]);
+        token[u] = (int64_t)t;
+        count[u] = n < vectors ? (int)min((int64_t)8, dim - (int64_t)at[u] * 8) : 0;
+        row[u] = count[u] > 0 ? token_row(tokens, token[u], num_rows) : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < kLookupVectors; ++u)
+        load_up_to_eight(table + row[u] * table_stride + (int64_t)at[u] * 8, table_vec, row[u] >= 0 ? count[u] : 0, v[u]);
+#pragma unroll
+    for (int u = 0; u < kLookupVectors; ++u) {
+        if (count[u] <= 0)
+            continue;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[u][i] = row[u] >= 0 ? v[u][i] * scale : 0.0f;
+        const int64_t e = token[u] * out_stride + (int64_t)at[u] * 8;
+        if (out_vec && count[u] == 8) {
+            store_vector_from_float<8>(out, out_dtype, e, v[u]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < count[u])
+                    store_from_float(out, out_dtype, e + i, v[u][i]);
+        }
+    }
+}
+
+// ---- sorting the tokens by row ---------------------------------------------------------------------------
+
+constexpr int kSortCluster = 8;
+constexpr int kSortThreads = 1024;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kDigits = 256;
+
+// Table rows [0, num_rows) are the keys; tokens outside get the key num_rows and end up last.
+// A stable radix sort, one byte per pass, least significant first.  Every warp of the cluster owns a
+// contiguous run of the list, so "stable" is: by digit, then block, then warp, then place in the run.
+template <typename Id>
+__device__ void sort_tokens(const Id* tokens, uint32_t n, uint32_t num_rows, int passes, uint2* a, uint2* b)
+{
+    cg::cluster_group cluster = cg::this_cluster();
+    __shared__ uint32_t next[kSortWarps][kDigits];      // per warp: count of a digit, then its next place
+    __shared__ uint32_t block_count[kDigits];
+    __shared__ uint32_t warp_sum[kDigits / 32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster.block_rank();
+    const uint32_t warps = kSortCluster * kSortWarps;
+    const uint32_t run = ((n + warps - 1) / warps + 31) / 32 * 32;        // whole rounds of 32
+    const uint64_t begin64 = (uint64_t)(rank * kSortWarps + warp) * run;
+    const uint32_t begin = begin64 < n ? (uint32_t)begin64 : n;
+    const uint32_t end = n - begin < run ? n : begin + run;
+
+    for (int pass = 0; pass < passes; ++pass) {
+        const uint2* src = (passes - pass) & 1 ? b : a;      // pass 0 reads the tokens themselves
+        uint2* dst = (passes - 1 - pass) & 1 ? b : a;        // the last pass writes a
+        const int shift = 8 * pass;
+        auto item = [&](uint32_t i) -> uint2 {
+            if (pass == 0) {
+                const int64_t id = (int64_t)tokens[i];
+                return make_uint2(id >= 0 && id < (int64_t)num_rows ? (uint32_t)id : num_rows, i);
+            }
+            return __ldcg(src + i);
+        };
+        for (int d = lane; d < kDigits; d += 32)
+            next[warp][d] = 0;
+        __syncwarp();
+        for (uint32_t i0 = begin; i0 < end; i0 += 32) {
+            const uint32_t i = i0 + lane;
+            const bool mine = i < end;
+            const uint32_t digit = mine ? (item(i).x >> shift) & (kDigits - 1) : kDigits;
+            const uint32_t same = __match_any_sync(0xffffffffu, digit);
+            if (mine && lane == __ffs(same) - 1)
+                next[warp][digit] += __popc(same);
+            __syncwarp();
+        }
+        __syncthreads();
+        // counts -> places within the block's share of each digit
+        uint32_t total = 0;
+        if (threadIdx.x < kDigits) {
+            for (int w = 0; w < kSortWarps; ++w) {
+                const uint32_t c = next[w][threadIdx.x];
+                next[w][threadIdx.x] = total;
+                total += c;
+            }
+            block_count[threadIdx.x] = total;
+        }
+        cluster.sync();
+        // where the digit starts: all smaller digits, then the same digit in the blocks before this one
+        uint32_t before = 0, everywhere = 0;
+        if (threadIdx.x < kDigits) {
+            for (uint32_t r = 0; r < kSortCluster; ++r) {
+                const uint32_t c = cluster.map_shared_rank(block_count, r)[threadIdx.x];
+                before += r < rank ? c : 0;
+                everywhere += c;
+            }
+        }
+        uint32_t scan = everywhere;                      // inclusive over the warp's 32 digits
+        for (int step = 1; step < 32; step *= 2) {
+            const uint32_t other = __shfl_up_sync(0xffffffffu, scan, step);
+            scan += lane >= step ? other : 0;
+        }
+        if (threadIdx.x < kDigits && lane == 31)
+            warp_sum[warp] = scan;
+        __syncthreads();
+        if (threadIdx.x < kDigits) {
+            uint32_t start = scan - everywhere + before;
+            for (int w = 0; w < warp; ++w)
+                start += warp_sum[w];
+            for (int w = 0; w < kSortWarps; ++w)
+                next[w][threadIdx.x] += start;
+        }
+        __syncthreads();
+        for (uint32_t i0 = begin; i0 < end; i0 += 32) {
+            const uint32_t i = i0 + lane;
+            const bool mine = i < end;
+            const uint2 it = mine ? item(i) : make_uint2(0, 0);
+            const uint32_t digit = mine ? (it.x >> shift) & (kDigits - 1) : kDigits;
+            const uint32_t same = __match_any_sync(0xffffffffu, digit);
+            uint32_t place = 0;
+            if (mine)
+                place = next[warp][digit] + __popc(same & ((1u << lane) - 1));
+            __syncwarp();
+            if (mine && lane == __ffs(same) - 1)
+                next[warp][digit] += __popc(same);
+            __syncwarp();
+            if (mine)
+                dst[place] = it;
+        }
+        cluster.sync();      // the pass's list is complete, and every block has read the counts
+    }
+}
+
+// Blocks beyond the first cluster: zeros over `bytes` bytes at p (any alignment of 2), in 16-byte stores.
+__device__ void write_zeros(char* p, int64_t bytes, int64_t worker, int64_t workers)
+{
+    const int64_t head = min(bytes, (int64_t)((16 - (uintptr_t)p % 16) % 16));
+    const int64_t vectors = (bytes - head) / 16, tail = bytes - head - vectors * 16;
+    uint4* body = reinterpret_cast<uint4*>(p + head);
+    const int64_t thread = worker * blockDim.x + threadIdx.x, threads = workers * blockDim.x;
+    for (int64_t i = thread; i < vectors; i += threads)
+        body[i] = make_uint4(0, 0, 0, 0);
+    if (thread < head / 2)
+        reinterpret_cast<uint16_t*>(p)[thread] = 0;
+    if (thread < tail / 2)
+        reinterpret_cast<uint16_t*>(p + bytes - tail)[thread] = 0;
+}
+
+// Block roles by cluster: cluster 0 sorts, the others write zeros.
+template <typename Id>
+__global__ void __cluster_dims__(kSortCluster, 1, 1) __launch_bounds__(kSortThreads, 1)
+embedding_sort_kernel(const Id* tokens, uint32_t n, uint32_t num_rows, int passes, uint2* sorted, uint2* spare,
+                      char* table, int64_t table_bytes)
+{
+    if (blockIdx.x < kSortCluster) {
+        if (n > 0)
+            sort_tokens(tokens, n, num_rows, passes, sorted, spare);
+    } else {
+        write_zeros(table, table_bytes, (int64_t)blockIdx.x - kSortCluster, (int64_t)gridDim.x - kSortCluster);
+    }
+}
+
+// ---- sums ------------------------------------------------------------------------------------------------
+
+constexpr int kSumThreads = 128;
+constexpr int kMaxTile = 64;
+constexpr int kInFlight = 8;            // terms whose loads are issued together
+
+struct SumArgs {
+    const uint2* sorted;
+    uint32_t n, num_rows;
+    int tile;                // entries per tile
+    int64_t stride, dim;
+    float scale;
+    void* table;
+    int table_dtype;
+    bool table_vec, accumulate;
+    float* edges;            // [tile][0: the run that enters from before, 1: the run that goes on][dim]
+};
+
+// VE consecutive elements starting at column `column` of row `row` of the table.
+template <int VE>
+__device__ __forceinline__ void write_row(const SumArgs& a, uint32_t row, int64_t column, const float (&sum)[VE])
+{
+    const int64_t e = (int64_t)row * a.dim + column;
+    float y[VE];
+#pragma unroll
+    for (int i = 0; i < VE; ++i)
+        y[i] = sum[i] * a.scale;
+    if constexpr (VE > 1) {
+        if (a.table_vec) {
+            if (a.accumulate)
+                add_vector_as_float<VE>(a.table, a.table_dtype, e, y);
+            store_vector_from_float<VE>(a.table, a.table_dtype, e, y);
+            return;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < VE; ++i) {
+        if (a.accumulate)
+            y[i] += load_as_float(a.table, a.table_dtype, e + i);
+        store_from_float(a.table, a.table_dtype, e + i, y[i]);
+    }
+}
+
+// VE: elements a thread owns; more than one only where a row divides into vectors that are 16-byte
+// aligned in grad_out.  grid.x = tiles, grid.y = blocks per row of kSumThreads * VE columns.
+template <typename T, int VE>
+__global__ void __launch_bounds__(kSumThreads)
+embedding_sum_kernel(SumArgs a, const T* __restrict__ grad)
+{
+    __shared__ uint32_t row[kMaxTile + 2], position[kMaxTile];       // row[0] and row[m + 1]: the neighbours
+    constexpr uint32_t kNone = 0xffffffffu;
+    const uint32_t begin = blockIdx.x * (uint32_t)a.tile;
+    const int m = (int)min((uint32_t)a.tile, a.n - begin);
+    for (int i = threadIdx.x; i < m + 2; i += kSumThreads) {
+        const int64_t at = (int64_t)begin + i - 1;
+        const uint2 it = at >= 0 && at < (int64_t)a.n ? a.sorted[at] : make_uint2(kNone, 0);
+        row[i] = it.x;
+        if (i >= 1 && i <= m)
+            position[i - 1] = it.y;
+    }
+    __syncthreads();
+    for (int64_t column = ((int64_t)blockIdx.y * kSumThreads + threadIdx.x) * VE; column < a.dim;
+         column += (int64_t)gridDim.y * kSumThreads * VE) {
+        float sum[VE];
+#pragma unroll
+        for (int i = 0; i < VE; ++i)
+            sum[i] = 0.0f;
+        int start = 0;                  // where the current run starts in the tile
+        auto flush = [&](int end) {
+            const uint32_t r = row[1 + start];
+            if (r < a.num_rows) {
+                const bool enters = start == 0 && row[0] == r, goes_on = end == m && row[m + 1] == r;
+                if (!enters && !goes_on) {
+                    write_row<VE>(a, r, column, sum);
+                } else {
+                    float* edge = a.edges + ((int64_t)blockIdx.x * 2 + (enters ? 0 : 1)) * a.dim + column;
+#pragma unroll
+                    for (int i = 0; i < VE; ++i)
+                        edge[i] = sum[i];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < VE; ++i)
+                sum[i] = 0.0f;
+            start = end;
+        };
+        for (int i0 = 0; i0 < m; i0 += kInFlight) {
+            float x[kInFlight][VE];
+#pragma unroll
+            for (int u = 0; u < kInFlight; ++u) {
+                if (i0 + u < m) {
+                    const T* p = grad + (int64_t)position[i0 + u] * a.stride + column;
+                    if constexpr (VE > 1)
+                        Element<T>::vec(p, x[u]);
+                    else
+                        x[u][0] = Element<T>::one(p);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kInFlight; ++u) {
+                if (i0 + u < m) {
+                    if (i0 + u > start && row[1 + i0 + u] != row[1 + start])
+                        flush(i0 + u);
+#pragma unroll
+                    for (int i = 0; i < VE; ++i)
+                        sum[i] += x[u][i];
+                }
+            }
+        }
+        flush(m);
+    }
+}
+
+// Rows that cross tiles: the tile in which the run starts owns the row.  grid.x = tiles (but the last),
+// grid.y = blocks per row of 32 columns; warp w adds every eighth part of the run's edges, and the warps'
+// sums are added in order.
+constexpr int kJoinThreads = 256;
+constexpr int kJoinWarps = kJoinThreads / 32;
+
+__global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(SumArgs a)
+{
+    __shared__ float part[kJoinWarps][32];
+    const uint32_t tile = blockIdx.x, tiles = (a.n + a.tile - 1) / a.tile;
+    const uint32_t begin = tile * (uint32_t)a.tile, next = begin + a.tile;      // next < n: not the last tile
+    const uint32_t r = a.sorted[next - 1].x;
+    if (r >= a.num_rows || a.sorted[next].x != r)
+        return;                                         // nothing goes on into the next tile
+    if (begin > 0 && a.sorted[begin - 1].x == r)
+        return;                                         // the run started before this tile: not the owner
+    // last tile of the run: the sorted rows ascend, so count the following tiles that begin with r
+    uint32_t count = 0;
+    for (;;) {
+        const uint64_t probe = (uint64_t)tile + 1 + count + threadIdx.x;
+        const bool inside = probe < tiles && a.sorted[probe * a.tile].x == r;
+        const uint32_t hits = __syncthreads_count(inside);
+        count += hits;
+        if (hits < kJoinThreads)
+            break;
+    }
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t edges = count + 1;                   // this tile's second edge, then `count` first edges
+    const uint32_t share = (edges + kJoinWarps - 1) / kJoinWarps;
+    for (int64_t column0 = (int64_t)blockIdx.y * 32; column0 < a.dim; column0 += (int64_t)gridDim.y * 32) {
+        const int64_t column = column0 + lane;
+        float sum = 0.0f;
+        if (column < a.dim) {
+            const uint32_t from = warp * share, to = min(edges, from + share);
+#pragma unroll 8
+            for (uint32_t k = from; k < to; ++k)
+                sum += a.edges[((int64_t)(tile + k) * 2 + (k == 0 ? 1 : 0)) * a.dim + column];
+        }
+        part[warp][lane] = sum;
+        __syncthreads();
+        if (warp == 0 && column < a.dim) {
+            float total[1] = {part[0][lane]};
+            for (int w = 1; w < kJoinWarps; ++w)
+                total[0] += part[w][lane];
+            write_row<1>(a, r, column, total);
+        }
+        __syncthreads();
+    }
+}
+
+// ---- host ------------------------------------------------------------------------------------------------
+
+// Entries per tile.
+int sum_tile(int64_t n) { return n < 16384 ? 32 : kMaxTile; }
+
+struct GradLayout {
+    size_t sorted, spare, edges, total;
+};
+GradLayout grad_layout(int64_t n, int64_t dim)
+{
+    auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    const size_t list = up((size_t)n * sizeof(uint2));
+    const int64_t tiles = (n + sum_tile(n) - 1) / sum_tile(n);
+    GradLayout l;
+    l.sorted = 0;
+    l.spare = list;
+    l.edges = 2 * list;
+    l.total = l.edges + up((size_t)tiles * 2 * (size_t)dim * sizeof(float));
+    if (l.total == 0)
+        l.total = 256;
+    return l;
+}
+
+constexpr int64_t kMaxDim = int64_t(1) << 22;
+
+adasum_status_t check_tokens(const void* tokens, int32_t token_bytes, int64_t num_tokens, int64_t num_rows,
+                             int64_t dim)
+{
+    if (!extent_ok(num_tokens) || !extent_ok(num_rows) || dim < 0 || dim > kMaxDim)
+        return fail(ADASUM_ERR_ARG, "num_tokens = %lld, num_rows = %lld, dim = %lld out of range",
+                    (long long)num_tokens, (long long)num_rows, (long long)dim);
+    if (token_bytes != 4 && token_bytes != 8)
+        return fail(ADASUM_ERR_ARG, "token_bytes = %d is neither 4 nor 8", (int)token_bytes);
+    if (num_tokens > 0 && !tokens)
+        return fail(ADASUM_ERR_NULL, "tokens is NULL");
+    if (!aligned_to(tokens, token_bytes))
+        return fail(ADASUM_ERR_ARG, "tokens is not aligned to its element size");
+    return ADASUM_OK;
+}
+
+template <typename F>
+void with_type(adasum_dtype_t dtype, F&& f)
+{
+    if (dtype == ADASUM_F32)
+        f(float{});
+    else if (dtype == ADASUM_F16)
+        f(__half{});
+    else
+        f(__nv_bfloat16{});
+}
+
+}  // namespace
+}  // namespace adasum
+
+extern "C" {
+
+adasum_status_t adasum_embedding_forward(const void* table, int64_t table_stride, int64_t num_rows, int64_t dim,
+                                         adasum_dtype_t table_dtype, const void* tokens, int32_t token_bytes,
+                                         int64_t num_tokens, float scale, void* out, int64_t out_stride,
+                                         adasum_dtype_t out_dtype, void* stream_ptr)
+{
+    using namespace adasum;
+    clear_error();
+    if (!operator_dtype(table_dtype) || !operator_dtype(out_dtype))
+        return fail(ADASUM_ERR_DTYPE, "dtypes %d, %d: fp32, fp16 or bf16", (int)table_dtype, (int)out_dtype);
+    const adasum_status_t status = check_tokens(tokens, token_bytes, num_tokens, num_rows, dim);
+    if (status != ADASUM_OK || num_tokens == 0 || dim == 0)
+        return status;
+    if ((num_rows > 0 && !table) || !out)
+        return fail(ADASUM_ERR_NULL, "table or out is NULL");
+    if (!aligned_to(table, operator_bytes(table_dtype)) || !aligned_to(out, operator_bytes(out_dtype)))
+        return fail(ADASUM_ERR_ARG, "table or out is not aligned to its element size");
+    if (!stride_ok(table_stride, dim) || !stride_ok(out_stride, dim))
+        return fail(ADASUM_ERR_ARG, "a stride is shorter than a row or out of range");
+    const size_t table_bytes = matrix_span(num_rows, dim, table_stride, operator_bytes(table_dtype));
+    const size_t out_bytes = matrix_span(num_tokens, dim, out_stride, operator_bytes(out_dtype));
+    if (spans_overlap(out, out_bytes, table, table_bytes) ||
+        spans_overlap(out, out_bytes, tokens, (size_t)num_tokens * token_bytes))
+        return fail(ADASUM_ERR_ARG, "out overlaps table or tokens");
+    // at least two vectors per row for the divider: a row of up to eight elements gets an empty one
+    const int64_t per_row = dim <= 8 ? 2 : (dim + 7) / 8;
+    const uint64_t vectors = (uint64_t)num_tokens * (uint64_t)per_row;
+    const uint64_t blocks = (vectors + kLookupBlock * kLookupVectors - 1) / (kLookupBlock * kLookupVectors);
+    if (blocks > 0x7fffffffu)
+        return fail(ADASUM_ERR_ARG, "%lld x %lld is too large", (long long)num_tokens, (long long)dim);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+    profile_mark(stream, -1, 0, 0, true);
+    with_type(table_dtype, [&](auto t) {
+        using T = decltype(t);
+        const T* rows = static_cast<const T*>(table);
+        const bool table_vec = rows_aligned(table, table_stride, sizeof(T));
+        const bool out_vec = rows_aligned(out, out_stride, operator_bytes(out_dtype));
+        if (token_bytes == 4)
+            embedding_forward_kernel<T, int32_t><<<(unsigned)blocks, kLookupBlock, 0, stream>>>(
+                rows, table_stride, table_vec, num_rows, dim, static_cast<const int32_t*>(tokens), scale, out,
+                (int)out_dtype, out_stride, out_vec, row_divider(per_row), vectors);
+        else
+            embedding_forward_kernel<T, int64_t><<<(unsigned)blocks, kLookupBlock, 0, stream>>>(
+                rows, table_stride, table_vec, num_rows, dim, static_cast<const int64_t*>(tokens), scale, out,
+                (int)out_dtype, out_stride, out_vec, row_divider(per_row), vectors);
+    });
+    ADASUM_CUDA_CHECK(cudaGetLastError());
+    profile_mark(stream, ADASUM_KERNEL_EMBEDDING, 0, 0, false);
+    return ADASUM_OK;
+}
+
+size_t adasum_embedding_grad_workspace_bytes(int64_t num_tokens, int64_t num_rows, int64_t dim)
+{
+    using namespace adasum;
+    if (!extent_ok(num_tokens) || !extent_ok(num_rows) || dim < 0 || dim > kMaxDim)
+        return 0;
+    return grad_layout(num_tokens, dim).total;
+}
+
+adasum_status_t adasum_embedding_grad(const void* grad_out, int64_t grad_out_stride, adasum_dtype_t dtype,
+                                      const void* tokens, int32_t token_bytes, int64_t num_tokens, float scale,
+                                      void* grad_table, int64_t num_rows, int64_t dim, adasum_dtype_t grad_dtype,
+                                      int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream_ptr)
+{
+    using namespace adasum;
+    clear_error();
+    if (!operator_dtype(dtype) || !operator_dtype(grad_dtype))
+        return fail(ADASUM_ERR_DTYPE, "dtypes %d, %d: fp32, fp16 or bf16", (int)dtype, (int)grad_dtype);
+    const adasum_status_t status = check_tokens(tokens, token_bytes, num_tokens, num_rows, dim);
+    if (status != ADASUM_OK || num_rows == 0 || dim == 0 || (num_tokens == 0 && accumulate))
+        return status;
+    if (!grad_table || (num_tokens > 0 && !grad_out))
+        return fail(ADASUM_ERR_NULL, "grad_out or grad_table is NULL");
+    if (!aligned_to(grad_out, operator_bytes(dtype)) || !aligned_to(grad_table, operator_bytes(grad_dtype)))
+        return fail(ADASUM_ERR_ARG, "grad_out or grad_table is not aligned to its element size");
+    if (num_tokens > 0 && !stride_ok(grad_out_stride, dim))
+        return fail(ADASUM_ERR_ARG, "grad_out_stride %lld is shorter than a row or out of range",
+                    (long long)grad_out_stride);
+    const GradLayout lay = grad_layout(num_tokens, dim);
+    if (!workspace || workspace_bytes < lay.total)
+        return fail(ADASUM_ERR_WORKSPACE, "workspace of %zu bytes, need %zu", workspace ? workspace_bytes : (size_t)0,
+                    lay.total);
+    if (!aligned_to(workspace, 256))
+        return fail(ADASUM_ERR_ARG, "workspace is not 256-byte aligned");
+    const size_t in_bytes = matrix_span(num_tokens, dim, grad_out_stride, operator_bytes(dtype));
+    const size_t token_span = (size_t)num_tokens * (size_t)token_bytes;
+    const int64_t table_bytes = num_rows * dim * operator_bytes(grad_dtype);
+    if (spans_overlap(grad_table, (size_t)table_bytes, grad_out, in_bytes) ||
+        spans_overlap(grad_table, (size_t)table_bytes, tokens, token_span))
+        return fail(ADASUM_ERR_ARG, "grad_table overlaps grad_out or tokens");
+    if (spans_overlap(workspace, lay.total, grad_out, in_bytes) || spans_overlap(workspace, lay.total, tokens, token_span) ||
+        spans_overlap(workspace, lay.total, grad_table, (size_t)table_bytes))
+        return fail(ADASUM_ERR_ARG, "workspace overlaps another buffer");
+    const int sms = device_sms();
+    if (sms <= 0)
+        return fail(ADASUM_ERR_CUDA, "no current device");
+
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+    char* ws = static_cast<char*>(workspace);
+    uint2* sorted = reinterpret_cast<uint2*>(ws + lay.sorted);
+    uint2* spare = reinterpret_cast<uint2*>(ws + lay.spare);
+    int passes = 1;
+    while (passes < 4 && ((uint64_t)num_rows >> (8 * passes)) != 0)     // the key num_rows itself included
+        ++passes;
+    const int64_t zero_bytes = accumulate ? 0 : table_bytes;
+    int64_t fill = (zero_bytes + kSortThreads * 16 * 4 - 1) / (kSortThreads * 16 * 4);
+    fill = (fill + kSortCluster - 1) / kSortCluster * kSortCluster;
+    const int64_t most = (int64_t)sms / kSortCluster * kSortCluster;
+    const unsigned blocks = (unsigned)(kSortCluster + (fill < most ? fill : most));
+    profile_mark(stream, -1, 0, 0, true);
+    if (token_bytes == 4)
+        embedding_sort_kernel<int32_t><<<blocks, kSortThreads, 0, stream>>>(
+            static_cast<const int32_t*>(tokens), (uint32_t)num_tokens, (uint32_t)num_rows, passes, sorted, spare,
+            static_cast<char*>(grad_table), zero_bytes);
+    else
+        embedding_sort_kernel<int64_t><<<blocks, kSortThreads, 0, stream>>>(
+            static_cast<const int64_t*>(tokens), (uint32_t)num_tokens, (uint32_t)num_rows, passes, sorted, spare,
+            static_cast<char*>(grad_table), zero_bytes);
+    ADASUM_CUDA_CHECK(cudaGetLastError());
+    profile_mark(stream, ADASUM_KERNEL_EMBEDDING_SORT, 0, 0, false);
+    if (num_tokens == 0)
+        return ADASUM_OK;
+
+    SumArgs a;
+    a.sorted = sorted;
+    a.n = (uint32_t)num_tokens;
+    a.num_rows = (uint32_t)num_rows;
+    a.tile = sum_tile(num_tokens);
+    a.stride = grad_out_stride;
+    a.dim = dim;
+    a.scale = scale;
+    a.table = grad_table;
+    a.table_dtype = (int)grad_dtype;
+    a.accumulate = accumulate != 0;
+    a.edges = reinterpret_cast<float*>(ws + lay.edges);
+    const unsigned tiles = (unsigned)((num_tokens + a.tile - 1) / a.tile);
+    with_type(dtype, [&](auto t) {
+        using T = decltype(t);
+        constexpr int VE = Element<T>::kVec;
+        const bool vec = rows_aligned(grad_out, grad_out_stride, sizeof(T)) && dim % VE == 0;
+        a.table_vec = vec && aligned_to(grad_table, 16) && dim * operator_bytes(grad_dtype) % 16 == 0;
+        const int64_t columns = (int64_t)kSumThreads * (vec ? VE : 1);
+        const int64_t slices = (dim + columns - 1) / columns;
+        const dim3 grid(tiles, (unsigned)(slices < 65535 ? slices : 65535));
+        if (vec)
+            embedding_sum_kernel<T, VE><<<grid, kSumThreads, 0, stream>>>(a, static_cast<const T*>(grad_out));
+        else
+            embedding_sum_kernel<T, 1><<<grid, kSumThreads, 0, stream>>>(a, static_cast<const T*>(grad_out));
+    });
+    ADASUM_CUDA_CHECK(cudaGetLastError());
+    profile_mark(stream, ADASUM_KERNEL_EMBEDDING_SUM, 0, 0, false);
+    if (tiles > 1) {
+        const int64_t slices = (dim + 31) / 32;
+        embedding_join_kernel<<<dim3(tiles - 1, (unsigned)(slices < 65535 ? slices : 65535)), kJoinThreads, 0, stream>>>(a);
+        ADASUM_CUDA_CHECK(cudaGetLastError());
+        profile_mark(stream, ADASUM_KERNEL_EMBEDDING_SUM, 1, 0, false);
+    }
+    return ADASUM_OK;
+}
+
+}  // extern "C"

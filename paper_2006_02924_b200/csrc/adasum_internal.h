@@ -17,6 +17,9 @@ namespace adasum {
 // Records the message for adasum_last_error() on the calling thread and returns `status`.
 adasum_status_t fail(adasum_status_t status, const char* fmt, ...);
 
+// Forgets the calling thread's message: the first thing that an entry point does.
+void clear_error();
+
 #define ADASUM_CUDA_CHECK(expr)                                                                  \
     do {                                                                                         \
         cudaError_t err__ = (expr);                                                              \

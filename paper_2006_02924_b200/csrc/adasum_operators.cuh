@@ -1,0 +1,130 @@
+// What the operators that produce a worker's gradients share (adasum_embedding.cu, adasum_checkpoint.cu,
+// adasum_weight_grad.cu): checks of matrix arguments and access to strided rows of any supported type.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "adasum_internal.h"
+
+namespace adasum {
+
+// ---- host: arguments -------------------------------------------------------------------------------
+
+inline bool operator_dtype(adasum_dtype_t dtype)
+{
+    return dtype == ADASUM_F32 || dtype == ADASUM_F16 || dtype == ADASUM_BF16;
+}
+inline int64_t operator_bytes(adasum_dtype_t dtype) { return dtype == ADASUM_F32 ? 4 : 2; }
+
+// Bytes from the first to past the last element of a strided matrix.
+inline size_t matrix_span(int64_t rows, int64_t cols, int64_t stride, int64_t elem_bytes)
+{
+    return rows > 0 && cols > 0 ? (size_t)((rows - 1) * stride + cols) * (size_t)elem_bytes : 0;
+}
+inline bool spans_overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes)
+{
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return a && b && a_bytes && b_bytes && x < y + b_bytes && y < x + a_bytes;
+}
+inline bool aligned_to(const void* p, int64_t bytes) { return (uintptr_t)p % (uintptr_t)bytes == 0; }
+// Rows that 16-byte accesses may be used on.
+inline bool rows_aligned(const void* p, int64_t stride, int64_t elem_bytes)
+{
+    return aligned_to(p, 16) && stride * elem_bytes % 16 == 0;
+}
+
+// Products such as rows * stride stay far inside 64 bits.
+constexpr int64_t kMaxExtent = (int64_t(1) << 31) - 256;
+inline bool extent_ok(int64_t n) { return n >= 0 && n <= kMaxExtent; }
+inline bool stride_ok(int64_t stride, int64_t cols) { return stride >= cols && stride <= (int64_t(1) << 31); }
+
+// Multiprocessors of the current device (0: unknown), looked up once per device.
+inline int device_sms()
+{
+    static int cached[64] = {};
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= 64)
+        return 0;
+    if (cached[device] == 0) {
+        int sms = 0;
+        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess)
+            return 0;
+        cached[device] = sms;
+    }
+    return cached[device];
+}
+
+// Division of vector indexes by the vectors of a row: q = floor(n / d) = high word of n * ceil(2^64 / d),
+// exact while n * d < 2^64 (the rounding of the factor adds less than n * d / 2^64 / d < 1 / d).
+struct RowDivider {
+    uint64_t factor;
+    uint32_t per_row;       // >= 2
+};
+inline RowDivider row_divider(int64_t per_row)
+{
+    return RowDivider{~uint64_t(0) / (uint64_t)per_row + 1, (uint32_t)per_row};
+}
+
+// ---- device ----------------------------------------------------------------------------------------
+
+__device__ __forceinline__ void divide_row(const RowDivider& d, uint64_t n, uint64_t& row, uint32_t& at)
+{
+    row = __umul64hi(n, d.factor);
+    at = (uint32_t)(n - row * d.per_row);
+}
+
+template <typename T>
+struct TypeCode;
+template <>
+struct TypeCode<float> { static constexpr int value = ADASUM_F32; };
+template <>
+struct TypeCode<__half> { static constexpr int value = ADASUM_F16; };
+template <>
+struct TypeCode<__nv_bfloat16> { static constexpr int value = ADASUM_BF16; };
+
+// Eight consecutive elements as floats; p is 16-byte aligned.  Plain loads: some callers overwrite the
+// same elements afterwards (in place).
+template <typename T>
+__device__ __forceinline__ void load_eight(const T* p, float (&x)[8])
+{
+    if constexpr (sizeof(T) == 4) {
+        const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+        x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    } else {
+        decode_vector<T>(*reinterpret_cast<const uint4*>(p), x);
+    }
+}
+__device__ __forceinline__ float load_one(const float* p) { return *p; }
+__device__ __forceinline__ float load_one(const __half* p) { return __half2float(*p); }
+__device__ __forceinline__ float load_one(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+
+// `count` (1 .. 8) elements, the rest zero.
+template <typename T>
+__device__ __forceinline__ void load_up_to_eight(const T* p, bool vec, int count, float (&x)[8])
+{
+    if (vec && count == 8) {
+        load_eight(p, x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            x[i] = i < count ? load_one(p + i) : 0.0f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store_up_to_eight(T* p, bool vec, int count, const float (&y)[8])
+{
+    if (vec && count == 8) {
+        store_vector_from_float<8>(p, TypeCode<T>::value, 0, y);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < count)
+                store_from_float(p, TypeCode<T>::value, i, y[i]);
+    }
+}
+
+}  // namespace adasum
