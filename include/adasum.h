@@ -501,6 +501,15 @@ adasum_status_t adasum_checkpoint_weight_grad(const void* checkpoint, int64_t ro
                                               adasum_dtype_t grad_dtype, int32_t accumulate,
                                               void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Device-side status of the last weight gradient that used this workspace: synchronises `stream` and
+ * returns ADASUM_OK, ADASUM_ERR_TIMEOUT if a bounded wait inside the product ran out (its gradients are
+ * then wrong), or an argument / CUDA error.  Sizes and type as for the call that is being asked about.
+ */
+adasum_status_t adasum_checkpoint_weight_grad_status(int64_t rows, int64_t features, int64_t outputs,
+                                                     adasum_dtype_t dtype, const void* workspace,
+                                                     void* stream);
+
 /* Static, human-readable name of a status code. */
 const char* adasum_status_string(adasum_status_t status);
 

@@ -669,3 +669,14 @@ def adasum_checkpoint_weight_grad(checkpoint, grad_out, features=None, grad_weig
                    _operator_dtype("grad_weight", grad_weight.dtype), int(accumulate), workspace.data_ptr(), ws_bytes,
                    _operator_stream(grad_out, stream))
     return grad_weight, grad_bias
+
+
+_lib.adasum_checkpoint_weight_grad_status.restype = ctypes.c_int
+_lib.adasum_checkpoint_weight_grad_status.argtypes = [_i64, _i64, _i64, ctypes.c_int, _vp, _vp]
+
+
+def adasum_checkpoint_weight_grad_status(rows: int, features: int, outputs: int, dtype, workspace, stream=None) -> int:
+    """``adasum_checkpoint_weight_grad_status`` of the C ABI: 0, or 7 (ADASUM_ERR_TIMEOUT) if a bounded wait of
+    the last weight gradient on ``workspace`` ran out.  Synchronises the stream."""
+    return int(_lib.adasum_checkpoint_weight_grad_status(int(rows), int(features), int(outputs), _dtype_code(dtype),
+                                                         workspace.data_ptr(), _operator_stream(workspace, stream)))

@@ -2,24 +2,84 @@
 //
 //     grad_weight[n][k] = scale * sum_t grad_out[t][n] * (kept x)[t][k]
 //     grad_bias[n]      = scale * sum_t grad_out[t][n]
+//
+// A product D[k][n] = X^T G on the fifth-generation tensor cores, summed over the tokens t: 2 T N K
+// operations on T (2 N + K) bytes, bound by the tensor cores from a few thousand tokens on.
+//
+// A pair of blocks (a cluster of two, on two neighbouring multiprocessors) owns a tile of 256 features x
+// 256 outputs.  Each block brings 128 features of X and 128 outputs of G per step of 64 tokens, and its
+// tensor core adds 128 features x 256 outputs: with both operands halved per block, shared memory and the
+// L2 deliver half of what two separate blocks would need.  Both operands arrive with the summed index t
+// as the slow one ("MN-major"), as they lie in memory; nothing is transposed.
+//
+//   G    one thread per block: bulk tensor copies of 64 outputs x 64 tokens, 128-byte swizzle, zeros
+//        beyond the matrix
+//   X    four warps per block: 16 codes per load, to the 16-bit type (exact: at most 7 significant bits
+//        times a power of two), to shared memory in the swizzled form the tensor core reads; loads run
+//        kAhead steps ahead in registers
+//   D    one thread of the pair's first block issues the multiplications; eight warps per block add the
+//        sums of every 256 tokens from tensor memory into fp32 registers
+//
+// The last point is for precision: the tensor core truncates where it adds, which over thousands of
+// tokens would be a bias of 1e-5; 16 additions of 16 products each between roundings to nearest keep the
+// result at the error of an fp32 sum.  Tensor memory holds two such sums, so the next is formed while the
+// previous one is read.
+//
+// The steps of all tiles, tile after tile, are cut into equal runs, one per pair, so every pair works to
+// the end whatever the sizes are; a tile whose steps fall to several pairs is joined, in their order, by
+// weight_grad_join_kernel.  The association of every sum is fixed by the sizes: results are deterministic.
+//
+// Every wait has a limit; a thread whose wait runs out records it, stops waiting and carries on (wrong
+// numbers, accesses in bounds), and adasum_checkpoint_weight_grad_status reports it.
+#include <cuda.h>
+
 #include "adasum_operators.cuh"
 
 namespace adasum {
 namespace {
 
-constexpr int kGroup = 32;
-constexpr int kTile = 64, kDepth = 16, kPerThread = 4;
+constexpr int kGroup = 32;                       // features that share a step byte
+constexpr int kHalf = 128;                       // features and outputs that a block of the pair brings
+constexpr int kTileSide = 256;                   // features and outputs of a pair's tile
+constexpr int kDepth = 64;                       // tokens per step
+constexpr int kChain = 4;                        // steps that are summed in tensor memory
+constexpr int kStages = 6;
+constexpr int kAhead = 3;                        // steps whose codes are on their way in registers
+constexpr int kPanelBytes = kDepth * 128;        // 64 features or outputs x 64 tokens, two bytes each
+constexpr int kOperandBytes = 2 * kPanelBytes;
+constexpr int kStageBytes = 2 * kOperandBytes;
+constexpr int kSumWarps = 8, kCodeWarps = 4;
+constexpr int kBlockThreads = 512;
+constexpr size_t kSharedBytes = (size_t)kStages * kStageBytes + 1024;       // + room to align to 1024
+constexpr int kMaxPairs = 74;                    // 148 multiprocessors
+constexpr int64_t kSlotFloats = (int64_t)kTileSide * kTileSide;
+constexpr uint32_t kWaitLimit = 1u << 22;        // about a tenth of a second; a real wait is microseconds
 
 struct WeightGradArgs {
     const int8_t* codes;
     const uint8_t* steps;
-    int64_t rows, features, width, outputs, stride;
+    int64_t rows, features, width, outputs;
     float scale;
     void* weight;
     void* bias;
     int out_dtype;
     bool accumulate;
+    // units of kChain steps, tile after tile (tiles of a column of outputs next to each other)
+    uint32_t tiles_k, tiles, iterations, chains, units;
+    int* status;             // one word per block
+    float* slots;            // [pair][first or last tile of its run][block][output][feature of the block]
+    float* bias_slots;       // [pair][first or last][256 outputs]
 };
+
+__host__ __device__ inline uint32_t first_unit(uint32_t units, uint32_t pairs, uint32_t pair)
+{
+    return (uint32_t)((uint64_t)pair * units / pairs);
+}
+// The pair whose run holds a unit: the largest p with floor(p units / pairs) <= unit.
+__host__ __device__ inline uint32_t pair_of_unit(uint32_t units, uint32_t pairs, uint32_t unit)
+{
+    return (uint32_t)((((uint64_t)unit + 1) * pairs - 1) / units);
+}
 
 __device__ __forceinline__ void write_gradient(const WeightGradArgs& a, void* dst, int64_t e, float sum)
 {
@@ -29,55 +89,666 @@ __device__ __forceinline__ void write_gradient(const WeightGradArgs& a, void* ds
     store_from_float(dst, a.out_dtype, e, y);
 }
 
-// One block: a 64 x 64 tile of grad_weight, fp32 throughout.
-template <typename T>
-__global__ void __launch_bounds__(256) weight_grad_kernel(WeightGradArgs a, const T* __restrict__ grad)
+// ---- instructions --------------------------------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t shared_address(const void* p)
 {
-    __shared__ float g[kDepth][kTile], x[kDepth][kTile];
-    const int64_t k0 = (int64_t)blockIdx.x * kTile, n0 = (int64_t)blockIdx.y * kTile;
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    float sum[kPerThread][kPerThread] = {};
-    float bias = 0.0f;
-    for (int64_t t0 = 0; t0 < a.rows; t0 += kDepth) {
-        for (int i = threadIdx.x; i < kDepth * kTile; i += 256) {
-            const int64_t t = t0 + i / kTile, n = n0 + i % kTile, k = k0 + i % kTile;
-            g[i / kTile][i % kTile] = t < a.rows && n < a.outputs ? load_one(grad + t * a.stride + n) : 0.0f;
-            x[i / kTile][i % kTile] =
-                t < a.rows && k < a.features
-                    ? (float)a.codes[t * a.width + k] *
-                          __uint_as_float((uint32_t)a.steps[t * (a.width / kGroup) + k / kGroup] << 23)
-                    : 0.0f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int d = 0; d < kDepth; ++d) {
-#pragma unroll
-            for (int i = 0; i < kPerThread; ++i)
-#pragma unroll
-                for (int j = 0; j < kPerThread; ++j)
-                    sum[i][j] = fmaf(g[d][ty + 16 * i], x[d][tx + 16 * j], sum[i][j]);
-            if (threadIdx.x < kTile)
-                bias += g[d][threadIdx.x];
-        }
-        __syncthreads();
+    return static_cast<uint32_t>(__cvta_generic_to_shared(p));
+}
+__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
+}
+// Waits for the phase, with the ordering of the whole cluster (arrivals come from both blocks).
+__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity)
+{
+    for (uint32_t spin = 0; spin < kWaitLimit; ++spin) {
+        uint32_t done;
+        asm volatile("{\n\t.reg .pred p;\n\t"
+                     "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done)
+                     : "r"(bar), "r"(parity)
+                     : "memory");
+        if (done)
+            return true;
     }
-    for (int i = 0; i < kPerThread; ++i)
-        for (int j = 0; j < kPerThread; ++j) {
-            const int64_t n = n0 + ty + 16 * i, k = k0 + tx + 16 * j;
-            if (n < a.outputs && k < a.features)
-                write_gradient(a, a.weight, n * a.features + k, sum[i][j]);
+    return false;
+}
+// Arrives on the same barrier of the pair's first block.
+__device__ __forceinline__ void arrive_at_first(uint32_t bar)
+{
+    asm volatile("{\n\t.reg .b32 remote;\n\tmapa.shared::cluster.u32 remote, %0, 0;\n\t"
+                 "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [remote];\n\t}" ::"r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void expect_bytes(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+                 "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void cluster_barrier()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Arrives on the barrier at this offset in both blocks once all multiplications issued so far are done.
+__device__ __forceinline__ void commit_to_both(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                 "h"((uint16_t)3)
+                 : "memory");
+}
+template <int REGS>
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS)); }
+template <int REGS>
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS)); }
+
+// Operand in shared memory with the summed index slow, 128-byte swizzle: rows of 64 features (outputs), one
+// row per token; eight rows 1024 bytes, the next 64 features one panel further.
+__device__ __forceinline__ uint64_t operand_descriptor(uint32_t address)
+{
+    return (uint64_t)((address & 0x3ffffu) >> 4) | (uint64_t)(kPanelBytes >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 |
+           (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+
+__device__ __forceinline__ void load_sums(uint32_t address, uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(address)
+        : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+// ---- the codes of a step --------------------------------------------------------------------------------
+
+// Four codes to two words of the 16-bit type: byte + 128 in the low bits of 2^23, 2^23 + 128 taken off
+// (exact), times the step (exact in 16 bits too, see the format).
+template <typename T>
+__device__ __forceinline__ uint2 decode_four(uint32_t packed, float step)
+{
+    const uint32_t u = packed ^ 0x80808080u;
+    float x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        x[i] = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7540 + i)) - 8388736.0f) * step;
+    uint2 w;
+    if constexpr (__is_same(T, __half)) {
+        const __half2 a = __floats2half2_rn(x[0], x[1]), b = __floats2half2_rn(x[2], x[3]);
+        w.x = *reinterpret_cast<const uint32_t*>(&a);
+        w.y = *reinterpret_cast<const uint32_t*>(&b);
+    } else {
+        const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
+        w.x = *reinterpret_cast<const uint32_t*>(&a);
+        w.y = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    return w;
+}
+
+// Where a pair stands in its run of units.
+struct Cursor {
+    uint32_t unit, tile, it, it_end;
+    __device__ __forceinline__ void enter(const WeightGradArgs& a)
+    {
+        tile = unit / a.chains;
+        it = (unit - tile * a.chains) * kChain;
+        it_end = min(it + kChain, a.iterations);
+    }
+    __device__ __forceinline__ void advance(const WeightGradArgs& a)
+    {
+        if (++it == it_end) {
+            ++unit;
+            enter(a);
         }
-    if (a.bias && blockIdx.x == 0 && threadIdx.x < kTile && n0 + threadIdx.x < a.outputs)
-        write_gradient(a, a.bias, n0 + threadIdx.x, bias);
+    }
+};
+
+// One thread's part of a step: four rows (tokens), 16 features each.
+struct CodeLoad {
+    uint4 codes[4];
+    uint32_t step[4];
+};
+
+// ---- kernel ---------------------------------------------------------------------------------------------
+//
+// T: 16-bit type of both operands.  PLANES: 1, or 3 for fp32 gradients, which arrive as three bf16 matrices
+// that add up to them; a step then is one plane of one block of tokens, planes fastest.
+// Warps 0 .. 7 sum, 8 .. 11 decode, 12 copies, 13 multiplies (first block only), 14 owns the tensor memory.
+// Registers: 256 x 184 + 128 x 104 + 128 x 40 = 512 x 128.
+template <typename T, int PLANES, bool BIAS>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kBlockThreads, 1)
+weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_constant__ CUtensorMap grad_map)
+{
+    extern __shared__ __align__(1024) unsigned char dynamic_shared[];
+    // landed: this block's copies of a step are there.  ready (first block): both blocks' operands are there.
+    // empty: the step has been multiplied (and, with BIAS, added up by the eight sum warps).
+    // formed / taken (first block): a sum in tensor memory is complete / has been read by both blocks.
+    __shared__ __align__(8) unsigned long long landed[kStages], ready[kStages], empty[kStages], formed[2], taken[2];
+    __shared__ uint32_t tensor_memory_slot;
+    __shared__ float bias_part[4][kHalf];
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const uint32_t unit_begin = first_unit(a.units, pairs, pair), unit_end = first_unit(a.units, pairs, pair + 1);
+    const uint32_t stage0 = (shared_address(dynamic_shared) + 1023u) & ~1023u;
+    const uint32_t landed0 = shared_address(landed), ready0 = shared_address(ready), empty0 = shared_address(empty);
+    const uint32_t formed0 = shared_address(formed), taken0 = shared_address(taken);
+
+    if (threadIdx.x == 0) {
+        a.status[blockIdx.x] = 0;
+        for (int s = 0; s < kStages; ++s) {
+            barrier_init(landed0 + 8 * s, 1);
+            barrier_init(ready0 + 8 * s, 2 * kCodeWarps);
+            barrier_init(empty0 + 8 * s, BIAS ? 1 + kSumWarps : 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            barrier_init(formed0 + 8 * s, 1);
+            barrier_init(taken0 + 8 * s, 2 * kSumWarps);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 14) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(
+            shared_address(&tensor_memory_slot)));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_barrier();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tensor_memory = tensor_memory_slot;
+
+    bool waiting = true;             // false after a wait of this thread ran out
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+        if (waiting && !wait_phase(bar, parity)) {
+            waiting = false;
+            a.status[blockIdx.x] = ADASUM_DEVICE_TIMEOUT;
+        }
+    };
+
+    if (warp < kSumWarps) {
+        // ---- sums: warp w reads tensor-memory lanes 32 (w % 4) .. + 31 (features), outputs 128 (w / 4) .. + 127
+        more_registers<184>();
+        const int quarter = warp & 3, side = warp >> 2;
+        float sum[128];
+        float bias_sum[2] = {0.0f, 0.0f};
+        uint32_t stage = 0, phase = 0, count = 0;
+        uint32_t chain_begin = 0;
+        for (uint32_t unit = unit_begin; unit < unit_end; ++unit, ++count) {
+            const uint32_t tile = unit / a.chains, chain = unit - tile * a.chains;
+            const uint32_t tile_k = tile % a.tiles_k, tile_n = tile / a.tiles_k;
+            if (unit == unit_begin || chain == 0) {
+                chain_begin = chain;
+                bias_sum[0] = bias_sum[1] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 128; ++i)
+                    sum[i] = 0.0f;
+            }
+            if constexpr (BIAS) {
+                // this block's 128 outputs: thread = two outputs, 16 of a step's 64 tokens.  Summed per
+                // unit, like the products.
+                const uint32_t steps = min((uint32_t)kChain, a.iterations - chain * kChain);
+                const int output = 2 * (threadIdx.x & 63), part = threadIdx.x >> 6;
+                float unit_sum[2] = {0.0f, 0.0f};
+                for (uint32_t s = 0; s < steps; ++s) {
+                    wait(landed0 + 8 * stage, phase);
+                    if (tile_k == 0) {
+                        const uint32_t panel = stage0 + stage * kStageBytes + kOperandBytes + (output >> 6) * kPanelBytes;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int row = part * 16 + i;
+                            uint32_t w;
+                            asm volatile("ld.shared.b32 %0, [%1];"
+                                         : "=r"(w)
+                                         : "r"(panel + row * 128 + ((((output & 63) >> 3) ^ (row & 7)) << 4) +
+                                               (output & 7) * 2));
+                            if constexpr (__is_same(T, __half)) {
+                                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+                                unit_sum[0] += f.x;
+                                unit_sum[1] += f.y;
+                            } else {
+                                unit_sum[0] += __uint_as_float(w << 16);
+                                unit_sum[1] += __uint_as_float(w & 0xffff0000u);
+                            }
+                        }
+                    }
+                    __syncwarp();
+                    if (lane == 0)
+                        mbarrier_arrive(empty0 + 8 * stage);
+                    if (++stage == kStages) {
+                        stage = 0;
+                        phase ^= 1;
+                    }
+                }
+                bias_sum[0] += unit_sum[0];
+                bias_sum[1] += unit_sum[1];
+            }
+            wait(formed0 + 8 * (count & 1), (count >> 1) & 1);
+            __syncwarp();
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t source = tensor_memory + (count & 1) * 256 + side * 128 + ((uint32_t)(32 * quarter) << 16);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                uint32_t r[32];
+                load_sums(source + 32 * g, r);
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    sum[32 * g + i] += __uint_as_float(r[i]);
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0)
+                arrive_at_first(taken0 + 8 * (count & 1));
+
+            if (chain + 1 != a.chains && unit + 1 != unit_end)
+                continue;
+            // ---- the pair's last unit of this tile: the result, or this pair's part of it
+            const bool whole = chain_begin == 0 && chain + 1 == a.chains;
+            const uint32_t slot = 2 * pair + (tile == unit_begin / a.chains ? 0 : 1);
+            const int feature = 32 * quarter + lane;
+            if (whole) {
+                const int64_t k = (int64_t)tile_k * kTileSide + rank * kHalf + feature;
+                const int64_t n = (int64_t)tile_n * kTileSide + side * kHalf;
+                if (k < a.features) {
+#pragma unroll
+                    for (int i = 0; i < 128; ++i)
+                        if (n + i < a.outputs)
+                            write_gradient(a, a.weight, (n + i) * a.features + k, sum[i]);
+                }
+            } else {
+                float* dst = a.slots + slot * kSlotFloats + (rank * kTileSide + side * kHalf) * kHalf + feature;
+#pragma unroll
+                for (int i = 0; i < 128; ++i)
+                    dst[i * kHalf] = sum[i];
+            }
+            if constexpr (BIAS) {
+                if (tile_k == 0) {
+                    const int output = 2 * (threadIdx.x & 63), part = threadIdx.x >> 6;
+                    bias_part[part][output] = bias_sum[0];
+                    bias_part[part][output + 1] = bias_sum[1];
+                    asm volatile("bar.sync 1, 256;" ::: "memory");
+                    if (threadIdx.x < kHalf) {
+                        const float total = (bias_part[0][threadIdx.x] + bias_part[1][threadIdx.x]) +
+                                            (bias_part[2][threadIdx.x] + bias_part[3][threadIdx.x]);
+                        const int64_t n = (int64_t)tile_n * kTileSide + rank * kHalf + threadIdx.x;
+                        if (!whole)
+                            a.bias_slots[(int64_t)slot * kTileSide + rank * kHalf + threadIdx.x] = total;
+                        else if (n < a.outputs)
+                            write_gradient(a, a.bias, n, total);
+                    }
+                    asm volatile("bar.sync 1, 256;" ::: "memory");
+                }
+            }
+        }
+    } else if (warp < kSumWarps + kCodeWarps) {
+        // ---- codes: a lane holds 16 features (one load) of four rows; a warp's load covers four rows of 128
+        // codes, and any eight neighbouring lanes write 16-byte pieces of eight different bank groups
+        fewer_registers<104>();
+        const int piece = (lane & 3) | ((lane >> 4) & 1) << 2;
+        const int row0 = ((lane >> 2) & 3) + 4 * (warp - kSumWarps);
+        const int64_t groups = a.width / kGroup;
+        auto load = [&](const Cursor& c, CodeLoad& l) {
+            const int64_t k = (int64_t)(c.tile % a.tiles_k) * kTileSide + rank * kHalf + piece * 16;
+            const int64_t t0 = (int64_t)(c.it / PLANES) * kDepth + row0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int64_t t = t0 + 16 * i;
+                if (t < a.rows && k < a.width) {
+                    l.codes[i] = load_keep_16B(a.codes + t * a.width + k);
+                    l.step[i] = __ldg(a.steps + t * groups + k / kGroup);
+                } else {
+                    l.codes[i] = make_uint4(0, 0, 0, 0);
+                    l.step[i] = 0;
+                }
+            }
+        };
+        uint32_t stage = 0, phase = 0;
+        auto store = [&](const CodeLoad& l) {
+            wait(empty0 + 8 * stage, phase ^ 1);
+            const uint32_t panel = stage0 + stage * kStageBytes + (piece >> 2) * kPanelBytes;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = row0 + 16 * i;
+                const float step = __uint_as_float(l.step[i] << 23);
+                const uint2 w0 = decode_four<T>(l.codes[i].x, step), w1 = decode_four<T>(l.codes[i].y, step);
+                const uint2 w2 = decode_four<T>(l.codes[i].z, step), w3 = decode_four<T>(l.codes[i].w, step);
+                const int at = 2 * (piece & 3);
+                store_shared_16B(panel + row * 128 + ((at ^ (row & 7)) << 4), make_uint4(w0.x, w0.y, w1.x, w1.y));
+                store_shared_16B(panel + row * 128 + (((at + 1) ^ (row & 7)) << 4), make_uint4(w2.x, w2.y, w3.x, w3.y));
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+                wait(landed0 + 8 * stage, phase);
+                arrive_at_first(ready0 + 8 * stage);
+            }
+            __syncwarp();
+            if (++stage == kStages) {
+                stage = 0;
+                phase ^= 1;
+            }
+        };
+        if (unit_begin < unit_end) {
+            CodeLoad l[kAhead];
+            Cursor c;
+            c.unit = unit_begin;
+            c.enter(a);
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                if (c.unit < unit_end) {
+                    load(c, l[j]);
+                    c.advance(a);
+                }
+            }
+            // steps of the run: whole units but for the last unit of a tile
+            uint32_t steps = 0;
+            for (Cursor d{unit_begin, 0, 0, 0}; d.unit < unit_end; ++d.unit) {
+                d.enter(a);
+                steps += d.it_end - d.it;
+            }
+            for (uint32_t s = 0; s < steps; s += kAhead) {
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j) {
+                    if (s + j < steps) {
+                        store(l[j]);
+                        if (c.unit < unit_end) {
+                            load(c, l[j]);
+                            c.advance(a);
+                        }
+                    }
+                }
+            }
+        }
+    } else {
+        fewer_registers<40>();
+        if (warp == 12 && lane == 0) {
+            // ---- copies of this block's half of the gradients
+            uint32_t stage = 0, phase = 0, issued = 0;
+            for (uint32_t unit = unit_begin; unit < unit_end && waiting; ++unit) {
+                Cursor c;
+                c.unit = unit;
+                c.enter(a);
+                const int n = (int)(c.tile / a.tiles_k) * kTileSide + (int)rank * kHalf;
+                for (; c.it < c.it_end; ++c.it) {
+                    wait(empty0 + 8 * stage, phase ^ 1);
+                    if (!waiting)
+                        break;
+                    const uint32_t dst = stage0 + stage * kStageBytes + kOperandBytes;
+                    const int t = (int)(c.it / PLANES) * kDepth, plane = (int)(c.it % PLANES);
+                    expect_bytes(landed0 + 8 * stage, kOperandBytes);
+                    copy_box(dst, &grad_map, n, t, plane, landed0 + 8 * stage);
+                    copy_box(dst + kPanelBytes, &grad_map, n + 64, t, plane, landed0 + 8 * stage);
+                    ++issued;
+                    if (++stage == kStages) {
+                        stage = 0;
+                        phase ^= 1;
+                    }
+                }
+            }
+            // nothing may still be on its way into shared memory when the block ends
+            waiting = true;
+            for (uint32_t back = min(issued, (uint32_t)kStages); back > 0; --back) {
+                const uint32_t step = issued - back;
+                wait(landed0 + 8 * (step % kStages), (step / kStages) & 1);
+            }
+        } else if (warp == 13 && lane == 0 && rank == 0) {
+            // ---- multiplications: fp32 sums, both operands of type T with the summed index slow, 256 x 256
+            constexpr uint32_t kFormat = __is_same(T, __half) ? 0u : 1u;
+            constexpr uint32_t kInstruction = (1u << 4) | (kFormat << 7) | (kFormat << 10) | (1u << 15) | (1u << 16) |
+                                              ((kTileSide >> 3) << 17) | ((kTileSide >> 4) << 24);
+            uint32_t stage = 0, phase = 0, count = 0;
+            for (uint32_t unit = unit_begin; unit < unit_end; ++unit, ++count) {
+                Cursor c;
+                c.unit = unit;
+                c.enter(a);
+                const uint32_t target = tensor_memory + (count & 1) * 256;
+                wait(taken0 + 8 * (count & 1), ((count >> 1) & 1) ^ 1);
+                uint32_t accumulate = 0;
+                for (; c.it < c.it_end; ++c.it) {
+                    wait(ready0 + 8 * stage, phase);
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t base = stage0 + stage * kStageBytes;
+#pragma unroll
+                    for (int s = 0; s < kDepth / 16; ++s) {
+                        const uint64_t x = operand_descriptor(base + s * 2048);
+                        const uint64_t g = operand_descriptor(base + kOperandBytes + s * 2048);
+                        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(target),
+                                     "l"(x), "l"(g), "r"(kInstruction), "r"(accumulate)
+                                     : "memory");
+                        accumulate = 1;
+                    }
+                    commit_to_both(empty0 + 8 * stage);
+                    if (++stage == kStages) {
+                        stage = 0;
+                        phase ^= 1;
+                    }
+                }
+                commit_to_both(formed0 + 8 * (count & 1));
+            }
+        }
+        __syncwarp();
+    }
+    // Neither block may end, nor free its tensor memory, while the other still multiplies or arrives here.
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncwarp();
+    cluster_barrier();
+    if (warp == 14)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tensor_memory) : "memory");
+}
+
+// Tiles whose units fell to several pairs: the pairs' parts added in order.  grid.x = tiles, grid.y = eighths
+// of the tile's outputs; thread = one feature of each block, every second output.
+constexpr int kJoinThreads = 256;
+constexpr int kJoinOutputs = 32;
+
+__global__ void __launch_bounds__(kJoinThreads)
+weight_grad_join_kernel(const __grid_constant__ WeightGradArgs a, uint32_t pairs)
+{
+    const uint32_t tile = blockIdx.x;
+    const uint32_t first = pair_of_unit(a.units, pairs, tile * a.chains);
+    const uint32_t last = pair_of_unit(a.units, pairs, tile * a.chains + a.chains - 1);
+    if (first == last)
+        return;                      // written by the product itself
+    const uint32_t tile_k = tile % a.tiles_k, tile_n = tile / a.tiles_k;
+    const int feature = threadIdx.x;
+    const int64_t k = (int64_t)tile_k * kTileSide + feature;
+    const float* source = a.slots + ((int64_t)(feature >> 7) * kTileSide) * kHalf + (feature & 127);
+    auto slot_of = [&](uint32_t pair) {
+        return 2 * pair + (tile == first_unit(a.units, pairs, pair) / a.chains ? 0 : 1);
+    };
+    for (int o = blockIdx.y * kJoinOutputs; o < (int)(blockIdx.y + 1) * kJoinOutputs; o += 8) {
+        float sum[8] = {};
+        for (uint32_t pair = first; pair <= last; ++pair) {
+            const float* s = source + slot_of(pair) * kSlotFloats;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                sum[i] += s[(o + i) * kHalf];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t n = (int64_t)tile_n * kTileSide + o + i;
+            if (n < a.outputs && k < a.features)
+                write_gradient(a, a.weight, n * a.features + k, sum[i]);
+        }
+    }
+    if (a.bias && tile_k == 0 && blockIdx.y == 0) {
+        const int64_t n = (int64_t)tile_n * kTileSide + threadIdx.x;
+        float sum = 0.0f;
+        for (uint32_t pair = first; pair <= last; ++pair)
+            sum += a.bias_slots[(int64_t)slot_of(pair) * kTileSide + threadIdx.x];
+        if (n < a.outputs)
+            write_gradient(a, a.bias, n, sum);
+    }
+}
+
+// ---- gradients that the tensor copies cannot read as they lie -------------------------------------------
+
+// fp32: three bf16 matrices [plane][rows][pitch] that add up to the gradients: the upper 8 significant bits
+// (truncated, so that nothing overflows), the next 8, the last 8.  16-bit types: rows moved to a pitch of
+// whole 16 bytes.  One thread per eight outputs.
+template <typename T>
+__global__ void __launch_bounds__(256)
+relay_gradients_kernel(const T* grad, int64_t stride, bool vec, int64_t rows, int64_t outputs, int64_t pitch, uint4* out,
+                       RowDivider divider, uint64_t vectors)
+{
+    const uint64_t n = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (n >= vectors)
+        return;
+    uint64_t row;
+    uint32_t at;
+    divide_row(divider, n, row, at);
+    const int64_t column = (int64_t)at * 8;
+    if (column >= pitch)
+        return;
+    const int count = (int)min((int64_t)8, outputs - column);
+    const int64_t place = ((int64_t)row * pitch + column) / 8;
+    const T* p = grad + (int64_t)row * stride + column;
+    if constexpr (sizeof(T) == 4) {
+        float x[8];
+        load_up_to_eight(p, vec, count, x);
+        uint32_t w[3][4] = {};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t part[3] = {__float_as_uint(x[i]) >> 16, 0, 0};
+            if (isfinite(x[i])) {
+                const float r1 = x[i] - __uint_as_float(part[0] << 16);
+                part[1] = __float_as_uint(r1) >> 16;
+                part[2] = __float_as_uint(r1 - __uint_as_float(part[1] << 16)) >> 16;
+            } else if (isnan(x[i])) {
+                part[0] |= 0x40;                         // a NaN whose bits are all in the lower half stays one
+            }
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                w[j][i >> 1] |= part[j] << (16 * (i & 1));
+        }
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+            out[j * (rows * pitch / 8) + place] = make_uint4(w[j][0], w[j][1], w[j][2], w[j][3]);
+    } else {
+        const unsigned short* q = reinterpret_cast<const unsigned short*>(p);
+        uint32_t w[4] = {};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < count)
+                w[i >> 1] |= (uint32_t)q[i] << (16 * (i & 1));
+        out[place] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// ---- host -------------------------------------------------------------------------------------------------
+
+struct WorkLayout {
+    uint32_t tiles_k, tiles, iterations, chains, units, pairs;
+    int64_t pitch;
+    size_t slots, bias_slots, gradients, total;
+    bool fits;
+};
+
+// `pairs` here is the most that any device may use; the launch takes at most half its multiprocessors.
+WorkLayout work_layout(int64_t rows, int64_t features, int64_t outputs, adasum_dtype_t dtype)
+{
+    auto up = [](int64_t x, int64_t to) { return (x + to - 1) / to * to; };
+    WorkLayout l{};
+    const int64_t planes = dtype == ADASUM_F32 ? 3 : 1;
+    const int64_t tiles_k = features > 0 ? (features + kTileSide - 1) / kTileSide : 1;
+    const int64_t tiles_n = (outputs + kTileSide - 1) / kTileSide;
+    const int64_t iterations = (rows + kDepth - 1) / kDepth * planes;
+    const int64_t chains = (iterations + kChain - 1) / kChain;
+    const int64_t limit = int64_t(1) << 31;
+    l.fits = tiles_k * tiles_n < limit && iterations < limit && (chains == 0 || tiles_k * tiles_n < limit / chains);
+    if (!l.fits)
+        return l;
+    l.tiles_k = (uint32_t)tiles_k;
+    l.tiles = (uint32_t)(tiles_k * tiles_n);
+    l.iterations = (uint32_t)iterations;
+    l.chains = (uint32_t)chains;
+    l.units = (uint32_t)(l.tiles * chains);
+    l.pairs = l.units < kMaxPairs ? l.units : kMaxPairs;
+    l.pitch = up(outputs, 8);
+    l.slots = 1024;                                    // the blocks' status words come first
+    l.bias_slots = l.slots + (size_t)l.pairs * 2 * kSlotFloats * sizeof(float);
+    l.gradients = l.bias_slots + (size_t)l.pairs * 2 * kTileSide * sizeof(float);
+    l.total = l.gradients + (size_t)up(planes * rows * l.pitch * 2, 256);
+    return l;
+}
+
+uint32_t launch_pairs(const WorkLayout& l)
+{
+    const uint32_t most = (uint32_t)device_sms() / 2;
+    return l.pairs < most ? l.pairs : most;
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled()
+{
+    static EncodeTiled cached = nullptr;
+    if (!cached) {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) == cudaSuccess &&
+            found == cudaDriverEntryPointSuccess)
+            cached = reinterpret_cast<EncodeTiled>(fn);
+    }
+    return cached;
+}
+
+adasum_status_t describe_gradients(CUtensorMap* map, const void* base, adasum_dtype_t type, int64_t outputs, int64_t rows,
+                                   int64_t planes, int64_t pitch)
+{
+    EncodeTiled encode = encode_tiled();
+    if (!encode)
+        return fail(ADASUM_ERR_CUDA, "the driver has no tensor map encoder");
+    const cuuint64_t dims[3] = {(cuuint64_t)outputs, (cuuint64_t)rows, (cuuint64_t)planes};
+    const cuuint64_t strides[2] = {(cuuint64_t)pitch * 2, (cuuint64_t)(rows * pitch * 2)};
+    const cuuint32_t box[3] = {64, kDepth, 1}, unit[3] = {1, 1, 1};
+    const CUresult err =
+        encode(map, type == ADASUM_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+               const_cast<void*>(base), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return err == CUDA_SUCCESS ? ADASUM_OK : fail(ADASUM_ERR_CUDA, "tensor map of the gradients: error %d", (int)err);
+}
+
+template <typename T, int PLANES, bool BIAS>
+cudaError_t launch_product(const WeightGradArgs& a, const CUtensorMap& map, uint32_t pairs, cudaStream_t stream)
+{
+    auto* kernel = weight_grad_kernel<T, PLANES, BIAS>;
+    const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedBytes);
+    if (err != cudaSuccess)
+        return err;
+    kernel<<<2 * pairs, kBlockThreads, kSharedBytes, stream>>>(a, map);
+    return cudaGetLastError();
+}
+template <typename T, int PLANES>
+cudaError_t launch_product(const WeightGradArgs& a, const CUtensorMap& map, uint32_t pairs, cudaStream_t stream)
+{
+    return a.bias ? launch_product<T, PLANES, true>(a, map, pairs, stream)
+                  : launch_product<T, PLANES, false>(a, map, pairs, stream);
 }
 
 template <typename T>
-void launch_weight_grad(const WeightGradArgs& a, const void* grad_out, cudaStream_t stream)
+cudaError_t launch_relay(const void* grad, int64_t stride, int64_t rows, int64_t outputs, int64_t pitch, void* out,
+                         cudaStream_t stream)
 {
-    // with no features the bias gradient still has its blocks
-    const dim3 grid((unsigned)((a.features + kTile - 1) / kTile + (a.features == 0)),
-                    (unsigned)((a.outputs + kTile - 1) / kTile));
-    weight_grad_kernel<T><<<grid, 256, 0, stream>>>(a, static_cast<const T*>(grad_out));
+    const int64_t per_row = pitch / 8 < 2 ? 2 : pitch / 8;
+    const uint64_t vectors = (uint64_t)rows * (uint64_t)per_row, blocks = (vectors + 255) / 256;
+    if (blocks > 0x7fffffffu)
+        return cudaErrorInvalidValue;
+    relay_gradients_kernel<T><<<(unsigned)blocks, 256, 0, stream>>>(
+        static_cast<const T*>(grad), stride, rows_aligned(grad, stride, sizeof(T)), rows, outputs, pitch,
+        static_cast<uint4*>(out), row_divider(per_row), vectors);
+    return cudaGetLastError();
 }
 
 }  // namespace
@@ -91,7 +762,7 @@ size_t adasum_checkpoint_weight_grad_workspace_bytes(int64_t rows, int64_t featu
     using namespace adasum;
     if (!extent_ok(rows) || !extent_ok(features) || !extent_ok(outputs) || !operator_dtype(dtype))
         return 0;
-    return 256;
+    return work_layout(rows, features, outputs, dtype).total;
 }
 
 adasum_status_t adasum_checkpoint_weight_grad(const void* checkpoint, int64_t rows, int64_t features,
@@ -121,7 +792,11 @@ adasum_status_t adasum_checkpoint_weight_grad(const void* checkpoint, int64_t ro
     if (rows > 0 && !stride_ok(grad_out_stride, outputs))
         return fail(ADASUM_ERR_ARG, "grad_out_stride %lld is shorter than a row or out of range",
                     (long long)grad_out_stride);
-    const size_t need = adasum_checkpoint_weight_grad_workspace_bytes(rows, features, outputs, dtype);
+    const WorkLayout l = work_layout(rows, features, outputs, dtype);
+    if (!l.fits)
+        return fail(ADASUM_ERR_ARG, "%lld x %lld x %lld is too large", (long long)rows, (long long)features,
+                    (long long)outputs);
+    const size_t need = l.total;
     if (!workspace || workspace_bytes < need)
         return fail(ADASUM_ERR_WORKSPACE, "workspace of %zu bytes, need %zu", workspace ? workspace_bytes : (size_t)0,
                     need);
@@ -141,6 +816,26 @@ adasum_status_t adasum_checkpoint_weight_grad(const void* checkpoint, int64_t ro
         return fail(ADASUM_ERR_ARG, "grad_weight, grad_bias and workspace overlap");
 
     cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+    if (rows == 0) {                       // empty sums: zeros of any type are zero bytes
+        if (weight_bytes)
+            ADASUM_CUDA_CHECK(cudaMemsetAsync(grad_weight, 0, weight_bytes, stream));
+        if (bias_bytes)
+            ADASUM_CUDA_CHECK(cudaMemsetAsync(grad_bias, 0, bias_bytes, stream));
+        return ADASUM_OK;
+    }
+    const uint32_t pairs = launch_pairs(l);
+    if (pairs == 0)
+        return fail(ADASUM_ERR_CUDA, "no current device");
+    char* ws = static_cast<char*>(workspace);
+    // 16-byte rows are copied as they lie; others, and fp32, are laid out in the workspace first
+    const bool relay = dtype == ADASUM_F32 || !rows_aligned(grad_out, grad_out_stride, eb);
+    const int64_t planes = dtype == ADASUM_F32 ? 3 : 1;
+    CUtensorMap map;
+    const adasum_status_t described =
+        describe_gradients(&map, relay ? ws + l.gradients : grad_out, dtype == ADASUM_F16 ? ADASUM_F16 : ADASUM_BF16,
+                           outputs, rows, planes, relay ? l.pitch : grad_out_stride);
+    if (described != ADASUM_OK)
+        return described;
     WeightGradArgs a;
     a.rows = rows;
     a.features = features;
@@ -148,21 +843,69 @@ adasum_status_t adasum_checkpoint_weight_grad(const void* checkpoint, int64_t ro
     a.codes = static_cast<const int8_t*>(checkpoint);
     a.steps = static_cast<const uint8_t*>(checkpoint) + rows * a.width;
     a.outputs = outputs;
-    a.stride = grad_out_stride;
     a.scale = scale;
     a.weight = grad_weight;
     a.bias = grad_bias;
     a.out_dtype = (int)grad_dtype;
     a.accumulate = accumulate != 0;
+    a.tiles_k = l.tiles_k;
+    a.tiles = l.tiles;
+    a.iterations = l.iterations;
+    a.chains = l.chains;
+    a.units = l.units;
+    a.status = reinterpret_cast<int*>(ws);
+    a.slots = reinterpret_cast<float*>(ws + l.slots);
+    a.bias_slots = reinterpret_cast<float*>(ws + l.bias_slots);
     profile_mark(stream, -1, 0, 0, true);
+    if (relay) {
+        void* to = ws + l.gradients;
+        ADASUM_CUDA_CHECK(dtype == ADASUM_F32
+                              ? launch_relay<float>(grad_out, grad_out_stride, rows, outputs, l.pitch, to, stream)
+                              : launch_relay<__half>(grad_out, grad_out_stride, rows, outputs, l.pitch, to, stream));
+        profile_mark(stream, ADASUM_KERNEL_WEIGHT_GRAD, 0, 0, false);
+    }
     if (dtype == ADASUM_F32)
-        launch_weight_grad<float>(a, grad_out, stream);
+        ADASUM_CUDA_CHECK((launch_product<__nv_bfloat16, 3>(a, map, pairs, stream)));
     else if (dtype == ADASUM_F16)
-        launch_weight_grad<__half>(a, grad_out, stream);
+        ADASUM_CUDA_CHECK((launch_product<__half, 1>(a, map, pairs, stream)));
     else
-        launch_weight_grad<__nv_bfloat16>(a, grad_out, stream);
-    ADASUM_CUDA_CHECK(cudaGetLastError());
+        ADASUM_CUDA_CHECK((launch_product<__nv_bfloat16, 1>(a, map, pairs, stream)));
     profile_mark(stream, ADASUM_KERNEL_WEIGHT_GRAD, 1, 0, false);
+    bool split = false;                    // does any tile fall to several pairs?
+    for (uint32_t p = 1; p < pairs && !split; ++p)
+        split = first_unit(l.units, pairs, p) % l.chains != 0;
+    if (split) {
+        weight_grad_join_kernel<<<dim3(l.tiles, kTileSide / kJoinOutputs), kJoinThreads, 0, stream>>>(a, pairs);
+        ADASUM_CUDA_CHECK(cudaGetLastError());
+        profile_mark(stream, ADASUM_KERNEL_WEIGHT_GRAD, 2, 0, false);
+    }
+    return ADASUM_OK;
+}
+
+adasum_status_t adasum_checkpoint_weight_grad_status(int64_t rows, int64_t features, int64_t outputs,
+                                                     adasum_dtype_t dtype, const void* workspace, void* stream_ptr)
+{
+    using namespace adasum;
+    clear_error();
+    if (!workspace)
+        return fail(ADASUM_ERR_NULL, "workspace is NULL");
+    if (!extent_ok(rows) || !extent_ok(features) || !extent_ok(outputs))
+        return fail(ADASUM_ERR_ARG, "invalid sizes");
+    if (!operator_dtype(dtype))
+        return fail(ADASUM_ERR_DTYPE, "dtype %d is not fp32, fp16 or bf16", (int)dtype);
+    const WorkLayout l = work_layout(rows, features, outputs, dtype);
+    if (!l.fits)
+        return fail(ADASUM_ERR_ARG, "invalid sizes");
+    if (l.units == 0)
+        return ADASUM_OK;                  // such a call launches no product
+    const uint32_t pairs = launch_pairs(l);
+    int words[2 * kMaxPairs] = {};
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+    ADASUM_CUDA_CHECK(cudaMemcpyAsync(words, workspace, 2 * pairs * sizeof(int), cudaMemcpyDeviceToHost, stream));
+    ADASUM_CUDA_CHECK(cudaStreamSynchronize(stream));
+    for (uint32_t i = 0; i < 2 * pairs; ++i)
+        if (words[i] == ADASUM_DEVICE_TIMEOUT)
+            return fail(ADASUM_ERR_TIMEOUT, "a bounded wait of block %u ran out", i);
     return ADASUM_OK;
 }
 
