@@ -13,10 +13,12 @@
 // as the slow one ("MN-major"), as they lie in memory; nothing is transposed.
 //
 //   G    one thread per block: bulk tensor copies of 64 outputs x 64 tokens, 128-byte swizzle, zeros
-//        beyond the matrix
-//   X    four warps per block: 16 codes per load, to the 16-bit type (exact: at most 7 significant bits
-//        times a power of two), to shared memory in the swizzled form the tensor core reads; loads run
-//        kAhead steps ahead in registers
+//        beyond the matrix; the codes of X (128 features x 64 tokens) come the same way, their step bytes,
+//        whose rows have no alignment, by ordinary loads of one warp
+//   X    four warps per block: 16 codes at a time from shared memory to the 16-bit type (exact: at most 7
+//        significant bits times a power of two) and back to shared memory in the swizzled form the tensor
+//        core reads.  (Codes loaded by these warps themselves, ahead of their use, were 3.5 times slower:
+//        the fence that makes their stores visible to the tensor core waits for every load on its way.)
 //   D    one thread of the pair's first block issues the multiplications; eight warps per block add the
 //        sums of every 256 tokens from tensor memory into fp32 registers
 //
@@ -43,17 +45,18 @@ constexpr int kHalf = 128;                       // features and outputs that a 
 constexpr int kTileSide = 256;                   // features and outputs of a pair's tile
 constexpr int kDepth = 64;                       // tokens per step
 constexpr int kChain = 4;                        // steps that are summed in tensor memory
-constexpr int kStages = 6;
-constexpr int kAhead = 3;                        // steps whose codes are on their way in registers
+constexpr int kStages = 7;                       // steps of gradients, codes and step bytes that are on their way
+constexpr int kDecoded = 3;                      // steps of decoded values
 constexpr int kPanelBytes = kDepth * 128;        // 64 features or outputs x 64 tokens, two bytes each
 constexpr int kOperandBytes = 2 * kPanelBytes;
-constexpr int kStageBytes = 2 * kOperandBytes;
+constexpr int kCodeBytes = kDepth * kHalf;
+constexpr int kStageBytes = kOperandBytes + kCodeBytes;          // gradients, then codes
 constexpr int kSumWarps = 8, kCodeWarps = 4;
 constexpr int kBlockThreads = 512;
-constexpr size_t kSharedBytes = (size_t)kStages * kStageBytes + 1024;       // + room to align to 1024
+constexpr size_t kSharedBytes = (size_t)kStages * kStageBytes + (size_t)kDecoded * kOperandBytes + 1024;   // + room to align to 1024
 constexpr int kMaxPairs = 74;                    // 148 multiprocessors
 constexpr int64_t kSlotFloats = (int64_t)kTileSide * kTileSide;
-constexpr uint32_t kWaitLimit = 1u << 22;        // about a tenth of a second; a real wait is microseconds
+constexpr long long kWaitCycles = 100000000;     // about a twentieth of a second; a real wait is microseconds
 
 struct WeightGradArgs {
     const int8_t* codes;
@@ -89,6 +92,29 @@ __device__ __forceinline__ void write_gradient(const WeightGradArgs& a, void* ds
     store_from_float(dst, a.out_dtype, e, y);
 }
 
+// A thread's column of a tile: one feature, 128 consecutive outputs.  Typed loops: the sums live in registers,
+// so every loop over them is unrolled, and a choice of type inside would be unrolled with it.
+template <typename TO>
+__device__ __forceinline__ void write_column(const WeightGradArgs& a, int64_t n, int64_t k, float (&sum)[128])
+{
+    TO* p = static_cast<TO*>(a.weight) + n * a.features + k;
+    const int count = (int)min((int64_t)128, a.outputs - n);
+    if (a.accumulate) {
+        const TO* q = p;
+#pragma unroll
+        for (int i = 0; i < 128; ++i, q += a.features)
+            sum[i] = fmaf(sum[i], a.scale, i < count ? load_one(q) : 0.0f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 128; ++i)
+            sum[i] *= a.scale;
+    }
+#pragma unroll
+    for (int i = 0; i < 128; ++i, p += a.features)
+        if (i < count)
+            store_from_float(p, TypeCode<TO>::value, 0, sum[i]);
+}
+
 // ---- instructions --------------------------------------------------------------------------------------
 
 __device__ __forceinline__ uint32_t shared_address(const void* p)
@@ -99,26 +125,27 @@ __device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count)
 {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
 }
-// Waits for the phase, with the ordering of the whole cluster (arrivals come from both blocks).
+// Returns false if the barrier does not complete the phase within kWaitCycles.
 __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity)
 {
-    for (uint32_t spin = 0; spin < kWaitLimit; ++spin) {
-        uint32_t done;
-        asm volatile("{\n\t.reg .pred p;\n\t"
-                     "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(done)
-                     : "r"(bar), "r"(parity)
-                     : "memory");
-        if (done)
+    long long began = 0;
+    for (uint32_t spin = 0;; ++spin) {
+        if (mbarrier_try_wait_parity(bar, parity))
             return true;
+        if ((spin & 255) == 0) {
+            const long long now = clock64();
+            if (spin == 0)
+                began = now;
+            else if (now - began > kWaitCycles)
+                return false;
+        }
     }
-    return false;
 }
 // Arrives on the same barrier of the pair's first block.
 __device__ __forceinline__ void arrive_at_first(uint32_t bar)
 {
     asm volatile("{\n\t.reg .b32 remote;\n\tmapa.shared::cluster.u32 remote, %0, 0;\n\t"
-                 "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [remote];\n\t}" ::"r"(bar)
+                 "mbarrier.arrive.shared::cluster.b64 _, [remote];\n\t}" ::"r"(bar)
                  : "memory");
 }
 __device__ __forceinline__ void expect_bytes(uint32_t bar, uint32_t bytes)
@@ -131,6 +158,12 @@ __device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, i
                  "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
                  : "memory");
 }
+__device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+                 "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar)
+                 : "memory");
+}
 __device__ __forceinline__ void cluster_barrier()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -141,6 +174,13 @@ __device__ __forceinline__ void commit_to_both(uint32_t bar)
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
                  "h"((uint16_t)3)
                  : "memory");
+}
+// One lane of a converged warp.  (With a lane number instead, the compiler cannot see that one thread issues.)
+__device__ __forceinline__ bool elected()
+{
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
 }
 template <int REGS>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS)); }
@@ -171,68 +211,143 @@ __device__ __forceinline__ void load_sums(uint32_t address, uint32_t (&r)[32])
 
 // ---- the codes of a step --------------------------------------------------------------------------------
 
-// Four codes to two words of the 16-bit type: byte + 128 in the low bits of 2^23, 2^23 + 128 taken off
-// (exact), times the step (exact in 16 bits too, see the format).
+// Two pairs of codes to two words of the 16-bit type, in that type (the packed instructions handle two values
+// and need no conversion at the end).
+//
+// bf16: a code's low seven bits l go into the last place of 128 + l, its sign bit b selects 128 + 128 b, and
+// the difference is the code; both are exact, and so is the product with a power of two between 2^-126 and
+// 2^121.
+//
+// fp16: code + 128 in the last place of 1024, 1152 taken off.  The step may be outside fp16's range while the
+// product is inside, so it is multiplied in two factors, each at most 2^15 and the first at least 2^-14: the
+// first product is exact or overflows only if the whole does; the second is the one rounding.
 template <typename T>
-__device__ __forceinline__ uint2 decode_four(uint32_t packed, float step)
-{
-    const uint32_t u = packed ^ 0x80808080u;
-    float x[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        x[i] = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7540 + i)) - 8388736.0f) * step;
-    uint2 w;
-    if constexpr (__is_same(T, __half)) {
-        const __half2 a = __floats2half2_rn(x[0], x[1]), b = __floats2half2_rn(x[2], x[3]);
-        w.x = *reinterpret_cast<const uint32_t*>(&a);
-        w.y = *reinterpret_cast<const uint32_t*>(&b);
-    } else {
-        const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
-        w.x = *reinterpret_cast<const uint32_t*>(&a);
-        w.y = *reinterpret_cast<const uint32_t*>(&b);
-    }
-    return w;
-}
-
-// Where a pair stands in its run of units.
-struct Cursor {
-    uint32_t unit, tile, it, it_end;
-    __device__ __forceinline__ void enter(const WeightGradArgs& a)
+struct Decoder;
+template <>
+struct Decoder<__nv_bfloat16> {
+    __nv_bfloat162 step;
+    __device__ __forceinline__ explicit Decoder(uint32_t byte)
     {
-        tile = unit / a.chains;
-        it = (unit - tile * a.chains) * kChain;
-        it_end = min(it + kChain, a.iterations);
+        const uint32_t w = byte * 0x00800080u;           // the exponent field of either half
+        step = *reinterpret_cast<const __nv_bfloat162*>(&w);
+    }
+    __device__ __forceinline__ uint32_t pair(uint32_t packed, uint32_t selector) const
+    {
+        const uint32_t w = __byte_perm(packed, 0x43434343u, selector);
+        const uint32_t low = w & 0xff7fff7fu, sign = w & 0xff80ff80u;
+        const __nv_bfloat162 x = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&low),
+                                                 *reinterpret_cast<const __nv_bfloat162*>(&sign)),
+                                         step);
+        return *reinterpret_cast<const uint32_t*>(&x);
+    }
+    __device__ __forceinline__ uint2 four(uint32_t packed) const
+    {
+        return make_uint2(pair(packed, 0x4140), pair(packed, 0x4342));
+    }
+};
+template <>
+struct Decoder<__half> {
+    __half2 first, second;
+    __device__ __forceinline__ explicit Decoder(uint32_t byte)
+    {
+        // 2^(byte - 127) = first * second; 255 (NaN) must stay NaN, 0 (beyond the matrix) be zero
+        const int e = (int)byte - 127, a = max(-14, min(15, e)), b = max(-25, min(15, e - a));
+        const float f = byte == 255u ? __uint_as_float(0x7fc00000u) : byte == 0u ? 0.0f : __uint_as_float((uint32_t)(a + 127) << 23);
+        first = __float2half2_rn(f);
+        second = __float2half2_rn(__uint_as_float((uint32_t)(b + 127) << 23));
+    }
+    __device__ __forceinline__ uint32_t pair(uint32_t biased, uint32_t selector) const
+    {
+        const uint32_t w = __byte_perm(biased, 0x64646464u, selector);
+        const uint32_t offset = 0x64806480u;             // 1024 + 128
+        const __half2 q = __hsub2(*reinterpret_cast<const __half2*>(&w), *reinterpret_cast<const __half2*>(&offset));
+        const __half2 x = __hmul2(__hmul2(q, first), second);
+        return *reinterpret_cast<const uint32_t*>(&x);
+    }
+    __device__ __forceinline__ uint2 four(uint32_t packed) const
+    {
+        const uint32_t biased = packed ^ 0x80808080u;
+        return make_uint2(pair(biased, 0x4140), pair(biased, 0x4342));
+    }
+};
+
+// Where a role stands in its pair's run of units.
+struct Cursor {
+    uint32_t unit, chain, tile_k, tile_n;
+    __device__ __forceinline__ Cursor(const WeightGradArgs& a, uint32_t begin) : unit(begin)
+    {
+        const uint32_t tile = begin / a.chains;
+        chain = begin - tile * a.chains;
+        tile_n = tile / a.tiles_k;
+        tile_k = tile - tile_n * a.tiles_k;
+    }
+    __device__ __forceinline__ uint32_t first_step() const { return chain * kChain; }
+    __device__ __forceinline__ uint32_t steps(const WeightGradArgs& a) const
+    {
+        return min((uint32_t)kChain, a.iterations - chain * kChain);
     }
     __device__ __forceinline__ void advance(const WeightGradArgs& a)
     {
-        if (++it == it_end) {
-            ++unit;
-            enter(a);
+        ++unit;
+        if (++chain == a.chains) {
+            chain = 0;
+            if (++tile_k == a.tiles_k) {
+                tile_k = 0;
+                ++tile_n;
+            }
         }
     }
 };
 
-// One thread's part of a step: four rows (tokens), 16 features each.
-struct CodeLoad {
-    uint4 codes[4];
-    uint32_t step[4];
+// A position in a ring of N stages and the parity of its current round.
+template <int N>
+struct Ring {
+    uint32_t stage = 0, phase = 0;
+    __device__ __forceinline__ void advance()
+    {
+        if (++stage == N) {
+            stage = 0;
+            phase ^= 1;
+        }
+    }
 };
+
+// Step bytes of one row (token) for the block's 128 features, zeros beyond the matrix.
+__device__ __forceinline__ uint32_t load_steps(const uint8_t* steps, int64_t groups, int64_t rows, int64_t row, int64_t group)
+{
+    if (row >= rows || group >= groups)
+        return 0;
+    const uint8_t* p = steps + row * groups + group;
+    if ((groups & 3) == 0)               // every row starts on a word: the table itself does too
+        return __ldg(reinterpret_cast<const uint32_t*>(p));
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (group + i < groups)
+            w |= (uint32_t)__ldg(p + i) << (8 * i);
+    return w;
+}
 
 // ---- kernel ---------------------------------------------------------------------------------------------
 //
 // T: 16-bit type of both operands.  PLANES: 1, or 3 for fp32 gradients, which arrive as three bf16 matrices
 // that add up to them; a step then is one plane of one block of tokens, planes fastest.
-// Warps 0 .. 7 sum, 8 .. 11 decode, 12 copies, 13 multiplies (first block only), 14 owns the tensor memory.
-// Registers: 256 x 184 + 128 x 104 + 128 x 40 = 512 x 128.
+// Warps 0 .. 7 sum, 8 .. 11 decode, 12 copies, 13 multiplies (first block only), 14 owns the tensor memory,
+// 15 loads step bytes.
+// Registers: 256 x 184 + 128 x 80 + 128 x 64 = 512 x 128.
 template <typename T, int PLANES, bool BIAS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kBlockThreads, 1)
-weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_constant__ CUtensorMap grad_map)
+weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_constant__ CUtensorMap grad_map,
+                   const __grid_constant__ CUtensorMap code_map)
 {
     extern __shared__ __align__(1024) unsigned char dynamic_shared[];
-    // landed: this block's copies of a step are there.  ready (first block): both blocks' operands are there.
-    // empty: the step has been multiplied (and, with BIAS, added up by the eight sum warps).
-    // formed / taken (first block): a sum in tensor memory is complete / has been read by both blocks.
-    __shared__ __align__(8) unsigned long long landed[kStages], ready[kStages], empty[kStages], formed[2], taken[2];
+    // landed: this block's gradients, codes and step bytes of a step are there; multiplied: the tensor cores
+    // are done with the step; added (BIAS): the sum warps are done with its gradients.  ready (first block):
+    // both blocks' decoded values are there, and their gradients.
+    // formed: a sum in tensor memory is complete; taken (first block): it has been read by both blocks.
+    __shared__ __align__(8) unsigned long long landed[kStages], multiplied[kStages], added[kStages], ready[kDecoded],
+        formed[2], taken[2];
+    __shared__ uint32_t step_words[kStages][kDepth];         // four step bytes per token
     __shared__ uint32_t tensor_memory_slot;
     __shared__ float bias_part[4][kHalf];
 
@@ -240,16 +355,20 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
     const uint32_t rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const uint32_t unit_begin = first_unit(a.units, pairs, pair), unit_end = first_unit(a.units, pairs, pair + 1);
     const uint32_t stage0 = (shared_address(dynamic_shared) + 1023u) & ~1023u;
-    const uint32_t landed0 = shared_address(landed), ready0 = shared_address(ready), empty0 = shared_address(empty);
+    const uint32_t decoded0 = stage0 + kStages * kStageBytes;
+    const uint32_t landed0 = shared_address(landed), ready0 = shared_address(ready);
+    const uint32_t multiplied0 = shared_address(multiplied), added0 = shared_address(added);
     const uint32_t formed0 = shared_address(formed), taken0 = shared_address(taken);
 
     if (threadIdx.x == 0) {
         a.status[blockIdx.x] = 0;
         for (int s = 0; s < kStages; ++s) {
-            barrier_init(landed0 + 8 * s, 1);
-            barrier_init(ready0 + 8 * s, 2 * kCodeWarps);
-            barrier_init(empty0 + 8 * s, BIAS ? 1 + kSumWarps : 1);
+            barrier_init(landed0 + 8 * s, 2);
+            barrier_init(multiplied0 + 8 * s, 1);
+            barrier_init(added0 + 8 * s, kSumWarps);
         }
+        for (int s = 0; s < kDecoded; ++s)
+            barrier_init(ready0 + 8 * s, 2 * kCodeWarps);
         for (int s = 0; s < 2; ++s) {
             barrier_init(formed0 + 8 * s, 1);
             barrier_init(taken0 + 8 * s, 2 * kSumWarps);
@@ -281,13 +400,13 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
         const int quarter = warp & 3, side = warp >> 2;
         float sum[128];
         float bias_sum[2] = {0.0f, 0.0f};
-        uint32_t stage = 0, phase = 0, count = 0;
-        uint32_t chain_begin = 0;
-        for (uint32_t unit = unit_begin; unit < unit_end; ++unit, ++count) {
-            const uint32_t tile = unit / a.chains, chain = unit - tile * a.chains;
-            const uint32_t tile_k = tile % a.tiles_k, tile_n = tile / a.tiles_k;
-            if (unit == unit_begin || chain == 0) {
-                chain_begin = chain;
+        Ring<kStages> ring;
+        uint32_t count = 0, chain_begin = 0;
+        uint32_t which = 0;                      // 0: the first tile of the pair's run, 1: a later one
+        for (Cursor c(a, unit_begin); c.unit < unit_end; c.advance(a), ++count) {
+            if (c.unit == unit_begin || c.chain == 0) {
+                which = c.unit == unit_begin ? 0 : 1;
+                chain_begin = c.chain;
                 bias_sum[0] = bias_sum[1] = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 128; ++i)
@@ -296,13 +415,13 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
             if constexpr (BIAS) {
                 // this block's 128 outputs: thread = two outputs, 16 of a step's 64 tokens.  Summed per
                 // unit, like the products.
-                const uint32_t steps = min((uint32_t)kChain, a.iterations - chain * kChain);
+                const uint32_t steps = c.steps(a);
                 const int output = 2 * (threadIdx.x & 63), part = threadIdx.x >> 6;
                 float unit_sum[2] = {0.0f, 0.0f};
                 for (uint32_t s = 0; s < steps; ++s) {
-                    wait(landed0 + 8 * stage, phase);
-                    if (tile_k == 0) {
-                        const uint32_t panel = stage0 + stage * kStageBytes + kOperandBytes + (output >> 6) * kPanelBytes;
+                    wait(landed0 + 8 * ring.stage, ring.phase);
+                    if (c.tile_k == 0) {
+                        const uint32_t panel = stage0 + ring.stage * kStageBytes + (output >> 6) * kPanelBytes;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const int row = part * 16 + i;
@@ -323,11 +442,8 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                     }
                     __syncwarp();
                     if (lane == 0)
-                        mbarrier_arrive(empty0 + 8 * stage);
-                    if (++stage == kStages) {
-                        stage = 0;
-                        phase ^= 1;
-                    }
+                        mbarrier_arrive(added0 + 8 * ring.stage);
+                    ring.advance();
                 }
                 bias_sum[0] += unit_sum[0];
                 bias_sum[1] += unit_sum[1];
@@ -349,20 +465,22 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
             if (lane == 0)
                 arrive_at_first(taken0 + 8 * (count & 1));
 
-            if (chain + 1 != a.chains && unit + 1 != unit_end)
+            if (c.chain + 1 != a.chains && c.unit + 1 != unit_end)
                 continue;
             // ---- the pair's last unit of this tile: the result, or this pair's part of it
-            const bool whole = chain_begin == 0 && chain + 1 == a.chains;
-            const uint32_t slot = 2 * pair + (tile == unit_begin / a.chains ? 0 : 1);
+            const bool whole = chain_begin == 0 && c.chain + 1 == a.chains;
+            const uint32_t slot = 2 * pair + which;
             const int feature = 32 * quarter + lane;
             if (whole) {
-                const int64_t k = (int64_t)tile_k * kTileSide + rank * kHalf + feature;
-                const int64_t n = (int64_t)tile_n * kTileSide + side * kHalf;
+                const int64_t k = (int64_t)c.tile_k * kTileSide + rank * kHalf + feature;
+                const int64_t n = (int64_t)c.tile_n * kTileSide + side * kHalf;
                 if (k < a.features) {
-#pragma unroll
-                    for (int i = 0; i < 128; ++i)
-                        if (n + i < a.outputs)
-                            write_gradient(a, a.weight, (n + i) * a.features + k, sum[i]);
+                    if (a.out_dtype == ADASUM_F32)
+                        write_column<float>(a, n, k, sum);
+                    else if (a.out_dtype == ADASUM_F16)
+                        write_column<__half>(a, n, k, sum);
+                    else
+                        write_column<__nv_bfloat16>(a, n, k, sum);
                 }
             } else {
                 float* dst = a.slots + slot * kSlotFloats + (rank * kTileSide + side * kHalf) * kHalf + feature;
@@ -371,7 +489,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                     dst[i * kHalf] = sum[i];
             }
             if constexpr (BIAS) {
-                if (tile_k == 0) {
+                if (c.tile_k == 0) {
                     const int output = 2 * (threadIdx.x & 63), part = threadIdx.x >> 6;
                     bias_part[part][output] = bias_sum[0];
                     bias_part[part][output + 1] = bias_sum[1];
@@ -379,7 +497,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                     if (threadIdx.x < kHalf) {
                         const float total = (bias_part[0][threadIdx.x] + bias_part[1][threadIdx.x]) +
                                             (bias_part[2][threadIdx.x] + bias_part[3][threadIdx.x]);
-                        const int64_t n = (int64_t)tile_n * kTileSide + rank * kHalf + threadIdx.x;
+                        const int64_t n = (int64_t)c.tile_n * kTileSide + rank * kHalf + threadIdx.x;
                         if (!whole)
                             a.bias_slots[(int64_t)slot * kTileSide + rank * kHalf + threadIdx.x] = total;
                         else if (n < a.outputs)
@@ -390,108 +508,81 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
             }
         }
     } else if (warp < kSumWarps + kCodeWarps) {
-        // ---- codes: a lane holds 16 features (one load) of four rows; a warp's load covers four rows of 128
-        // codes, and any eight neighbouring lanes write 16-byte pieces of eight different bank groups
-        fewer_registers<104>();
-        const int piece = (lane & 3) | ((lane >> 4) & 1) << 2;
-        const int row0 = ((lane >> 2) & 3) + 4 * (warp - kSumWarps);
-        const int64_t groups = a.width / kGroup;
-        auto load = [&](const Cursor& c, CodeLoad& l) {
-            const int64_t k = (int64_t)(c.tile % a.tiles_k) * kTileSide + rank * kHalf + piece * 16;
-            const int64_t t0 = (int64_t)(c.it / PLANES) * kDepth + row0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t t = t0 + 16 * i;
-                if (t < a.rows && k < a.width) {
-                    l.codes[i] = load_keep_16B(a.codes + t * a.width + k);
-                    l.step[i] = __ldg(a.steps + t * groups + k / kGroup);
+        // ---- codes: a lane decodes 16 features of four rows (tokens).  Of eight neighbouring lanes four hold the
+        // first panel's pieces of one row and four the second's of the row's neighbour: their reads, and then
+        // both of their writes, fall on eight different groups of banks.
+        fewer_registers<80>();
+        const int piece = lane & 7, upper = piece >> 2;
+        const int row0 = ((lane >> 3) + 4 * (warp - kSumWarps)) ^ upper;
+        const uint32_t from = row0 * kHalf + ((piece ^ (row0 & 7)) << 4);
+        const uint32_t to = upper * kPanelBytes + row0 * 128 + (((2 * (piece & 3)) ^ (row0 & 7)) << 4);
+        Ring<kStages> ring, behind;              // behind: the step whose place among the decoded ones is taken next
+        Ring<kDecoded> out;
+        int filling = kDecoded;                  // places that are still free
+        for (Cursor c(a, unit_begin); c.unit < unit_end; c.advance(a)) {
+            for (uint32_t steps = c.steps(a); steps > 0; --steps) {
+                if (filling > 0) {
+                    --filling;
                 } else {
-                    l.codes[i] = make_uint4(0, 0, 0, 0);
-                    l.step[i] = 0;
+                    wait(multiplied0 + 8 * behind.stage, behind.phase);
+                    behind.advance();
                 }
-            }
-        };
-        uint32_t stage = 0, phase = 0;
-        auto store = [&](const CodeLoad& l) {
-            wait(empty0 + 8 * stage, phase ^ 1);
-            const uint32_t panel = stage0 + stage * kStageBytes + (piece >> 2) * kPanelBytes;
+                wait(landed0 + 8 * ring.stage, ring.phase);
+                const uint32_t source = stage0 + ring.stage * kStageBytes + kOperandBytes + from;
+                const uint32_t target = decoded0 + out.stage * kOperandBytes + to;
+                uint4 codes[4];
+                uint32_t words[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = row0 + 16 * i;
-                const float step = __uint_as_float(l.step[i] << 23);
-                const uint2 w0 = decode_four<T>(l.codes[i].x, step), w1 = decode_four<T>(l.codes[i].y, step);
-                const uint2 w2 = decode_four<T>(l.codes[i].z, step), w3 = decode_four<T>(l.codes[i].w, step);
-                const int at = 2 * (piece & 3);
-                store_shared_16B(panel + row * 128 + ((at ^ (row & 7)) << 4), make_uint4(w0.x, w0.y, w1.x, w1.y));
-                store_shared_16B(panel + row * 128 + (((at + 1) ^ (row & 7)) << 4), make_uint4(w2.x, w2.y, w3.x, w3.y));
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) {
-                wait(landed0 + 8 * stage, phase);
-                arrive_at_first(ready0 + 8 * stage);
-            }
-            __syncwarp();
-            if (++stage == kStages) {
-                stage = 0;
-                phase ^= 1;
-            }
-        };
-        if (unit_begin < unit_end) {
-            CodeLoad l[kAhead];
-            Cursor c;
-            c.unit = unit_begin;
-            c.enter(a);
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                if (c.unit < unit_end) {
-                    load(c, l[j]);
-                    c.advance(a);
+                for (int i = 0; i < 4; ++i) {
+                    codes[i] = load_shared_16B(source + 16 * i * kHalf);
+                    words[i] = step_words[ring.stage][row0 + 16 * i];
                 }
-            }
-            // steps of the run: whole units but for the last unit of a tile
-            uint32_t steps = 0;
-            for (Cursor d{unit_begin, 0, 0, 0}; d.unit < unit_end; ++d.unit) {
-                d.enter(a);
-                steps += d.it_end - d.it;
-            }
-            for (uint32_t s = 0; s < steps; s += kAhead) {
 #pragma unroll
-                for (int j = 0; j < kAhead; ++j) {
-                    if (s + j < steps) {
-                        store(l[j]);
-                        if (c.unit < unit_end) {
-                            load(c, l[j]);
-                            c.advance(a);
-                        }
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    const Decoder<T> decode((words[i] >> (8 * (piece >> 1))) & 0xffu);
+                    const uint2 w0 = decode.four(codes[i].x), w1 = decode.four(codes[i].y);
+                    const uint2 w2 = decode.four(codes[i].z), w3 = decode.four(codes[i].w);
+                    store_shared_16B(target + 16 * i * 128, make_uint4(w0.x, w0.y, w1.x, w1.y));
+                    store_shared_16B((target ^ 16) + 16 * i * 128, make_uint4(w2.x, w2.y, w3.x, w3.y));
                 }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0)
+                    arrive_at_first(ready0 + 8 * out.stage);
+                ring.advance();
+                out.advance();
             }
         }
     } else {
-        fewer_registers<40>();
-        if (warp == 12 && lane == 0) {
-            // ---- copies of this block's half of the gradients
-            uint32_t stage = 0, phase = 0, issued = 0;
-            for (uint32_t unit = unit_begin; unit < unit_end && waiting; ++unit) {
-                Cursor c;
-                c.unit = unit;
-                c.enter(a);
-                const int n = (int)(c.tile / a.tiles_k) * kTileSide + (int)rank * kHalf;
-                for (; c.it < c.it_end; ++c.it) {
-                    wait(empty0 + 8 * stage, phase ^ 1);
+        fewer_registers<64>();
+        if (warp == 12) {
+            // ---- copies of this block's half of the gradients, and of the codes
+            Ring<kStages> ring;
+            uint32_t issued = 0;
+            const uint32_t bytes = kOperandBytes + (a.width > 0 ? kCodeBytes : 0);
+            for (Cursor c(a, unit_begin); c.unit < unit_end && waiting; c.advance(a)) {
+                const int n = (int)c.tile_n * kTileSide + (int)rank * kHalf, k = (int)c.tile_k * kTileSide + (int)rank * kHalf;
+                const uint32_t end = c.first_step() + c.steps(a);
+                for (uint32_t step = c.first_step(); step < end; ++step) {
+                    const uint32_t bar = landed0 + 8 * ring.stage;
+                    wait(multiplied0 + 8 * ring.stage, ring.phase ^ 1);
+                    if constexpr (BIAS)
+                        wait(added0 + 8 * ring.stage, ring.phase ^ 1);
+                    waiting = __all_sync(0xffffffffu, waiting);
                     if (!waiting)
                         break;
-                    const uint32_t dst = stage0 + stage * kStageBytes + kOperandBytes;
-                    const int t = (int)(c.it / PLANES) * kDepth, plane = (int)(c.it % PLANES);
-                    expect_bytes(landed0 + 8 * stage, kOperandBytes);
-                    copy_box(dst, &grad_map, n, t, plane, landed0 + 8 * stage);
-                    copy_box(dst + kPanelBytes, &grad_map, n + 64, t, plane, landed0 + 8 * stage);
-                    ++issued;
-                    if (++stage == kStages) {
-                        stage = 0;
-                        phase ^= 1;
+                    const uint32_t dst = stage0 + ring.stage * kStageBytes;
+                    const int t = (int)(step / PLANES) * kDepth, plane = (int)(step % PLANES);
+                    if (elected()) {
+                        expect_bytes(bar, bytes);
+                        copy_box(dst, &grad_map, n, t, plane, bar);
+                        copy_box(dst + kPanelBytes, &grad_map, n + 64, t, plane, bar);
+                        if (a.width > 0)
+                            copy_box(dst + kOperandBytes, &code_map, k, t, bar);
                     }
+                    __syncwarp();
+                    ++issued;
+                    ring.advance();
                 }
             }
             // nothing may still be on its way into shared memory when the block ends
@@ -500,40 +591,81 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                 const uint32_t step = issued - back;
                 wait(landed0 + 8 * (step % kStages), (step / kStages) & 1);
             }
-        } else if (warp == 13 && lane == 0 && rank == 0) {
+        } else if (warp == 13 && rank == 0) {
             // ---- multiplications: fp32 sums, both operands of type T with the summed index slow, 256 x 256
             constexpr uint32_t kFormat = __is_same(T, __half) ? 0u : 1u;
             constexpr uint32_t kInstruction = (1u << 4) | (kFormat << 7) | (kFormat << 10) | (1u << 15) | (1u << 16) |
                                               ((kTileSide >> 3) << 17) | ((kTileSide >> 4) << 24);
-            uint32_t stage = 0, phase = 0, count = 0;
-            for (uint32_t unit = unit_begin; unit < unit_end; ++unit, ++count) {
-                Cursor c;
-                c.unit = unit;
-                c.enter(a);
+            Ring<kStages> ring;
+            Ring<kDecoded> in;
+            uint32_t count = 0;
+            for (Cursor c(a, unit_begin); c.unit < unit_end; c.advance(a), ++count) {
                 const uint32_t target = tensor_memory + (count & 1) * 256;
                 wait(taken0 + 8 * (count & 1), ((count >> 1) & 1) ^ 1);
                 uint32_t accumulate = 0;
-                for (; c.it < c.it_end; ++c.it) {
-                    wait(ready0 + 8 * stage, phase);
+                for (uint32_t steps = c.steps(a); steps > 0; --steps) {
+                    wait(ready0 + 8 * in.stage, in.phase);
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t base = stage0 + stage * kStageBytes;
+                    const uint64_t x = operand_descriptor(decoded0 + in.stage * kOperandBytes);
+                    const uint64_t g = operand_descriptor(stage0 + ring.stage * kStageBytes);
+                    if (elected()) {
 #pragma unroll
-                    for (int s = 0; s < kDepth / 16; ++s) {
-                        const uint64_t x = operand_descriptor(base + s * 2048);
-                        const uint64_t g = operand_descriptor(base + kOperandBytes + s * 2048);
-                        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(target),
-                                     "l"(x), "l"(g), "r"(kInstruction), "r"(accumulate)
-                                     : "memory");
-                        accumulate = 1;
+                        for (int s = 0; s < kDepth / 16; ++s) {
+                            // 16 tokens are 2048 bytes further on: 128 in the descriptors' units
+                            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                                         "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(target),
+                                         "l"(x + 128 * s), "l"(g + 128 * s), "r"(kInstruction), "r"(s > 0 ? 1u : accumulate)
+                                         : "memory");
+                        }
+                        commit_to_both(multiplied0 + 8 * ring.stage);
+                        if (steps == 1)
+                            commit_to_both(formed0 + 8 * (count & 1));
                     }
-                    commit_to_both(empty0 + 8 * stage);
-                    if (++stage == kStages) {
-                        stage = 0;
-                        phase ^= 1;
+                    __syncwarp();
+                    accumulate = 1;
+                    ring.advance();
+                    in.advance();
+                }
+            }
+        } else if (warp == 15) {
+            // ---- step bytes: a lane loads two rows per step, a whole unit ahead of their use
+            const int64_t groups = a.width / kGroup;
+            uint32_t w[kChain][2];
+            Ring<kStages> ring;
+            auto load = [&](const Cursor& c) {
+                const int64_t group = (int64_t)c.tile_k * (kTileSide / kGroup) + rank * (kHalf / kGroup);
+#pragma unroll
+                for (int j = 0; j < kChain; ++j) {
+                    const int64_t t = (int64_t)((c.first_step() + j) / PLANES) * kDepth + lane;
+                    w[j][0] = load_steps(a.steps, groups, a.rows, t, group);
+                    w[j][1] = load_steps(a.steps, groups, a.rows, t + 32, group);
+                }
+            };
+            Cursor c(a, unit_begin);
+            load(c);
+            while (c.unit < unit_end) {
+                uint32_t v[kChain][2];
+#pragma unroll
+                for (int j = 0; j < kChain; ++j) {
+                    v[j][0] = w[j][0];
+                    v[j][1] = w[j][1];
+                }
+                const uint32_t steps = c.steps(a);
+                c.advance(a);
+                if (c.unit < unit_end)
+                    load(c);
+#pragma unroll
+                for (int j = 0; j < kChain; ++j) {
+                    if (j < (int)steps) {
+                        wait(multiplied0 + 8 * ring.stage, ring.phase ^ 1);
+                        step_words[ring.stage][lane] = v[j][0];
+                        step_words[ring.stage][lane + 32] = v[j][1];
+                        __syncwarp();
+                        if (lane == 0)
+                            mbarrier_arrive(landed0 + 8 * ring.stage);
+                        ring.advance();
                     }
                 }
-                commit_to_both(formed0 + 8 * (count & 1));
             }
         }
         __syncwarp();
@@ -546,13 +678,13 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tensor_memory) : "memory");
 }
 
-// Tiles whose units fell to several pairs: the pairs' parts added in order.  grid.x = tiles, grid.y = eighths
-// of the tile's outputs; thread = one feature of each block, every second output.
+// Tiles whose units fell to several pairs: the pairs' parts added in order.  grid.x = tiles, grid.y = parts of
+// the tile's 2 x 256 rows of 128 features; one warp per row, four features per lane.
 constexpr int kJoinThreads = 256;
-constexpr int kJoinOutputs = 32;
+constexpr int kJoinParts = 2 * kTileSide / (kJoinThreads / 32);
 
 __global__ void __launch_bounds__(kJoinThreads)
-weight_grad_join_kernel(const __grid_constant__ WeightGradArgs a, uint32_t pairs)
+weight_grad_join_kernel(const __grid_constant__ WeightGradArgs a, uint32_t pairs, bool vec)
 {
     const uint32_t tile = blockIdx.x;
     const uint32_t first = pair_of_unit(a.units, pairs, tile * a.chains);
@@ -560,34 +692,45 @@ weight_grad_join_kernel(const __grid_constant__ WeightGradArgs a, uint32_t pairs
     if (first == last)
         return;                      // written by the product itself
     const uint32_t tile_k = tile % a.tiles_k, tile_n = tile / a.tiles_k;
-    const int feature = threadIdx.x;
-    const int64_t k = (int64_t)tile_k * kTileSide + feature;
-    const float* source = a.slots + ((int64_t)(feature >> 7) * kTileSide) * kHalf + (feature & 127);
-    auto slot_of = [&](uint32_t pair) {
-        return 2 * pair + (tile == first_unit(a.units, pairs, pair) / a.chains ? 0 : 1);
-    };
-    for (int o = blockIdx.y * kJoinOutputs; o < (int)(blockIdx.y + 1) * kJoinOutputs; o += 8) {
-        float sum[8] = {};
-        for (uint32_t pair = first; pair <= last; ++pair) {
-            const float* s = source + slot_of(pair) * kSlotFloats;
+    // only the first pair's run can have started in an earlier tile
+    const uint32_t first_slot = 2 * first + (tile == first_unit(a.units, pairs, first) / a.chains ? 0 : 1);
+    auto slot_of = [&](uint32_t pair) { return pair == first ? first_slot : 2 * pair; };
+    const int row = blockIdx.y * (kJoinThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const float* source = a.slots + (int64_t)row * kHalf + 4 * lane;
+    float sum[4] = {};
+#pragma unroll 4
+    for (uint32_t pair = first; pair <= last; ++pair) {
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(source + slot_of(pair) * kSlotFloats));
+        sum[0] += v.x;
+        sum[1] += v.y;
+        sum[2] += v.z;
+        sum[3] += v.w;
+    }
+    const int64_t n = (int64_t)tile_n * kTileSide + (row & (kTileSide - 1));
+    const int64_t k = (int64_t)tile_k * kTileSide + (row / kTileSide) * kHalf + 4 * lane;
+    if (n < a.outputs && k < a.features) {
+        const int64_t e = n * a.features + k;
+        if (vec) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                sum[i] += s[(o + i) * kHalf];
-        }
+            for (int i = 0; i < 4; ++i)
+                sum[i] *= a.scale;
+            if (a.accumulate)
+                add_vector_as_float<4>(a.weight, a.out_dtype, e, sum);
+            store_vector_from_float<4>(a.weight, a.out_dtype, e, sum);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int64_t n = (int64_t)tile_n * kTileSide + o + i;
-            if (n < a.outputs && k < a.features)
-                write_gradient(a, a.weight, n * a.features + k, sum[i]);
+            for (int i = 0; i < 4; ++i)
+                if (k + i < a.features)
+                    write_gradient(a, a.weight, e + i, sum[i]);
         }
     }
     if (a.bias && tile_k == 0 && blockIdx.y == 0) {
-        const int64_t n = (int64_t)tile_n * kTileSide + threadIdx.x;
-        float sum = 0.0f;
+        const int64_t bias_n = (int64_t)tile_n * kTileSide + threadIdx.x;
+        float total = 0.0f;
         for (uint32_t pair = first; pair <= last; ++pair)
-            sum += a.bias_slots[(int64_t)slot_of(pair) * kTileSide + threadIdx.x];
-        if (n < a.outputs)
-            write_gradient(a, a.bias, n, sum);
+            total += a.bias_slots[(int64_t)slot_of(pair) * kTileSide + threadIdx.x];
+        if (bias_n < a.outputs)
+            write_gradient(a, a.bias, bias_n, total);
     }
 }
 
@@ -704,6 +847,20 @@ EncodeTiled encode_tiled()
     return cached;
 }
 
+// The codes of a checkpoint: [rows][width] bytes.
+adasum_status_t describe_codes(CUtensorMap* map, const void* codes, int64_t width, int64_t rows)
+{
+    EncodeTiled encode = encode_tiled();
+    if (!encode)
+        return fail(ADASUM_ERR_CUDA, "the driver has no tensor map encoder");
+    const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)width};
+    const cuuint32_t box[2] = {kHalf, kDepth}, unit[2] = {1, 1};
+    const CUresult err = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(codes), dims, strides, box, unit,
+                                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return err == CUDA_SUCCESS ? ADASUM_OK : fail(ADASUM_ERR_CUDA, "tensor map of the codes: error %d", (int)err);
+}
+
 adasum_status_t describe_gradients(CUtensorMap* map, const void* base, adasum_dtype_t type, int64_t outputs, int64_t rows,
                                    int64_t planes, int64_t pitch)
 {
@@ -721,17 +878,17 @@ adasum_status_t describe_gradients(CUtensorMap* map, const void* base, adasum_dt
 }
 
 template <typename T, int PLANES, bool BIAS>
-cudaError_t launch_product(const WeightGradArgs& a, const CUtensorMap& map, uint32_t pairs, cudaStream_t stream)
+cudaError_t launch_product(const WeightGradArgs& a, const CUtensorMap (&map)[2], uint32_t pairs, cudaStream_t stream)
 {
     auto* kernel = weight_grad_kernel<T, PLANES, BIAS>;
     const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedBytes);
     if (err != cudaSuccess)
         return err;
-    kernel<<<2 * pairs, kBlockThreads, kSharedBytes, stream>>>(a, map);
+    kernel<<<2 * pairs, kBlockThreads, kSharedBytes, stream>>>(a, map[0], map[1]);
     return cudaGetLastError();
 }
 template <typename T, int PLANES>
-cudaError_t launch_product(const WeightGradArgs& a, const CUtensorMap& map, uint32_t pairs, cudaStream_t stream)
+cudaError_t launch_product(const WeightGradArgs& a, const CUtensorMap (&map)[2], uint32_t pairs, cudaStream_t stream)
 {
     return a.bias ? launch_product<T, PLANES, true>(a, map, pairs, stream)
                   : launch_product<T, PLANES, false>(a, map, pairs, stream);
@@ -830,10 +987,12 @@ adasum_status_t adasum_checkpoint_weight_grad(const void* checkpoint, int64_t ro
     // 16-byte rows are copied as they lie; others, and fp32, are laid out in the workspace first
     const bool relay = dtype == ADASUM_F32 || !rows_aligned(grad_out, grad_out_stride, eb);
     const int64_t planes = dtype == ADASUM_F32 ? 3 : 1;
-    CUtensorMap map;
-    const adasum_status_t described =
-        describe_gradients(&map, relay ? ws + l.gradients : grad_out, dtype == ADASUM_F16 ? ADASUM_F16 : ADASUM_BF16,
+    CUtensorMap map[2] = {};               // gradients; codes, if there are any
+    adasum_status_t described =
+        describe_gradients(&map[0], relay ? ws + l.gradients : grad_out, dtype == ADASUM_F16 ? ADASUM_F16 : ADASUM_BF16,
                            outputs, rows, planes, relay ? l.pitch : grad_out_stride);
+    if (described == ADASUM_OK && features > 0)
+        described = describe_codes(&map[1], checkpoint, (features + kGroup - 1) / kGroup * kGroup, rows);
     if (described != ADASUM_OK)
         return described;
     WeightGradArgs a;
@@ -875,7 +1034,8 @@ adasum_status_t adasum_checkpoint_weight_grad(const void* checkpoint, int64_t ro
     for (uint32_t p = 1; p < pairs && !split; ++p)
         split = first_unit(l.units, pairs, p) % l.chains != 0;
     if (split) {
-        weight_grad_join_kernel<<<dim3(l.tiles, kTileSide / kJoinOutputs), kJoinThreads, 0, stream>>>(a, pairs);
+        const bool vec = aligned_to(grad_weight, 16) && features % 4 == 0;
+        weight_grad_join_kernel<<<dim3(l.tiles, kJoinParts), kJoinThreads, 0, stream>>>(a, pairs, vec);
         ADASUM_CUDA_CHECK(cudaGetLastError());
         profile_mark(stream, ADASUM_KERNEL_WEIGHT_GRAD, 2, 0, false);
     }
