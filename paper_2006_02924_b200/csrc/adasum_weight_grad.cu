@@ -15,7 +15,7 @@
 //   G    one thread per block: bulk tensor copies of 64 outputs x 64 tokens, 128-byte swizzle, zeros
 //        beyond the matrix; the codes of X (128 features x 64 tokens) come the same way, their step bytes,
 //        whose rows have no alignment, by ordinary loads of one warp
-//   X    four warps per block: 16 codes at a time from shared memory to the 16-bit type (exact: at most 7
+//   X    two groups of four warps per block in turn: 16 codes at a time from shared memory to the 16-bit type (exact: at most 7
 //        significant bits times a power of two) and back to shared memory in the swizzled form the tensor
 //        core reads.  (Codes loaded by these warps themselves, ahead of their use, were 3.5 times slower:
 //        the fence that makes their stores visible to the tensor core waits for every load on its way.)
@@ -51,8 +51,11 @@ constexpr int kPanelBytes = kDepth * 128;        // 64 features or outputs x 64 
 constexpr int kOperandBytes = 2 * kPanelBytes;
 constexpr int kCodeBytes = kDepth * kHalf;
 constexpr int kStageBytes = kOperandBytes + kCodeBytes;          // gradients, then codes
-constexpr int kSumWarps = 8, kCodeWarps = 4;
-constexpr int kBlockThreads = 512;
+constexpr int kSumWarps = 8;
+constexpr int kCodeWarps = 4, kCodeGroups = 2;   // warps that decode a step; groups of them that take turns
+constexpr int kFirstCodeWarp = kSumWarps, kCopyWarp = kFirstCodeWarp + kCodeWarps * kCodeGroups;
+constexpr int kMultiplyWarp = kCopyWarp + 1, kMemoryWarp = kCopyWarp + 2, kStepWarp = kCopyWarp + 3;
+constexpr int kBlockThreads = 32 * (kCopyWarp + 4);
 constexpr size_t kSharedBytes = (size_t)kStages * kStageBytes + (size_t)kDecoded * kOperandBytes + 1024;   // + room to align to 1024
 constexpr int kMaxPairs = 74;                    // 148 multiprocessors
 constexpr int64_t kSlotFloats = (int64_t)kTileSide * kTileSide;
@@ -195,17 +198,13 @@ __device__ __forceinline__ uint64_t operand_descriptor(uint32_t address)
            (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
 
-__device__ __forceinline__ void load_sums(uint32_t address, uint32_t (&r)[32])
+__device__ __forceinline__ void load_sums(uint32_t address, uint32_t (&r)[16])
 {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(address)
-        : "memory");
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(address)
+                 : "memory");
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
@@ -332,9 +331,9 @@ __device__ __forceinline__ uint32_t load_steps(const uint8_t* steps, int64_t gro
 //
 // T: 16-bit type of both operands.  PLANES: 1, or 3 for fp32 gradients, which arrive as three bf16 matrices
 // that add up to them; a step then is one plane of one block of tokens, planes fastest.
-// Warps 0 .. 7 sum, 8 .. 11 decode, 12 copies, 13 multiplies (first block only), 14 owns the tensor memory,
-// 15 loads step bytes.
-// Registers: 256 x 184 + 128 x 80 + 128 x 64 = 512 x 128.
+// Warps 0 .. 7 sum, 8 .. 15 decode, 16 copies, 17 multiplies (first block only), 18 owns the tensor memory,
+// 19 loads step bytes.
+// Registers: 256 x 152 + 256 x 64 + 128 x 48 = 640 x 96.
 template <typename T, int PLANES, bool BIAS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kBlockThreads, 1)
 weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_constant__ CUtensorMap grad_map,
@@ -375,7 +374,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 14) {
+    if (warp == kMemoryWarp) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(
             shared_address(&tensor_memory_slot)));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
@@ -396,7 +395,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
 
     if (warp < kSumWarps) {
         // ---- sums: warp w reads tensor-memory lanes 32 (w % 4) .. + 31 (features), outputs 128 (w / 4) .. + 127
-        more_registers<184>();
+        more_registers<152>();
         const int quarter = warp & 3, side = warp >> 2;
         float sum[128];
         float bias_sum[2] = {0.0f, 0.0f};
@@ -453,12 +452,12 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t source = tensor_memory + (count & 1) * 256 + side * 128 + ((uint32_t)(32 * quarter) << 16);
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                uint32_t r[32];
-                load_sums(source + 32 * g, r);
+            for (int g = 0; g < 8; ++g) {
+                uint32_t r[16];
+                load_sums(source + 16 * g, r);
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    sum[32 * g + i] += __uint_as_float(r[i]);
+                for (int i = 0; i < 16; ++i)
+                    sum[16 * g + i] += __uint_as_float(r[i]);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
@@ -507,26 +506,25 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                 }
             }
         }
-    } else if (warp < kSumWarps + kCodeWarps) {
+    } else if (warp < kCopyWarp) {
         // ---- codes: a lane decodes 16 features of four rows (tokens).  Of eight neighbouring lanes four hold the
         // first panel's pieces of one row and four the second's of the row's neighbour: their reads, and then
         // both of their writes, fall on eight different groups of banks.
-        fewer_registers<80>();
+        fewer_registers<64>();
         const int piece = lane & 7, upper = piece >> 2;
-        const int row0 = ((lane >> 3) + 4 * (warp - kSumWarps)) ^ upper;
+        const int group = (warp - kFirstCodeWarp) / kCodeWarps;
+        const int row0 = ((lane >> 3) + 4 * ((warp - kFirstCodeWarp) % kCodeWarps)) ^ upper;
         const uint32_t from = row0 * kHalf + ((piece ^ (row0 & 7)) << 4);
         const uint32_t to = upper * kPanelBytes + row0 * 128 + (((2 * (piece & 3)) ^ (row0 & 7)) << 4);
         Ring<kStages> ring, behind;              // behind: the step whose place among the decoded ones is taken next
         Ring<kDecoded> out;
-        int filling = kDecoded;                  // places that are still free
+        uint32_t taken_places = 0;               // the first kDecoded steps find theirs free
+        int turn = 0;
         for (Cursor c(a, unit_begin); c.unit < unit_end; c.advance(a)) {
             for (uint32_t steps = c.steps(a); steps > 0; --steps) {
-                if (filling > 0) {
-                    --filling;
-                } else {
+                if (turn == group) {
+                if (taken_places == kDecoded)
                     wait(multiplied0 + 8 * behind.stage, behind.phase);
-                    behind.advance();
-                }
                 wait(landed0 + 8 * ring.stage, ring.phase);
                 const uint32_t source = stage0 + ring.stage * kStageBytes + kOperandBytes + from;
                 const uint32_t target = decoded0 + out.stage * kOperandBytes + to;
@@ -549,13 +547,20 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                 __syncwarp();
                 if (lane == 0)
                     arrive_at_first(ready0 + 8 * out.stage);
+                }
+                if (taken_places == kDecoded)
+                    behind.advance();
+                else
+                    ++taken_places;
+                if (++turn == kCodeGroups)
+                    turn = 0;
                 ring.advance();
                 out.advance();
             }
         }
     } else {
-        fewer_registers<64>();
-        if (warp == 12) {
+        fewer_registers<48>();
+        if (warp == kCopyWarp) {
             // ---- copies of this block's half of the gradients, and of the codes
             Ring<kStages> ring;
             uint32_t issued = 0;
@@ -591,7 +596,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                 const uint32_t step = issued - back;
                 wait(landed0 + 8 * (step % kStages), (step / kStages) & 1);
             }
-        } else if (warp == 13 && rank == 0) {
+        } else if (warp == kMultiplyWarp && rank == 0) {
             // ---- multiplications: fp32 sums, both operands of type T with the summed index slow, 256 x 256
             constexpr uint32_t kFormat = __is_same(T, __half) ? 0u : 1u;
             constexpr uint32_t kInstruction = (1u << 4) | (kFormat << 7) | (kFormat << 10) | (1u << 15) | (1u << 16) |
@@ -627,7 +632,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                     in.advance();
                 }
             }
-        } else if (warp == 15) {
+        } else if (warp == kStepWarp) {
             // ---- step bytes: a lane loads two rows per step, a whole unit ahead of their use
             const int64_t groups = a.width / kGroup;
             uint32_t w[kChain][2];
@@ -674,7 +679,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncwarp();
     cluster_barrier();
-    if (warp == 14)
+    if (warp == kMemoryWarp)
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tensor_memory) : "memory");
 }
 
