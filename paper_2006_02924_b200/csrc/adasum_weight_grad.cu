@@ -270,15 +270,47 @@ struct Decoder<__half> {
     }
 };
 
-// Where a role stands in its pair's run of units.
+// Where a role stands in its pair's run of units [begin, end).
+//
+// A run is the end of one tile, some whole tiles and the beginning of another.  They are walked in the order
+// beginning, end, whole tiles: all runs are equally long, so at any time the pairs stand at one of two tokens
+// (the beginnings at s, all others at the same distance from it, modulo the tokens), read the same rows of both
+// matrices at the same time and find them in the L2's nearer half.
 struct Cursor {
-    uint32_t unit, chain, tile_k, tile_n;
-    __device__ __forceinline__ Cursor(const WeightGradArgs& a, uint32_t begin) : unit(begin)
+    uint32_t unit, stop, chain, tile_k, tile_n, part;
+    uint32_t begin, end;
+    __device__ __forceinline__ Cursor(const WeightGradArgs& a, uint32_t b, uint32_t e) : part(0), begin(b), end(e)
     {
-        const uint32_t tile = begin / a.chains;
-        chain = begin - tile * a.chains;
+        unit = max(b, e / a.chains * a.chains);          // the beginning of the last tile, if it is cut off
+        stop = e;
+        if (e / a.chains == b / a.chains)
+            unit = stop;                                 // a run inside one tile is an "end" throughout
+        enter(a);
+    }
+    __device__ __forceinline__ void enter(const WeightGradArgs& a)
+    {
+        while (unit == stop && part < 3) {
+            ++part;
+            const uint32_t first_whole =
+                end / a.chains == begin / a.chains ? end : (begin + a.chains - 1) / a.chains * a.chains;
+            if (part == 1) {
+                unit = begin;
+                stop = min(end, first_whole);
+            } else if (part == 2) {
+                unit = min(end, first_whole);
+                stop = max(unit, end / a.chains * a.chains);
+            }
+        }
+        const uint32_t tile = unit / a.chains;
+        chain = unit - tile * a.chains;
         tile_n = tile / a.tiles_k;
         tile_k = tile - tile_n * a.tiles_k;
+    }
+    __device__ __forceinline__ bool done() const { return part == 3; }
+    // Is this the last unit of the pair's share of the tile?
+    __device__ __forceinline__ bool last_of_share(const WeightGradArgs& a) const
+    {
+        return unit + 1 == stop || chain + 1 == a.chains;
     }
     __device__ __forceinline__ uint32_t first_step() const { return chain * kChain; }
     __device__ __forceinline__ uint32_t steps(const WeightGradArgs& a) const
@@ -288,7 +320,9 @@ struct Cursor {
     __device__ __forceinline__ void advance(const WeightGradArgs& a)
     {
         ++unit;
-        if (++chain == a.chains) {
+        if (unit == stop) {
+            enter(a);
+        } else if (++chain == a.chains) {
             chain = 0;
             if (++tile_k == a.tiles_k) {
                 tile_k = 0;
@@ -401,10 +435,10 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
         float bias_sum[2] = {0.0f, 0.0f};
         Ring<kStages> ring;
         uint32_t count = 0, chain_begin = 0;
-        uint32_t which = 0;                      // 0: the first tile of the pair's run, 1: a later one
-        for (Cursor c(a, unit_begin); c.unit < unit_end; c.advance(a), ++count) {
-            if (c.unit == unit_begin || c.chain == 0) {
-                which = c.unit == unit_begin ? 0 : 1;
+        bool fresh = true;                       // the next unit is the first of its tile's share
+        for (Cursor c(a, unit_begin, unit_end); !c.done(); c.advance(a), ++count) {
+            if (fresh) {
+                fresh = false;
                 chain_begin = c.chain;
                 bias_sum[0] = bias_sum[1] = 0.0f;
 #pragma unroll
@@ -464,11 +498,12 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
             if (lane == 0)
                 arrive_at_first(taken0 + 8 * (count & 1));
 
-            if (c.chain + 1 != a.chains && c.unit + 1 != unit_end)
+            if (!c.last_of_share(a))
                 continue;
+            fresh = true;
             // ---- the pair's last unit of this tile: the result, or this pair's part of it
             const bool whole = chain_begin == 0 && c.chain + 1 == a.chains;
-            const uint32_t slot = 2 * pair + which;
+            const uint32_t slot = 2 * pair + (c.part == 0 ? 1 : 0);
             const int feature = 32 * quarter + lane;
             if (whole) {
                 const int64_t k = (int64_t)c.tile_k * kTileSide + rank * kHalf + feature;
@@ -520,7 +555,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
         Ring<kDecoded> out;
         uint32_t taken_places = 0;               // the first kDecoded steps find theirs free
         int turn = 0;
-        for (Cursor c(a, unit_begin); c.unit < unit_end; c.advance(a)) {
+        for (Cursor c(a, unit_begin, unit_end); !c.done(); c.advance(a)) {
             for (uint32_t steps = c.steps(a); steps > 0; --steps) {
                 if (turn == group) {
                 if (taken_places == kDecoded)
@@ -565,7 +600,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
             Ring<kStages> ring;
             uint32_t issued = 0;
             const uint32_t bytes = kOperandBytes + (a.width > 0 ? kCodeBytes : 0);
-            for (Cursor c(a, unit_begin); c.unit < unit_end && waiting; c.advance(a)) {
+            for (Cursor c(a, unit_begin, unit_end); !c.done() && waiting; c.advance(a)) {
                 const int n = (int)c.tile_n * kTileSide + (int)rank * kHalf, k = (int)c.tile_k * kTileSide + (int)rank * kHalf;
                 const uint32_t end = c.first_step() + c.steps(a);
                 for (uint32_t step = c.first_step(); step < end; ++step) {
@@ -604,7 +639,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
             Ring<kStages> ring;
             Ring<kDecoded> in;
             uint32_t count = 0;
-            for (Cursor c(a, unit_begin); c.unit < unit_end; c.advance(a), ++count) {
+            for (Cursor c(a, unit_begin, unit_end); !c.done(); c.advance(a), ++count) {
                 const uint32_t target = tensor_memory + (count & 1) * 256;
                 wait(taken0 + 8 * (count & 1), ((count >> 1) & 1) ^ 1);
                 uint32_t accumulate = 0;
@@ -646,9 +681,9 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                     w[j][1] = load_steps(a.steps, groups, a.rows, t + 32, group);
                 }
             };
-            Cursor c(a, unit_begin);
+            Cursor c(a, unit_begin, unit_end);
             load(c);
-            while (c.unit < unit_end) {
+            while (!c.done()) {
                 uint32_t v[kChain][2];
 #pragma unroll
                 for (int j = 0; j < kChain; ++j) {
@@ -657,7 +692,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                 }
                 const uint32_t steps = c.steps(a);
                 c.advance(a);
-                if (c.unit < unit_end)
+                if (!c.done())
                     load(c);
 #pragma unroll
                 for (int j = 0; j < kChain; ++j) {
