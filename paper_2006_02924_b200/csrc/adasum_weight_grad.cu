@@ -74,7 +74,7 @@ struct WeightGradArgs {
     uint32_t tiles_k, tiles, iterations, chains, units;
     int* status;             // one word per block
     float* slots;            // [pair][first or last tile of its run][block][output][feature of the block]
-    float* bias_slots;       // [pair][first or last][256 outputs]
+    float* bias_slots;       // [pair + tile][256 outputs]: the pairs' shares of the tiles' parts of the bias gradient
 };
 
 __host__ __device__ inline uint32_t first_unit(uint32_t units, uint32_t pairs, uint32_t pair)
@@ -447,13 +447,16 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
             }
             if constexpr (BIAS) {
                 // this block's 128 outputs: thread = two outputs, 16 of a step's 64 tokens.  Summed per
-                // unit, like the products.
+                // unit, like the products.  The tiles of a column of outputs share the work: each adds up
+                // every tiles_k-th step, so that none is slower than the others.
                 const uint32_t steps = c.steps(a);
+                uint32_t to_mine = (c.tile_k + a.tiles_k - c.first_step() % a.tiles_k) % a.tiles_k;
                 const int output = 2 * (threadIdx.x & 63), part = threadIdx.x >> 6;
                 float unit_sum[2] = {0.0f, 0.0f};
                 for (uint32_t s = 0; s < steps; ++s) {
                     wait(landed0 + 8 * ring.stage, ring.phase);
-                    if (c.tile_k == 0) {
+                    if (to_mine-- == 0) {
+                        to_mine = a.tiles_k - 1;
                         const uint32_t panel = stage0 + ring.stage * kStageBytes + (output >> 6) * kPanelBytes;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
@@ -523,22 +526,15 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                     dst[i * kHalf] = sum[i];
             }
             if constexpr (BIAS) {
-                if (c.tile_k == 0) {
-                    const int output = 2 * (threadIdx.x & 63), part = threadIdx.x >> 6;
-                    bias_part[part][output] = bias_sum[0];
-                    bias_part[part][output + 1] = bias_sum[1];
-                    asm volatile("bar.sync 1, 256;" ::: "memory");
-                    if (threadIdx.x < kHalf) {
-                        const float total = (bias_part[0][threadIdx.x] + bias_part[1][threadIdx.x]) +
-                                            (bias_part[2][threadIdx.x] + bias_part[3][threadIdx.x]);
-                        const int64_t n = (int64_t)c.tile_n * kTileSide + rank * kHalf + threadIdx.x;
-                        if (!whole)
-                            a.bias_slots[(int64_t)slot * kTileSide + rank * kHalf + threadIdx.x] = total;
-                        else if (n < a.outputs)
-                            write_gradient(a, a.bias, n, total);
-                    }
-                    asm volatile("bar.sync 1, 256;" ::: "memory");
-                }
+                const int output = 2 * (threadIdx.x & 63), part = threadIdx.x >> 6;
+                bias_part[part][output] = bias_sum[0];
+                bias_part[part][output + 1] = bias_sum[1];
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                if (threadIdx.x < kHalf)
+                    a.bias_slots[(int64_t)(pair + c.tile_n * a.tiles_k + c.tile_k) * kTileSide + rank * kHalf + threadIdx.x] =
+                        (bias_part[0][threadIdx.x] + bias_part[1][threadIdx.x]) +
+                        (bias_part[2][threadIdx.x] + bias_part[3][threadIdx.x]);
+                asm volatile("bar.sync 1, 256;" ::: "memory");
             }
         }
     } else if (warp < kCopyWarp) {
@@ -718,7 +714,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tensor_memory) : "memory");
 }
 
-// Tiles whose units fell to several pairs: the pairs' parts added in order.  grid.x = tiles, grid.y = parts of
+// Bias gradients, and tiles whose units fell to several pairs: the pairs' parts added in order.  grid.x = tiles, grid.y = parts of
 // the tile's 2 x 256 rows of 128 features; one warp per row, four features per lane.
 constexpr int kJoinThreads = 256;
 constexpr int kJoinParts = 2 * kTileSide / (kJoinThreads / 32);
@@ -729,9 +725,20 @@ weight_grad_join_kernel(const __grid_constant__ WeightGradArgs a, uint32_t pairs
     const uint32_t tile = blockIdx.x;
     const uint32_t first = pair_of_unit(a.units, pairs, tile * a.chains);
     const uint32_t last = pair_of_unit(a.units, pairs, tile * a.chains + a.chains - 1);
+    const uint32_t tile_k = tile % a.tiles_k, tile_n = tile / a.tiles_k;
+    if (a.bias && tile_k == 0 && blockIdx.y == 0) {
+        const int64_t n = (int64_t)tile_n * kTileSide + threadIdx.x;
+        float total = 0.0f;
+        for (uint32_t t = tile; t < tile + a.tiles_k; ++t) {
+            const uint32_t to = pair_of_unit(a.units, pairs, t * a.chains + a.chains - 1);
+            for (uint32_t pair = pair_of_unit(a.units, pairs, t * a.chains); pair <= to; ++pair)
+                total += __ldcg(a.bias_slots + (int64_t)(pair + t) * kTileSide + threadIdx.x);
+        }
+        if (n < a.outputs)
+            write_gradient(a, a.bias, n, total);
+    }
     if (first == last)
         return;                      // written by the product itself
-    const uint32_t tile_k = tile % a.tiles_k, tile_n = tile / a.tiles_k;
     // only the first pair's run can have started in an earlier tile
     const uint32_t first_slot = 2 * first + (tile == first_unit(a.units, pairs, first) / a.chains ? 0 : 1);
     auto slot_of = [&](uint32_t pair) { return pair == first ? first_slot : 2 * pair; };
@@ -763,14 +770,6 @@ weight_grad_join_kernel(const __grid_constant__ WeightGradArgs a, uint32_t pairs
                 if (k + i < a.features)
                     write_gradient(a, a.weight, e + i, sum[i]);
         }
-    }
-    if (a.bias && tile_k == 0 && blockIdx.y == 0) {
-        const int64_t bias_n = (int64_t)tile_n * kTileSide + threadIdx.x;
-        float total = 0.0f;
-        for (uint32_t pair = first; pair <= last; ++pair)
-            total += a.bias_slots[(int64_t)slot_of(pair) * kTileSide + threadIdx.x];
-        if (bias_n < a.outputs)
-            write_gradient(a, a.bias, bias_n, total);
     }
 }
 
@@ -860,7 +859,7 @@ WorkLayout work_layout(int64_t rows, int64_t features, int64_t outputs, adasum_d
     l.pitch = up(outputs, 8);
     l.slots = 1024;                                    // the blocks' status words come first
     l.bias_slots = l.slots + (size_t)l.pairs * 2 * kSlotFloats * sizeof(float);
-    l.gradients = l.bias_slots + (size_t)l.pairs * 2 * kTileSide * sizeof(float);
+    l.gradients = l.bias_slots + (size_t)(l.pairs + l.tiles) * kTileSide * sizeof(float);
     l.total = l.gradients + (size_t)up(planes * rows * l.pitch * 2, 256);
     return l;
 }
@@ -1073,9 +1072,9 @@ adasum_status_t adasum_checkpoint_weight_grad(const void* checkpoint, int64_t ro
     bool split = false;                    // does any tile fall to several pairs?
     for (uint32_t p = 1; p < pairs && !split; ++p)
         split = first_unit(l.units, pairs, p) % l.chains != 0;
-    if (split) {
+    if (split || grad_bias) {
         const bool vec = aligned_to(grad_weight, 16) && features % 4 == 0;
-        weight_grad_join_kernel<<<dim3(l.tiles, kJoinParts), kJoinThreads, 0, stream>>>(a, pairs, vec);
+        weight_grad_join_kernel<<<dim3(l.tiles, split ? kJoinParts : 1), kJoinThreads, 0, stream>>>(a, pairs, vec);
         ADASUM_CUDA_CHECK(cudaGetLastError());
         profile_mark(stream, ADASUM_KERNEL_WEIGHT_GRAD, 2, 0, false);
     }
