@@ -3,7 +3,9 @@
 //
 // Every kernel here is one pass over a matrix, bound by HBM traffic.  A thread handles vectors of eight
 // consecutive features; four neighbouring lanes hold a group of 32, so a group's largest magnitude is
-// two shuffles away, and rows are filled up to whole groups, so a vector never leaves its row.
+// two shuffles away, and rows are filled up to whole groups, so a vector never leaves its row.  A warp takes a
+// strip of up to 32 vectors of a row (of several rows, if rows are short) on kRows rows below each other: all
+// loads of a thread go out before the first is used, and its addresses are one sum apart.
 #include "adasum_operators.cuh"
 
 namespace adasum {
@@ -11,22 +13,9 @@ namespace {
 
 constexpr int kGroup = 32;                 // features that share a step
 constexpr int kBlock = 256;
-constexpr int kVectors = 4;                // independent vectors per thread: loads in flight
-
-struct CheckpointView {
-    int8_t* codes;          // [rows][width]
-    uint8_t* steps;         // [rows][width / 32]
-    int64_t rows, features, width;
-};
+constexpr int kRows = 4;                   // vectors per thread, in as many rows: loads in flight
 
 int64_t checkpoint_width(int64_t features) { return (features + kGroup - 1) / kGroup * kGroup; }
-
-CheckpointView view_of(const void* checkpoint, int64_t rows, int64_t features)
-{
-    const int64_t width = checkpoint_width(features);
-    int8_t* codes = static_cast<int8_t*>(const_cast<void*>(checkpoint));
-    return CheckpointView{codes, reinterpret_cast<uint8_t*>(codes + rows * width), rows, features, width};
-}
 
 // ---- activations -------------------------------------------------------------------------------------
 
@@ -138,14 +127,19 @@ __device__ __forceinline__ uint32_t step_byte(uint32_t top_bits)
 __device__ __forceinline__ float step_value(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 // Four codes of x[0 .. 3] packed; inv = 1 / step.  Adding 1.5 * 2^23 rounds to an integer, ties to even,
-// and leaves it in the low bits.
+// and leaves it in the low bits.  LIMIT: a magnitude may round to 128.
+template <bool LIMIT>
 __device__ __forceinline__ uint32_t pack_codes(const float* x, float inv)
 {
     constexpr float kMagic = 12582912.0f;
     uint32_t b[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        b[i] = __float_as_uint(fminf(fmaxf(fmaf(x[i], inv, kMagic), kMagic - 127.0f), kMagic + 127.0f));
+    for (int i = 0; i < 4; ++i) {
+        float r = fmaf(x[i], inv, kMagic);
+        if constexpr (LIMIT)
+            r = fminf(fmaxf(r, kMagic - 127.0f), kMagic + 127.0f);
+        b[i] = __float_as_uint(r);
+    }
     return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
 }
 // Values of four packed codes: byte + 128 placed in the low bits of 2^23, 2^23 + 128 taken off again
@@ -160,31 +154,83 @@ __device__ __forceinline__ void unpack_codes(uint32_t packed, float step, float*
 
 // ---- kernels -----------------------------------------------------------------------------------------
 
-// grid: ceil(vectors / (kBlock * kVectors)); vectors = rows * width / 8 (a multiple of 4, so the lanes of
-// a group are all inside or all outside).
-template <typename T, int ACT>
+// A matrix cut into strips: 2^lane_bits vectors of a row x 2^(5 - lane_bits) rows per lane row.
+struct Strips {
+    int64_t rows, features, width;       // width: features filled up to whole groups
+    int per_row;                         // vectors of a row, a multiple of 4
+    int lane_bits;
+    RowDivider strips_per_row;
+    uint64_t warps;
+};
+
+struct Place {
+    int64_t row0;            // first of the thread's rows; the next ones are `step` further
+    int step;
+    int column;              // first feature
+    int count;               // features of the vector inside the matrix (<= 0: only padding)
+    bool inside;             // the vector exists (padding included)
+};
+__device__ __forceinline__ Place place_of(const Strips& s)
+{
+    const uint64_t warp = (uint64_t)blockIdx.x * (kBlock / 32) + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    uint64_t band;
+    uint32_t strip;
+    divide_row(s.strips_per_row, warp, band, strip);
+    Place p;
+    p.step = 32 >> s.lane_bits;
+    p.row0 = (int64_t)band * (kRows * p.step) + (lane >> s.lane_bits);
+    const int vector = ((int)strip << s.lane_bits) + (lane & ((1 << s.lane_bits) - 1));
+    p.inside = warp < s.warps && vector < s.per_row;
+    p.column = vector * 8;
+    p.count = p.inside ? (int)min((int64_t)8, s.features - p.column) : 0;
+    return p;
+}
+
+// VEC: every row of x, y, grad and out starts on 16 bytes and features is a multiple of 8, so each vector is
+// either whole or only padding.
+template <bool VEC, typename T>
+__device__ __forceinline__ void load_vector(const T* p, int count, float (&x)[8])
+{
+    if constexpr (VEC) {
+        if (count > 0) {
+            load_eight(p, x);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                x[i] = 0.0f;
+        }
+    } else {
+        load_up_to_eight(p, false, count, x);
+    }
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ void store_vector(T* p, int count, const float (&y)[8])
+{
+    if constexpr (VEC) {
+        if (count > 0)
+            store_vector_from_float<8>(p, TypeCode<T>::value, 0, y);
+    } else {
+        store_up_to_eight(p, false, count, y);
+    }
+}
+
+template <typename T, int ACT, bool VEC>
 __global__ void __launch_bounds__(kBlock)
-checkpoint_save_kernel(const T* x, int64_t x_stride, bool x_vec, T* y, int64_t y_stride, bool y_vec,
-                       CheckpointView c, RowDivider divider, uint64_t vectors)
+checkpoint_save_kernel(const __grid_constant__ Strips s, const T* x, int64_t x_stride, T* y, int64_t y_stride,
+                       int8_t* codes, uint8_t* steps)
 {
     constexpr bool WIDE = sizeof(T) == 4;
-    const uint64_t first = (uint64_t)blockIdx.x * (kBlock * kVectors) + threadIdx.x;
-    float v[kVectors][8];
-    int64_t row[kVectors];
-    int column[kVectors], count[kVectors];
+    const Place p = place_of(s);
+    float v[kRows][8];
 #pragma unroll
-    for (int u = 0; u < kVectors; ++u) {
-        const uint64_t n = first + u * kBlock;
-        uint64_t r;
-        uint32_t at;
-        divide_row(divider, n, r, at);
-        row[u] = (int64_t)r;
-        column[u] = (int)(at * 8);
-        count[u] = n < vectors ? (int)min((int64_t)8, c.features - column[u]) : 0;     // <= 0: only padding
-        load_up_to_eight(x + row[u] * x_stride + column[u], x_vec, count[u], v[u]);
+    for (int u = 0; u < kRows; ++u) {
+        const int64_t row = p.row0 + u * p.step;
+        load_vector<VEC>(x + row * x_stride + p.column, row < s.rows ? p.count : 0, v[u]);
     }
 #pragma unroll
-    for (int u = 0; u < kVectors; ++u) {
+    for (int u = 0; u < kRows; ++u) {
+        const int64_t row = p.row0 + u * p.step;
         uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -193,66 +239,67 @@ checkpoint_save_kernel(const T* x, int64_t x_stride, bool x_vec, T* y, int64_t y
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
         const uint32_t byte = step_byte(top);
         const float inv = __uint_as_float((254u - min(byte, 254u)) << 23);
-        const uint32_t keep = byte == 255u ? 0u : 0xffffffffu;
-        const uint2 codes = make_uint2(pack_codes(v[u], inv) & keep, pack_codes(v[u] + 4, inv) & keep);
-        const uint64_t n = first + u * kBlock;
-        if (n < vectors) {
-            *reinterpret_cast<uint2*>(c.codes + n * 8) = codes;
-            if ((n & 3) == 0)
-                c.steps[n >> 2] = (uint8_t)byte;
+        uint2 packed;
+        if ((top & 0x7fffffu) < 0x7f0000u) {     // the largest magnitude is below 127 steps (or a power of two less)
+            packed = make_uint2(pack_codes<false>(v[u], inv), pack_codes<false>(v[u] + 4, inv));
+        } else {
+            packed = make_uint2(pack_codes<true>(v[u], inv), pack_codes<true>(v[u] + 4, inv));
+        }
+        if (byte == 255u)
+            packed = make_uint2(0, 0);
+        if (p.inside && row < s.rows) {
+            const int64_t at = row * s.width + p.column;
+            *reinterpret_cast<uint2*>(codes + at) = packed;
+            if ((p.column & (kGroup - 1)) == 0)
+                steps[at / kGroup] = (uint8_t)byte;
             if (y) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     v[u][i] = activation<ACT, WIDE>(v[u][i]);
-                store_up_to_eight(y + row[u] * y_stride + column[u], y_vec, count[u], v[u]);
+                store_vector<VEC>(y + row * y_stride + p.column, p.count, v[u]);
             }
         }
     }
 }
 
 // ACT < 0: the values kept themselves; else out = grad * slope(kept value).
-template <typename T, int ACT>
+template <typename T, int ACT, bool VEC>
 __global__ void __launch_bounds__(kBlock)
-checkpoint_apply_kernel(CheckpointView c, const T* grad, int64_t grad_stride, bool grad_vec, T* out,
-                        int64_t out_stride, bool out_vec, RowDivider divider, uint64_t vectors)
+checkpoint_apply_kernel(const __grid_constant__ Strips s, const int8_t* codes, const uint8_t* steps, const T* grad,
+                        int64_t grad_stride, T* out, int64_t out_stride)
 {
     constexpr bool WIDE = sizeof(T) == 4;
-    const uint64_t first = (uint64_t)blockIdx.x * (kBlock * kVectors) + threadIdx.x;
-    uint2 codes[kVectors];
-    uint32_t byte[kVectors];
-    float g[kVectors][8];
-    int64_t row[kVectors];
-    int column[kVectors], count[kVectors];
+    const Place p = place_of(s);
+    if (p.count <= 0)
+        return;
+    uint2 packed[kRows];
+    uint32_t byte[kRows];
+    float g[kRows][8];
 #pragma unroll
-    for (int u = 0; u < kVectors; ++u) {
-        const uint64_t n = first + u * kBlock;
-        uint64_t r;
-        uint32_t at;
-        divide_row(divider, n, r, at);
-        row[u] = (int64_t)r;
-        column[u] = (int)(at * 8);
-        count[u] = n < vectors ? (int)min((int64_t)8, c.features - column[u]) : 0;
-        if (count[u] > 0) {
-            codes[u] = *reinterpret_cast<const uint2*>(c.codes + n * 8);
-            byte[u] = c.steps[n >> 2];
-        } else {
-            codes[u] = make_uint2(0, 0);
-            byte[u] = 0;
+    for (int u = 0; u < kRows; ++u) {
+        const int64_t row = p.row0 + u * p.step;
+        if (row < s.rows) {
+            const int64_t at = row * s.width + p.column;
+            packed[u] = *reinterpret_cast<const uint2*>(codes + at);
+            byte[u] = steps[at / kGroup];
+            if constexpr (ACT >= 0)
+                load_vector<VEC>(grad + row * grad_stride + p.column, p.count, g[u]);
         }
-        if constexpr (ACT >= 0)
-            load_up_to_eight(grad + row[u] * grad_stride + column[u], grad_vec, count[u], g[u]);
     }
 #pragma unroll
-    for (int u = 0; u < kVectors; ++u) {
-        float x[8];
-        unpack_codes(codes[u].x, step_value(byte[u]), x);
-        unpack_codes(codes[u].y, step_value(byte[u]), x + 4);
-        if constexpr (ACT >= 0) {
+    for (int u = 0; u < kRows; ++u) {
+        const int64_t row = p.row0 + u * p.step;
+        if (row < s.rows) {
+            float x[8];
+            unpack_codes(packed[u].x, step_value(byte[u]), x);
+            unpack_codes(packed[u].y, step_value(byte[u]), x + 4);
+            if constexpr (ACT >= 0) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                x[i] = g[u][i] * activation_slope<ACT, WIDE>(x[i]);
+                for (int i = 0; i < 8; ++i)
+                    x[i] = g[u][i] * activation_slope<ACT, WIDE>(x[i]);
+            }
+            store_vector<VEC>(out + row * out_stride + p.column, p.count, x);
         }
-        store_up_to_eight(out + row[u] * out_stride + column[u], out_vec, count[u], x);
     }
 }
 
@@ -284,38 +331,25 @@ adasum_status_t check_matrix(const char* name, const void* p, int64_t stride, in
     return ADASUM_OK;
 }
 
-struct Launch {
-    RowDivider divider;
-    uint64_t vectors;
-    unsigned blocks;
-};
-bool plan_launch(int64_t rows, int64_t width, Launch* launch)
+bool plan_strips(int64_t rows, int64_t features, Strips* s, unsigned* blocks)
 {
-    launch->divider = row_divider(width / 8);
-    launch->vectors = (uint64_t)rows * (uint64_t)(width / 8);
-    const uint64_t blocks = (launch->vectors + kBlock * kVectors - 1) / (kBlock * kVectors);
-    launch->blocks = (unsigned)blocks;
-    return blocks <= 0x7fffffffu;
+    s->rows = rows;
+    s->features = features;
+    s->width = checkpoint_width(features);
+    s->per_row = (int)(s->width / 8);
+    s->lane_bits = 2;
+    while (s->lane_bits < 5 && (1 << s->lane_bits) < s->per_row)
+        ++s->lane_bits;
+    const int64_t strips = (s->per_row + (1 << s->lane_bits) - 1) >> s->lane_bits;
+    const int64_t band = (int64_t)kRows * (32 >> s->lane_bits);
+    s->strips_per_row = row_divider(strips);
+    s->warps = (uint64_t)((rows + band - 1) / band) * (uint64_t)strips;
+    const uint64_t n = (s->warps + kBlock / 32 - 1) / (kBlock / 32);
+    *blocks = (unsigned)n;
+    return n <= 0x7fffffffu;
 }
 
-template <typename T, int ACT>
-void launch_save(const void* x, int64_t x_stride, void* y, int64_t y_stride, const CheckpointView& c, const Launch& l,
-                 cudaStream_t stream)
-{
-    checkpoint_save_kernel<T, ACT><<<l.blocks, kBlock, 0, stream>>>(
-        static_cast<const T*>(x), x_stride, rows_aligned(x, x_stride, sizeof(T)), static_cast<T*>(y), y_stride,
-        rows_aligned(y, y_stride, sizeof(T)), c, l.divider, l.vectors);
-}
-template <typename T, int ACT>
-void launch_apply(const CheckpointView& c, const void* grad, int64_t grad_stride, void* out, int64_t out_stride,
-                  const Launch& l, cudaStream_t stream)
-{
-    checkpoint_apply_kernel<T, ACT><<<l.blocks, kBlock, 0, stream>>>(
-        c, static_cast<const T*>(grad), grad_stride, rows_aligned(grad, grad_stride, sizeof(T)), static_cast<T*>(out),
-        out_stride, rows_aligned(out, out_stride, sizeof(T)), l.divider, l.vectors);
-}
-
-// Calls f.template operator()<T, ACT>() for the run-time type and activation.
+// Calls f with a value of the run-time type, the constant of the run-time activation, or of a truth value.
 template <typename F>
 void with_type(adasum_dtype_t dtype, F&& f)
 {
@@ -339,6 +373,28 @@ void with_activation(adasum_activation_t act, F&& f)
     case ADASUM_ACT_SILU: f(Constant<ADASUM_ACT_SILU>{}); break;
     }
 }
+template <typename F>
+void with_flag(bool flag, F&& f)
+{
+    if (flag)
+        f(Constant<1>{});
+    else
+        f(Constant<0>{});
+}
+
+template <typename T, int ACT>
+void launch_apply(const void* checkpoint, const Strips& s, unsigned blocks, const void* grad, int64_t grad_stride,
+                  void* out, int64_t out_stride, cudaStream_t stream)
+{
+    const int8_t* codes = static_cast<const int8_t*>(checkpoint);
+    const bool vec = s.features % 8 == 0 && rows_aligned(grad, grad_stride, sizeof(T)) && rows_aligned(out, out_stride, sizeof(T));
+    with_flag(vec, [&](auto v) {
+        checkpoint_apply_kernel<T, ACT, decltype(v)::value != 0><<<blocks, kBlock, 0, stream>>>(
+            s, codes, reinterpret_cast<const uint8_t*>(codes + s.rows * s.width), static_cast<const T*>(grad), grad_stride,
+            static_cast<T*>(out), out_stride);
+    });
+}
+
 bool known_activation(int act) { return act >= ADASUM_ACT_NONE && act <= ADASUM_ACT_SILU; }
 
 adasum_status_t launched(cudaStream_t stream, int kernel)
@@ -386,15 +442,22 @@ adasum_status_t adasum_checkpoint_save(const void* x, int64_t x_stride, int64_t 
         return fail(ADASUM_ERR_ARG, "y overlaps x without being the same matrix");
     if (spans_overlap(checkpoint, c_bytes, x, x_bytes) || spans_overlap(checkpoint, c_bytes, y, y_bytes))
         return fail(ADASUM_ERR_ARG, "checkpoint overlaps x or y");
-    const CheckpointView c = view_of(checkpoint, rows, features);
-    Launch l;
-    if (!plan_launch(rows, c.width, &l))
+    Strips s;
+    unsigned blocks;
+    if (!plan_strips(rows, features, &s, &blocks))
         return fail(ADASUM_ERR_ARG, "%lld x %lld is too large", (long long)rows, (long long)features);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
     profile_mark(stream, -1, 0, 0, true);
     with_type(dtype, [&](auto t) {
         with_activation(act, [&](auto a) {
-            launch_save<decltype(t), decltype(a)::value>(x, x_stride, y, y_stride, c, l, stream);
+            using T = decltype(t);
+            const bool vec = features % 8 == 0 && rows_aligned(x, x_stride, sizeof(T)) && rows_aligned(y, y_stride, sizeof(T));
+            int8_t* codes = static_cast<int8_t*>(checkpoint);
+            with_flag(vec, [&](auto v) {
+                checkpoint_save_kernel<T, decltype(a)::value, decltype(v)::value != 0><<<blocks, kBlock, 0, stream>>>(
+                    s, static_cast<const T*>(x), x_stride, static_cast<T*>(y), y_stride, codes,
+                    reinterpret_cast<uint8_t*>(codes + s.rows * s.width));
+            });
         });
     });
     return launched(stream, ADASUM_KERNEL_CHECKPOINT_SAVE);
@@ -413,13 +476,13 @@ adasum_status_t adasum_checkpoint_load(const void* checkpoint, int64_t rows, int
     if (spans_overlap(checkpoint, adasum_checkpoint_bytes(rows, features), out,
                       matrix_span(rows, features, out_stride, operator_bytes(dtype))))
         return fail(ADASUM_ERR_ARG, "checkpoint overlaps out");
-    const CheckpointView c = view_of(checkpoint, rows, features);
-    Launch l;
-    if (!plan_launch(rows, c.width, &l))
+    Strips s;
+    unsigned blocks;
+    if (!plan_strips(rows, features, &s, &blocks))
         return fail(ADASUM_ERR_ARG, "%lld x %lld is too large", (long long)rows, (long long)features);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
     profile_mark(stream, -1, 0, 0, true);
-    with_type(dtype, [&](auto t) { launch_apply<decltype(t), -1>(c, nullptr, 0, out, out_stride, l, stream); });
+    with_type(dtype, [&](auto t) { launch_apply<decltype(t), -1>(checkpoint, s, blocks, nullptr, 0, out, out_stride, stream); });
     return launched(stream, ADASUM_KERNEL_CHECKPOINT_LOAD);
 }
 
@@ -447,16 +510,16 @@ adasum_status_t adasum_checkpoint_act_grad(const void* checkpoint, int64_t rows,
         return fail(ADASUM_ERR_ARG, "grad_in overlaps grad_out without being the same matrix");
     if (spans_overlap(checkpoint, adasum_checkpoint_bytes(rows, features), grad_in, in_bytes))
         return fail(ADASUM_ERR_ARG, "checkpoint overlaps grad_in");
-    const CheckpointView c = view_of(checkpoint, rows, features);
-    Launch l;
-    if (!plan_launch(rows, c.width, &l))
+    Strips s;
+    unsigned blocks;
+    if (!plan_strips(rows, features, &s, &blocks))
         return fail(ADASUM_ERR_ARG, "%lld x %lld is too large", (long long)rows, (long long)features);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
     profile_mark(stream, -1, 0, 0, true);
     with_type(dtype, [&](auto t) {
         with_activation(act, [&](auto a) {
-            launch_apply<decltype(t), decltype(a)::value>(c, grad_out, grad_out_stride, grad_in, grad_in_stride, l,
-                                                          stream);
+            launch_apply<decltype(t), decltype(a)::value>(checkpoint, s, blocks, grad_out, grad_out_stride, grad_in,
+                                                          grad_in_stride, stream);
         });
     });
     return launched(stream, ADASUM_KERNEL_ACT_GRAD);

@@ -453,8 +453,7 @@ adasum_status_t adasum_embedding_forward(const void* table, int64_t table_stride
     if (spans_overlap(out, out_bytes, table, table_bytes) ||
         spans_overlap(out, out_bytes, tokens, (size_t)num_tokens * token_bytes))
         return fail(ADASUM_ERR_ARG, "out overlaps table or tokens");
-    // at least two vectors per row for the divider: a row of up to eight elements gets an empty one
-    const int64_t per_row = dim <= 8 ? 2 : (dim + 7) / 8;
+    const int64_t per_row = (dim + 7) / 8;
     const uint64_t vectors = (uint64_t)num_tokens * (uint64_t)per_row;
     const uint64_t blocks = (vectors + kLookupBlock * kLookupVectors - 1) / (kLookupBlock * kLookupVectors);
     if (blocks > 0x7fffffffu)

@@ -61,18 +61,18 @@ inline int device_sms()
 // exact while n * d < 2^64 (the rounding of the factor adds less than n * d / 2^64 / d < 1 / d).
 struct RowDivider {
     uint64_t factor;
-    uint32_t per_row;       // >= 2
+    uint32_t per_row;
 };
 inline RowDivider row_divider(int64_t per_row)
 {
-    return RowDivider{~uint64_t(0) / (uint64_t)per_row + 1, (uint32_t)per_row};
+    return RowDivider{per_row > 1 ? ~uint64_t(0) / (uint64_t)per_row + 1 : 0, (uint32_t)per_row};
 }
 
 // ---- device ----------------------------------------------------------------------------------------
 
 __device__ __forceinline__ void divide_row(const RowDivider& d, uint64_t n, uint64_t& row, uint32_t& at)
 {
-    row = __umul64hi(n, d.factor);
+    row = d.per_row > 1 ? __umul64hi(n, d.factor) : n;
     at = (uint32_t)(n - row * d.per_row);
 }
 

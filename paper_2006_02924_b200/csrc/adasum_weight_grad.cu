@@ -790,8 +790,6 @@ relay_gradients_kernel(const T* grad, int64_t stride, bool vec, int64_t rows, in
     uint32_t at;
     divide_row(divider, n, row, at);
     const int64_t column = (int64_t)at * 8;
-    if (column >= pitch)
-        return;
     const int count = (int)min((int64_t)8, outputs - column);
     const int64_t place = ((int64_t)row * pitch + column) / 8;
     const T* p = grad + (int64_t)row * stride + column;
@@ -937,7 +935,7 @@ template <typename T>
 cudaError_t launch_relay(const void* grad, int64_t stride, int64_t rows, int64_t outputs, int64_t pitch, void* out,
                          cudaStream_t stream)
 {
-    const int64_t per_row = pitch / 8 < 2 ? 2 : pitch / 8;
+    const int64_t per_row = pitch / 8;
     const uint64_t vectors = (uint64_t)rows * (uint64_t)per_row, blocks = (vectors + 255) / 256;
     if (blocks > 0x7fffffffu)
         return cudaErrorInvalidValue;
