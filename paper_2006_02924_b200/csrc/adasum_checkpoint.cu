@@ -4,18 +4,69 @@
 // Every kernel here is one pass over a matrix, bound by HBM traffic.  A thread handles vectors of eight
 // consecutive features; four neighbouring lanes hold a group of 32, so a group's largest magnitude is
 // two shuffles away, and rows are filled up to whole groups, so a vector never leaves its row.  A warp takes a
-// strip of up to 32 vectors of a row (of several rows, if rows are short) on kRows rows below each other: all
+// strip of up to 32 vectors of a row (of several rows, if rows are short) on a few rows below each other: all
 // loads of a thread go out before the first is used, and its addresses are one sum apart.
 #include "adasum_operators.cuh"
+
+#include <type_traits>
 
 namespace adasum {
 namespace {
 
 constexpr int kGroup = 32;                 // features that share a step
-constexpr int kBlock = 256;
-constexpr int kRows = 4;                   // vectors per thread, in as many rows: loads in flight
+constexpr int kBlock = 128;
+// Vectors per thread, in as many rows: loads in flight.  Measured on 16384 x 4096 bf16 (1, 2, 4, 8 rows): saving with
+// GELU 80, 72, 70, 82 us; GELU's gradient 78, 78, 82, 121 us; loading 43, 41, 45, 55 us.
+constexpr int kSaveRows = 4;
+constexpr int kApplyRows = 2;
 
 int64_t checkpoint_width(int64_t features) { return (features + kGroup - 1) / kGroup * kGroup; }
+
+// ---- pairs of fp32 values ----------------------------------------------------------------------------
+//
+// With one instruction per value these kernels were bound by instruction issue (30 instructions a value, 64 % of
+// all issue slots at half the memory's speed); the packed forms do two values per instruction.
+
+struct Pair {
+    unsigned long long v;
+};
+__device__ __forceinline__ Pair pair_of(float a, float b)
+{
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p.v) : "f"(a), "f"(b));
+    return p;
+}
+__device__ __forceinline__ Pair both(float a) { return pair_of(a, a); }
+__device__ __forceinline__ float2 values_of(Pair p)
+{
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(p.v));
+    return f;
+}
+__device__ __forceinline__ Pair operator+(Pair a, Pair b)
+{
+    Pair c;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(c.v) : "l"(a.v), "l"(b.v));
+    return c;
+}
+__device__ __forceinline__ Pair operator*(Pair a, Pair b)
+{
+    Pair c;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(c.v) : "l"(a.v), "l"(b.v));
+    return c;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c)
+{
+    Pair d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return d;
+}
+template <typename F>
+__device__ __forceinline__ Pair each(Pair a, F f)
+{
+    const float2 v = values_of(a);
+    return pair_of(f(v.x), f(v.y));
+}
 
 // ---- activations -------------------------------------------------------------------------------------
 
@@ -31,6 +82,7 @@ __device__ __forceinline__ float reciprocal_approx(float x)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ Pair magnitude(Pair a) { return Pair{a.v & 0x7fffffff7fffffffull}; }
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kInvSqrt2Pi = 0.3989422804014327f;
@@ -41,19 +93,20 @@ constexpr float kTanhCubic = 0.044715f;
 // and r is a polynomial of degree 6 without constant term in t = 1 / (1 + 0.31 a): a fit to r on
 // 0 <= a <= 14 that levels out the relative error (5e-6, against 5e-4 / 2 for one rounding to fp16; beyond 14 both
 // factors of the result vanish in 16 bits).  fp32 results call erfcf and expf.
-__device__ __forceinline__ float normal_cdf_16(float x, float& e)
+__device__ __forceinline__ Pair normal_cdf_16(Pair x, Pair& e)
 {
-    const float a = fabsf(x);
-    e = exp2_approx(-0.5f * kLog2e * x * x);
-    const float t = reciprocal_approx(fmaf(0.31f, a, 1.0f));
-    float r = -0.0739287332f;
-    r = fmaf(r, t, 0.180449123f);
-    r = fmaf(r, t, 0.0157461931f);
-    r = fmaf(r, t, 0.133428877f);
-    r = fmaf(r, t, 0.120441553f);
-    r = fmaf(r, t, 0.123860669f);
-    const float tail = r * t * e;
-    return x < 0.0f ? tail : 1.0f - tail;
+    e = each(x * x * both(-0.5f * kLog2e), exp2_approx);
+    const Pair t = each(fma2(both(0.31f), magnitude(x), both(1.0f)), reciprocal_approx);
+    Pair r = both(-0.0739287332f);
+    r = fma2(r, t, both(0.180449123f));
+    r = fma2(r, t, both(0.0157461931f));
+    r = fma2(r, t, both(0.133428877f));
+    r = fma2(r, t, both(0.120441553f));
+    r = fma2(r, t, both(0.123860669f));
+    const Pair tail = r * t * e;
+    // x < 0: tail; else 1 - tail, as side * tail + (1 - side) / 2 with side = -sign(x)
+    const Pair side{((~x.v) & 0x8000000080000000ull) | 0x3f8000003f800000ull};
+    return fma2(side, tail, fma2(side, both(-0.5f), both(0.5f)));
 }
 
 // s = 1 / (1 + exp(-z)), and 1 - s without the subtraction (which would leave nothing of it for large z).
@@ -65,59 +118,177 @@ __device__ __forceinline__ float logistic(float z, float& rest)
     rest = z >= 0.0f ? small : large;
     return z >= 0.0f ? large : small;
 }
+template <bool WIDE>
+__device__ __forceinline__ Pair logistic(Pair z, Pair& rest)
+{
+    const float2 v = values_of(z);
+    float2 s, r;
+    s.x = logistic<WIDE>(v.x, r.x);
+    s.y = logistic<WIDE>(v.y, r.y);
+    rest = pair_of(r.x, r.y);
+    return pair_of(s.x, s.y);
+}
 
 // WIDE: the result is stored in fp32, so the accurate functions are used.
 template <int ACT, bool WIDE>
-__device__ __forceinline__ float activation(float x)
+__device__ __forceinline__ Pair activation(Pair x)
 {
     if constexpr (ACT == ADASUM_ACT_RELU)
-        return x > 0.0f ? x : 0.0f * x;
+        return each(x, [](float a) { return a > 0.0f ? a : 0.0f * a; });
     if constexpr (ACT == ADASUM_ACT_GELU) {
         if constexpr (WIDE) {
-            return x * (0.5f * erfcf(-0.70710678f * x));
+            return each(x, [](float a) { return a * (0.5f * erfcf(-0.70710678f * a)); });
         } else {
-            float e;
+            Pair e;
             return x * normal_cdf_16(x, e);
         }
     }
-    float rest;
+    Pair rest;
     if constexpr (ACT == ADASUM_ACT_GELU_TANH)      // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u))
-        return x * logistic<WIDE>(2.0f * kTanhScale * x * fmaf(kTanhCubic * x, x, 1.0f), rest);
+        return x * logistic<WIDE>(both(2.0f * kTanhScale) * x * fma2(both(kTanhCubic) * x, x, both(1.0f)), rest);
     if constexpr (ACT == ADASUM_ACT_SILU)
         return x * logistic<WIDE>(x, rest);
     return x;
 }
 
 template <int ACT, bool WIDE>
-__device__ __forceinline__ float activation_slope(float x)
+__device__ __forceinline__ Pair activation_slope(Pair x)
 {
     if constexpr (ACT == ADASUM_ACT_RELU)
-        return x > 0.0f ? 1.0f : 0.0f;
+        return each(x, [](float a) { return a > 0.0f ? 1.0f : 0.0f; });
     if constexpr (ACT == ADASUM_ACT_GELU) {         // Phi + x phi
         if constexpr (WIDE) {
-            return fmaf(x * kInvSqrt2Pi, expf(-0.5f * x * x), 0.5f * erfcf(-0.70710678f * x));
+            return each(x, [](float a) {
+                return fmaf(a * kInvSqrt2Pi, expf(-0.5f * a * a), 0.5f * erfcf(-0.70710678f * a));
+            });
         } else {
-            float e;
-            const float cdf = normal_cdf_16(x, e);
-            return fmaf(x * kInvSqrt2Pi, e, cdf);
+            Pair e;
+            const Pair cdf = normal_cdf_16(x, e);
+            return fma2(x * both(kInvSqrt2Pi), e, cdf);
         }
     }
-    float rest;
+    Pair rest;
     if constexpr (ACT == ADASUM_ACT_GELU_TANH) {    // s + x s (1 - s) 2 u'
-        const float s = logistic<WIDE>(2.0f * kTanhScale * x * fmaf(kTanhCubic * x, x, 1.0f), rest);
-        const float du = 2.0f * kTanhScale * x * fmaf(3.0f * kTanhCubic * x, x, 1.0f);
-        return fmaf(s * rest, du, s);
+        const Pair s = logistic<WIDE>(both(2.0f * kTanhScale) * x * fma2(both(kTanhCubic) * x, x, both(1.0f)), rest);
+        const Pair du = both(2.0f * kTanhScale) * x * fma2(both(3.0f * kTanhCubic) * x, x, both(1.0f));
+        return fma2(s * rest, du, s);
     }
     if constexpr (ACT == ADASUM_ACT_SILU) {
-        const float s = logistic<WIDE>(x, rest);
-        return fmaf(s * rest, x, s);
+        const Pair s = logistic<WIDE>(x, rest);
+        return fma2(s * rest, x, s);
     }
-    return 1.0f;
+    return both(1.0f);
+}
+
+// ---- vectors of eight ----------------------------------------------------------------------------------
+
+struct Eight {
+    Pair p[4];
+};
+
+// A vector as it lies in memory: eight elements of T.
+template <typename T>
+struct Raw {
+    uint4 w[sizeof(T) / 2];
+};
+
+// VEC: every row starts on 16 bytes and features is a multiple of 8, so each vector is either whole or only
+// padding.  Otherwise the elements are taken one by one.
+template <bool VEC, typename T>
+__device__ __forceinline__ Raw<T> load_vector(const T* p, int count)
+{
+    Raw<T> raw;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i)
+        raw.w[i] = make_uint4(0, 0, 0, 0);
+    if constexpr (VEC) {
+        if (count > 0) {
+#pragma unroll
+            for (int i = 0; i < (int)(sizeof(T) / 2); ++i)
+                raw.w[i] = reinterpret_cast<const uint4*>(p)[i];
+        }
+    } else {
+        using Word = typename std::conditional<sizeof(T) == 4, uint32_t, uint16_t>::type;
+        const Word* q = reinterpret_cast<const Word*>(p);
+        uint32_t* w = reinterpret_cast<uint32_t*>(raw.w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < count) {
+                if constexpr (sizeof(T) == 4)
+                    w[i] = q[i];
+                else
+                    w[i / 2] |= (uint32_t)q[i] << (16 * (i & 1));
+            }
+    }
+    return raw;
+}
+template <typename T>
+__device__ __forceinline__ Eight decode(const Raw<T>& raw)
+{
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(raw.w);
+    Eight x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (__is_same(T, float)) {
+            x.p[i] = pair_of(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+        } else if constexpr (__is_same(T, __half)) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+            x.p[i] = pair_of(f.x, f.y);
+        } else {
+            x.p[i] = pair_of(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+        }
+    }
+    return x;
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ void store_vector(T* p, int count, const Eight& x)
+{
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = values_of(x.p[i]);
+        y[2 * i] = f.x;
+        y[2 * i + 1] = f.y;
+    }
+    if constexpr (VEC) {
+        if (count > 0)
+            store_vector_from_float<8>(p, TypeCode<T>::value, 0, y);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < count)
+                store_from_float(p, TypeCode<T>::value, i, y[i]);
+    }
+}
+
+// Bits of the largest magnitude as an fp32 number; NaN or Inf (exponent 255) if there is one.
+template <typename T>
+__device__ __forceinline__ uint32_t largest(const Raw<T>& raw)
+{
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(raw.w);
+    if constexpr (__is_same(T, float)) {
+        uint32_t top = 0;                       // as integers NaN > Inf > every number
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            top = max(top, w[i] & 0x7fffffffu);
+        return top;
+    } else {
+        using T2 = typename std::conditional<__is_same(T, __half), __half2, __nv_bfloat162>::type;
+        auto half = [&](int i) { return __habs2(*reinterpret_cast<const T2*>(&w[i])); };
+        const T2 m = __hmax2_nan(__hmax2_nan(half(0), half(1)), __hmax2_nan(half(2), half(3)));
+        const float2 f = [&] {
+            if constexpr (__is_same(T, __half))
+                return __half22float2(m);
+            else
+                return __bfloat1622float2(m);
+        }();
+        return max(__float_as_uint(f.x) & 0x7fffffffu, __float_as_uint(f.y) & 0x7fffffffu);
+    }
 }
 
 // ---- codes -------------------------------------------------------------------------------------------
 
-// Step byte of a group from the bits of its largest magnitude (as an integer NaN > Inf > every number).
+// Step byte of a group from the bits of its largest magnitude.
 __device__ __forceinline__ uint32_t step_byte(uint32_t top_bits)
 {
     const uint32_t exponent = top_bits >> 23;                // E + 127 (0: zero or subnormal)
@@ -126,30 +297,30 @@ __device__ __forceinline__ uint32_t step_byte(uint32_t top_bits)
 // 2^(byte - 127); Inf for 255, whose codes are 0, so that code * step is NaN.
 __device__ __forceinline__ float step_value(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-// Four codes of x[0 .. 3] packed; inv = 1 / step.  Adding 1.5 * 2^23 rounds to an integer, ties to even,
+// Four codes of two pairs packed; inv = 1 / step.  Adding 1.5 * 2^23 rounds to an integer, ties to even,
 // and leaves it in the low bits.  LIMIT: a magnitude may round to 128.
 template <bool LIMIT>
-__device__ __forceinline__ uint32_t pack_codes(const float* x, float inv)
+__device__ __forceinline__ uint32_t pack_codes(Pair x, Pair y, Pair inv)
 {
     constexpr float kMagic = 12582912.0f;
-    uint32_t b[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float r = fmaf(x[i], inv, kMagic);
-        if constexpr (LIMIT)
-            r = fminf(fmaxf(r, kMagic - 127.0f), kMagic + 127.0f);
-        b[i] = __float_as_uint(r);
+    float2 a = values_of(fma2(x, inv, both(kMagic))), b = values_of(fma2(y, inv, both(kMagic)));
+    if constexpr (LIMIT) {
+        auto limit = [](float r) { return fminf(fmaxf(r, kMagic - 127.0f), kMagic + 127.0f); };
+        a = make_float2(limit(a.x), limit(a.y));
+        b = make_float2(limit(b.x), limit(b.y));
     }
-    return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+    return __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040),
+                       __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
 }
 // Values of four packed codes: byte + 128 placed in the low bits of 2^23, 2^23 + 128 taken off again
 // (exact), times the step (exact).
-__device__ __forceinline__ void unpack_codes(uint32_t packed, float step, float* x)
+__device__ __forceinline__ void unpack_codes(uint32_t packed, Pair step, Pair& x, Pair& y)
 {
     const uint32_t u = packed ^ 0x80808080u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        x[i] = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7540 + i)) - 8388736.0f) * step;
+    auto value = [&](uint32_t selector) { return __uint_as_float(__byte_perm(u, 0x4b000000u, selector)); };
+    const Pair offset = both(-8388736.0f);
+    x = (pair_of(value(0x7540), value(0x7541)) + offset) * step;
+    y = (pair_of(value(0x7542), value(0x7543)) + offset) * step;
 }
 
 // ---- kernels -----------------------------------------------------------------------------------------
@@ -170,6 +341,7 @@ struct Place {
     int count;               // features of the vector inside the matrix (<= 0: only padding)
     bool inside;             // the vector exists (padding included)
 };
+template <int ROWS>
 __device__ __forceinline__ Place place_of(const Strips& s)
 {
     const uint64_t warp = (uint64_t)blockIdx.x * (kBlock / 32) + (threadIdx.x >> 5);
@@ -179,40 +351,12 @@ __device__ __forceinline__ Place place_of(const Strips& s)
     divide_row(s.strips_per_row, warp, band, strip);
     Place p;
     p.step = 32 >> s.lane_bits;
-    p.row0 = (int64_t)band * (kRows * p.step) + (lane >> s.lane_bits);
+    p.row0 = (int64_t)band * (ROWS * p.step) + (lane >> s.lane_bits);
     const int vector = ((int)strip << s.lane_bits) + (lane & ((1 << s.lane_bits) - 1));
     p.inside = warp < s.warps && vector < s.per_row;
     p.column = vector * 8;
     p.count = p.inside ? (int)min((int64_t)8, s.features - p.column) : 0;
     return p;
-}
-
-// VEC: every row of x, y, grad and out starts on 16 bytes and features is a multiple of 8, so each vector is
-// either whole or only padding.
-template <bool VEC, typename T>
-__device__ __forceinline__ void load_vector(const T* p, int count, float (&x)[8])
-{
-    if constexpr (VEC) {
-        if (count > 0) {
-            load_eight(p, x);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                x[i] = 0.0f;
-        }
-    } else {
-        load_up_to_eight(p, false, count, x);
-    }
-}
-template <bool VEC, typename T>
-__device__ __forceinline__ void store_vector(T* p, int count, const float (&y)[8])
-{
-    if constexpr (VEC) {
-        if (count > 0)
-            store_vector_from_float<8>(p, TypeCode<T>::value, 0, y);
-    } else {
-        store_up_to_eight(p, false, count, y);
-    }
 }
 
 template <typename T, int ACT, bool VEC>
@@ -221,29 +365,27 @@ checkpoint_save_kernel(const __grid_constant__ Strips s, const T* x, int64_t x_s
                        int8_t* codes, uint8_t* steps)
 {
     constexpr bool WIDE = sizeof(T) == 4;
-    const Place p = place_of(s);
-    float v[kRows][8];
+    const Place p = place_of<kSaveRows>(s);
+    Raw<T> raw[kSaveRows];
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
+    for (int u = 0; u < kSaveRows; ++u) {
         const int64_t row = p.row0 + u * p.step;
-        load_vector<VEC>(x + row * x_stride + p.column, row < s.rows ? p.count : 0, v[u]);
+        raw[u] = load_vector<VEC>(x + row * x_stride + p.column, row < s.rows ? p.count : 0);
     }
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
+    for (int u = 0; u < kSaveRows; ++u) {
         const int64_t row = p.row0 + u * p.step;
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            top = max(top, __float_as_uint(v[u][i]) & 0x7fffffffu);
+        uint32_t top = largest(raw[u]);
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
         const uint32_t byte = step_byte(top);
-        const float inv = __uint_as_float((254u - min(byte, 254u)) << 23);
+        const Pair inv = both(__uint_as_float((254u - min(byte, 254u)) << 23));
+        Eight v = decode(raw[u]);
         uint2 packed;
-        if ((top & 0x7fffffu) < 0x7f0000u) {     // the largest magnitude is below 127 steps (or a power of two less)
-            packed = make_uint2(pack_codes<false>(v[u], inv), pack_codes<false>(v[u] + 4, inv));
+        if ((top & 0x7fffffu) < 0x7f0000u) {     // the largest magnitude is below 127 steps
+            packed = make_uint2(pack_codes<false>(v.p[0], v.p[1], inv), pack_codes<false>(v.p[2], v.p[3], inv));
         } else {
-            packed = make_uint2(pack_codes<true>(v[u], inv), pack_codes<true>(v[u] + 4, inv));
+            packed = make_uint2(pack_codes<true>(v.p[0], v.p[1], inv), pack_codes<true>(v.p[2], v.p[3], inv));
         }
         if (byte == 255u)
             packed = make_uint2(0, 0);
@@ -254,9 +396,9 @@ checkpoint_save_kernel(const __grid_constant__ Strips s, const T* x, int64_t x_s
                 steps[at / kGroup] = (uint8_t)byte;
             if (y) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    v[u][i] = activation<ACT, WIDE>(v[u][i]);
-                store_vector<VEC>(y + row * y_stride + p.column, p.count, v[u]);
+                for (int i = 0; i < 4; ++i)
+                    v.p[i] = activation<ACT, WIDE>(v.p[i]);
+                store_vector<VEC>(y + row * y_stride + p.column, p.count, v);
             }
         }
     }
@@ -269,34 +411,36 @@ checkpoint_apply_kernel(const __grid_constant__ Strips s, const int8_t* codes, c
                         int64_t grad_stride, T* out, int64_t out_stride)
 {
     constexpr bool WIDE = sizeof(T) == 4;
-    const Place p = place_of(s);
+    const Place p = place_of<kApplyRows>(s);
     if (p.count <= 0)
         return;
-    uint2 packed[kRows];
-    uint32_t byte[kRows];
-    float g[kRows][8];
+    uint2 packed[kApplyRows];
+    uint32_t byte[kApplyRows];
+    Raw<T> g[kApplyRows];
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
+    for (int u = 0; u < kApplyRows; ++u) {
         const int64_t row = p.row0 + u * p.step;
         if (row < s.rows) {
             const int64_t at = row * s.width + p.column;
             packed[u] = *reinterpret_cast<const uint2*>(codes + at);
             byte[u] = steps[at / kGroup];
             if constexpr (ACT >= 0)
-                load_vector<VEC>(grad + row * grad_stride + p.column, p.count, g[u]);
+                g[u] = load_vector<VEC>(grad + row * grad_stride + p.column, p.count);
         }
     }
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
+    for (int u = 0; u < kApplyRows; ++u) {
         const int64_t row = p.row0 + u * p.step;
         if (row < s.rows) {
-            float x[8];
-            unpack_codes(packed[u].x, step_value(byte[u]), x);
-            unpack_codes(packed[u].y, step_value(byte[u]), x + 4);
+            const Pair step = both(step_value(byte[u]));
+            Eight x;
+            unpack_codes(packed[u].x, step, x.p[0], x.p[1]);
+            unpack_codes(packed[u].y, step, x.p[2], x.p[3]);
             if constexpr (ACT >= 0) {
+                const Eight d = decode(g[u]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    x[i] = g[u][i] * activation_slope<ACT, WIDE>(x[i]);
+                for (int i = 0; i < 4; ++i)
+                    x.p[i] = d.p[i] * activation_slope<ACT, WIDE>(x.p[i]);
             }
             store_vector<VEC>(out + row * out_stride + p.column, p.count, x);
         }
@@ -331,7 +475,7 @@ adasum_status_t check_matrix(const char* name, const void* p, int64_t stride, in
     return ADASUM_OK;
 }
 
-bool plan_strips(int64_t rows, int64_t features, Strips* s, unsigned* blocks)
+bool plan_strips(int64_t rows, int64_t features, int rows_per_thread, Strips* s, unsigned* blocks)
 {
     s->rows = rows;
     s->features = features;
@@ -341,7 +485,7 @@ bool plan_strips(int64_t rows, int64_t features, Strips* s, unsigned* blocks)
     while (s->lane_bits < 5 && (1 << s->lane_bits) < s->per_row)
         ++s->lane_bits;
     const int64_t strips = (s->per_row + (1 << s->lane_bits) - 1) >> s->lane_bits;
-    const int64_t band = (int64_t)kRows * (32 >> s->lane_bits);
+    const int64_t band = (int64_t)rows_per_thread * (32 >> s->lane_bits);
     s->strips_per_row = row_divider(strips);
     s->warps = (uint64_t)((rows + band - 1) / band) * (uint64_t)strips;
     const uint64_t n = (s->warps + kBlock / 32 - 1) / (kBlock / 32);
@@ -444,7 +588,7 @@ adasum_status_t adasum_checkpoint_save(const void* x, int64_t x_stride, int64_t 
         return fail(ADASUM_ERR_ARG, "checkpoint overlaps x or y");
     Strips s;
     unsigned blocks;
-    if (!plan_strips(rows, features, &s, &blocks))
+    if (!plan_strips(rows, features, kSaveRows, &s, &blocks))
         return fail(ADASUM_ERR_ARG, "%lld x %lld is too large", (long long)rows, (long long)features);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
     profile_mark(stream, -1, 0, 0, true);
@@ -478,7 +622,7 @@ adasum_status_t adasum_checkpoint_load(const void* checkpoint, int64_t rows, int
         return fail(ADASUM_ERR_ARG, "checkpoint overlaps out");
     Strips s;
     unsigned blocks;
-    if (!plan_strips(rows, features, &s, &blocks))
+    if (!plan_strips(rows, features, kApplyRows, &s, &blocks))
         return fail(ADASUM_ERR_ARG, "%lld x %lld is too large", (long long)rows, (long long)features);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
     profile_mark(stream, -1, 0, 0, true);
@@ -512,7 +656,7 @@ adasum_status_t adasum_checkpoint_act_grad(const void* checkpoint, int64_t rows,
         return fail(ADASUM_ERR_ARG, "checkpoint overlaps grad_in");
     Strips s;
     unsigned blocks;
-    if (!plan_strips(rows, features, &s, &blocks))
+    if (!plan_strips(rows, features, kApplyRows, &s, &blocks))
         return fail(ADASUM_ERR_ARG, "%lld x %lld is too large", (long long)rows, (long long)features);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
     profile_mark(stream, -1, 0, 0, true);

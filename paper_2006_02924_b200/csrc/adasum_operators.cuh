@@ -114,17 +114,5 @@ __device__ __forceinline__ void load_up_to_eight(const T* p, bool vec, int count
             x[i] = i < count ? load_one(p + i) : 0.0f;
     }
 }
-template <typename T>
-__device__ __forceinline__ void store_up_to_eight(T* p, bool vec, int count, const float (&y)[8])
-{
-    if (vec && count == 8) {
-        store_vector_from_float<8>(p, TypeCode<T>::value, 0, y);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < count)
-                store_from_float(p, TypeCode<T>::value, i, y[i]);
-    }
-}
 
 }  // namespace adasum
