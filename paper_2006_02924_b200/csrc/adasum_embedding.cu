@@ -7,10 +7,11 @@
 //                          of a large vocabulary is the larger part of the traffic, and most of its rows
 //                          have no token)
 //   embedding_sum_kernel   cuts the sorted list into tiles of equal length, whatever the rows' counts
-//                          are; a block walks its tile once, a row's terms in registers, and writes rows
-//                          that lie inside the tile; the sums of the rows that cross the tile's ends
-//                          go to the workspace
-//   embedding_join_kernel  adds those, tile by tile in order, and writes the rows
+//                          are; a block has all terms of its tile on their way into shared memory at once,
+//                          adds them up run by run and writes the rows.  A run that goes on beyond the tile
+//                          is followed for up to one more tile's length; of longer runs every tile leaves
+//                          its share in the workspace
+//   embedding_join_kernel  adds those shares, tile by tile in order, and writes the rows
 //
 // Every sum has a fixed association, so results are deterministic without atomics.
 #include <cooperative_groups.h>
@@ -83,6 +84,7 @@ constexpr int kSortCluster = 8;
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kDigits = 256;
+constexpr int kSortAhead = 4;              // rounds of 32 whose loads are issued together
 
 // Table rows [0, num_rows) are the keys; tokens outside get the key num_rows and end up last.
 // A stable radix sort, one byte per pass, least significant first.  Every warp of the cluster owns a
@@ -116,14 +118,20 @@ __device__ void sort_tokens(const Id* tokens, uint32_t n, uint32_t num_rows, int
         for (int d = lane; d < kDigits; d += 32)
             next[warp][d] = 0;
         __syncwarp();
-        for (uint32_t i0 = begin; i0 < end; i0 += 32) {
-            const uint32_t i = i0 + lane;
-            const bool mine = i < end;
-            const uint32_t digit = mine ? (item(i).x >> shift) & (kDigits - 1) : kDigits;
-            const uint32_t same = __match_any_sync(0xffffffffu, digit);
-            if (mine && lane == __ffs(same) - 1)
-                next[warp][digit] += __popc(same);
-            __syncwarp();
+        for (uint32_t i0 = begin; i0 < end; i0 += 32 * kSortAhead) {
+            uint32_t digit[kSortAhead];
+#pragma unroll
+            for (int j = 0; j < kSortAhead; ++j) {
+                const uint32_t i = i0 + 32 * j + lane;
+                digit[j] = i < end ? (item(i).x >> shift) & (kDigits - 1) : kDigits;
+            }
+#pragma unroll
+            for (int j = 0; j < kSortAhead; ++j) {
+                const uint32_t same = __match_any_sync(0xffffffffu, digit[j]);
+                if (digit[j] < kDigits && lane == __ffs(same) - 1)
+                    next[warp][digit[j]] += __popc(same);
+                __syncwarp();
+            }
         }
         __syncthreads();
         // counts -> places within the block's share of each digit
@@ -162,21 +170,28 @@ __device__ void sort_tokens(const Id* tokens, uint32_t n, uint32_t num_rows, int
                 next[w][threadIdx.x] += start;
         }
         __syncthreads();
-        for (uint32_t i0 = begin; i0 < end; i0 += 32) {
-            const uint32_t i = i0 + lane;
-            const bool mine = i < end;
-            const uint2 it = mine ? item(i) : make_uint2(0, 0);
-            const uint32_t digit = mine ? (it.x >> shift) & (kDigits - 1) : kDigits;
-            const uint32_t same = __match_any_sync(0xffffffffu, digit);
-            uint32_t place = 0;
-            if (mine)
-                place = next[warp][digit] + __popc(same & ((1u << lane) - 1));
-            __syncwarp();
-            if (mine && lane == __ffs(same) - 1)
-                next[warp][digit] += __popc(same);
-            __syncwarp();
-            if (mine)
-                dst[place] = it;
+        for (uint32_t i0 = begin; i0 < end; i0 += 32 * kSortAhead) {
+            uint2 it[kSortAhead];
+#pragma unroll
+            for (int j = 0; j < kSortAhead; ++j) {
+                const uint32_t i = i0 + 32 * j + lane;
+                it[j] = i < end ? item(i) : make_uint2(0, 0);
+            }
+#pragma unroll
+            for (int j = 0; j < kSortAhead; ++j) {
+                const bool mine = i0 + 32 * j + lane < end;
+                const uint32_t digit = mine ? (it[j].x >> shift) & (kDigits - 1) : kDigits;
+                const uint32_t same = __match_any_sync(0xffffffffu, digit);
+                uint32_t place = 0;
+                if (mine)
+                    place = next[warp][digit] + __popc(same & ((1u << lane) - 1));
+                __syncwarp();
+                if (mine && lane == __ffs(same) - 1)
+                    next[warp][digit] += __popc(same);
+                __syncwarp();
+                if (mine)
+                    dst[place] = it[j];
+            }
         }
         cluster.sync();      // the pass's list is complete, and every block has read the counts
     }
@@ -189,7 +204,13 @@ __device__ void write_zeros(char* p, int64_t bytes, int64_t worker, int64_t work
     const int64_t vectors = (bytes - head) / 16, tail = bytes - head - vectors * 16;
     uint4* body = reinterpret_cast<uint4*>(p + head);
     const int64_t thread = worker * blockDim.x + threadIdx.x, threads = workers * blockDim.x;
-    for (int64_t i = thread; i < vectors; i += threads)
+    int64_t i = thread;
+    for (; i + 3 * threads < vectors; i += 4 * threads) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            body[i + j * threads] = make_uint4(0, 0, 0, 0);
+    }
+    for (; i < vectors; i += threads)
         body[i] = make_uint4(0, 0, 0, 0);
     if (thread < head / 2)
         reinterpret_cast<uint16_t*>(p)[thread] = 0;
@@ -214,8 +235,7 @@ embedding_sort_kernel(const Id* tokens, uint32_t n, uint32_t num_rows, int passe
 // ---- sums ------------------------------------------------------------------------------------------------
 
 constexpr int kSumThreads = 128;
-constexpr int kMaxTile = 64;
-constexpr int kInFlight = 8;            // terms whose loads are issued together
+constexpr int kMaxTile = 32;
 
 struct SumArgs {
     const uint2* sorted;
@@ -255,91 +275,128 @@ __device__ __forceinline__ void write_row(const SumArgs& a, uint32_t row, int64_
 }
 
 // VE: elements a thread owns; more than one only where a row divides into vectors that are 16-byte
-// aligned in grad_out.  grid.x = tiles, grid.y = blocks per row of kSumThreads * VE columns.
+// aligned in grad_out.  grid.x = tiles, grid.y = blocks per row of kSumThreads * VE columns; dynamic shared
+// memory: one tile's terms (16 bytes, or one float, per thread and term; a thread reads back only its own).
 template <typename T, int VE>
 __global__ void __launch_bounds__(kSumThreads)
-embedding_sum_kernel(SumArgs a, const T* __restrict__ grad)
+embedding_sum_kernel(const __grid_constant__ SumArgs a, const T* __restrict__ grad)
 {
-    __shared__ uint32_t row[kMaxTile + 2], position[kMaxTile];       // row[0] and row[m + 1]: the neighbours
+    extern __shared__ __align__(16) unsigned char terms[];
+    // row[1 + i], position[i]: entry i of the tile, on into the next tile; row[0]: the entry before
+    __shared__ uint32_t row[2 * kMaxTile + 2], position[2 * kMaxTile + 1];
     constexpr uint32_t kNone = 0xffffffffu;
     const uint32_t begin = blockIdx.x * (uint32_t)a.tile;
     const int m = (int)min((uint32_t)a.tile, a.n - begin);
-    for (int i = threadIdx.x; i < m + 2; i += kSumThreads) {
+    for (int i = threadIdx.x; i < m + a.tile + 2; i += kSumThreads) {
         const int64_t at = (int64_t)begin + i - 1;
         const uint2 it = at >= 0 && at < (int64_t)a.n ? a.sorted[at] : make_uint2(kNone, 0);
         row[i] = it.x;
-        if (i >= 1 && i <= m)
+        if (i >= 1)
             position[i - 1] = it.y;
     }
+    // did the run that this tile begins with start in the tile before?  (entry before that tile)
+    const uint32_t earlier = begin > (uint32_t)a.tile ? a.sorted[begin - a.tile - 1].x : kNone;
     __syncthreads();
+    const uint32_t first = row[1], last = row[m];
+    int skip = 0;                      // leading entries that the tile before adds up
+    bool enters = false;               // the leading run is a long one that started earlier
+    if (row[0] == first) {
+        int length = 1;                // of the leading run from here, as far as it matters
+        while (length <= a.tile && row[1 + length] == first)
+            ++length;
+        if (earlier != first && length <= a.tile)
+            skip = length;
+        else
+            enters = true;
+    }
+    int extra = 0;                     // entries of the last run beyond the tile
+    bool goes_on = false;              // more than one tile's length of them: left to the join
+    if (skip < m && !(enters && first == last)) {
+        while (extra <= a.tile && row[1 + m + extra] == last)
+            ++extra;
+        goes_on = extra > a.tile;
+        if (goes_on)
+            extra = 0;
+    }
+    const int stop = m + extra;
+    const uint32_t stage = static_cast<uint32_t>(__cvta_generic_to_shared(terms)) + threadIdx.x * (VE > 1 ? 16 : 4);
+    constexpr int kPitch = kSumThreads * (VE > 1 ? 16 : 4);          // bytes from term to term
     for (int64_t column = ((int64_t)blockIdx.y * kSumThreads + threadIdx.x) * VE; column < a.dim;
          column += (int64_t)gridDim.y * kSumThreads * VE) {
         float sum[VE];
 #pragma unroll
         for (int i = 0; i < VE; ++i)
             sum[i] = 0.0f;
-        int start = 0;                  // where the current run starts in the tile
-        auto flush = [&](int end) {
-            const uint32_t r = row[1 + start];
-            if (r < a.num_rows) {
-                const bool enters = start == 0 && row[0] == r, goes_on = end == m && row[m + 1] == r;
-                if (!enters && !goes_on) {
-                    write_row<VE>(a, r, column, sum);
-                } else {
-                    float* edge = a.edges + ((int64_t)blockIdx.x * 2 + (enters ? 0 : 1)) * a.dim + column;
-#pragma unroll
-                    for (int i = 0; i < VE; ++i)
-                        edge[i] = sum[i];
+        int start = skip;              // where the current run starts
+        for (int base = skip; base < stop; base += a.tile) {
+            const int batch = min(a.tile, stop - base);
+            if constexpr (VE > 1) {
+#pragma unroll 4
+                for (int i = 0; i < batch; ++i)
+                    if (row[1 + base + i] < a.num_rows)
+                        cp_async_16B_shared(stage + i * kPitch, grad + (int64_t)position[base + i] * a.stride + column);
+                cp_async_commit();
+                cp_async_wait<0>();
+            } else {
+#pragma unroll 8
+                for (int i = 0; i < batch; ++i) {
+                    const float x = row[1 + base + i] < a.num_rows
+                                        ? Element<T>::one(grad + (int64_t)position[base + i] * a.stride + column)
+                                        : 0.0f;
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(stage + i * kPitch), "f"(x));
                 }
             }
+            for (int i = 0; i < batch; ++i) {
+                float x[VE];
+                if constexpr (VE > 1)
+                    decode_vector<T>(load_shared_16B(stage + i * kPitch), x);
+                else
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[0]) : "r"(stage + i * kPitch));
 #pragma unroll
-            for (int i = 0; i < VE; ++i)
-                sum[i] = 0.0f;
-            start = end;
-        };
-        for (int i0 = 0; i0 < m; i0 += kInFlight) {
-            float x[kInFlight][VE];
+                for (int e = 0; e < VE; ++e)
+                    sum[e] += x[e];
+                const int end = base + i + 1;
+                const uint32_t r = row[end];
+                if (end < stop && row[1 + end] == r)
+                    continue;
+                // the run ends here, or the tile's share of it
+                if (r < a.num_rows) {
+                    const bool from_before = start == 0 && enters;
+                    if (!from_before && !(end == stop && goes_on)) {
+                        write_row<VE>(a, r, column, sum);
+                    } else {
+                        float* edge = a.edges + ((int64_t)blockIdx.x * 2 + (from_before ? 0 : 1)) * a.dim + column;
 #pragma unroll
-            for (int u = 0; u < kInFlight; ++u) {
-                if (i0 + u < m) {
-                    const T* p = grad + (int64_t)position[i0 + u] * a.stride + column;
-                    if constexpr (VE > 1)
-                        Element<T>::vec(p, x[u]);
-                    else
-                        x[u][0] = Element<T>::one(p);
+                        for (int e = 0; e < VE; ++e)
+                            edge[e] = sum[e];
+                    }
                 }
-            }
 #pragma unroll
-            for (int u = 0; u < kInFlight; ++u) {
-                if (i0 + u < m) {
-                    if (i0 + u > start && row[1 + i0 + u] != row[1 + start])
-                        flush(i0 + u);
-#pragma unroll
-                    for (int i = 0; i < VE; ++i)
-                        sum[i] += x[u][i];
-                }
+                for (int e = 0; e < VE; ++e)
+                    sum[e] = 0.0f;
+                start = end;
             }
         }
-        flush(m);
     }
 }
 
-// Rows that cross tiles: the tile in which the run starts owns the row.  grid.x = tiles (but the last),
+// Rows whose run goes on for more than a tile's length beyond the tile in which it starts, which owns the row.  grid.x = tiles (but the last),
 // grid.y = blocks per row of 32 columns; warp w adds every eighth part of the run's edges, and the warps'
 // sums are added in order.
 constexpr int kJoinThreads = 256;
 constexpr int kJoinWarps = kJoinThreads / 32;
 
-__global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(SumArgs a)
+__global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(const __grid_constant__ SumArgs a)
 {
     __shared__ float part[kJoinWarps][32];
     const uint32_t tile = blockIdx.x, tiles = (a.n + a.tile - 1) / a.tile;
     const uint32_t begin = tile * (uint32_t)a.tile, next = begin + a.tile;      // next < n: not the last tile
-    const uint32_t r = a.sorted[next - 1].x;
-    if (r >= a.num_rows || a.sorted[next].x != r)
-        return;                                         // nothing goes on into the next tile
-    if (begin > 0 && a.sorted[begin - 1].x == r)
-        return;                                         // the run started before this tile: not the owner
+    if ((uint64_t)next + a.tile >= a.n)
+        return;
+    const uint32_t r = a.sorted[next - 1].x, beyond = a.sorted[next + a.tile].x;
+    const uint32_t before = begin > 0 ? a.sorted[begin - 1].x : 0xffffffffu;
+    if (r >= a.num_rows || beyond != r || before == r)
+        return;                                         // no long run starts in this tile
     // last tile of the run: the sorted rows ascend, so count the following tiles that begin with r
     uint32_t count = 0;
     for (;;) {
@@ -377,7 +434,7 @@ __global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(SumArgs a)
 // ---- host ------------------------------------------------------------------------------------------------
 
 // Entries per tile.
-int sum_tile(int64_t n) { return n < 16384 ? 32 : kMaxTile; }
+int sum_tile(int64_t n) { return n < 2048 ? 8 : n < 8192 ? 16 : kMaxTile; }
 
 struct GradLayout {
     size_t sorted, spare, edges, total;
@@ -564,6 +621,7 @@ adasum_status_t adasum_embedding_grad(const void* grad_out, int64_t grad_out_str
     a.accumulate = accumulate != 0;
     a.edges = reinterpret_cast<float*>(ws + lay.edges);
     const unsigned tiles = (unsigned)((num_tokens + a.tile - 1) / a.tile);
+    cudaError_t launch_error = cudaSuccess;
     with_type(dtype, [&](auto t) {
         using T = decltype(t);
         constexpr int VE = Element<T>::kVec;
@@ -572,11 +630,18 @@ adasum_status_t adasum_embedding_grad(const void* grad_out, int64_t grad_out_str
         const int64_t columns = (int64_t)kSumThreads * (vec ? VE : 1);
         const int64_t slices = (dim + columns - 1) / columns;
         const dim3 grid(tiles, (unsigned)(slices < 65535 ? slices : 65535));
-        if (vec)
-            embedding_sum_kernel<T, VE><<<grid, kSumThreads, 0, stream>>>(a, static_cast<const T*>(grad_out));
-        else
-            embedding_sum_kernel<T, 1><<<grid, kSumThreads, 0, stream>>>(a, static_cast<const T*>(grad_out));
+        const size_t bytes = (size_t)a.tile * kSumThreads * (vec ? 16 : 4);
+        if (vec) {
+            if (bytes > 48 * 1024)
+                launch_error = cudaFuncSetAttribute(embedding_sum_kernel<T, VE>,
+                                                    cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+            if (launch_error == cudaSuccess)
+                embedding_sum_kernel<T, VE><<<grid, kSumThreads, bytes, stream>>>(a, static_cast<const T*>(grad_out));
+        } else {
+            embedding_sum_kernel<T, 1><<<grid, kSumThreads, bytes, stream>>>(a, static_cast<const T*>(grad_out));
+        }
     });
+    ADASUM_CUDA_CHECK(launch_error);
     ADASUM_CUDA_CHECK(cudaGetLastError());
     profile_mark(stream, ADASUM_KERNEL_EMBEDDING_SUM, 0, 0, false);
     if (tiles > 1) {
