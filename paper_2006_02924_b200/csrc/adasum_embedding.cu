@@ -431,21 +431,33 @@ embedding_sum_kernel(const __grid_constant__ SumArgs a, const T* __restrict__ gr
     }
 }
 
-// Rows whose run goes on for more than a tile's length beyond the tile in which it starts.  A block takes 32
-// columns of one such run at a time; warp w adds every eighth part of the run's edges, and the warps' sums are
-// added in order.
-constexpr int kJoinThreads = 256;
+__device__ __forceinline__ void load_sums(const float* p, float (&x)[4])
+{
+    const float4 v = *reinterpret_cast<const float4*>(p);
+    x[0] = v.x;
+    x[1] = v.y;
+    x[2] = v.z;
+    x[3] = v.w;
+}
+
+__device__ __forceinline__ void load_sums(const float* p, float (&x)[1]) { x[0] = *p; }
+
+// Rows whose run goes on for more than a tile's length beyond the tile in which it starts.  A block takes 32 VE
+// columns of one such run at a time; every warp adds its part of the run's edges, and the warps' sums are added in
+// order.
+constexpr int kJoinThreads = 512;
+constexpr int kInFlight = 8;            // edges whose loads are issued together
 constexpr int kJoinWarps = kJoinThreads / 32;
 
-__global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(const __grid_constant__ SumArgs a)
+template <int VE>
+__device__ void join_runs(const SumArgs& a, uint32_t runs, float (*part)[32 * 4])
 {
-    __shared__ float part[kJoinWarps][32];
-    const uint32_t runs = *a.long_runs, tiles = (a.n + a.tile - 1) / a.tile;
-    const int64_t slices = (a.dim + 31) / 32;
+    const uint32_t tiles = (a.n + a.tile - 1) / a.tile;
+    const int64_t slices = (a.dim + 32 * VE - 1) / (32 * VE);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int64_t item = blockIdx.x; item < runs * slices; item += gridDim.x) {
         const uint32_t tile = a.long_runs[1 + item / slices];
-        const int64_t column = item % slices * 32 + lane;
+        const int64_t column = (item % slices * 32 + lane) * VE;
         const uint32_t r = a.sorted[(int64_t)(tile + 1) * a.tile - 1].x;
         // last tile of the run: the sorted rows ascend, so count the following tiles that begin with r
         uint32_t count = 0;
@@ -459,23 +471,50 @@ __global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(const __gr
         }
         const uint32_t edges = count + 1;               // this tile's second edge, then `count` first edges
         const uint32_t share = (edges + kJoinWarps - 1) / kJoinWarps;
-        float sum = 0.0f;
+        float sum[VE] = {};
         if (column < a.dim) {
             const uint32_t from = warp * share, to = min(edges, from + share);
-#pragma unroll 8
-            for (uint32_t k = from; k < to; ++k)
-                sum += a.edges[((int64_t)(tile + k) * 2 + (k == 0 ? 1 : 0)) * a.dim + column];
+            const float* first = a.edges + (int64_t)tile * 2 * a.dim + column;
+            for (uint32_t k0 = from; k0 < to; k0 += kInFlight) {
+                float x[kInFlight][VE];
+#pragma unroll
+                for (int j = 0; j < kInFlight; ++j) {
+                    const uint32_t k = min(k0 + j, to - 1);
+                    load_sums(first + ((int64_t)k * 2 + (k == 0 ? 1 : 0)) * a.dim, x[j]);
+                }
+#pragma unroll
+                for (int j = 0; j < kInFlight; ++j)
+                    if (k0 + j < to) {
+#pragma unroll
+                        for (int e = 0; e < VE; ++e)
+                            sum[e] += x[j][e];
+                    }
+            }
         }
-        part[warp][lane] = sum;
+#pragma unroll
+        for (int e = 0; e < VE; ++e)
+            part[warp][lane * VE + e] = sum[e];
         __syncthreads();
         if (warp == 0 && column < a.dim) {
-            float total[1] = {part[0][lane]};
-            for (int w = 1; w < kJoinWarps; ++w)
-                total[0] += part[w][lane];
-            write_row<1>(a, r, column, total);
+#pragma unroll
+            for (int e = 0; e < VE; ++e)
+                for (int w = 1; w < kJoinWarps; ++w)
+                    sum[e] += part[w][lane * VE + e];
+            write_row<VE>(a, r, column, sum);
         }
         __syncthreads();
     }
+}
+
+__global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(const __grid_constant__ SumArgs a)
+{
+    __shared__ float part[kJoinWarps][32 * 4];
+    const uint32_t runs = *a.long_runs;
+    // four columns per lane where that still leaves every block something to do
+    if (a.table_vec && runs * ((a.dim + 127) / 128) >= gridDim.x)
+        join_runs<4>(a, runs, part);
+    else
+        join_runs<1>(a, runs, part);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------
@@ -723,7 +762,9 @@ adasum_status_t adasum_embedding_grad(const void* grad_out, int64_t grad_out_str
     profile_mark(stream, ADASUM_KERNEL_EMBEDDING_SUM, 0, 0, false);
     if (num_tokens > 2 * a.tile) {         // a long run has more than a tile's length beyond its first entry's tile
         const int64_t slices = (dim + 31) / 32;
-        const int64_t most = slices * (num_tokens / a.tile), resident = (int64_t)sms * 4;
+        const int64_t most = slices * (num_tokens / a.tile), resident = (int64_t)sms * 2;
+        // rows of four-element vectors, 16-byte aligned in the workspace and at least 8-byte aligned in the table
+        a.table_vec = aligned_to(grad_table, 16) && dim % 4 == 0;
         embedding_join_kernel<<<(unsigned)(most < resident ? most : resident), kJoinThreads, 0, stream>>>(a);
         ADASUM_CUDA_CHECK(cudaGetLastError());
         profile_mark(stream, ADASUM_KERNEL_EMBEDDING_SUM, 1, 0, false);
