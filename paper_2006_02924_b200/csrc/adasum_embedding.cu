@@ -270,6 +270,7 @@ __global__ void __cluster_dims__(kSortCluster, 1, 1) __launch_bounds__(kSortThre
 embedding_sort_kernel(const Id* tokens, uint32_t n, uint32_t num_rows, int passes, uint2* sorted, uint2* spare,
                       uint32_t* long_runs, char* table, int64_t table_bytes)
 {
+    start_next_kernel();
     if (blockIdx.x < kSortCluster) {
         if (blockIdx.x == 0 && threadIdx.x == 0)
             *long_runs = 0;
@@ -330,6 +331,8 @@ template <typename T, int VE>
 __global__ void __launch_bounds__(kSumThreads)
 embedding_sum_kernel(const __grid_constant__ SumArgs a, const T* __restrict__ grad)
 {
+    wait_for_previous_kernel();
+    start_next_kernel();
     extern __shared__ __align__(16) unsigned char terms[];
     // row[1 + i], position[i]: entry i of the tile, on into the next tile; row[0]: the entry before
     __shared__ uint32_t row[2 * kMaxTile + 2], position[2 * kMaxTile + 1];
@@ -508,6 +511,7 @@ __device__ void join_runs(const SumArgs& a, uint32_t runs, float (*part)[32 * 4]
 
 __global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(const __grid_constant__ SumArgs a)
 {
+    wait_for_previous_kernel();
     __shared__ float part[kJoinWarps][32 * 4];
     const uint32_t runs = *a.long_runs;
     // four columns per lane where that still leaves every block something to do
@@ -743,6 +747,7 @@ adasum_status_t adasum_embedding_grad(const void* grad_out, int64_t grad_out_str
     a.long_runs = long_runs;
     a.edges = reinterpret_cast<float*>(ws + lay.edges);
     const unsigned tiles = (unsigned)((num_tokens + a.tile - 1) / a.tile);
+    cudaError_t launch_error = cudaSuccess;
     with_type(dtype, [&](auto t) {
         using T = decltype(t);
         constexpr int VE = Element<T>::kVec;
@@ -753,20 +758,22 @@ adasum_status_t adasum_embedding_grad(const void* grad_out, int64_t grad_out_str
         const dim3 grid(tiles, (unsigned)(slices < 65535 ? slices : 65535));
         const size_t bytes = (size_t)a.tile * kSumThreads * (vec ? 16 : 4);
         if (vec) {
-            embedding_sum_kernel<T, VE><<<grid, kSumThreads, bytes, stream>>>(a, static_cast<const T*>(grad_out));
+            launch_error = launch_after(embedding_sum_kernel<T, VE>, grid, kSumThreads, bytes, stream, a,
+                                        static_cast<const T*>(grad_out));
         } else {
-            embedding_sum_kernel<T, 1><<<grid, kSumThreads, bytes, stream>>>(a, static_cast<const T*>(grad_out));
+            launch_error = launch_after(embedding_sum_kernel<T, 1>, grid, kSumThreads, bytes, stream, a,
+                                        static_cast<const T*>(grad_out));
         }
     });
-    ADASUM_CUDA_CHECK(cudaGetLastError());
+    ADASUM_CUDA_CHECK(launch_error);
     profile_mark(stream, ADASUM_KERNEL_EMBEDDING_SUM, 0, 0, false);
     if (num_tokens > 2 * a.tile) {         // a long run has more than a tile's length beyond its first entry's tile
         const int64_t slices = (dim + 31) / 32;
         const int64_t most = slices * (num_tokens / a.tile), resident = (int64_t)sms * 2;
         // rows of four-element vectors, 16-byte aligned in the workspace and at least 8-byte aligned in the table
         a.table_vec = aligned_to(grad_table, 16) && dim % 4 == 0;
-        embedding_join_kernel<<<(unsigned)(most < resident ? most : resident), kJoinThreads, 0, stream>>>(a);
-        ADASUM_CUDA_CHECK(cudaGetLastError());
+        ADASUM_CUDA_CHECK(launch_after(embedding_join_kernel, dim3((unsigned)(most < resident ? most : resident)), kJoinThreads,
+                                       0, stream, a));
         profile_mark(stream, ADASUM_KERNEL_EMBEDDING_SUM, 1, 0, false);
     }
     return ADASUM_OK;

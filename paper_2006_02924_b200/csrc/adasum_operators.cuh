@@ -68,6 +68,25 @@ inline RowDivider row_divider(int64_t per_row)
     return RowDivider{per_row > 1 ? ~uint64_t(0) / (uint64_t)per_row + 1 : 0, (uint32_t)per_row};
 }
 
+// Launches a kernel that begins with wait_for_previous_kernel(): it may be brought in while the stream's previous
+// kernel still runs (one that called start_next_kernel()), which hides the launch.
+template <typename... Params, typename... Args>
+cudaError_t launch_after(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t shared_bytes, cudaStream_t stream,
+                         Args&&... args)
+{
+    cudaLaunchConfig_t config = {};
+    config.gridDim = grid;
+    config.blockDim = dim3(threads);
+    config.dynamicSmemBytes = shared_bytes;
+    config.stream = stream;
+    cudaLaunchAttribute attribute;
+    attribute.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attribute.val.programmaticStreamSerializationAllowed = 1;
+    config.attrs = &attribute;
+    config.numAttrs = 1;
+    return cudaLaunchKernelEx(&config, kernel, Params(args)...);
+}
+
 // ---- device ----------------------------------------------------------------------------------------
 
 __device__ __forceinline__ void divide_row(const RowDivider& d, uint64_t n, uint64_t& row, uint32_t& at)
@@ -75,6 +94,12 @@ __device__ __forceinline__ void divide_row(const RowDivider& d, uint64_t n, uint
     row = d.per_row > 1 ? __umul64hi(n, d.factor) : n;
     at = (uint32_t)(n - row * d.per_row);
 }
+
+// Until the previous kernel of the stream has ended and its writes are visible.  The first thing that every
+// thread of a kernel launched by launch_after does: then "ended" also covers the kernels before that one.
+__device__ __forceinline__ void wait_for_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// From here on the stream's next kernel may be brought in.
+__device__ __forceinline__ void start_next_kernel() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 template <typename T>
 struct TypeCode;

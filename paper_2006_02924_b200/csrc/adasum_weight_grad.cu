@@ -19,12 +19,11 @@
 //        significant bits times a power of two) and back to shared memory in the swizzled form the tensor
 //        core reads.  (Codes loaded by these warps themselves, ahead of their use, were 3.5 times slower:
 //        the fence that makes their stores visible to the tensor core waits for every load on its way.)
-//   D    one thread of the pair's first block issues the multiplications; eight warps per block add the
-//        sums of every 256 tokens from tensor memory into fp32 registers
+//   D    one thread of the pair's first block issues the multiplications; eight warps per block add sums of every 512 tokens from tensor memory into fp32 registers
 //
-// The last point is for precision: the tensor core truncates where it adds, which over thousands of
-// tokens would be a bias of 1e-5; 16 additions of 16 products each between roundings to nearest keep the
-// result at the error of an fp32 sum.  Tensor memory holds two such sums, so the next is formed while the
+// The last point is for precision: the tensor core truncates where it adds, and over thousands of tokens that
+// adds up; 32 additions of 16 products each between roundings to nearest stay below the error of an fp32
+// sum.  (256, 512 or 1024 tokens: 134, 128, 126 us for 16384 tokens of 1024 x 4096.)  Tensor memory holds two such sums, so the next is formed while the
 // previous one is read.
 //
 // The steps of all tiles, tile after tile, are cut into equal runs, one per pair, so every pair works to
@@ -44,7 +43,7 @@ constexpr int kGroup = 32;                       // features that share a step b
 constexpr int kHalf = 128;                       // features and outputs that a block of the pair brings
 constexpr int kTileSide = 256;                   // features and outputs of a pair's tile
 constexpr int kDepth = 64;                       // tokens per step
-constexpr int kChain = 4;                        // steps that are summed in tensor memory
+constexpr int kChain = 8;                        // steps that are summed in tensor memory
 constexpr int kStages = 7;                       // steps of gradients, codes and step bytes that are on their way
 constexpr int kDecoded = 3;                      // steps of decoded values
 constexpr int kPanelBytes = kDepth * 128;        // 64 features or outputs x 64 tokens, two bytes each
@@ -384,6 +383,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
     __shared__ uint32_t tensor_memory_slot;
     __shared__ float bias_part[4][kHalf];
 
+    start_next_kernel();             // the join; it waits for this kernel's end by itself
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const uint32_t unit_begin = first_unit(a.units, pairs, pair), unit_end = first_unit(a.units, pairs, pair + 1);
@@ -414,6 +414,11 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    if (warp == kCopyWarp && lane == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&grad_map) : "memory");
+        if (a.width > 0)
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&code_map) : "memory");
+    }
     __syncthreads();
     cluster_barrier();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -664,35 +669,41 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                 }
             }
         } else if (warp == kStepWarp) {
-            // ---- step bytes: a lane loads two rows per step, a whole unit ahead of their use
+            // ---- step bytes: a lane loads two rows per step, kBatch steps ahead of their use
+            constexpr int kBatch = 4;
             const int64_t groups = a.width / kGroup;
-            uint32_t w[kChain][2];
+            uint32_t w[kBatch][2];
             Ring<kStages> ring;
-            auto load = [&](const Cursor& c) {
+            auto load = [&](const Cursor& c, uint32_t from) {
                 const int64_t group = (int64_t)c.tile_k * (kTileSide / kGroup) + rank * (kHalf / kGroup);
 #pragma unroll
-                for (int j = 0; j < kChain; ++j) {
-                    const int64_t t = (int64_t)((c.first_step() + j) / PLANES) * kDepth + lane;
+                for (int j = 0; j < kBatch; ++j) {
+                    const int64_t t = (int64_t)((c.first_step() + from + j) / PLANES) * kDepth + lane;
                     w[j][0] = load_steps(a.steps, groups, a.rows, t, group);
                     w[j][1] = load_steps(a.steps, groups, a.rows, t + 32, group);
                 }
             };
             Cursor c(a, unit_begin, unit_end);
-            load(c);
+            uint32_t from = 0;               // first step of the batch within the unit
+            load(c, from);
             while (!c.done()) {
-                uint32_t v[kChain][2];
+                uint32_t v[kBatch][2];
 #pragma unroll
-                for (int j = 0; j < kChain; ++j) {
+                for (int j = 0; j < kBatch; ++j) {
                     v[j][0] = w[j][0];
                     v[j][1] = w[j][1];
                 }
-                const uint32_t steps = c.steps(a);
-                c.advance(a);
+                const int steps = (int)min((uint32_t)kBatch, c.steps(a) - from);
+                from += kBatch;
+                if (from >= c.steps(a)) {
+                    from = 0;
+                    c.advance(a);
+                }
                 if (!c.done())
-                    load(c);
+                    load(c, from);
 #pragma unroll
-                for (int j = 0; j < kChain; ++j) {
-                    if (j < (int)steps) {
+                for (int j = 0; j < kBatch; ++j) {
+                    if (j < steps) {
                         wait(multiplied0 + 8 * ring.stage, ring.phase ^ 1);
                         step_words[ring.stage][lane] = v[j][0];
                         step_words[ring.stage][lane + 32] = v[j][1];
@@ -722,6 +733,7 @@ constexpr int kJoinParts = 2 * kTileSide / (kJoinThreads / 32);
 __global__ void __launch_bounds__(kJoinThreads)
 weight_grad_join_kernel(const __grid_constant__ WeightGradArgs a, uint32_t pairs, bool vec)
 {
+    wait_for_previous_kernel();
     const uint32_t tile = blockIdx.x;
     const uint32_t first = pair_of_unit(a.units, pairs, tile * a.chains);
     const uint32_t last = pair_of_unit(a.units, pairs, tile * a.chains + a.chains - 1);
@@ -834,7 +846,7 @@ struct WorkLayout {
     bool fits;
 };
 
-// `pairs` here is the most that any device may use; the launch takes at most half its multiprocessors.
+// `pairs` here is the most that any device may use; the launch takes no more than are resident at once.
 WorkLayout work_layout(int64_t rows, int64_t features, int64_t outputs, adasum_dtype_t dtype)
 {
     auto up = [](int64_t x, int64_t to) { return (x + to - 1) / to * to; };
@@ -862,9 +874,47 @@ WorkLayout work_layout(int64_t rows, int64_t features, int64_t outputs, adasum_d
     return l;
 }
 
-uint32_t launch_pairs(const WorkLayout& l)
+// Pairs that are resident at once.  A pair keeps to one group of multiprocessors, so groups with an odd number of
+// them leave one without a partner: fewer than half the multiprocessors.  One pair too many would do its whole
+// run after all others' (twice the time).
+template <typename T, int PLANES, bool BIAS>
+uint32_t resident_pairs()
 {
-    const uint32_t most = (uint32_t)device_sms() / 2;
+    static uint32_t cached[64] = {};
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= 64)
+        return 0;
+    if (cached[device] == 0) {
+        auto* kernel = weight_grad_kernel<T, PLANES, BIAS>;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedBytes) != cudaSuccess)
+            return 0;
+        cudaLaunchConfig_t config = {};
+        config.gridDim = dim3(2 * kMaxPairs);
+        config.blockDim = dim3(kBlockThreads);
+        config.dynamicSmemBytes = kSharedBytes;
+        cudaLaunchAttribute attribute;
+        attribute.id = cudaLaunchAttributeClusterDimension;
+        attribute.val.clusterDim.x = 2;
+        attribute.val.clusterDim.y = attribute.val.clusterDim.z = 1;
+        config.attrs = &attribute;
+        config.numAttrs = 1;
+        int clusters = 0;
+        if (cudaOccupancyMaxActiveClusters(&clusters, kernel, &config) != cudaSuccess || clusters < 1)
+            return 0;
+        cached[device] = clusters < kMaxPairs ? (uint32_t)clusters : kMaxPairs;
+    }
+    return cached[device];
+}
+// For a call's type; which of the two kernels is asked makes no difference to the shape of its blocks.
+uint32_t launch_pairs(const WorkLayout& l, adasum_dtype_t dtype, bool bias)
+{
+    uint32_t most = 0;
+    if (dtype == ADASUM_F32)
+        most = bias ? resident_pairs<__nv_bfloat16, 3, true>() : resident_pairs<__nv_bfloat16, 3, false>();
+    else if (dtype == ADASUM_F16)
+        most = bias ? resident_pairs<__half, 1, true>() : resident_pairs<__half, 1, false>();
+    else
+        most = bias ? resident_pairs<__nv_bfloat16, 1, true>() : resident_pairs<__nv_bfloat16, 1, false>();
     return l.pairs < most ? l.pairs : most;
 }
 
@@ -917,11 +967,7 @@ adasum_status_t describe_gradients(CUtensorMap* map, const void* base, adasum_dt
 template <typename T, int PLANES, bool BIAS>
 cudaError_t launch_product(const WeightGradArgs& a, const CUtensorMap (&map)[2], uint32_t pairs, cudaStream_t stream)
 {
-    auto* kernel = weight_grad_kernel<T, PLANES, BIAS>;
-    const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedBytes);
-    if (err != cudaSuccess)
-        return err;
-    kernel<<<2 * pairs, kBlockThreads, kSharedBytes, stream>>>(a, map[0], map[1]);
+    weight_grad_kernel<T, PLANES, BIAS><<<2 * pairs, kBlockThreads, kSharedBytes, stream>>>(a, map[0], map[1]);
     return cudaGetLastError();
 }
 template <typename T, int PLANES>
@@ -1017,9 +1063,9 @@ adasum_status_t adasum_checkpoint_weight_grad(const void* checkpoint, int64_t ro
             ADASUM_CUDA_CHECK(cudaMemsetAsync(grad_bias, 0, bias_bytes, stream));
         return ADASUM_OK;
     }
-    const uint32_t pairs = launch_pairs(l);
+    const uint32_t pairs = launch_pairs(l, dtype, grad_bias != nullptr);
     if (pairs == 0)
-        return fail(ADASUM_ERR_CUDA, "no current device");
+        return fail(ADASUM_ERR_CUDA, "no device that can run a pair of blocks");
     char* ws = static_cast<char*>(workspace);
     // 16-byte rows are copied as they lie; others, and fp32, are laid out in the workspace first
     const bool relay = dtype == ADASUM_F32 || !rows_aligned(grad_out, grad_out_stride, eb);
@@ -1072,8 +1118,8 @@ adasum_status_t adasum_checkpoint_weight_grad(const void* checkpoint, int64_t ro
         split = first_unit(l.units, pairs, p) % l.chains != 0;
     if (split || grad_bias) {
         const bool vec = aligned_to(grad_weight, 16) && features % 4 == 0;
-        weight_grad_join_kernel<<<dim3(l.tiles, split ? kJoinParts : 1), kJoinThreads, 0, stream>>>(a, pairs, vec);
-        ADASUM_CUDA_CHECK(cudaGetLastError());
+        ADASUM_CUDA_CHECK(launch_after(weight_grad_join_kernel, dim3(l.tiles, split ? kJoinParts : 1), kJoinThreads, 0, stream,
+                                       a, pairs, vec));
         profile_mark(stream, ADASUM_KERNEL_WEIGHT_GRAD, 2, 0, false);
     }
     return ADASUM_OK;
@@ -1095,12 +1141,12 @@ adasum_status_t adasum_checkpoint_weight_grad_status(int64_t rows, int64_t featu
         return fail(ADASUM_ERR_ARG, "invalid sizes");
     if (l.units == 0)
         return ADASUM_OK;                  // such a call launches no product
-    const uint32_t pairs = launch_pairs(l);
+    const uint32_t blocks = 2 * launch_pairs(l, dtype, false);
     int words[2 * kMaxPairs] = {};
     cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
-    ADASUM_CUDA_CHECK(cudaMemcpyAsync(words, workspace, 2 * pairs * sizeof(int), cudaMemcpyDeviceToHost, stream));
+    ADASUM_CUDA_CHECK(cudaMemcpyAsync(words, workspace, blocks * sizeof(int), cudaMemcpyDeviceToHost, stream));
     ADASUM_CUDA_CHECK(cudaStreamSynchronize(stream));
-    for (uint32_t i = 0; i < 2 * pairs; ++i)
+    for (uint32_t i = 0; i < blocks; ++i)
         if (words[i] == ADASUM_DEVICE_TIMEOUT)
             return fail(ADASUM_ERR_TIMEOUT, "a bounded wait of block %u ran out", i);
     return ADASUM_OK;
