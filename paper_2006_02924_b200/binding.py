@@ -440,71 +440,68 @@ _lib.adasum_checkpoint_weight_grad.argtypes = [_vp, _i64, _i64, _vp, _i64, _i64,
                                                ctypes.c_int, _i32, _vp, ctypes.c_size_t, _vp]
 
 
+# These calls sit in a training step's inner loop: their wrappers avoid what costs a microsecond each in Python
+# (device objects, context managers, tensors built from keyword-laden factories).
+
 def _matrix(name: str, t, rows=None, cols=None):
     """Checks a CUDA matrix with contiguous rows; returns its row stride in elements."""
     if t.dim() != 2 or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA matrix")
-    shape = t.shape
+    shape, strides = t.shape, t.stride()
     if (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
         raise ValueError(f"{name} is {tuple(shape)}, need ({rows}, {cols})")
-    row_stride, col_stride = t.stride()
-    if col_stride != 1 and shape[1] > 1:
+    if strides[1] != 1 and shape[1] > 1:
         raise ValueError(f"{name} must have contiguous rows")
-    return row_stride if shape[0] > 1 else max(row_stride, shape[1])
+    return strides[0] if shape[0] > 1 else max(strides[0], shape[1])
 
 
-def _operator_dtype(name: str, dtype) -> int:
+def _operator_dtype(dtype) -> int:
     code = _DTYPES.get(dtype)
     if code is None:
-        raise TypeError(f"{name} is {dtype}: fp32, fp16 or bf16")
+        raise TypeError(f"{dtype}: fp32, fp16 or bf16")
     return code
 
 
-def _one_device(first, *others):
-    for t in others:
-        if t is not None and t.device != first.device:
-            raise ValueError(f"tensors on {first.device} and {t.device}")
+def _same_device(device: int, *tensors):
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"a tensor is on {t.device}, not on cuda:{device}")
 
 
-def _operator_stream(first, stream):
-    """Stream handle for a call on the tensors' device: the given stream, or that device's current one."""
+def _operator_call(device: int, stream, function, *args):
+    """Calls ``function(*args, stream handle)`` with the tensors' device current, on ``stream`` or that device's
+    current one; raises on any status but ADASUM_OK."""
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(first.device.index)
-    return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
-
-
-def _operator_call(first, function, *args):
-    """Calls `function` with the tensors' device current; raises on any status but ADASUM_OK."""
-    index = first.device.index
-    if index == torch.cuda.current_device():
-        status = function(*args)
+        handle = torch._C._cuda_getCurrentRawStream(device)
     else:
-        with torch.cuda.device(index):
-            status = function(*args)
+        handle = int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
+    if device == torch._C._cuda_getDevice():
+        status = function(*args, handle)
+    else:
+        with torch.cuda.device(device):
+            status = function(*args, handle)
     if status != ADASUM_OK:
         raise AdasumError(status)
 
 
-def _allocate(first, stream, shape, dtype):
+def _allocate(like, stream, shape, dtype):
     """A tensor for a call on `stream`: the caching allocator must not hand it on before that stream is done."""
-    t = torch.empty(shape, dtype=dtype, device=first.device)
+    t = like.new_empty(shape, dtype=dtype)
     if stream is not None and t.numel() > 0:
         if not hasattr(stream, "cuda_stream"):
-            stream = torch.cuda.ExternalStream(int(stream), device=first.device)
+            stream = torch.cuda.ExternalStream(int(stream), device=like.device)
         # the memory may still be in use on the current stream, from which it was handed out
-        stream.wait_stream(torch.cuda.current_stream(first.device))
+        stream.wait_stream(torch.cuda.current_stream(like.device))
         t.record_stream(stream)
     return t
 
 
-def _operator_workspace(first, stream, workspace, need: int):
+def _operator_workspace(like, stream, workspace, need: int):
     if workspace is None:
-        workspace = _allocate(first, stream, max(need, 256), torch.uint8)
-    elif not workspace.is_contiguous():
+        return _allocate(like, stream, max(need, 256), torch.uint8)
+    if not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
-    else:
-        _one_device(first, workspace)
-    return workspace, workspace.numel() * workspace.element_size()
+    return workspace
 
 
 def _tokens(tokens):
@@ -523,12 +520,14 @@ def adasum_embedding_forward(table, tokens, scale: float = 1.0, out=None, out_dt
     count = tokens.numel()
     num_rows, dim = table.shape
     if out is None:
-        out = _allocate(table, stream, (count, dim), out_dtype or table.dtype)
-    _one_device(table, tokens, out)
-    _operator_call(table, _lib.adasum_embedding_forward, table.data_ptr(), table_stride, num_rows, dim,
-                   _operator_dtype("table", table.dtype), tokens.data_ptr(), tokens.element_size(), count, scale,
-                   out.data_ptr(), _matrix("out", out, count, dim), _operator_dtype("out", out.dtype),
-                   _operator_stream(table, stream))
+        out, out_stride = _allocate(table, stream, (count, dim), out_dtype or table.dtype), dim
+    else:
+        out_stride = _matrix("out", out, count, dim)
+    device = table.get_device()
+    _same_device(device, tokens, out)
+    _operator_call(device, stream, _lib.adasum_embedding_forward, table.data_ptr(), table_stride, num_rows, dim,
+                   _operator_dtype(table.dtype), tokens.data_ptr(), tokens.element_size(), count, scale, out.data_ptr(),
+                   out_stride, _operator_dtype(out.dtype))
     return out
 
 
@@ -555,13 +554,14 @@ def adasum_embedding_grad(grad_out, tokens, num_rows=None, grad_table=None, grad
         num_rows = grad_table.shape[0] if grad_table.dim() == 2 else grad_table.numel() // max(dim, 1)
     if grad_table.numel() != num_rows * dim or (grad_table.dim() == 2 and grad_table.shape[1] != dim):
         raise ValueError(f"grad_table is {tuple(grad_table.shape)}, need ({num_rows}, {dim})")
-    _one_device(grad_out, tokens, grad_table)
-    workspace, ws_bytes = _operator_workspace(
-        grad_out, stream, workspace, _lib.adasum_embedding_grad_workspace_bytes(count, num_rows, dim))
-    _operator_call(grad_out, _lib.adasum_embedding_grad, grad_out.data_ptr(), stride,
-                   _operator_dtype("grad_out", grad_out.dtype), tokens.data_ptr(), tokens.element_size(), count, scale,
-                   grad_table.data_ptr(), num_rows, dim, _operator_dtype("grad_table", grad_table.dtype),
-                   int(accumulate), workspace.data_ptr(), ws_bytes, _operator_stream(grad_out, stream))
+    workspace = _operator_workspace(grad_out, stream, workspace,
+                                    _lib.adasum_embedding_grad_workspace_bytes(count, num_rows, dim))
+    device = grad_out.get_device()
+    _same_device(device, tokens, grad_table, workspace)
+    _operator_call(device, stream, _lib.adasum_embedding_grad, grad_out.data_ptr(), stride,
+                   _operator_dtype(grad_out.dtype), tokens.data_ptr(), tokens.element_size(), count, scale,
+                   grad_table.data_ptr(), num_rows, dim, _operator_dtype(grad_table.dtype), int(accumulate),
+                   workspace.data_ptr(), workspace.numel() * workspace.element_size())
     return grad_table
 
 
@@ -569,13 +569,19 @@ def adasum_checkpoint_bytes(rows: int, features: int) -> int:
     return int(_lib.adasum_checkpoint_bytes(int(rows), int(features)))
 
 
-def _checkpoint(first, checkpoint, rows: int, features: int):
+def _checkpoint_size(rows: int, features: int) -> int:
+    groups = -(-features // ADASUM_CHECKPOINT_GROUP)
+    return rows * groups * (ADASUM_CHECKPOINT_GROUP + 1)
+
+
+def _checkpoint(device: int, checkpoint, rows: int, features: int):
     if checkpoint.dtype != torch.uint8 or not checkpoint.is_contiguous():
         raise TypeError("checkpoint must be a contiguous tensor of uint8")
-    need = _lib.adasum_checkpoint_bytes(rows, features)
+    need = _checkpoint_size(rows, features)
     if checkpoint.numel() < need:
         raise ValueError(f"checkpoint has {checkpoint.numel()} bytes, {rows} x {features} needs {need}")
-    _one_device(first, checkpoint)
+    if checkpoint.get_device() != device:
+        raise ValueError(f"checkpoint is on {checkpoint.device}, not on cuda:{device}")
     return checkpoint.data_ptr()
 
 
@@ -584,27 +590,36 @@ def adasum_checkpoint_save(x, activation: str = "none", out=None, checkpoint=Non
     itself.  With ``want_out=False`` only the checkpoint is written and the first item is None."""
     stride = _matrix("x", x)
     rows, features = x.shape
+    device = x.get_device()
     if checkpoint is None:
-        checkpoint = _allocate(x, stream, _lib.adasum_checkpoint_bytes(rows, features), torch.uint8)
-    if out is None and want_out:
+        checkpoint = _allocate(x, stream, _checkpoint_size(rows, features), torch.uint8)
+    out_stride, out_ptr = features, None
+    if out is not None:
+        out_stride = _matrix("out", out, rows, features)
+        if out.dtype != x.dtype:
+            raise TypeError("out must have the type of x")
+        _same_device(device, out)
+        out_ptr = out.data_ptr()
+    elif want_out:
         out = _allocate(x, stream, (rows, features), x.dtype)
-    if out is not None and out.dtype != x.dtype:
-        raise TypeError("out must have the type of x")
-    _one_device(x, out)
-    _operator_call(x, _lib.adasum_checkpoint_save, x.data_ptr(), stride, rows, features,
-                   _operator_dtype("x", x.dtype), ADASUM_ACT[activation], None if out is None else out.data_ptr(),
-                   0 if out is None else _matrix("out", out, rows, features),
-                   _checkpoint(x, checkpoint, rows, features), _operator_stream(x, stream))
+        out_ptr = out.data_ptr()
+    _operator_call(device, stream, _lib.adasum_checkpoint_save, x.data_ptr(), stride, rows, features,
+                   _operator_dtype(x.dtype), ADASUM_ACT[activation], out_ptr, out_stride,
+                   _checkpoint(device, checkpoint, rows, features))
     return out, checkpoint
 
 
 def adasum_checkpoint_load(checkpoint, rows: int, features: int, dtype=None, out=None, stream=None):
     """``adasum_checkpoint_load`` of the C ABI: the kept values, in ``dtype`` (fp32 by default) or ``out``."""
     if out is None:
-        out = _allocate(checkpoint, stream, (rows, features), dtype or torch.float32)
-    _operator_call(checkpoint, _lib.adasum_checkpoint_load, _checkpoint(out, checkpoint, rows, features), rows,
-                   features, out.data_ptr(), _matrix("out", out, rows, features), _operator_dtype("out", out.dtype),
-                   _operator_stream(checkpoint, stream))
+        if not checkpoint.is_cuda:
+            raise TypeError("checkpoint must be a CUDA tensor")
+        out, out_stride = _allocate(checkpoint, stream, (rows, features), dtype or torch.float32), features
+    else:
+        out_stride = _matrix("out", out, rows, features)
+    device = out.get_device()
+    _operator_call(device, stream, _lib.adasum_checkpoint_load, _checkpoint(device, checkpoint, rows, features), rows,
+                   features, out.data_ptr(), out_stride, _operator_dtype(out.dtype))
     return out
 
 
@@ -613,15 +628,17 @@ def adasum_checkpoint_act_grad(checkpoint, grad_out, activation: str, grad_in=No
     ``grad_out`` itself."""
     stride = _matrix("grad_out", grad_out)
     rows, features = grad_out.shape
+    device = grad_out.get_device()
     if grad_in is None:
-        grad_in = _allocate(grad_out, stream, (rows, features), grad_out.dtype)
-    elif grad_in.dtype != grad_out.dtype:
-        raise TypeError("grad_in must have the type of grad_out")
-    _one_device(grad_out, grad_in)
-    _operator_call(grad_out, _lib.adasum_checkpoint_act_grad, _checkpoint(grad_out, checkpoint, rows, features), rows,
-                   features, ADASUM_ACT[activation], grad_out.data_ptr(), stride,
-                   _operator_dtype("grad_out", grad_out.dtype), grad_in.data_ptr(),
-                   _matrix("grad_in", grad_in, rows, features), _operator_stream(grad_out, stream))
+        grad_in, in_stride = _allocate(grad_out, stream, (rows, features), grad_out.dtype), features
+    else:
+        in_stride = _matrix("grad_in", grad_in, rows, features)
+        if grad_in.dtype != grad_out.dtype:
+            raise TypeError("grad_in must have the type of grad_out")
+        _same_device(device, grad_in)
+    _operator_call(device, stream, _lib.adasum_checkpoint_act_grad, _checkpoint(device, checkpoint, rows, features),
+                   rows, features, ADASUM_ACT[activation], grad_out.data_ptr(), stride,
+                   _operator_dtype(grad_out.dtype), grad_in.data_ptr(), in_stride)
     return grad_in
 
 
@@ -658,16 +675,15 @@ def adasum_checkpoint_weight_grad(checkpoint, grad_out, features=None, grad_weig
             raise TypeError("grad_bias must have the type of grad_weight")
         if not grad_bias.is_contiguous() or grad_bias.numel() != outputs:
             raise ValueError(f"grad_bias must be contiguous and have {outputs} elements")
-    _one_device(grad_out, grad_weight, grad_bias)
-    code = _operator_dtype("grad_out", grad_out.dtype)
-    workspace, ws_bytes = _operator_workspace(
-        grad_out, stream, workspace,
-        _lib.adasum_checkpoint_weight_grad_workspace_bytes(rows, features, outputs, code))
-    _operator_call(grad_out, _lib.adasum_checkpoint_weight_grad, _checkpoint(grad_out, checkpoint, rows, features),
+    code = _operator_dtype(grad_out.dtype)
+    workspace = _operator_workspace(grad_out, stream, workspace,
+                                    _lib.adasum_checkpoint_weight_grad_workspace_bytes(rows, features, outputs, code))
+    device = grad_out.get_device()
+    _same_device(device, grad_weight, grad_bias, workspace)
+    _operator_call(device, stream, _lib.adasum_checkpoint_weight_grad, _checkpoint(device, checkpoint, rows, features),
                    rows, features, grad_out.data_ptr(), stride, outputs, code, scale, grad_weight.data_ptr(),
-                   None if grad_bias is None else grad_bias.data_ptr(),
-                   _operator_dtype("grad_weight", grad_weight.dtype), int(accumulate), workspace.data_ptr(), ws_bytes,
-                   _operator_stream(grad_out, stream))
+                   None if grad_bias is None else grad_bias.data_ptr(), _operator_dtype(grad_weight.dtype),
+                   int(accumulate), workspace.data_ptr(), workspace.numel() * workspace.element_size())
     return grad_weight, grad_bias
 
 
@@ -679,4 +695,4 @@ def adasum_checkpoint_weight_grad_status(rows: int, features: int, outputs: int,
     """``adasum_checkpoint_weight_grad_status`` of the C ABI: 0, or 7 (ADASUM_ERR_TIMEOUT) if a bounded wait of
     the last weight gradient on ``workspace`` ran out.  Synchronises the stream."""
     return int(_lib.adasum_checkpoint_weight_grad_status(int(rows), int(features), int(outputs), _dtype_code(dtype),
-                                                         workspace.data_ptr(), _operator_stream(workspace, stream)))
+                                                         workspace.data_ptr(), _stream_handle(stream)))
