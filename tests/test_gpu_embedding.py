@@ -165,3 +165,51 @@ def test_other_stream_and_graph(b):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(table, want) and torch.equal(out, looked)
+
+
+def test_grad_large_offsets(b):
+    """Gradients beyond 2^31 elements, more tokens than the sort keeps in registers."""
+    n = (1 << 21) + 9
+    dy = torch.zeros(n, 1024, dtype=torch.bfloat16, device="cuda")
+    dy[-5:] = 1.0
+    ids = (torch.arange(n, device="cuda") % 300).to(torch.int32)
+    got = b.adasum_embedding_grad(dy, ids, 301)
+    want = torch.zeros(301, 1024, device="cuda")
+    want[ids[-5:].long()] = 1.0
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("lengths", [[8, 8, 8, 8], [1, 15, 16, 17, 31, 32, 33, 47, 48, 49], [16, 16, 32, 64, 1, 1, 7],
+                                     [7, 1, 9, 24, 25, 3], [2000, 5, 40, 33]])
+@pytest.mark.parametrize("extra", [0, 1, 2100])
+def test_runs_at_the_tiles_ends(b, lengths, extra):
+    """Runs of equal tokens that start, end and go on at every place of the sorted list's tiles (8 or 16 entries),
+    followed by tokens outside the table."""
+    ids = torch.cat([torch.full((c,), 3 * i) for i, c in enumerate(lengths)] + [torch.full((extra,), -7)])
+    gen = _gen(6)
+    ids = ids[torch.randperm(ids.numel())].cuda()
+    dy = torch.randint(-9, 10, (ids.numel(), 40), generator=gen, device="cuda").float()
+    got = b.adasum_embedding_grad(dy, ids, 3 * len(lengths))
+    want, _ = embedding_grad(to64(dy), ids.cpu().numpy(), 3 * len(lengths), 1.0)
+    assert np.array_equal(to64(got), want)          # whole numbers: exact
+
+
+def test_refusals(b):
+    table, ids = torch.ones(5, 8, device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda")
+    with pytest.raises(b.AdasumError, match="DTYPE"):
+        b.adasum_embedding_forward(table.double(), ids)
+    with pytest.raises(ValueError):
+        b.adasum_embedding_forward(table.t(), ids)
+    with pytest.raises(TypeError):
+        b.adasum_embedding_forward(table, ids.float())
+    with pytest.raises(ValueError):
+        b.adasum_embedding_forward(table, ids, out=torch.empty(3, 9, device="cuda"))
+    dy = torch.ones(3, 8, device="cuda")
+    with pytest.raises(ValueError):
+        b.adasum_embedding_grad(dy, ids[:2], 5)
+    with pytest.raises(ValueError):
+        b.adasum_embedding_grad(dy, ids, grad_table=torch.empty(8, 5, device="cuda"))
+    with pytest.raises(ValueError):
+        b.adasum_embedding_grad(dy, ids)
+    with pytest.raises(b.AdasumError, match="WORKSPACE"):
+        b.adasum_embedding_grad(dy, ids, 5, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))

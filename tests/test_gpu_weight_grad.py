@@ -162,3 +162,37 @@ def test_other_stream_and_graph(b):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(dw, want)
+
+
+def test_status_and_refusals(b):
+    x, dy = torch.ones(130, 64, device="cuda"), torch.ones(130, 24, device="cuda")
+    _, kept = b.adasum_checkpoint_save(x, want_out=False)
+    ws = torch.empty(b.adasum_checkpoint_weight_grad_workspace_bytes(130, 64, 24, "f32"), dtype=torch.uint8, device="cuda")
+    b.adasum_checkpoint_weight_grad(kept, dy, features=64, workspace=ws)
+    assert b.adasum_checkpoint_weight_grad_status(130, 64, 24, "f32", ws) == 0
+    with pytest.raises(b.AdasumError, match="WORKSPACE"):
+        b.adasum_checkpoint_weight_grad(kept, dy, features=64, workspace=ws[:1024])
+    with pytest.raises(b.AdasumError, match="DTYPE"):
+        b.adasum_checkpoint_weight_grad(kept, dy.double(), features=64)
+    with pytest.raises(ValueError):
+        b.adasum_checkpoint_weight_grad(kept, dy, features=256)                  # the checkpoint is too small
+    with pytest.raises(ValueError):
+        b.adasum_checkpoint_weight_grad(kept, dy, grad_weight=torch.empty(64, 24, device="cuda"))
+    with pytest.raises(ValueError):
+        b.adasum_checkpoint_weight_grad(kept, dy.t(), features=64)
+    with pytest.raises(TypeError):
+        b.adasum_checkpoint_weight_grad(kept.float(), dy, features=64)
+    with pytest.raises(ValueError):
+        b.adasum_checkpoint_weight_grad(kept, dy, features=64, accumulate=True)  # onto nothing
+
+
+def test_large_offsets(b):
+    """Codes beyond 2^32 bytes: only the last rows hold anything."""
+    rows, features = (1 << 20) + 70, 4160
+    kept = torch.zeros(b.adasum_checkpoint_bytes(rows, features), dtype=torch.uint8, device="cuda")
+    kept[rows * features:] = 127                                                 # step 1
+    kept[(rows - 3) * features:rows * features] = 5
+    dy = torch.zeros(rows, 8, dtype=torch.bfloat16, device="cuda")
+    dy[-2:] = 1.0
+    dw, db = b.adasum_checkpoint_weight_grad(kept, dy, features=features, want_bias=True)
+    assert torch.all(dw == 10.0) and torch.all(db == 2.0)
