@@ -2,15 +2,17 @@
 //
 // The gradient of row v is a sum over the tokens that point at v.  Three launches:
 //
-//   embedding_sort_kernel  the first cluster of blocks sorts (row, position) pairs, stably, by row; all
-//                          other blocks write zeros into the whole gradient table meanwhile (the table
-//                          of a large vocabulary is the larger part of the traffic, and most of its rows
-//                          have no token)
+//   embedding_rank_kernel  (short lists) or embedding_sort_kernel (one cluster of blocks, radix sort): (row,
+//                          position) pairs in the order of rows and, within a row, of positions.  The radix
+//                          sort keeps eight multiprocessors busy for a while; the others write zeros into the
+//                          whole gradient table meanwhile
 //   embedding_sum_kernel   cuts the sorted list into tiles of equal length, whatever the rows' counts
 //                          are; a block has all terms of its tile on their way into shared memory at once,
 //                          adds them up run by run and writes the rows.  A run that goes on beyond the tile
 //                          is followed for up to one more tile's length; of longer runs every tile leaves
-//                          its share in the workspace
+//                          its share in the workspace.  After a ranking, more blocks of the same launch write
+//                          zeros to the rows without a token: for a large vocabulary that is most of the
+//                          traffic, and it hides the sums' latency
 //   embedding_join_kernel  adds those shares, tile by tile in order, and writes the rows
 //
 // Every sum has a fixed association, so results are deterministic without atomics.
@@ -237,7 +239,7 @@ __device__ void sort_tokens(const Id* tokens, uint32_t n, uint32_t num_rows, int
 }
 
 // Blocks beyond the first cluster: zeros over `bytes` bytes at p (any alignment of 2), by bulk copies of a
-// zeroed piece of shared memory (stores of 16 bytes per thread reached 3.9 TB/s here).
+// zeroed piece of shared memory.
 constexpr int kZeroBytes = 8 * 1024;
 __device__ void write_zeros(char* p, int64_t bytes, int64_t worker, int64_t workers)
 {
@@ -264,7 +266,7 @@ __device__ void write_zeros(char* p, int64_t bytes, int64_t worker, int64_t work
         reinterpret_cast<uint16_t*>(p + bytes - tail)[threadIdx.x] = 0;
 }
 
-// Block roles by cluster: cluster 0 sorts, the others write zeros.
+// Cluster 0 sorts; the others write zeros into the whole gradient table meanwhile.
 template <typename Id>
 __global__ void __cluster_dims__(kSortCluster, 1, 1) __launch_bounds__(kSortThreads, 1)
 embedding_sort_kernel(const Id* tokens, uint32_t n, uint32_t num_rows, int passes, uint2* sorted, uint2* spare,
@@ -274,10 +276,58 @@ embedding_sort_kernel(const Id* tokens, uint32_t n, uint32_t num_rows, int passe
     if (blockIdx.x < kSortCluster) {
         if (blockIdx.x == 0 && threadIdx.x == 0)
             *long_runs = 0;
-        if (n > 0)
-            sort_tokens(tokens, n, num_rows, passes, sorted, spare);
+        sort_tokens(tokens, n, num_rows, passes, sorted, spare);
     } else {
         write_zeros(table, table_bytes, (int64_t)blockIdx.x - kSortCluster, (int64_t)gridDim.x - kSortCluster);
+    }
+}
+
+// Short lists: an item's place is the number of items that come before it.  Every block holds all keys in shared
+// memory; a warp counts for one item at a time.  n^2 comparisons, but spread over all multiprocessors and
+// without the radix sort's chain of passes (4608 tokens of 30522 rows: 3 us against 10 us).
+constexpr int kRankThreads = 1024;
+constexpr int64_t kRankMost = 6144;
+
+template <typename Id>
+__global__ void __launch_bounds__(kRankThreads)
+embedding_rank_kernel(const Id* tokens, uint32_t n, uint32_t num_rows, uint2* sorted, uint32_t* long_runs)
+{
+    extern __shared__ __align__(16) uint32_t keys[];         // padded to whole rounds with the largest key
+    start_next_kernel();
+    if (blockIdx.x == 0 && threadIdx.x == 0)
+        *long_runs = 0;
+    const uint32_t padded = (n + 127) / 128 * 128;
+    for (uint32_t i = threadIdx.x; i < padded; i += kRankThreads) {
+        uint32_t key = 0xffffffffu;
+        if (i < n) {
+            const int64_t id = (int64_t)tokens[i];
+            key = id >= 0 && id < (int64_t)num_rows ? (uint32_t)id : num_rows;
+        }
+        keys[i] = key;
+    }
+    __syncthreads();
+    const uint32_t lane = threadIdx.x & 31, warps = gridDim.x * (kRankThreads / 32);
+    for (uint32_t i = blockIdx.x * (kRankThreads / 32) + (threadIdx.x >> 5); i < n; i += warps) {
+        const uint32_t mine = keys[i];
+        // an equal key comes before if its position does: count keys below `mine + 1` in the rounds before the
+        // item's own, below `mine` in those after it, and by position in its own
+        uint32_t before = 0;
+        const uint32_t own = i / 128 * 128;
+        auto count = [&](uint32_t from, uint32_t to, uint32_t limit) {
+#pragma unroll 4
+            for (uint32_t j0 = from; j0 < to; j0 += 128) {
+                const uint4 k = *reinterpret_cast<const uint4*>(keys + j0 + 4 * lane);
+                before += (k.x < limit) + (k.y < limit) + (k.z < limit) + (k.w < limit);
+            }
+        };
+        count(0, own, mine + 1);
+        count(own + 128, padded, mine);
+        const uint32_t j = own + 4 * lane;
+        const uint4 k = *reinterpret_cast<const uint4*>(keys + j);
+        before += (k.x < mine + (j < i)) + (k.y < mine + (j + 1 < i)) + (k.z < mine + (j + 2 < i)) + (k.w < mine + (j + 3 < i));
+        before = __reduce_add_sync(0xffffffffu, before);
+        if (lane == 0)
+            sorted[before] = make_uint2(mine, i);
     }
 }
 
@@ -295,6 +345,8 @@ struct SumArgs {
     void* table;
     int table_dtype;
     bool table_vec, accumulate;
+    uint32_t tiles;          // the first blocks of embedding_sum_kernel; those after them write zeros
+    uint32_t zero_rows;      // rows per such block
     uint32_t* long_runs;     // how many there are, then the tiles in which they start (in no particular order)
     float* edges;            // [tile][0: the run that enters from before, 1: the run that goes on][dim]
 };
@@ -324,8 +376,74 @@ __device__ __forceinline__ void write_row(const SumArgs& a, uint32_t row, int64_
     }
 }
 
+// First entry of the sorted list whose row is not below `row`: a warp narrows the range to a 32nd per step.
+__device__ uint32_t first_entry(const SumArgs& a, uint32_t row)
+{
+    const uint32_t lane = threadIdx.x & 31;
+    uint32_t low = 0, high = a.n;               // the answer is in [low, high]
+    while (low < high) {
+        const uint32_t step = (high - low + 31) / 32;
+        const uint64_t probe = (uint64_t)low + (uint64_t)(lane + 1) * step - 1;
+        const bool less = probe < high && a.sorted[probe].x < row;
+        const uint32_t steps = __popc(__ballot_sync(0xffffffffu, less));      // the rows ascend
+        high = (uint32_t)min((uint64_t)high, (uint64_t)low + (uint64_t)(steps + 1) * step - 1);
+        low += steps * step;
+    }
+    return low;
+}
+
+// Zeros to the rows [from, to) that are not in the sorted list.
+constexpr uint32_t kZeroRows = 256;
+__device__ void write_zero_rows(const SumArgs& a, uint32_t from, uint32_t to)
+{
+    __shared__ bool taken[kZeroRows];
+    for (uint32_t i = threadIdx.x; i < to - from; i += kSumThreads)
+        taken[i] = false;
+    const uint32_t lane = threadIdx.x & 31;
+    const uint32_t low = first_entry(a, from), high = first_entry(a, to);
+    __syncthreads();
+    if (high - low <= 16 * kSumThreads) {
+#pragma unroll 4
+        for (uint32_t i = low + threadIdx.x; i < high; i += kSumThreads)
+            taken[a.sorted[i].x - from] = true;
+    } else {                                    // long runs: looked for row by row
+        for (uint32_t r = threadIdx.x; r < to - from; r += kSumThreads) {
+            uint32_t left = low, right = high;
+            while (left < right) {
+                const uint32_t middle = left + (right - left) / 2;
+                if (a.sorted[middle].x < from + r)
+                    left = middle + 1;
+                else
+                    right = middle;
+            }
+            taken[r] = left < high && a.sorted[left].x == from + r;
+        }
+    }
+    __syncthreads();
+    const int64_t bytes = a.dim * (a.table_dtype == ADASUM_F32 ? 4 : 2);
+    char* rows = static_cast<char*>(a.table) + (int64_t)from * bytes;
+    const int warp = threadIdx.x >> 5;
+    const bool by_sixteen = ((uintptr_t)a.table | (uintptr_t)bytes) % 16 == 0, by_four = ((uintptr_t)a.table | (uintptr_t)bytes) % 4 == 0;
+    for (uint32_t r = warp; r < to - from; r += kSumThreads / 32) {
+        if (taken[r])
+            continue;
+        char* p = rows + (int64_t)r * bytes;
+        if (by_sixteen) {
+            for (int64_t i = lane; i < bytes / 16; i += 32)
+                reinterpret_cast<uint4*>(p)[i] = make_uint4(0, 0, 0, 0);
+        } else if (by_four) {
+            for (int64_t i = lane; i < bytes / 4; i += 32)
+                reinterpret_cast<uint32_t*>(p)[i] = 0;
+        } else {
+            for (int64_t i = lane; i < bytes / 2; i += 32)
+                reinterpret_cast<uint16_t*>(p)[i] = 0;
+        }
+    }
+}
+
 // VE: elements a thread owns; more than one only where a row divides into vectors that are 16-byte
-// aligned in grad_out.  grid.x = tiles, grid.y = blocks per row of kSumThreads * VE columns; dynamic shared
+// aligned in grad_out.  grid.x = tiles (and blocks that write zeros), grid.y = blocks per row of kSumThreads * VE
+// columns (the zeros are left to the first of them); dynamic shared
 // memory: one tile's terms (16 bytes, or one float, per thread and term; a thread reads back only its own).
 template <typename T, int VE>
 __global__ void __launch_bounds__(kSumThreads)
@@ -337,6 +455,12 @@ embedding_sum_kernel(const __grid_constant__ SumArgs a, const T* __restrict__ gr
     // row[1 + i], position[i]: entry i of the tile, on into the next tile; row[0]: the entry before
     __shared__ uint32_t row[2 * kMaxTile + 2], position[2 * kMaxTile + 1];
     constexpr uint32_t kNone = 0xffffffffu;
+    if (blockIdx.x >= a.tiles) {
+        const uint32_t from = (blockIdx.x - a.tiles) * a.zero_rows;
+        if (blockIdx.y == 0)
+            write_zero_rows(a, from, min(a.num_rows, from + a.zero_rows));
+        return;
+    }
     const uint32_t begin = blockIdx.x * (uint32_t)a.tile;
     const int m = (int)min((uint32_t)a.tile, a.n - begin);
     for (int i = threadIdx.x; i < m + a.tile + 2; i += kSumThreads) {
@@ -526,7 +650,7 @@ __global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(const __gr
 // Entries per tile.
 // Measured with 8, 16, 32: 999 tokens (dim 203, fp32) 26, 28, 38 us, 16384 tokens on two rows 44, 36, 38 us, 200000 tokens
 // (dim 256) 237, 222, 234 us.
-int sum_tile(int64_t n) { return n < 2048 ? kMaxTile / 2 : kMaxTile; }
+int sum_tile(int64_t n) { return n > 2 * kMaxTile && n < 2048 ? kMaxTile / 2 : kMaxTile; }
 
 // Clusters of embedding_sort_kernel that are resident at once (a cluster keeps to one group of
 // multiprocessors, so some of these stay without): with one more, its share of the zeros would be written
@@ -713,25 +837,34 @@ adasum_status_t adasum_embedding_grad(const void* grad_out, int64_t grad_out_str
     int passes = 1;
     while (passes < 4 && ((uint64_t)num_rows >> (8 * passes)) != 0)     // the key num_rows itself included
         ++passes;
-    const int64_t zero_bytes = accumulate ? 0 : table_bytes;
-    int64_t fill = (zero_bytes + kZeroBytes - 1) / kZeroBytes;
-    fill = (fill + kSortCluster - 1) / kSortCluster * kSortCluster;
-    const int clusters = token_bytes == 4 ? resident_sort_clusters<int32_t>() : resident_sort_clusters<int64_t>();
-    const int64_t most = (int64_t)(clusters - 1) * kSortCluster;
-    const unsigned blocks = (unsigned)(kSortCluster + (fill < most ? fill : most));
     profile_mark(stream, -1, 0, 0, true);
+    if (num_tokens == 0) {                 // zeros of any type are zero bytes
+        ADASUM_CUDA_CHECK(cudaMemsetAsync(grad_table, 0, (size_t)table_bytes, stream));
+        return ADASUM_OK;
+    }
+    auto sort = [&](auto id) {
+        using Id = decltype(id);
+        const Id* ids = static_cast<const Id*>(tokens);
+        if (num_tokens <= kRankMost) {
+            const int64_t wanted = (num_tokens + kRankThreads / 32 - 1) / (kRankThreads / 32);
+            embedding_rank_kernel<Id><<<(unsigned)(wanted < sms ? wanted : sms), kRankThreads,
+                                        (size_t)((num_tokens + 127) / 128 * 128) * sizeof(uint32_t), stream>>>(
+                ids, (uint32_t)num_tokens, (uint32_t)num_rows, sorted, long_runs);
+        } else {
+            const int64_t zero_bytes = accumulate ? 0 : table_bytes;
+            const int64_t wanted = ((zero_bytes + kZeroBytes - 1) / kZeroBytes + kSortCluster - 1) / kSortCluster + 1;
+            const int64_t clusters = resident_sort_clusters<Id>();
+            embedding_sort_kernel<Id><<<(unsigned)((wanted < clusters ? wanted : clusters) * kSortCluster), kSortThreads, 0,
+                                        stream>>>(ids, (uint32_t)num_tokens, (uint32_t)num_rows, passes, sorted, spare,
+                                                  long_runs, static_cast<char*>(grad_table), zero_bytes);
+        }
+    };
     if (token_bytes == 4)
-        embedding_sort_kernel<int32_t><<<blocks, kSortThreads, 0, stream>>>(
-            static_cast<const int32_t*>(tokens), (uint32_t)num_tokens, (uint32_t)num_rows, passes, sorted, spare,
-            long_runs, static_cast<char*>(grad_table), zero_bytes);
+        sort(int32_t{});
     else
-        embedding_sort_kernel<int64_t><<<blocks, kSortThreads, 0, stream>>>(
-            static_cast<const int64_t*>(tokens), (uint32_t)num_tokens, (uint32_t)num_rows, passes, sorted, spare,
-            long_runs, static_cast<char*>(grad_table), zero_bytes);
+        sort(int64_t{});
     ADASUM_CUDA_CHECK(cudaGetLastError());
     profile_mark(stream, ADASUM_KERNEL_EMBEDDING_SORT, 0, 0, false);
-    if (num_tokens == 0)
-        return ADASUM_OK;
 
     SumArgs a;
     a.sorted = sorted;
@@ -746,7 +879,13 @@ adasum_status_t adasum_embedding_grad(const void* grad_out, int64_t grad_out_str
     a.accumulate = accumulate != 0;
     a.long_runs = long_runs;
     a.edges = reinterpret_cast<float*>(ws + lay.edges);
-    const unsigned tiles = (unsigned)((num_tokens + a.tile - 1) / a.tile);
+    a.tiles = (uint32_t)((num_tokens + a.tile - 1) / a.tile);
+    // about 64 KB of zeros per block
+    const int64_t row_bytes = dim * operator_bytes(grad_dtype), fit = 65536 / row_bytes;
+    a.zero_rows = (uint32_t)(fit < 1 ? 1 : fit < kZeroRows ? fit : kZeroRows);
+    const int64_t zero_blocks = accumulate || num_tokens > kRankMost ? 0 : (num_rows + a.zero_rows - 1) / a.zero_rows;
+    if (a.tiles + zero_blocks > 0x7fffffff)
+        return fail(ADASUM_ERR_ARG, "%lld tokens and %lld rows are too many", (long long)num_tokens, (long long)num_rows);
     cudaError_t launch_error = cudaSuccess;
     with_type(dtype, [&](auto t) {
         using T = decltype(t);
@@ -755,7 +894,7 @@ adasum_status_t adasum_embedding_grad(const void* grad_out, int64_t grad_out_str
         a.table_vec = vec && aligned_to(grad_table, 16) && dim * operator_bytes(grad_dtype) % 16 == 0;
         const int64_t columns = (int64_t)kSumThreads * (vec ? VE : 1);
         const int64_t slices = (dim + columns - 1) / columns;
-        const dim3 grid(tiles, (unsigned)(slices < 65535 ? slices : 65535));
+        const dim3 grid((unsigned)(a.tiles + zero_blocks), (unsigned)(slices < 65535 ? slices : 65535));
         const size_t bytes = (size_t)a.tile * kSumThreads * (vec ? 16 : 4);
         if (vec) {
             launch_error = launch_after(embedding_sum_kernel<T, VE>, grid, kSumThreads, bytes, stream, a,
