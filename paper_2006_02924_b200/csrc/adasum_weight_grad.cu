@@ -915,6 +915,10 @@ uint32_t launch_pairs(const WorkLayout& l, adasum_dtype_t dtype, bool bias)
         most = bias ? resident_pairs<__half, 1, true>() : resident_pairs<__half, 1, false>();
     else
         most = bias ? resident_pairs<__nv_bfloat16, 1, true>() : resident_pairs<__nv_bfloat16, 1, false>();
+    // Short sums are not cut: 16 steps take 5 us, leaving and joining a tile's parts as long, in one more launch
+    // (18 steps, 333 fp32 tokens of 1000 x 257: 12.6 + 4 us cut into three, 16 us whole).
+    if (l.tiles <= most && l.iterations <= 16)
+        return l.tiles;
     return l.pairs < most ? l.pairs : most;
 }
 
