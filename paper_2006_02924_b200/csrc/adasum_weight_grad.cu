@@ -43,7 +43,8 @@ constexpr int kGroup = 32;                       // features that share a step b
 constexpr int kHalf = 128;                       // features and outputs that a block of the pair brings
 constexpr int kTileSide = 256;                   // features and outputs of a pair's tile
 constexpr int kDepth = 64;                       // tokens per step
-constexpr int kChain = 8;                        // steps that are summed in tensor memory
+// Steps that are summed in tensor memory; fp32 gradients take three steps for the same tokens, each of which truncates.
+constexpr int kChain = 8, kChainPlanes = 4;
 constexpr int kStages = 7;                       // steps of gradients, codes and step bytes that are on their way
 constexpr int kDecoded = 3;                      // steps of decoded values
 constexpr int kPanelBytes = kDepth * 128;        // 64 features or outputs x 64 tokens, two bytes each
@@ -69,8 +70,8 @@ struct WeightGradArgs {
     void* bias;
     int out_dtype;
     bool accumulate;
-    // units of kChain steps, tile after tile (tiles of a column of outputs next to each other)
-    uint32_t tiles_k, tiles, iterations, chains, units;
+    // units of chain_steps steps, tile after tile (tiles of a column of outputs next to each other)
+    uint32_t tiles_k, tiles, iterations, chain_steps, chains, units;
     int* status;             // one word per block
     float* slots;            // [pair][first or last tile of its run][block][output][feature of the block]
     float* bias_slots;       // [pair + tile][256 outputs]: the pairs' shares of the tiles' parts of the bias gradient
@@ -311,10 +312,10 @@ struct Cursor {
     {
         return unit + 1 == stop || chain + 1 == a.chains;
     }
-    __device__ __forceinline__ uint32_t first_step() const { return chain * kChain; }
+    __device__ __forceinline__ uint32_t first_step(const WeightGradArgs& a) const { return chain * a.chain_steps; }
     __device__ __forceinline__ uint32_t steps(const WeightGradArgs& a) const
     {
-        return min((uint32_t)kChain, a.iterations - chain * kChain);
+        return min(a.chain_steps, a.iterations - chain * a.chain_steps);
     }
     __device__ __forceinline__ void advance(const WeightGradArgs& a)
     {
@@ -455,7 +456,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                 // unit, like the products.  The tiles of a column of outputs share the work: each adds up
                 // every tiles_k-th step, so that none is slower than the others.
                 const uint32_t steps = c.steps(a);
-                uint32_t to_mine = (c.tile_k + a.tiles_k - c.first_step() % a.tiles_k) % a.tiles_k;
+                uint32_t to_mine = (c.tile_k + a.tiles_k - c.first_step(a) % a.tiles_k) % a.tiles_k;
                 const int output = 2 * (threadIdx.x & 63), part = threadIdx.x >> 6;
                 float unit_sum[2] = {0.0f, 0.0f};
                 for (uint32_t s = 0; s < steps; ++s) {
@@ -603,8 +604,8 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
             const uint32_t bytes = kOperandBytes + (a.width > 0 ? kCodeBytes : 0);
             for (Cursor c(a, unit_begin, unit_end); !c.done() && waiting; c.advance(a)) {
                 const int n = (int)c.tile_n * kTileSide + (int)rank * kHalf, k = (int)c.tile_k * kTileSide + (int)rank * kHalf;
-                const uint32_t end = c.first_step() + c.steps(a);
-                for (uint32_t step = c.first_step(); step < end; ++step) {
+                const uint32_t end = c.first_step(a) + c.steps(a);
+                for (uint32_t step = c.first_step(a); step < end; ++step) {
                     const uint32_t bar = landed0 + 8 * ring.stage;
                     wait(multiplied0 + 8 * ring.stage, ring.phase ^ 1);
                     if constexpr (BIAS)
@@ -678,7 +679,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                 const int64_t group = (int64_t)c.tile_k * (kTileSide / kGroup) + rank * (kHalf / kGroup);
 #pragma unroll
                 for (int j = 0; j < kBatch; ++j) {
-                    const int64_t t = (int64_t)((c.first_step() + from + j) / PLANES) * kDepth + lane;
+                    const int64_t t = (int64_t)((c.first_step(a) + from + j) / PLANES) * kDepth + lane;
                     w[j][0] = load_steps(a.steps, groups, a.rows, t, group);
                     w[j][1] = load_steps(a.steps, groups, a.rows, t + 32, group);
                 }
@@ -840,7 +841,7 @@ relay_gradients_kernel(const T* grad, int64_t stride, bool vec, int64_t rows, in
 // ---- host -------------------------------------------------------------------------------------------------
 
 struct WorkLayout {
-    uint32_t tiles_k, tiles, iterations, chains, units, pairs;
+    uint32_t tiles_k, tiles, iterations, chain_steps, chains, units, pairs;
     int64_t pitch;
     size_t slots, bias_slots, gradients, total;
     bool fits;
@@ -855,7 +856,8 @@ WorkLayout work_layout(int64_t rows, int64_t features, int64_t outputs, adasum_d
     const int64_t tiles_k = features > 0 ? (features + kTileSide - 1) / kTileSide : 1;
     const int64_t tiles_n = (outputs + kTileSide - 1) / kTileSide;
     const int64_t iterations = (rows + kDepth - 1) / kDepth * planes;
-    const int64_t chains = (iterations + kChain - 1) / kChain;
+    const int64_t chain_steps = planes > 1 ? kChainPlanes : kChain;
+    const int64_t chains = (iterations + chain_steps - 1) / chain_steps;
     const int64_t limit = int64_t(1) << 31;
     l.fits = tiles_k * tiles_n < limit && iterations < limit && (chains == 0 || tiles_k * tiles_n < limit / chains);
     if (!l.fits)
@@ -863,6 +865,7 @@ WorkLayout work_layout(int64_t rows, int64_t features, int64_t outputs, adasum_d
     l.tiles_k = (uint32_t)tiles_k;
     l.tiles = (uint32_t)(tiles_k * tiles_n);
     l.iterations = (uint32_t)iterations;
+    l.chain_steps = (uint32_t)chain_steps;
     l.chains = (uint32_t)chains;
     l.units = (uint32_t)(l.tiles * chains);
     l.pairs = l.units < kMaxPairs ? l.units : kMaxPairs;
@@ -1097,6 +1100,7 @@ adasum_status_t adasum_checkpoint_weight_grad(const void* checkpoint, int64_t ro
     a.tiles_k = l.tiles_k;
     a.tiles = l.tiles;
     a.iterations = l.iterations;
+    a.chain_steps = l.chain_steps;
     a.chains = l.chains;
     a.units = l.units;
     a.status = reinterpret_cast<int*>(ws);
