@@ -70,6 +70,7 @@ struct WeightGradArgs {
     void* bias;
     int out_dtype;
     bool accumulate;
+    bool cut;                // some tile falls to several pairs: the join runs
     // units of chain_steps steps, tile after tile (tiles of a column of outputs next to each other)
     uint32_t tiles_k, tiles, iterations, chain_steps, chains, units;
     int* status;             // one word per block
@@ -453,16 +454,18 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
             }
             if constexpr (BIAS) {
                 // this block's 128 outputs: thread = two outputs, 16 of a step's 64 tokens.  Summed per
-                // unit, like the products.  The tiles of a column of outputs share the work: each adds up
-                // every tiles_k-th step, so that none is slower than the others.
+                // unit, like the products.  Where the join runs anyway, the tiles of a column of outputs share
+                // the work: each adds up every tiles_k-th step, so that none is slower than the others.
                 const uint32_t steps = c.steps(a);
-                uint32_t to_mine = (c.tile_k + a.tiles_k - c.first_step(a) % a.tiles_k) % a.tiles_k;
+                const uint32_t sharers = a.cut ? a.tiles_k : 1;
+                // steps until this tile's next one; never, for the tiles that leave the bias to the first
+                uint32_t to_mine = a.cut ? (c.tile_k + sharers - c.first_step(a) % sharers) % sharers : c.tile_k == 0 ? 0 : ~0u;
                 const int output = 2 * (threadIdx.x & 63), part = threadIdx.x >> 6;
                 float unit_sum[2] = {0.0f, 0.0f};
                 for (uint32_t s = 0; s < steps; ++s) {
                     wait(landed0 + 8 * ring.stage, ring.phase);
                     if (to_mine-- == 0) {
-                        to_mine = a.tiles_k - 1;
+                        to_mine = sharers - 1;
                         const uint32_t panel = stage0 + ring.stage * kStageBytes + (output >> 6) * kPanelBytes;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
@@ -536,10 +539,16 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                 bias_part[part][output] = bias_sum[0];
                 bias_part[part][output + 1] = bias_sum[1];
                 asm volatile("bar.sync 1, 256;" ::: "memory");
-                if (threadIdx.x < kHalf)
-                    a.bias_slots[(int64_t)(pair + c.tile_n * a.tiles_k + c.tile_k) * kTileSide + rank * kHalf + threadIdx.x] =
-                        (bias_part[0][threadIdx.x] + bias_part[1][threadIdx.x]) +
-                        (bias_part[2][threadIdx.x] + bias_part[3][threadIdx.x]);
+                if (threadIdx.x < kHalf) {
+                    const float total = (bias_part[0][threadIdx.x] + bias_part[1][threadIdx.x]) +
+                                        (bias_part[2][threadIdx.x] + bias_part[3][threadIdx.x]);
+                    const int output = rank * kHalf + threadIdx.x;
+                    const int64_t n = (int64_t)c.tile_n * kTileSide + output;
+                    if (a.cut)
+                        a.bias_slots[(int64_t)(pair + c.tile_n * a.tiles_k + c.tile_k) * kTileSide + output] = total;
+                    else if (c.tile_k == 0 && n < a.outputs)
+                        write_gradient(a, a.bias, n, total);
+                }
                 asm volatile("bar.sync 1, 256;" ::: "memory");
             }
         }
@@ -726,8 +735,9 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tensor_memory) : "memory");
 }
 
-// Bias gradients, and tiles whose units fell to several pairs: the pairs' parts added in order.  grid.x = tiles, grid.y = parts of
-// the tile's 2 x 256 rows of 128 features; one warp per row, four features per lane.
+// Where some tile's units fell to several pairs: those tiles, and the bias gradient, the pairs' parts added in
+// order.  grid.x = tiles, grid.y = parts of a tile's 2 x 256 rows of 128 features; one warp per row, four
+// features per lane.
 constexpr int kJoinThreads = 256;
 constexpr int kJoinParts = 2 * kTileSide / (kJoinThreads / 32);
 
@@ -1097,6 +1107,9 @@ adasum_status_t adasum_checkpoint_weight_grad(const void* checkpoint, int64_t ro
     a.bias = grad_bias;
     a.out_dtype = (int)grad_dtype;
     a.accumulate = accumulate != 0;
+    a.cut = false;
+    for (uint32_t p = 1; p < pairs && !a.cut; ++p)
+        a.cut = first_unit(l.units, pairs, p) % l.chains != 0;
     a.tiles_k = l.tiles_k;
     a.tiles = l.tiles;
     a.iterations = l.iterations;
@@ -1121,12 +1134,9 @@ adasum_status_t adasum_checkpoint_weight_grad(const void* checkpoint, int64_t ro
     else
         ADASUM_CUDA_CHECK((launch_product<__nv_bfloat16, 1>(a, map, pairs, stream)));
     profile_mark(stream, ADASUM_KERNEL_WEIGHT_GRAD, 1, 0, false);
-    bool split = false;                    // does any tile fall to several pairs?
-    for (uint32_t p = 1; p < pairs && !split; ++p)
-        split = first_unit(l.units, pairs, p) % l.chains != 0;
-    if (split || grad_bias) {
+    if (a.cut) {
         const bool vec = aligned_to(grad_weight, 16) && features % 4 == 0;
-        ADASUM_CUDA_CHECK(launch_after(weight_grad_join_kernel, dim3(l.tiles, split ? kJoinParts : 1), kJoinThreads, 0, stream,
+        ADASUM_CUDA_CHECK(launch_after(weight_grad_join_kernel, dim3(l.tiles, kJoinParts), kJoinThreads, 0, stream,
                                        a, pairs, vec));
         profile_mark(stream, ADASUM_KERNEL_WEIGHT_GRAD, 2, 0, false);
     }
