@@ -3,9 +3,7 @@
 //
 // Every kernel here is one pass over a matrix, bound by HBM traffic.  A thread handles vectors of eight
 // consecutive features; four neighbouring lanes hold a group of 32, so a group's largest magnitude is
-// two shuffles away, and rows are filled up to whole groups, so a vector never leaves its row.  A warp takes a
-// strip of up to 32 vectors of a row (of several rows, if rows are short) on a few rows below each other: all
-// loads of a thread go out before the first is used, and its addresses are one sum apart.
+// two shuffles away, and rows are filled up to whole groups, so a vector never leaves its row.
 #include "adasum_operators.cuh"
 
 #include <type_traits>
@@ -14,9 +12,9 @@ namespace adasum {
 namespace {
 
 constexpr int kGroup = 32;                 // features that share a step
-constexpr int kBlock = 128;
 // Vectors per thread, in as many rows: loads in flight.  Measured on 16384 x 4096 bf16 (1, 2, 4, 8 rows): saving with
-// GELU 80, 72, 70, 82 us; GELU's gradient 78, 78, 82, 121 us; loading 43, 41, 45, 55 us.
+// GELU 80, 72, 70, 82 us; GELU's gradient 78, 78, 82, 121 us (72 us with two rows and registers for 16 blocks per
+// multiprocessor); loading 43, 41, 45, 55 us.
 constexpr int kSaveRows = 4;
 constexpr int kApplyRows = 2;
 
@@ -89,22 +87,25 @@ constexpr float kInvSqrt2Pi = 0.3989422804014327f;
 constexpr float kTanhScale = 0.7978845608028654f;     // sqrt(2 / pi)
 constexpr float kTanhCubic = 0.044715f;
 
-// Phi(x) and e = exp(-x^2 / 2) for 16-bit results.  Phi(-a) = e * r(a) with r(a) = erfcx(a / sqrt 2) / 2,
-// and r is a polynomial of degree 6 without constant term in t = 1 / (1 + 0.31 a): a fit to r on
-// 0 <= a <= 14 that levels out the relative error (5e-6, against 5e-4 / 2 for one rounding to fp16; beyond 14 both
-// factors of the result vanish in 16 bits).  fp32 results call erfcf and expf.
-__device__ __forceinline__ Pair normal_cdf_16(Pair x, Pair& e)
+// The normal distribution function for 16-bit results: Phi(-a) = e * r(a) for a >= 0, with e = exp(-a^2 / 2) and
+// r(a) = erfcx(a / sqrt 2) / 2.  r is a polynomial of degree 6 without constant term in t = 1 / (1 + 0.31 a): a fit to r
+// on 0 <= a <= 14 that levels out the relative error (5e-6, against 5e-4 / 2 for one rounding to fp16; beyond 14
+// both factors of the result vanish in 16 bits).  Returns r.  fp32 results call erfcf and expf.
+__device__ __forceinline__ Pair normal_tail_16(Pair a, Pair& e)
 {
-    e = each(x * x * both(-0.5f * kLog2e), exp2_approx);
-    const Pair t = each(fma2(both(0.31f), magnitude(x), both(1.0f)), reciprocal_approx);
+    e = each(a * a * both(-0.5f * kLog2e), exp2_approx);
+    const Pair t = each(fma2(both(0.31f), a, both(1.0f)), reciprocal_approx);
     Pair r = both(-0.0739287332f);
     r = fma2(r, t, both(0.180449123f));
     r = fma2(r, t, both(0.0157461931f));
     r = fma2(r, t, both(0.133428877f));
     r = fma2(r, t, both(0.120441553f));
     r = fma2(r, t, both(0.123860669f));
-    const Pair tail = r * t * e;
-    // x < 0: tail; else 1 - tail, as side * tail + (1 - side) / 2 with side = -sign(x)
+    return r * t;
+}
+// x < 0: tail; else 1 - tail, as side * tail + (1 - side) / 2 with side = -sign(x).
+__device__ __forceinline__ Pair tail_or_rest(Pair x, Pair tail)
+{
     const Pair side{((~x.v) & 0x8000000080000000ull) | 0x3f8000003f800000ull};
     return fma2(side, tail, fma2(side, both(-0.5f), both(0.5f)));
 }
@@ -140,7 +141,8 @@ __device__ __forceinline__ Pair activation(Pair x)
             return each(x, [](float a) { return a * (0.5f * erfcf(-0.70710678f * a)); });
         } else {
             Pair e;
-            return x * normal_cdf_16(x, e);
+            const Pair r = normal_tail_16(magnitude(x), e);
+            return x * tail_or_rest(x, r * e);
         }
     }
     Pair rest;
@@ -156,15 +158,15 @@ __device__ __forceinline__ Pair activation_slope(Pair x)
 {
     if constexpr (ACT == ADASUM_ACT_RELU)
         return each(x, [](float a) { return a > 0.0f ? 1.0f : 0.0f; });
-    if constexpr (ACT == ADASUM_ACT_GELU) {         // Phi + x phi
+    if constexpr (ACT == ADASUM_ACT_GELU) {         // Phi + x phi; at -a: e (r - a / sqrt(2 pi)), at a: 1 minus that
         if constexpr (WIDE) {
             return each(x, [](float a) {
                 return fmaf(a * kInvSqrt2Pi, expf(-0.5f * a * a), 0.5f * erfcf(-0.70710678f * a));
             });
         } else {
             Pair e;
-            const Pair cdf = normal_cdf_16(x, e);
-            return fma2(x * both(kInvSqrt2Pi), e, cdf);
+            const Pair a = magnitude(x), r = normal_tail_16(a, e);
+            return tail_or_rest(x, fma2(a, both(-kInvSqrt2Pi), r) * e);
         }
     }
     Pair rest;
@@ -325,42 +327,8 @@ __device__ __forceinline__ void unpack_codes(uint32_t packed, Pair step, Pair& x
 
 // ---- kernels -----------------------------------------------------------------------------------------
 
-// A matrix cut into strips: 2^lane_bits vectors of a row x 2^(5 - lane_bits) rows per lane row.
-struct Strips {
-    int64_t rows, features, width;       // width: features filled up to whole groups
-    int per_row;                         // vectors of a row, a multiple of 4
-    int lane_bits;
-    RowDivider strips_per_row;
-    uint64_t warps;
-};
-
-struct Place {
-    int64_t row0;            // first of the thread's rows; the next ones are `step` further
-    int step;
-    int column;              // first feature
-    int count;               // features of the vector inside the matrix (<= 0: only padding)
-    bool inside;             // the vector exists (padding included)
-};
-template <int ROWS>
-__device__ __forceinline__ Place place_of(const Strips& s)
-{
-    const uint64_t warp = (uint64_t)blockIdx.x * (kBlock / 32) + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
-    uint64_t band;
-    uint32_t strip;
-    divide_row(s.strips_per_row, warp, band, strip);
-    Place p;
-    p.step = 32 >> s.lane_bits;
-    p.row0 = (int64_t)band * (ROWS * p.step) + (lane >> s.lane_bits);
-    const int vector = ((int)strip << s.lane_bits) + (lane & ((1 << s.lane_bits) - 1));
-    p.inside = warp < s.warps && vector < s.per_row;
-    p.column = vector * 8;
-    p.count = p.inside ? (int)min((int64_t)8, s.features - p.column) : 0;
-    return p;
-}
-
 template <typename T, int ACT, bool VEC>
-__global__ void __launch_bounds__(kBlock)
+__global__ void __launch_bounds__(kStripThreads)
 checkpoint_save_kernel(const __grid_constant__ Strips s, const T* x, int64_t x_stride, T* y, int64_t y_stride,
                        int8_t* codes, uint8_t* steps)
 {
@@ -390,7 +358,7 @@ checkpoint_save_kernel(const __grid_constant__ Strips s, const T* x, int64_t x_s
         if (byte == 255u)
             packed = make_uint2(0, 0);
         if (p.inside && row < s.rows) {
-            const int64_t at = row * s.width + p.column;
+            const int64_t at = row * (int64_t)s.per_row * 8 + p.column;
             *reinterpret_cast<uint2*>(codes + at) = packed;
             if ((p.column & (kGroup - 1)) == 0)
                 steps[at / kGroup] = (uint8_t)byte;
@@ -406,7 +374,7 @@ checkpoint_save_kernel(const __grid_constant__ Strips s, const T* x, int64_t x_s
 
 // ACT < 0: the values kept themselves; else out = grad * slope(kept value).
 template <typename T, int ACT, bool VEC>
-__global__ void __launch_bounds__(kBlock)
+__global__ void __launch_bounds__(kStripThreads, sizeof(T) == 2 && VEC ? 16 : 8)
 checkpoint_apply_kernel(const __grid_constant__ Strips s, const int8_t* codes, const uint8_t* steps, const T* grad,
                         int64_t grad_stride, T* out, int64_t out_stride)
 {
@@ -421,7 +389,7 @@ checkpoint_apply_kernel(const __grid_constant__ Strips s, const int8_t* codes, c
     for (int u = 0; u < kApplyRows; ++u) {
         const int64_t row = p.row0 + u * p.step;
         if (row < s.rows) {
-            const int64_t at = row * s.width + p.column;
+            const int64_t at = row * (int64_t)s.per_row * 8 + p.column;
             packed[u] = *reinterpret_cast<const uint2*>(codes + at);
             byte[u] = steps[at / kGroup];
             if constexpr (ACT >= 0)
@@ -475,24 +443,6 @@ adasum_status_t check_matrix(const char* name, const void* p, int64_t stride, in
     return ADASUM_OK;
 }
 
-bool plan_strips(int64_t rows, int64_t features, int rows_per_thread, Strips* s, unsigned* blocks)
-{
-    s->rows = rows;
-    s->features = features;
-    s->width = checkpoint_width(features);
-    s->per_row = (int)(s->width / 8);
-    s->lane_bits = 2;
-    while (s->lane_bits < 5 && (1 << s->lane_bits) < s->per_row)
-        ++s->lane_bits;
-    const int64_t strips = (s->per_row + (1 << s->lane_bits) - 1) >> s->lane_bits;
-    const int64_t band = (int64_t)rows_per_thread * (32 >> s->lane_bits);
-    s->strips_per_row = row_divider(strips);
-    s->warps = (uint64_t)((rows + band - 1) / band) * (uint64_t)strips;
-    const uint64_t n = (s->warps + kBlock / 32 - 1) / (kBlock / 32);
-    *blocks = (unsigned)n;
-    return n <= 0x7fffffffu;
-}
-
 // Calls f with a value of the run-time type, the constant of the run-time activation, or of a truth value.
 template <typename F>
 void with_type(adasum_dtype_t dtype, F&& f)
@@ -533,8 +483,8 @@ void launch_apply(const void* checkpoint, const Strips& s, unsigned blocks, cons
     const int8_t* codes = static_cast<const int8_t*>(checkpoint);
     const bool vec = s.features % 8 == 0 && rows_aligned(grad, grad_stride, sizeof(T)) && rows_aligned(out, out_stride, sizeof(T));
     with_flag(vec, [&](auto v) {
-        checkpoint_apply_kernel<T, ACT, decltype(v)::value != 0><<<blocks, kBlock, 0, stream>>>(
-            s, codes, reinterpret_cast<const uint8_t*>(codes + s.rows * s.width), static_cast<const T*>(grad), grad_stride,
+        checkpoint_apply_kernel<T, ACT, decltype(v)::value != 0><<<blocks, kStripThreads, 0, stream>>>(
+            s, codes, reinterpret_cast<const uint8_t*>(codes + s.rows * (int64_t)s.per_row * 8), static_cast<const T*>(grad), grad_stride,
             static_cast<T*>(out), out_stride);
     });
 }
@@ -588,7 +538,7 @@ adasum_status_t adasum_checkpoint_save(const void* x, int64_t x_stride, int64_t 
         return fail(ADASUM_ERR_ARG, "checkpoint overlaps x or y");
     Strips s;
     unsigned blocks;
-    if (!plan_strips(rows, features, kSaveRows, &s, &blocks))
+    if (!plan_strips(rows, features, checkpoint_width(features) / 8, kSaveRows, &s, &blocks))
         return fail(ADASUM_ERR_ARG, "%lld x %lld is too large", (long long)rows, (long long)features);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
     profile_mark(stream, -1, 0, 0, true);
@@ -598,9 +548,9 @@ adasum_status_t adasum_checkpoint_save(const void* x, int64_t x_stride, int64_t 
             const bool vec = features % 8 == 0 && rows_aligned(x, x_stride, sizeof(T)) && rows_aligned(y, y_stride, sizeof(T));
             int8_t* codes = static_cast<int8_t*>(checkpoint);
             with_flag(vec, [&](auto v) {
-                checkpoint_save_kernel<T, decltype(a)::value, decltype(v)::value != 0><<<blocks, kBlock, 0, stream>>>(
+                checkpoint_save_kernel<T, decltype(a)::value, decltype(v)::value != 0><<<blocks, kStripThreads, 0, stream>>>(
                     s, static_cast<const T*>(x), x_stride, static_cast<T*>(y), y_stride, codes,
-                    reinterpret_cast<uint8_t*>(codes + s.rows * s.width));
+                    reinterpret_cast<uint8_t*>(codes + s.rows * (int64_t)s.per_row * 8));
             });
         });
     });
@@ -622,7 +572,7 @@ adasum_status_t adasum_checkpoint_load(const void* checkpoint, int64_t rows, int
         return fail(ADASUM_ERR_ARG, "checkpoint overlaps out");
     Strips s;
     unsigned blocks;
-    if (!plan_strips(rows, features, kApplyRows, &s, &blocks))
+    if (!plan_strips(rows, features, checkpoint_width(features) / 8, kApplyRows, &s, &blocks))
         return fail(ADASUM_ERR_ARG, "%lld x %lld is too large", (long long)rows, (long long)features);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
     profile_mark(stream, -1, 0, 0, true);
@@ -656,7 +606,7 @@ adasum_status_t adasum_checkpoint_act_grad(const void* checkpoint, int64_t rows,
         return fail(ADASUM_ERR_ARG, "checkpoint overlaps grad_in");
     Strips s;
     unsigned blocks;
-    if (!plan_strips(rows, features, kApplyRows, &s, &blocks))
+    if (!plan_strips(rows, features, checkpoint_width(features) / 8, kApplyRows, &s, &blocks))
         return fail(ADASUM_ERR_ARG, "%lld x %lld is too large", (long long)rows, (long long)features);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
     profile_mark(stream, -1, 0, 0, true);

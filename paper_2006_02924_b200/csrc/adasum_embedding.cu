@@ -34,47 +34,47 @@ __device__ __forceinline__ int64_t token_row(const Id* tokens, int64_t t, int64_
     return id >= 0 && id < num_rows ? id : -1;
 }
 
-constexpr int kLookupBlock = 128;
-constexpr int kLookupVectors = 4;
+constexpr int kLookupRows = 4;             // tokens per thread
 
-// One thread: kLookupVectors vectors of eight elements of the output.
-template <typename T, typename Id>
-__global__ void __launch_bounds__(kLookupBlock)
-embedding_forward_kernel(const T* table, int64_t table_stride, bool table_vec, int64_t num_rows, int64_t dim,
-                         const Id* tokens, float scale, void* out, int out_dtype, int64_t out_stride, bool out_vec,
-                         RowDivider divider, uint64_t vectors)
+// VEC: every row of the table and of the output starts on 16 bytes and dim is a multiple of 8.
+template <typename T, typename Id, bool VEC>
+__global__ void __launch_bounds__(kStripThreads)
+embedding_forward_kernel(const __grid_constant__ Strips s, const T* table, int64_t table_stride, int64_t num_rows,
+                         const Id* tokens, float scale, void* out, int out_dtype, int64_t out_stride)
 {
-    const uint64_t first = (uint64_t)blockIdx.x * (kLookupBlock * kLookupVectors) + threadIdx.x;
-    float v[kLookupVectors][8];
-    int64_t token[kLookupVectors], row[kLookupVectors];
-    int count[kLookupVectors];
-    uint32_t at[kLookupVectors];
+    const Place p = place_of<kLookupRows>(s);
+    if (p.count <= 0)
+        return;
+    int64_t row[kLookupRows];
+    float v[kLookupRows][8];
 #pragma unroll
-    for (int u = 0; u < kLookupVectors; ++u) {
-        const uint64_t n = first + u * kLookupBlock;
-        uint64_t t;
-        divide_row(divider, n, t, at[u]);
-        token[u] = (int64_t)t;
-        count[u] = n < vectors ? (int)min((int64_t)8, dim - (int64_t)at[u] * 8) : 0;
-        row[u] = count[u] > 0 ? token_row(tokens, token[u], num_rows) : -1;
+    for (int u = 0; u < kLookupRows; ++u) {
+        const int64_t t = p.row0 + u * p.step;
+        row[u] = t < s.rows ? token_row(tokens, t, num_rows) : -1;
     }
 #pragma unroll
-    for (int u = 0; u < kLookupVectors; ++u)
-        load_up_to_eight(table + row[u] * table_stride + (int64_t)at[u] * 8, table_vec, row[u] >= 0 ? count[u] : 0, v[u]);
+    for (int u = 0; u < kLookupRows; ++u) {
+        if (VEC && row[u] >= 0) {
+            load_eight(table + row[u] * table_stride + p.column, v[u]);
+        } else {
+            load_up_to_eight(table + row[u] * table_stride + p.column, false, row[u] >= 0 ? p.count : 0, v[u]);
+        }
+    }
 #pragma unroll
-    for (int u = 0; u < kLookupVectors; ++u) {
-        if (count[u] <= 0)
-            continue;
+    for (int u = 0; u < kLookupRows; ++u) {
+        const int64_t t = p.row0 + u * p.step;
+        if (t >= s.rows)
+            break;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             v[u][i] = row[u] >= 0 ? v[u][i] * scale : 0.0f;
-        const int64_t e = token[u] * out_stride + (int64_t)at[u] * 8;
-        if (out_vec && count[u] == 8) {
+        const int64_t e = t * out_stride + p.column;
+        if constexpr (VEC) {
             store_vector_from_float<8>(out, out_dtype, e, v[u]);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (i < count[u])
+                if (i < p.count)
                     store_from_float(out, out_dtype, e + i, v[u][i]);
         }
     }
@@ -757,26 +757,27 @@ adasum_status_t adasum_embedding_forward(const void* table, int64_t table_stride
     if (spans_overlap(out, out_bytes, table, table_bytes) ||
         spans_overlap(out, out_bytes, tokens, (size_t)num_tokens * token_bytes))
         return fail(ADASUM_ERR_ARG, "out overlaps table or tokens");
-    const int64_t per_row = (dim + 7) / 8;
-    const uint64_t vectors = (uint64_t)num_tokens * (uint64_t)per_row;
-    const uint64_t blocks = (vectors + kLookupBlock * kLookupVectors - 1) / (kLookupBlock * kLookupVectors);
-    if (blocks > 0x7fffffffu)
+    Strips s;
+    unsigned blocks;
+    if (!plan_strips(num_tokens, dim, (dim + 7) / 8, kLookupRows, &s, &blocks))
         return fail(ADASUM_ERR_ARG, "%lld x %lld is too large", (long long)num_tokens, (long long)dim);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
     profile_mark(stream, -1, 0, 0, true);
     with_type(table_dtype, [&](auto t) {
         using T = decltype(t);
-        const T* rows = static_cast<const T*>(table);
-        const bool table_vec = rows_aligned(table, table_stride, sizeof(T));
-        const bool out_vec = rows_aligned(out, out_stride, operator_bytes(out_dtype));
+        const bool vec = dim % 8 == 0 && rows_aligned(table, table_stride, sizeof(T)) &&
+                         rows_aligned(out, out_stride, operator_bytes(out_dtype));
+        auto launch = [&](auto id) {
+            using Id = decltype(id);
+            auto* kernel = vec ? embedding_forward_kernel<T, Id, true> : embedding_forward_kernel<T, Id, false>;
+            kernel<<<blocks, kStripThreads, 0, stream>>>(s, static_cast<const T*>(table), table_stride, num_rows,
+                                                         static_cast<const Id*>(tokens), scale, out, (int)out_dtype,
+                                                         out_stride);
+        };
         if (token_bytes == 4)
-            embedding_forward_kernel<T, int32_t><<<(unsigned)blocks, kLookupBlock, 0, stream>>>(
-                rows, table_stride, table_vec, num_rows, dim, static_cast<const int32_t*>(tokens), scale, out,
-                (int)out_dtype, out_stride, out_vec, row_divider(per_row), vectors);
+            launch(int32_t{});
         else
-            embedding_forward_kernel<T, int64_t><<<(unsigned)blocks, kLookupBlock, 0, stream>>>(
-                rows, table_stride, table_vec, num_rows, dim, static_cast<const int64_t*>(tokens), scale, out,
-                (int)out_dtype, out_stride, out_vec, row_divider(per_row), vectors);
+            launch(int64_t{});
     });
     ADASUM_CUDA_CHECK(cudaGetLastError());
     profile_mark(stream, ADASUM_KERNEL_EMBEDDING, 0, 0, false);

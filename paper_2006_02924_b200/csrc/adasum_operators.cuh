@@ -68,6 +68,36 @@ inline RowDivider row_divider(int64_t per_row)
     return RowDivider{per_row > 1 ? ~uint64_t(0) / (uint64_t)per_row + 1 : 0, (uint32_t)per_row};
 }
 
+// How the elementwise kernels walk a matrix.  A thread handles vectors of eight consecutive elements; a warp takes a
+// strip of up to 32 vectors of a row (of several rows, if rows are short) on a few rows below each other: all loads
+// of a thread go out before the first is used, and its addresses are one sum apart.
+constexpr int kStripThreads = 128;
+// A matrix cut into strips: 2^lane_bits vectors of a row x 2^(5 - lane_bits) rows per lane row.
+struct Strips {
+    int64_t rows, features;
+    int per_row;                         // vectors of a row
+    int lane_bits;
+    RowDivider strips_per_row;
+    uint64_t warps;
+};
+
+inline bool plan_strips(int64_t rows, int64_t features, int64_t per_row, int rows_per_thread, Strips* s, unsigned* blocks)
+{
+    s->rows = rows;
+    s->features = features;
+    s->per_row = (int)per_row;
+    s->lane_bits = 2;
+    while (s->lane_bits < 5 && (1 << s->lane_bits) < s->per_row)
+        ++s->lane_bits;
+    const int64_t strips = (s->per_row + (1 << s->lane_bits) - 1) >> s->lane_bits;
+    const int64_t band = (int64_t)rows_per_thread * (32 >> s->lane_bits);
+    s->strips_per_row = row_divider(strips);
+    s->warps = (uint64_t)((rows + band - 1) / band) * (uint64_t)strips;
+    const uint64_t n = (s->warps + kStripThreads / 32 - 1) / (kStripThreads / 32);
+    *blocks = (unsigned)n;
+    return n <= 0x7fffffffu;
+}
+
 // Launches a kernel that begins with wait_for_previous_kernel(): it may be brought in while the stream's previous
 // kernel still runs (one that called start_next_kernel()), which hides the launch.
 template <typename... Params, typename... Args>
@@ -138,6 +168,32 @@ __device__ __forceinline__ void load_up_to_eight(const T* p, bool vec, int count
         for (int i = 0; i < 8; ++i)
             x[i] = i < count ? load_one(p + i) : 0.0f;
     }
+}
+
+// A thread's vectors: ROWS rows, one column.
+struct Place {
+    int64_t row0;            // first of the thread's rows; the next ones are `step` further
+    int step;
+    int column;              // first element
+    int count;               // elements of the vector inside the matrix (<= 0: only padding)
+    bool inside;             // the vector exists (padding included)
+};
+template <int ROWS>
+__device__ __forceinline__ Place place_of(const Strips& s)
+{
+    const uint64_t warp = (uint64_t)blockIdx.x * (kStripThreads / 32) + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    uint64_t band;
+    uint32_t strip;
+    divide_row(s.strips_per_row, warp, band, strip);
+    Place p;
+    p.step = 32 >> s.lane_bits;
+    p.row0 = (int64_t)band * (ROWS * p.step) + (lane >> s.lane_bits);
+    const int vector = ((int)strip << s.lane_bits) + (lane & ((1 << s.lane_bits) - 1));
+    p.inside = warp < s.warps && vector < s.per_row;
+    p.column = vector * 8;
+    p.count = p.inside ? (int)min((int64_t)8, s.features - p.column) : 0;
+    return p;
 }
 
 }  // namespace adasum
