@@ -80,19 +80,44 @@ __device__ __forceinline__ float reciprocal_approx(float x)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ Pair negative(Pair a) { return Pair{a.v ^ 0x8000000080000000ull}; }
 __device__ __forceinline__ Pair magnitude(Pair a) { return Pair{a.v & 0x7fffffff7fffffffull}; }
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2eLow = (float)(1.4426950408889634 - (double)kLog2e);
+constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kInvSqrt2Pi = 0.3989422804014327f;
 constexpr float kTanhScale = 0.7978845608028654f;     // sqrt(2 / pi)
 constexpr float kTanhCubic = 0.044715f;
 
-// The normal distribution function for 16-bit results: Phi(-a) = e * r(a) for a >= 0, with e = exp(-a^2 / 2) and
-// r(a) = erfcx(a / sqrt 2) / 2.  r is a polynomial of degree 6 without constant term in t = 1 / (1 + 0.31 a): a fit to r
-// on 0 <= a <= 14 that levels out the relative error (5e-6, against 5e-4 / 2 for one rounding to fp16; beyond 14
-// both factors of the result vanish in 16 bits).  Returns r.  fp32 results call erfcf and expf.
-__device__ __forceinline__ Pair normal_tail_16(Pair a, Pair& e)
+// The normal distribution function's tail: Phi(-a) = e * r(a) for a >= 0, with e = exp(-a^2 / 2) and
+// r(a) = erfcx(a / sqrt 2) / 2.  r is a polynomial without constant term in t = 1 / (1 + p a), fitted to r on
+// 0 <= a <= 14 so that the relative error is level: for 16-bit results p = 0.31 and degree 6 (5e-6, against 5e-4 / 2 for one
+// rounding to fp16), for fp32 p = 0.34 and degree 9 (3e-8; 3e-7 as evaluated, what erfcf has, at half its cost).
+// Beyond 14 the tail vanishes in either type.  Returns r.
+template <bool WIDE>
+__device__ __forceinline__ Pair normal_tail(Pair a, Pair& e)
 {
+    if constexpr (WIDE) {
+        // a^2 / 2 log2(e) with its rounding errors (twice 2^-24 of up to 100), which the exponential would multiply
+        const Pair scale = both(-0.5f * kLog2e), square = a * a;
+        const Pair y = square * scale;
+        const Pair square_low = fma2(a, a, negative(square));
+        const Pair low = fma2(square_low, scale, fma2(square, both(-0.5f * kLog2eLow), fma2(square, scale, negative(y))));
+        e = each(y, exp2_approx);
+        e = fma2(e, low * both(kLn2), e);
+        const Pair t = each(fma2(both(0.34f), a, both(1.0f)), reciprocal_approx);
+        Pair r = both(-0.026122383f);
+        r = fma2(r, t, both(0.139508666f));
+        r = fma2(r, t, both(-0.273151377f));
+        r = fma2(r, t, both(0.202203477f));
+        r = fma2(r, t, both(-0.0447323639f));
+        r = fma2(r, t, both(0.115364844f));
+        r = fma2(r, t, both(0.115196281f));
+        r = fma2(r, t, both(0.136112377f));
+        r = fma2(r, t, both(0.135620494f));
+        return r * t;
+    }
     e = each(a * a * both(-0.5f * kLog2e), exp2_approx);
     const Pair t = each(fma2(both(0.31f), a, both(1.0f)), reciprocal_approx);
     Pair r = both(-0.0739287332f);
@@ -102,6 +127,18 @@ __device__ __forceinline__ Pair normal_tail_16(Pair a, Pair& e)
     r = fma2(r, t, both(0.120441553f));
     r = fma2(r, t, both(0.123860669f));
     return r * t;
+}
+// |x|, for fp32 results up to 40 only (the square of a large one would not be a number); NaN stays.
+template <bool WIDE>
+__device__ __forceinline__ Pair tail_argument(Pair x)
+{
+    if constexpr (!WIDE)
+        return magnitude(x);
+    return each(magnitude(x), [](float a) {
+        float m;
+        asm("min.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(40.0f));
+        return m;
+    });
 }
 // x < 0: tail; else 1 - tail, as side * tail + (1 - side) / 2 with side = -sign(x).
 __device__ __forceinline__ Pair tail_or_rest(Pair x, Pair tail)
@@ -135,15 +172,15 @@ template <int ACT, bool WIDE>
 __device__ __forceinline__ Pair activation(Pair x)
 {
     if constexpr (ACT == ADASUM_ACT_RELU)
-        return each(x, [](float a) { return a > 0.0f ? a : 0.0f * a; });
+        return each(x, [](float a) {
+            float m;                                // NaN stays
+            asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(0.0f));
+            return m;
+        });
     if constexpr (ACT == ADASUM_ACT_GELU) {
-        if constexpr (WIDE) {
-            return each(x, [](float a) { return a * (0.5f * erfcf(-0.70710678f * a)); });
-        } else {
-            Pair e;
-            const Pair r = normal_tail_16(magnitude(x), e);
-            return x * tail_or_rest(x, r * e);
-        }
+        Pair e;
+        const Pair r = normal_tail<WIDE>(tail_argument<WIDE>(x), e);
+        return x * tail_or_rest(x, r * e);
     }
     Pair rest;
     if constexpr (ACT == ADASUM_ACT_GELU_TANH)      // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u))
@@ -159,15 +196,9 @@ __device__ __forceinline__ Pair activation_slope(Pair x)
     if constexpr (ACT == ADASUM_ACT_RELU)
         return each(x, [](float a) { return a > 0.0f ? 1.0f : 0.0f; });
     if constexpr (ACT == ADASUM_ACT_GELU) {         // Phi + x phi; at -a: e (r - a / sqrt(2 pi)), at a: 1 minus that
-        if constexpr (WIDE) {
-            return each(x, [](float a) {
-                return fmaf(a * kInvSqrt2Pi, expf(-0.5f * a * a), 0.5f * erfcf(-0.70710678f * a));
-            });
-        } else {
-            Pair e;
-            const Pair a = magnitude(x), r = normal_tail_16(a, e);
-            return tail_or_rest(x, fma2(a, both(-kInvSqrt2Pi), r) * e);
-        }
+        Pair e;
+        const Pair a = tail_argument<WIDE>(x), r = normal_tail<WIDE>(a, e);
+        return tail_or_rest(x, fma2(a, both(-kInvSqrt2Pi), r) * e);
     }
     Pair rest;
     if constexpr (ACT == ADASUM_ACT_GELU_TANH) {    // s + x s (1 - s) 2 u'

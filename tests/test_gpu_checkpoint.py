@@ -171,3 +171,22 @@ def test_large_matrix(b):
     assert torch.all(out[-1] == 3.0) and torch.all(out[:5] == 0)
     b.adasum_checkpoint_load(kept, rows, cols, out=out)
     assert torch.all(out[-1] == 3.0) and out[-2, 100] == -1.0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("name", ACTS)
+def test_activation_of_inf_and_nan(b, dtype, name):
+    x = torch.ones(3, 40, dtype=TORCH[dtype], device="cuda")
+    x[0, 1], x[1, 38], x[2, 0] = float("inf"), float("nan"), -float("inf")
+    y, kept = b.adasum_checkpoint_save(x, name)
+    assert y[0, 1] == float("inf") and torch.isnan(y[1, 38])
+    if name in ("none", "relu"):
+        assert y[2, 0] == (0 if name == "relu" else -float("inf"))
+    assert torch.isfinite(y).sum() >= 120 - 3
+    values = b.adasum_checkpoint_load(kept, 3, 40)
+    bad = torch.zeros(3, 40, dtype=torch.bool, device="cuda")
+    bad[0, :32], bad[1, 32:], bad[2, :32] = True, True, True
+    assert torch.equal(torch.isnan(values), bad)
+    slope = b.adasum_checkpoint_act_grad(kept, torch.ones_like(x), name)
+    if name not in ("none", "relu"):                 # their slope is 1 or 0 whatever the value
+        assert torch.equal(torch.isnan(slope), bad)
