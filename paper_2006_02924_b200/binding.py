@@ -485,20 +485,31 @@ def _operator_call(device: int, stream, function, *args):
 
 
 def _allocate(like, stream, shape, dtype):
-    """A tensor for a call on `stream`: the caching allocator must not hand it on before that stream is done."""
-    t = like.new_empty(shape, dtype=dtype)
-    if stream is not None and t.numel() > 0:
+    """A tensor for a call on `stream`."""
+    t = like.new_empty(*shape) if dtype is like.dtype else like.new_empty(shape, dtype=dtype)
+    return t if stream is None else _hand_over(t, stream)
+
+
+def _allocate_like(like, stream):
+    """A matrix of the same shape and type with contiguous rows."""
+    t = torch.empty_like(like)
+    return t if stream is None else _hand_over(t, stream)
+
+
+def _hand_over(t, stream):
+    """The caching allocator must not hand a tensor on before the stream that it is used on is done with it."""
+    if t.numel() > 0:
         if not hasattr(stream, "cuda_stream"):
-            stream = torch.cuda.ExternalStream(int(stream), device=like.device)
+            stream = torch.cuda.ExternalStream(int(stream), device=t.device)
         # the memory may still be in use on the current stream, from which it was handed out
-        stream.wait_stream(torch.cuda.current_stream(like.device))
+        stream.wait_stream(torch.cuda.current_stream(t.device))
         t.record_stream(stream)
     return t
 
 
 def _operator_workspace(like, stream, workspace, need: int):
     if workspace is None:
-        return _allocate(like, stream, max(need, 256), torch.uint8)
+        return _allocate(like, stream, (max(need, 256),), torch.uint8)
     if not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
     return workspace
@@ -592,7 +603,7 @@ def adasum_checkpoint_save(x, activation: str = "none", out=None, checkpoint=Non
     rows, features = x.shape
     device = x.get_device()
     if checkpoint is None:
-        checkpoint = _allocate(x, stream, _checkpoint_size(rows, features), torch.uint8)
+        checkpoint = _allocate(x, stream, (_checkpoint_size(rows, features),), torch.uint8)
     out_stride, out_ptr = features, None
     if out is not None:
         out_stride = _matrix("out", out, rows, features)
@@ -601,7 +612,7 @@ def adasum_checkpoint_save(x, activation: str = "none", out=None, checkpoint=Non
         _same_device(device, out)
         out_ptr = out.data_ptr()
     elif want_out:
-        out = _allocate(x, stream, (rows, features), x.dtype)
+        out = _allocate_like(x, stream)
         out_ptr = out.data_ptr()
     _operator_call(device, stream, _lib.adasum_checkpoint_save, x.data_ptr(), stride, rows, features,
                    _operator_dtype(x.dtype), ADASUM_ACT[activation], out_ptr, out_stride,
@@ -630,7 +641,7 @@ def adasum_checkpoint_act_grad(checkpoint, grad_out, activation: str, grad_in=No
     rows, features = grad_out.shape
     device = grad_out.get_device()
     if grad_in is None:
-        grad_in, in_stride = _allocate(grad_out, stream, (rows, features), grad_out.dtype), features
+        grad_in, in_stride = _allocate_like(grad_out, stream), features
     else:
         in_stride = _matrix("grad_in", grad_in, rows, features)
         if grad_in.dtype != grad_out.dtype:
