@@ -358,6 +358,8 @@ __device__ __forceinline__ void unpack_codes(uint32_t packed, Pair step, Pair& x
 
 // ---- kernels -----------------------------------------------------------------------------------------
 
+// 16384 x 4096 bf16: GELU 70 us (4.8 TB/s, 77 % of the issue slots: bound by both), ReLU 55 us (6.1 TB/s); fp32 GELU
+// 96 us (6.3 TB/s).
 template <typename T, int ACT, bool VEC>
 __global__ void __launch_bounds__(kStripThreads)
 checkpoint_save_kernel(const __grid_constant__ Strips s, const T* x, int64_t x_stride, T* y, int64_t y_stride,
@@ -403,7 +405,9 @@ checkpoint_save_kernel(const __grid_constant__ Strips s, const T* x, int64_t x_s
     }
 }
 
-// ACT < 0: the values kept themselves; else out = grad * slope(kept value).
+// ACT < 0: the values kept themselves; else out = grad * slope(kept value).  16384 x 4096 bf16: load 41 us (5 TB/s,
+// two thirds of it writes), GELU 73 us (4.6 TB/s, instruction issue), ReLU 55 us (6.1 TB/s); fp32 GELU 111 us
+// (5.5 TB/s).
 template <typename T, int ACT, bool VEC>
 __global__ void __launch_bounds__(kStripThreads, sizeof(T) == 2 && VEC ? 16 : 8)
 checkpoint_apply_kernel(const __grid_constant__ Strips s, const int8_t* codes, const uint8_t* steps, const T* grad,
