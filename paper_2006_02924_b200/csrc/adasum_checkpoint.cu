@@ -201,10 +201,11 @@ __device__ __forceinline__ Pair activation_slope(Pair x)
         return tail_or_rest(x, fma2(a, both(-kInvSqrt2Pi), r) * e);
     }
     Pair rest;
-    if constexpr (ACT == ADASUM_ACT_GELU_TANH) {    // s + x s (1 - s) 2 u'
+    if constexpr (ACT == ADASUM_ACT_GELU_TANH) {    // s + x s (1 - s) 2 u', with u' = k (1 + 3 c x^2)
         const Pair s = logistic<WIDE>(both(2.0f * kTanhScale) * x * fma2(both(kTanhCubic) * x, x, both(1.0f)), rest);
-        const Pair du = both(2.0f * kTanhScale) * x * fma2(both(3.0f * kTanhCubic) * x, x, both(1.0f));
-        return fma2(s * rest, du, s);
+        // s (1 - s) comes first: it vanishes long before a power of x could overflow, and a zero stays one
+        const Pair t = s * rest * x;
+        return fma2(both(2.0f * kTanhScale), fma2(t * x * x, both(3.0f * kTanhCubic), t), s);
     }
     if constexpr (ACT == ADASUM_ACT_SILU) {
         const Pair s = logistic<WIDE>(x, rest);

@@ -1,0 +1,48 @@
+"""Activations and their gradients where a kept value is far outside the range that the functions change in, and
+where a group is kept as NaN."""
+import pytest
+import torch
+
+from operator_reference import TORCH
+
+pytestmark = pytest.mark.gpu
+
+ACTS = ["none", "relu", "gelu", "gelu_tanh", "silu"]
+LARGE = {"f32": [1e4, 1e9, 1e13, 1.2e13, 2e13, 1e15, 6e18, 1e20, 1e30, 3.4028234e38],
+         "f16": [1e4, 3e4, 65504.0],
+         "bf16": [1e4, 1e9, 1e13, 1.2e13, 2e13, 1e15, 6e18, 1e20, 1e30, 3.38e38]}
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_2006_02924_b200 import binding
+
+    return binding
+
+
+def _large(dtype, pad):
+    """One large value per group of 32, and where they are; `pad` more columns cut off again (unaligned rows)."""
+    values = torch.tensor(LARGE[dtype] + [-v for v in LARGE[dtype]], device="cuda")
+    at = 32 * torch.arange(values.numel(), device="cuda") + 5
+    x = torch.zeros(3, 32 * values.numel() + pad, dtype=TORCH[dtype], device="cuda")
+    x[1, at] = values.to(TORCH[dtype])
+    x[1, at + 9] = 1.0                       # far below the step: its code is 0
+    return x[:, :32 * values.numel()], at
+
+
+@pytest.mark.parametrize("pad", [0, 3])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("name", ACTS)
+def test_large_values(b, name, dtype, pad):
+    """From |x| = 1e4 on the slope is 1 or 0, and y is x or 0, to fp32 precision (the tails are below exp(-1e4)):
+    exact equality, at every magnitude that the type holds."""
+    x, at = _large(dtype, pad)
+    y, kept = b.adasum_checkpoint_save(x, name)
+    positive = (x[1, at] > 0) | (name == "none")
+    assert torch.equal(y[1, at], torch.where(positive, x[1, at], 0))
+    values = b.adasum_checkpoint_load(kept, *x.shape)
+    assert torch.isfinite(values).all() and torch.equal(values[1, at] > 0, x[1, at] > 0)
+    dy = torch.full_like(x, 3.0)
+    got = b.adasum_checkpoint_act_grad(kept, dy, name)
+    assert torch.isfinite(got).all()
+    assert torch.equal(got[1, at], torch.where(positive, dy[1, at], 0))
