@@ -190,6 +190,7 @@ __device__ __forceinline__ Pair activation(Pair x)
     return x;
 }
 
+// x: a kept value whose step is at most slope_step().
 template <int ACT, bool WIDE>
 __device__ __forceinline__ Pair activation_slope(Pair x)
 {
@@ -201,11 +202,10 @@ __device__ __forceinline__ Pair activation_slope(Pair x)
         return tail_or_rest(x, fma2(a, both(-kInvSqrt2Pi), r) * e);
     }
     Pair rest;
-    if constexpr (ACT == ADASUM_ACT_GELU_TANH) {    // s + x s (1 - s) 2 u', with u' = k (1 + 3 c x^2)
-        const Pair s = logistic<WIDE>(both(2.0f * kTanhScale) * x * fma2(both(kTanhCubic) * x, x, both(1.0f)), rest);
-        // s (1 - s) comes first: it vanishes long before a power of x could overflow, and a zero stays one
-        const Pair t = s * rest * x;
-        return fma2(both(2.0f * kTanhScale), fma2(t * x * x, both(3.0f * kTanhCubic), t), s);
+    if constexpr (ACT == ADASUM_ACT_GELU_TANH) {    // s + s (1 - s) x z', with z = v (1 + c x^2) and x z' = 3 z - 2 v
+        const Pair v = both(2.0f * kTanhScale) * x, z = v * fma2(both(kTanhCubic) * x, x, both(1.0f));
+        const Pair s = logistic<WIDE>(z, rest);
+        return fma2(s * rest, fma2(both(3.0f), z, both(-2.0f) * v), s);
     }
     if constexpr (ACT == ADASUM_ACT_SILU) {
         const Pair s = logistic<WIDE>(x, rest);
@@ -330,6 +330,14 @@ __device__ __forceinline__ uint32_t step_byte(uint32_t top_bits)
 }
 // 2^(byte - 127); Inf for 255, whose codes are 0, so that code * step is NaN.
 __device__ __forceinline__ float step_value(uint32_t byte) { return __uint_as_float(byte << 23); }
+// The step that a group's slopes are computed with.  tanh-GELU has powers of x that would overflow beside factors that
+// have become zero, and make NaN of the slope: a step of more than 2^30 is taken for 2^30, which leaves a code of 0
+// at 0 and all others at magnitudes (2^30 .. 2^37) where the slope is 1 or 0.
+template <int ACT>
+__device__ __forceinline__ float slope_step(uint32_t byte)
+{
+    return step_value(ACT == ADASUM_ACT_GELU_TANH && byte != 255u ? min(byte, 127u + 30u) : byte);
+}
 
 // Four codes of two pairs packed; inv = 1 / step.  Adding 1.5 * 2^23 rounds to an integer, ties to even,
 // and leaves it in the low bits.  LIMIT: a magnitude may round to 128.
@@ -436,7 +444,7 @@ checkpoint_apply_kernel(const __grid_constant__ Strips s, const int8_t* codes, c
     for (int u = 0; u < kApplyRows; ++u) {
         const int64_t row = p.row0 + u * p.step;
         if (row < s.rows) {
-            const Pair step = both(step_value(byte[u]));
+            const Pair step = both(slope_step<ACT>(byte[u]));
             Eight x;
             unpack_codes(packed[u].x, step, x.p[0], x.p[1]);
             unpack_codes(packed[u].y, step, x.p[2], x.p[3]);
