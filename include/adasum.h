@@ -445,7 +445,7 @@ size_t adasum_checkpoint_bytes(int64_t rows, int64_t features);
 
 typedef enum {
     ADASUM_ACT_NONE = 0,        /* y = x */
-    ADASUM_ACT_RELU = 1,        /* slope 0 at x <= 0 */
+    ADASUM_ACT_RELU = 1,        /* slope 0 at x <= 0, NaN where NaN is kept */
     ADASUM_ACT_GELU = 2,        /* x Phi(x), Phi the normal distribution function */
     ADASUM_ACT_GELU_TANH = 3,   /* x / 2 (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) */
     ADASUM_ACT_SILU = 4         /* x / (1 + exp(-x)) */

@@ -195,7 +195,7 @@ template <int ACT, bool WIDE>
 __device__ __forceinline__ Pair activation_slope(Pair x)
 {
     if constexpr (ACT == ADASUM_ACT_RELU)
-        return each(x, [](float a) { return a > 0.0f ? 1.0f : 0.0f; });
+        return each(x, [](float a) { return a > 0.0f ? 1.0f : 0.0f * fabsf(a); });      // NaN stays
     if constexpr (ACT == ADASUM_ACT_GELU) {         // Phi + x phi; at -a: e (r - a / sqrt(2 pi)), at a: 1 minus that
         Pair e;
         const Pair a = tail_argument<WIDE>(x), r = normal_tail<WIDE>(a, e);

@@ -46,3 +46,24 @@ def test_large_values(b, name, dtype, pad):
     got = b.adasum_checkpoint_act_grad(kept, dy, name)
     assert torch.isfinite(got).all()
     assert torch.equal(got[1, at], torch.where(positive, dy[1, at], 0))
+
+
+@pytest.mark.parametrize("pad", [0, 3])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("name", ["relu", "gelu", "gelu_tanh", "silu"])
+def test_a_group_kept_as_nan_has_no_gradient(b, name, dtype, pad):
+    """The values of such a group are not known, so neither is the slope: NaN, whichever activation, so that an
+    overflow on the way forward shows in the gradients.  Its neighbours are not touched."""
+    x = torch.ones(4, 96 + pad, dtype=TORCH[dtype], device="cuda")
+    x[0, 40], x[1, 3], x[2, 95] = float("inf"), float("nan"), -float("inf")
+    x[3] = -1.0
+    x = x[:, :96]
+    bad = torch.zeros(4, 96, dtype=torch.bool, device="cuda")
+    bad[0, 32:64], bad[1, :32], bad[2, 64:] = True, True, True
+    _, kept = b.adasum_checkpoint_save(x, want_out=False)
+    dy = torch.full_like(x, 2.0)
+    dy[:, 7] = 0.0
+    got = b.adasum_checkpoint_act_grad(kept, dy, name)
+    assert torch.equal(torch.isnan(got), bad)
+    if name == "relu":
+        assert torch.equal(got[~bad], torch.where(x > 0, dy, 0)[~bad])
