@@ -415,8 +415,8 @@ adasum_status_t adasum_embedding_forward(const void* table, int64_t table_stride
  *   grad_out      device, num_tokens x dim of `dtype`, rows grad_out_stride apart
  *   grad_table    device, num_rows x dim of grad_dtype, contiguous
  *   workspace     device, adasum_embedding_grad_workspace_bytes(...) bytes, 256-byte aligned; contents
- *                 on entry are ignored
- *   limits        num_tokens, num_rows < 2^31, dim <= 2^22 (ADASUM_ERR_ARG)
+ *                 on entry are ignored.  One that is large enough for a list does for every shorter one
+ *   limits        num_tokens, num_rows <= 2^31 - 256, dim <= 2^22 (ADASUM_ERR_ARG)
  */
 size_t adasum_embedding_grad_workspace_bytes(int64_t num_tokens, int64_t num_rows, int64_t dim);
 adasum_status_t adasum_embedding_grad(const void* grad_out, int64_t grad_out_stride, adasum_dtype_t dtype,
@@ -485,7 +485,7 @@ adasum_status_t adasum_checkpoint_act_grad(const void* checkpoint, int64_t rows,
  *   grad_bias     device, `outputs` elements of grad_dtype, or NULL
  *   workspace     device, adasum_checkpoint_weight_grad_workspace_bytes(...) bytes, 256-byte aligned;
  *                 contents on entry are ignored
- *   limits        rows, features, outputs < 2^31 - 256 (ADASUM_ERR_ARG)
+ *   limits        rows, features, outputs <= 2^31 - 256 (ADASUM_ERR_ARG)
  *
  * Products are exact (fp16 and bf16 gradients multiply the kept values in their own type; fp32
  * gradients go in as three bf16 terms that add up to them exactly, except bits below 2^-133); sums are

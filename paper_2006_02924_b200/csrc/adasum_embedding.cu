@@ -658,7 +658,16 @@ __global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(const __gr
 // Entries per tile.
 // Measured with 8, 16, 32: 999 tokens (dim 203, fp32) 26, 28, 38 us, 16384 tokens on two rows 44, 36, 38 us, 200000 tokens
 // (dim 256) 237, 222, 234 us.
-int sum_tile(int64_t n) { return n > 2 * kMaxTile && n < 2048 ? kMaxTile / 2 : kMaxTile; }
+constexpr int64_t kShortTilesBelow = 2048;
+int sum_tile(int64_t n) { return n > 2 * kMaxTile && n < kShortTilesBelow ? kMaxTile / 2 : kMaxTile; }
+int64_t sum_tiles(int64_t n) { return (n + sum_tile(n) - 1) / sum_tile(n); }
+// Tiles that the workspace has room for: the most that any list of up to n entries has, so that a workspace for a
+// long list does for every shorter one.
+int64_t most_sum_tiles(int64_t n)
+{
+    const int64_t own = sum_tiles(n), shorter = n < kShortTilesBelow ? 0 : sum_tiles(kShortTilesBelow - 1);
+    return own > shorter ? own : shorter;
+}
 
 // Clusters of embedding_sort_kernel that are resident at once (a cluster keeps to one group of
 // multiprocessors, so some of these stay without): with one more, its share of the zeros would be written
@@ -697,7 +706,7 @@ GradLayout grad_layout(int64_t n, int64_t dim)
 {
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     const size_t list = up((size_t)n * sizeof(uint2));
-    const int64_t tiles = (n + sum_tile(n) - 1) / sum_tile(n);
+    const int64_t tiles = most_sum_tiles(n);
     GradLayout l;
     l.sorted = 0;
     l.spare = list;
@@ -888,7 +897,7 @@ adasum_status_t adasum_embedding_grad(const void* grad_out, int64_t grad_out_str
     a.accumulate = accumulate != 0;
     a.long_runs = long_runs;
     a.edges = reinterpret_cast<float*>(ws + lay.edges);
-    a.tiles = (uint32_t)((num_tokens + a.tile - 1) / a.tile);
+    a.tiles = (uint32_t)sum_tiles(num_tokens);
     // about 64 KB of zeros per block
     const int64_t row_bytes = dim * operator_bytes(grad_dtype), fit = 65536 / row_bytes;
     a.zero_rows = (uint32_t)(fit < 1 ? 1 : fit < kZeroRows ? fit : kZeroRows);

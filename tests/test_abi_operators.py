@@ -175,3 +175,18 @@ def test_units_of_the_weight_gradient_are_covered_once():
             for u in range(begin, end):
                 assert ((u + 1) * pairs - 1) // units == p          # the join's inverse of the split
         assert sorted(seen) == list(range(units))
+
+
+def test_a_workspace_for_a_long_list_does_for_a_shorter_one():
+    """The last batch of an epoch uses the workspace of the others: sizes never fall as a count rises."""
+    from paper_2006_02924_b200 import binding as b
+
+    for dim in (1, 203, 1024):
+        sizes = [b.adasum_embedding_grad_workspace_bytes(n, 5, dim) for n in range(5000)]
+        assert all(x <= y for x, y in zip(sizes, sizes[1:])), dim
+        more = [b.adasum_embedding_grad_workspace_bytes(n, 5, dim) for n in (4999, 6144, 6145, 8192, 100000, 1 << 30)]
+        assert sizes[-1] <= more[0] and all(x <= y for x, y in zip(more, more[1:]))
+    for dtype in ("f32", "f16", "bf16"):
+        for features, outputs in ((1, 1), (1000, 257), (4096, 1024)):
+            sizes = [b.adasum_checkpoint_weight_grad_workspace_bytes(n, features, outputs, dtype) for n in range(0, 6000, 7)]
+            assert all(x <= y for x, y in zip(sizes, sizes[1:]))
