@@ -510,6 +510,28 @@ adasum_status_t adasum_checkpoint_weight_grad_status(int64_t rows, int64_t featu
                                                      adasum_dtype_t dtype, const void* workspace,
                                                      void* stream);
 
+/*
+ * A self-test of the product's bounded waits, not a way to compute gradients: the weight gradient with one kind of
+ * hand-over inside the product that never completes, and with waits of a millisecond instead of a second.  The
+ * waits run out, the kernel records it, lets its copies and multiplications finish, frees its tensor memory and
+ * returns; adasum_checkpoint_weight_grad_status then reports ADASUM_ERR_TIMEOUT, unless the sizes need no hand-over of
+ * that kind.  The next weight gradient on the workspace is not affected.
+ */
+#define ADASUM_HAND_OVER_NONE 0
+#define ADASUM_HAND_OVER_LANDED 1     /* a step's gradients, codes and step bytes in shared memory */
+#define ADASUM_HAND_OVER_MULTIPLIED 2 /* the multiplications of a step */
+#define ADASUM_HAND_OVER_ADDED 3      /* the bias's share of a step (with grad_bias only) */
+#define ADASUM_HAND_OVER_READY 4      /* a step's decoded values */
+#define ADASUM_HAND_OVER_FORMED 5     /* a sum in tensor memory */
+#define ADASUM_HAND_OVER_TAKEN 6      /* its reading */
+adasum_status_t adasum_checkpoint_weight_grad_selftest(const void* checkpoint, int64_t rows, int64_t features,
+                                                       const void* grad_out, int64_t grad_out_stride,
+                                                       int64_t outputs, adasum_dtype_t dtype, float scale,
+                                                       void* grad_weight, void* grad_bias,
+                                                       adasum_dtype_t grad_dtype, int32_t accumulate,
+                                                       void* workspace, size_t workspace_bytes, void* stream,
+                                                       int32_t hand_over);
+
 /* Static, human-readable name of a status code. */
 const char* adasum_status_string(adasum_status_t status);
 

@@ -707,3 +707,23 @@ def adasum_checkpoint_weight_grad_status(rows: int, features: int, outputs: int,
     the last weight gradient on ``workspace`` ran out.  Synchronises the stream."""
     return int(_lib.adasum_checkpoint_weight_grad_status(int(rows), int(features), int(outputs), _dtype_code(dtype),
                                                          workspace.data_ptr(), _stream_handle(stream)))
+
+
+ADASUM_HAND_OVER = {"landed": 1, "multiplied": 2, "added": 3, "ready": 4, "formed": 5, "taken": 6}
+
+_lib.adasum_checkpoint_weight_grad_selftest.restype = ctypes.c_int
+_lib.adasum_checkpoint_weight_grad_selftest.argtypes = _lib.adasum_checkpoint_weight_grad.argtypes + [_i32]
+
+
+def adasum_checkpoint_weight_grad_selftest(hand_over: str, checkpoint, grad_out, grad_weight, grad_bias, workspace):
+    """``adasum_checkpoint_weight_grad_selftest`` of the C ABI, on the current stream: the named kind of hand-over
+    inside the product never completes, so its bounded waits run out and are reported."""
+    rows, outputs = grad_out.shape
+    features = grad_weight.shape[1]
+    status = _lib.adasum_checkpoint_weight_grad_selftest(
+        _checkpoint(grad_out.get_device(), checkpoint, rows, features), rows, features, grad_out.data_ptr(),
+        _matrix("grad_out", grad_out), outputs, _operator_dtype(grad_out.dtype), 1.0, grad_weight.data_ptr(),
+        None if grad_bias is None else grad_bias.data_ptr(), _operator_dtype(grad_weight.dtype), 0, workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream_handle(None), ADASUM_HAND_OVER[hand_over])
+    if status != ADASUM_OK:
+        raise AdasumError(status)

@@ -32,8 +32,11 @@
 // weight_grad_join_kernel.  The association of every sum is fixed by the sizes and
 // the number of pairs that fit the device: results are deterministic.
 //
-// Every wait has a limit; a thread whose wait runs out records it, stops waiting and carries on (wrong
-// numbers, accesses in bounds), and adasum_checkpoint_weight_grad_status reports it.
+// Every wait has a limit.  A thread whose wait runs out records it and goes on without waiting, but hands over and
+// issues nothing more, so the waits that depend on it run out in turn and the launch ends, a few limits later;
+// adasum_checkpoint_weight_grad_status reports it.  Before a block ends its copies have landed, and the pair's
+// multiplications and their arrivals are done: a last commit says so, whatever happened before.  (Those two waits have
+// limits as well; copies and multiplications need microseconds, so one that ran out means that the device itself is stuck.)
 #include <cuda.h>
 
 #include "adasum_operators.cuh"
@@ -61,7 +64,9 @@ constexpr int kBlockThreads = 32 * (kCopyWarp + 4);
 constexpr size_t kSharedBytes = (size_t)kStages * kStageBytes + (size_t)kDecoded * kOperandBytes + 1024;   // + room to align to 1024
 constexpr int kMaxPairs = 74;                    // 148 multiprocessors
 constexpr int64_t kSlotFloats = (int64_t)kTileSide * kTileSide;
-constexpr long long kWaitCycles = 100000000;     // about a twentieth of a second; a real wait is microseconds
+constexpr long long kWaitCycles = 2000000000;    // about a second (a real wait is microseconds): the clock counts pauses too
+constexpr long long kSelftestCycles = 2000000;   // about a millisecond
+constexpr int kLastWait = 4;                     // limits, for the last commit: other warps' waits may have to run out first
 
 struct WeightGradArgs {
     const int8_t* codes;
@@ -76,6 +81,8 @@ struct WeightGradArgs {
     // units of chain_steps steps, tile after tile (tiles of a column of outputs next to each other)
     uint32_t tiles_k, tiles, iterations, chain_steps, chains, units;
     int* status;             // one word per block
+    long long wait_cycles;   // limit of a wait
+    int withheld;            // hand-over that never completes (self-test), or ADASUM_HAND_OVER_NONE
     float* slots;            // [pair][first or last tile of its run][block][output][feature of the block]
     float* bias_slots;       // [pair + tile][256 outputs]: the pairs' shares of the tiles' parts of the bias gradient
 };
@@ -131,18 +138,18 @@ __device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count)
 {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
 }
-// Returns false if the barrier does not complete the phase within kWaitCycles.
-__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity)
+// Returns false if the barrier does not complete the phase within `cycles`.
+__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, long long cycles)
 {
     long long began = 0;
     for (uint32_t spin = 0;; ++spin) {
         if (mbarrier_try_wait_parity(bar, parity))
             return true;
-        if ((spin & 255) == 0) {
+        if ((spin & 15) == 0) {                  // an attempt may itself pause for a while
             const long long now = clock64();
             if (spin == 0)
                 began = now;
-            else if (now - began > kWaitCycles)
+            else if (now - began > cycles)
                 return false;
         }
     }
@@ -387,8 +394,9 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
     // are done with the step; added (BIAS): the sum warps are done with its gradients.  ready (first block):
     // both blocks' decoded values are there, and their gradients.
     // formed: a sum in tensor memory is complete; taken (first block): it has been read by both blocks.
+    // finished: so are all multiplications that were ever issued.  nowhere: what threads that gave up arrive on.
     __shared__ __align__(8) unsigned long long landed[kStages], multiplied[kStages], added[kStages], ready[kDecoded],
-        formed[2], taken[2];
+        formed[2], taken[2], finished, nowhere[kDecoded];
     __shared__ uint32_t step_words[kStages][kDepth];         // four step bytes per token
     __shared__ uint32_t tensor_memory_slot;
     __shared__ float bias_part[4][kHalf];
@@ -402,20 +410,26 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
     const uint32_t landed0 = shared_address(landed), ready0 = shared_address(ready);
     const uint32_t multiplied0 = shared_address(multiplied), added0 = shared_address(added);
     const uint32_t formed0 = shared_address(formed), taken0 = shared_address(taken);
+    const uint32_t finished0 = shared_address(&finished), nowhere0 = shared_address(nowhere);
 
     if (threadIdx.x == 0) {
         a.status[blockIdx.x] = 0;
+        // a barrier that expects one arrival too many never completes a phase
+        auto init = [&](uint32_t bar, uint32_t count, int hand_over) { barrier_init(bar, count + (a.withheld == hand_over)); };
         for (int s = 0; s < kStages; ++s) {
-            barrier_init(landed0 + 8 * s, 2);
-            barrier_init(multiplied0 + 8 * s, 1);
-            barrier_init(added0 + 8 * s, kSumWarps);
+            init(landed0 + 8 * s, 2, ADASUM_HAND_OVER_LANDED);
+            init(multiplied0 + 8 * s, 1, ADASUM_HAND_OVER_MULTIPLIED);
+            init(added0 + 8 * s, kSumWarps, ADASUM_HAND_OVER_ADDED);
         }
         for (int s = 0; s < kDecoded; ++s)
-            barrier_init(ready0 + 8 * s, 2 * kCodeWarps);
+            init(ready0 + 8 * s, 2 * kCodeWarps, ADASUM_HAND_OVER_READY);
         for (int s = 0; s < 2; ++s) {
-            barrier_init(formed0 + 8 * s, 1);
-            barrier_init(taken0 + 8 * s, 2 * kSumWarps);
+            init(formed0 + 8 * s, 1, ADASUM_HAND_OVER_FORMED);
+            init(taken0 + 8 * s, 2 * kSumWarps, ADASUM_HAND_OVER_TAKEN);
         }
+        barrier_init(finished0, 1);
+        for (int s = 0; s < kDecoded; ++s)
+            barrier_init(nowhere0 + 8 * s, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kMemoryWarp) {
@@ -434,13 +448,19 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tensor_memory = tensor_memory_slot;
 
-    bool waiting = true;             // false after a wait of this thread ran out
-    auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (waiting && !wait_phase(bar, parity)) {
-            waiting = false;
+    // After a wait of this thread ran out it neither waits nor acts for its warp (arrives, multiplies, commits) any more.
+    // The hand-overs to the thread that multiplies are turned aside rather than left out: a second condition beside
+    // the lane's number cost 1 %, whole warps in step (a vote per wait) 7 % of the product's time.
+    bool waiting = true, arrives = lane == 0;
+    uint32_t ready_at = ready0, taken_at = taken0;
+    auto wait_up_to = [&](uint32_t bar, uint32_t parity, long long cycles) {
+        if (waiting && !wait_phase(bar, parity, cycles)) {
+            waiting = arrives = false;
+            ready_at = taken_at = nowhere0;
             a.status[blockIdx.x] = ADASUM_DEVICE_TIMEOUT;
         }
     };
+    auto wait = [&](uint32_t bar, uint32_t parity) { wait_up_to(bar, parity, a.wait_cycles); };
 
     if (warp < kSumWarps) {
         // ---- sums: warp w reads tensor-memory lanes 32 (w % 4) .. + 31 (features), outputs 128 (w / 4) .. + 127
@@ -494,7 +514,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                         }
                     }
                     __syncwarp();
-                    if (lane == 0)
+                    if (arrives)
                         mbarrier_arrive(added0 + 8 * ring.stage);
                     ring.advance();
                 }
@@ -516,7 +536,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
             if (lane == 0)
-                arrive_at_first(taken0 + 8 * (count & 1));
+                arrive_at_first(taken_at + 8 * (count & 1));
 
             if (!c.last_of_share(a))
                 continue;
@@ -560,6 +580,11 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                 asm volatile("bar.sync 1, 256;" ::: "memory");
             }
         }
+        // The last commit arrives in both blocks, and each waits for its own: in this warp, which has just seen the last sum.
+        if (warp == 0) {
+            waiting = true;
+            wait_up_to(finished0, 0, kLastWait * a.wait_cycles);
+        }
     } else if (warp < kCopyWarp) {
         // ---- codes: a lane decodes 16 features of four rows (tokens).  Of eight neighbouring lanes four hold the
         // first panel's pieces of one row and four the second's of the row's neighbour: their reads, and then
@@ -600,7 +625,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0)
-                    arrive_at_first(ready0 + 8 * out.stage);
+                    arrive_at_first(ready_at + 8 * out.stage);
                 }
                 if (taken_places == kDecoded)
                     behind.advance();
@@ -667,7 +692,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint64_t x = operand_descriptor(decoded0 + in.stage * kOperandBytes);
                     const uint64_t g = operand_descriptor(stage0 + ring.stage * kStageBytes);
-                    if (elected()) {
+                    if (elected() && waiting) {
 #pragma unroll
                         for (int s = 0; s < kDepth / 16; ++s) {
                             // 16 tokens are 2048 bytes further on: 128 in the descriptors' units
@@ -686,6 +711,9 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                     in.advance();
                 }
             }
+            if (elected())
+                commit_to_both(finished0);
+            __syncwarp();
         } else if (warp == kStepWarp) {
             // ---- step bytes: a lane loads two rows per step, kBatch steps ahead of their use
             constexpr int kBatch = 4;
@@ -726,7 +754,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                         step_words[ring.stage][lane] = v[j][0];
                         step_words[ring.stage][lane + 32] = v[j][1];
                         __syncwarp();
-                        if (lane == 0)
+                        if (arrives)
                             mbarrier_arrive(landed0 + 8 * ring.stage);
                         ring.advance();
                     }
@@ -735,7 +763,8 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
         }
         __syncwarp();
     }
-    // Neither block may end, nor free its tensor memory, while the other still multiplies or arrives here.
+    // Neither block may end, nor free its tensor memory, while the other still multiplies or arrives here: both have
+    // waited for the last commit, the first block's copies of it included.
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncwarp();
     cluster_barrier();
@@ -1016,27 +1045,11 @@ cudaError_t launch_relay(const void* grad, int64_t stride, int64_t rows, int64_t
     return cudaGetLastError();
 }
 
-}  // namespace
-}  // namespace adasum
-
-extern "C" {
-
-size_t adasum_checkpoint_weight_grad_workspace_bytes(int64_t rows, int64_t features, int64_t outputs,
-                                                     adasum_dtype_t dtype)
+adasum_status_t weight_grad(const void* checkpoint, int64_t rows, int64_t features, const void* grad_out,
+                            int64_t grad_out_stride, int64_t outputs, adasum_dtype_t dtype, float scale, void* grad_weight,
+                            void* grad_bias, adasum_dtype_t grad_dtype, int32_t accumulate, void* workspace,
+                            size_t workspace_bytes, void* stream_ptr, int hand_over)
 {
-    using namespace adasum;
-    if (!extent_ok(rows) || !extent_ok(features) || !extent_ok(outputs) || !operator_dtype(dtype))
-        return 0;
-    return work_layout(rows, features, outputs, dtype).total;
-}
-
-adasum_status_t adasum_checkpoint_weight_grad(const void* checkpoint, int64_t rows, int64_t features,
-                                              const void* grad_out, int64_t grad_out_stride, int64_t outputs,
-                                              adasum_dtype_t dtype, float scale, void* grad_weight, void* grad_bias,
-                                              adasum_dtype_t grad_dtype, int32_t accumulate, void* workspace,
-                                              size_t workspace_bytes, void* stream_ptr)
-{
-    using namespace adasum;
     clear_error();
     if (!extent_ok(rows) || !extent_ok(features) || !extent_ok(outputs))
         return fail(ADASUM_ERR_ARG, "rows = %lld, features = %lld, outputs = %lld out of range", (long long)rows,
@@ -1125,6 +1138,8 @@ adasum_status_t adasum_checkpoint_weight_grad(const void* checkpoint, int64_t ro
     a.chains = l.chains;
     a.units = l.units;
     a.status = reinterpret_cast<int*>(ws);
+    a.wait_cycles = hand_over == ADASUM_HAND_OVER_NONE ? kWaitCycles : kSelftestCycles;
+    a.withheld = hand_over;
     a.slots = reinterpret_cast<float*>(ws + l.slots);
     a.bias_slots = reinterpret_cast<float*>(ws + l.bias_slots);
     profile_mark(stream, -1, 0, 0, true);
@@ -1149,6 +1164,45 @@ adasum_status_t adasum_checkpoint_weight_grad(const void* checkpoint, int64_t ro
         profile_mark(stream, ADASUM_KERNEL_WEIGHT_GRAD, 2, 0, false);
     }
     return ADASUM_OK;
+}
+
+}  // namespace
+}  // namespace adasum
+
+extern "C" {
+
+size_t adasum_checkpoint_weight_grad_workspace_bytes(int64_t rows, int64_t features, int64_t outputs,
+                                                     adasum_dtype_t dtype)
+{
+    using namespace adasum;
+    if (!extent_ok(rows) || !extent_ok(features) || !extent_ok(outputs) || !operator_dtype(dtype))
+        return 0;
+    return work_layout(rows, features, outputs, dtype).total;
+}
+
+adasum_status_t adasum_checkpoint_weight_grad(const void* checkpoint, int64_t rows, int64_t features,
+                                              const void* grad_out, int64_t grad_out_stride, int64_t outputs,
+                                              adasum_dtype_t dtype, float scale, void* grad_weight, void* grad_bias,
+                                              adasum_dtype_t grad_dtype, int32_t accumulate, void* workspace,
+                                              size_t workspace_bytes, void* stream_ptr)
+{
+    return adasum::weight_grad(checkpoint, rows, features, grad_out, grad_out_stride, outputs, dtype, scale, grad_weight, grad_bias,
+                               grad_dtype, accumulate, workspace, workspace_bytes, stream_ptr, ADASUM_HAND_OVER_NONE);
+}
+
+adasum_status_t adasum_checkpoint_weight_grad_selftest(const void* checkpoint, int64_t rows, int64_t features,
+                                                       const void* grad_out, int64_t grad_out_stride, int64_t outputs,
+                                                       adasum_dtype_t dtype, float scale, void* grad_weight,
+                                                       void* grad_bias, adasum_dtype_t grad_dtype, int32_t accumulate,
+                                                       void* workspace, size_t workspace_bytes, void* stream_ptr,
+                                                       int32_t hand_over)
+{
+    using namespace adasum;
+    clear_error();
+    if (hand_over < ADASUM_HAND_OVER_LANDED || hand_over > ADASUM_HAND_OVER_TAKEN)
+        return fail(ADASUM_ERR_ARG, "unknown hand-over %d", (int)hand_over);
+    return weight_grad(checkpoint, rows, features, grad_out, grad_out_stride, outputs, dtype, scale, grad_weight, grad_bias,
+                       grad_dtype, accumulate, workspace, workspace_bytes, stream_ptr, hand_over);
 }
 
 adasum_status_t adasum_checkpoint_weight_grad_status(int64_t rows, int64_t features, int64_t outputs,

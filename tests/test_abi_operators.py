@@ -190,3 +190,13 @@ def test_a_workspace_for_a_long_list_does_for_a_shorter_one():
         for features, outputs in ((1, 1), (1000, 257), (4096, 1024)):
             sizes = [b.adasum_checkpoint_weight_grad_workspace_bytes(n, features, outputs, dtype) for n in range(0, 6000, 7)]
             assert all(x <= y for x, y in zip(sizes, sizes[1:]))
+
+
+def test_weight_grad_selftest_refusals(b):
+    def call(hand_over, kept=A, ws=W):
+        return _status(b, b.raw().adasum_checkpoint_weight_grad_selftest(kept, 50, 40, B, 24, 24, BF16, 1.0, C, C + 0x100000,
+                                                                         F32, 0, ws, BIG, None, hand_over))
+
+    assert call(0) == call(7) == call(-1) == "ADASUM_ERR_ARG" and "hand-over" in b.adasum_last_error()
+    assert call(1, kept=None) == "ADASUM_ERR_NULL"
+    assert call(6, ws=None) == "ADASUM_ERR_WORKSPACE"
