@@ -503,8 +503,8 @@ adasum_status_t adasum_checkpoint_weight_grad(const void* checkpoint, int64_t ro
 
 /*
  * Device-side status of the last weight gradient that used this workspace: synchronises `stream` and
- * returns ADASUM_OK, ADASUM_ERR_TIMEOUT if a bounded wait inside the product ran out (its gradients are
- * then wrong), or an argument / CUDA error.  Sizes and type as for the call that is being asked about.
+ * returns ADASUM_OK, ADASUM_ERR_TIMEOUT if a bounded wait inside the product ran out, or an argument / CUDA error.
+ * Without asking, a caller finds NaN in the gradients (all to which the blocks in question contributed).  Sizes and type as for the call that is being asked about.
  */
 adasum_status_t adasum_checkpoint_weight_grad_status(int64_t rows, int64_t features, int64_t outputs,
                                                      adasum_dtype_t dtype, const void* workspace,
@@ -514,8 +514,8 @@ adasum_status_t adasum_checkpoint_weight_grad_status(int64_t rows, int64_t featu
  * A self-test of the product's bounded waits, not a way to compute gradients: the weight gradient with one kind of
  * hand-over inside the product that never completes, and with waits of a millisecond instead of a second.  The
  * waits run out, the kernel records it, lets its copies and multiplications finish, frees its tensor memory and
- * returns; adasum_checkpoint_weight_grad_status then reports ADASUM_ERR_TIMEOUT, unless the sizes need no hand-over of
- * that kind.  The next weight gradient on the workspace is not affected.
+ * returns; gradients are NaN and adasum_checkpoint_weight_grad_status reports ADASUM_ERR_TIMEOUT, unless the sizes need
+ * no hand-over of that kind.  The next weight gradient on the workspace is not affected.
  */
 #define ADASUM_HAND_OVER_NONE 0
 #define ADASUM_HAND_OVER_LANDED 1     /* a step's gradients, codes and step bytes in shared memory */

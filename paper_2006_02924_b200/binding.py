@@ -664,7 +664,9 @@ def adasum_checkpoint_weight_grad(checkpoint, grad_out, features=None, grad_weig
     """``adasum_checkpoint_weight_grad`` of the C ABI.  ``grad_out``: ``[rows, outputs]``.  The gradients go to
     ``grad_weight`` (``[outputs, features]`` or flat) and ``grad_bias`` (``[outputs]``), both contiguous;
     what is not given is allocated here (fp32 unless ``grad_dtype`` says otherwise; a bias gradient only
-    with ``want_bias``).  Returns ``(grad_weight, grad_bias)``."""
+    with ``want_bias``).  Returns ``(grad_weight, grad_bias)``.  fp16 gradients round kept values of fp32 or bf16
+    activations to fp16.  A product that the device did not finish (a bounded wait ran out) leaves NaN;
+    ``adasum_checkpoint_weight_grad_status`` tells, for a ``workspace`` of the caller's."""
     stride = _matrix("grad_out", grad_out)
     rows, outputs = grad_out.shape
     if grad_weight is None:

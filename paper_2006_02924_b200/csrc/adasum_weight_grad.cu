@@ -34,7 +34,8 @@
 //
 // Every wait has a limit.  A thread whose wait runs out records it and goes on without waiting, but hands over and
 // issues nothing more, so the waits that depend on it run out in turn and the launch ends, a few limits later;
-// adasum_checkpoint_weight_grad_status reports it.  Before a block ends its copies have landed, and the pair's
+// adasum_checkpoint_weight_grad_status reports it, and the block leaves NaN for all its shares of tiles, so that no caller
+// takes a part of a sum for a gradient.  Before a block ends its copies have landed, and the pair's
 // multiplications and their arrivals are done: a last commit says so, whatever happened before.  (Those two waits have
 // limits as well; copies and multiplications need microseconds, so one that ran out means that the device itself is stuck.)
 #include <cuda.h>
@@ -344,6 +345,42 @@ struct Cursor {
     }
 };
 
+// What a thread of the warps that sum leaves for its feature and outputs where a wait of its block ran out: NaN, over
+// whatever it has left for any tile of the pair's run.  (Inlined, it costs the whole kernel 10 %.)
+__device__ __noinline__ void leave_nan(const WeightGradArgs& a, uint32_t begin, uint32_t end, uint32_t pair, uint32_t rank,
+                                       uint32_t thread)
+{
+    const float nan = __uint_as_float(0x7fc00000u);
+    const int feature = 32 * ((thread >> 5) & 3) + (thread & 31), side = thread >> 7;
+    uint32_t chain_begin = 0;
+    bool fresh = true;
+    for (Cursor c(a, begin, end); !c.done(); c.advance(a)) {
+        if (fresh)
+            chain_begin = c.chain;
+        fresh = c.last_of_share(a);
+        if (!fresh)
+            continue;
+        const int64_t k = (int64_t)c.tile_k * kTileSide + rank * kHalf + feature;
+        const int64_t n = (int64_t)c.tile_n * kTileSide + side * kHalf;
+        if (chain_begin == 0 && c.chain + 1 == a.chains) {
+            for (int i = 0; i < kHalf && k < a.features && n + i < a.outputs; ++i)
+                store_from_float(a.weight, a.out_dtype, (n + i) * a.features + k, nan);
+        } else {
+            float* dst = a.slots + (2 * pair + (c.part == 0 ? 1 : 0)) * kSlotFloats + (rank * kTileSide + side * kHalf) * kHalf + feature;
+            for (int i = 0; i < kHalf; ++i)
+                dst[i * kHalf] = nan;
+        }
+        if (a.bias && thread < kHalf) {
+            const int output = rank * kHalf + thread;
+            const int64_t m = (int64_t)c.tile_n * kTileSide + output;
+            if (a.cut)
+                a.bias_slots[(int64_t)(pair + c.tile_n * a.tiles_k + c.tile_k) * kTileSide + output] = nan;
+            else if (c.tile_k == 0 && m < a.outputs)
+                store_from_float(a.bias, a.out_dtype, m, nan);
+        }
+    }
+}
+
 // A position in a ring of N stages and the parity of its current round.
 template <int N>
 struct Ring {
@@ -399,6 +436,9 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
         formed[2], taken[2], finished, nowhere[kDecoded];
     __shared__ uint32_t step_words[kStages][kDepth];         // four step bytes per token
     __shared__ uint32_t tensor_memory_slot;
+    // Some wait of this block ran out.  The other block needs no word of it: a thread that acts for its warp stops, so the
+    // other block's waits run out too; one that does not can only have spoilt this block's decoded values.
+    __shared__ volatile uint32_t gave_up;
     __shared__ float bias_part[4][kHalf];
 
     start_next_kernel();             // the join; it waits for this kernel's end by itself
@@ -414,6 +454,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
 
     if (threadIdx.x == 0) {
         a.status[blockIdx.x] = 0;
+        gave_up = 0;
         // a barrier that expects one arrival too many never completes a phase
         auto init = [&](uint32_t bar, uint32_t count, int hand_over) { barrier_init(bar, count + (a.withheld == hand_over)); };
         for (int s = 0; s < kStages; ++s) {
@@ -457,6 +498,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
         if (waiting && !wait_phase(bar, parity, cycles)) {
             waiting = arrives = false;
             ready_at = taken_at = nowhere0;
+            gave_up = 1;
             a.status[blockIdx.x] = ADASUM_DEVICE_TIMEOUT;
         }
     };
@@ -580,6 +622,8 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                 asm volatile("bar.sync 1, 256;" ::: "memory");
             }
         }
+        if (gave_up != 0)
+            leave_nan(a, unit_begin, unit_end, pair, rank, threadIdx.x);
         // The last commit arrives in both blocks, and each waits for its own: in this warp, which has just seen the last sum.
         if (warp == 0) {
             waiting = true;

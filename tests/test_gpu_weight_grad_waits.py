@@ -45,3 +45,23 @@ def test_a_wait_that_runs_out(b, hand_over, bias, dtype, rows):
     assert "bounded wait" in b.adasum_last_error()
     got, got_b = good()
     assert torch.equal(got, want) and (db is None or torch.equal(got_b, want_b))
+
+
+@pytest.mark.parametrize("out_type", [torch.float32, torch.float16])
+@pytest.mark.parametrize("rows,features,outputs", [(4 * 512 * 74, 40, 24), (520, 3000, 9000)])
+@pytest.mark.parametrize("hand_over", ["landed", "ready", "formed"])
+def test_an_unfinished_sum_is_no_gradient(b, hand_over, rows, features, outputs, out_type):
+    """Nothing of a product whose waits ran out looks like a gradient: NaN everywhere, be the tiles cut among pairs of
+    blocks (one tile of many tokens) or written by one pair each (many tiles); these hand-overs fail in the first sum."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(4)
+    x = torch.randn(rows, features, generator=gen, device="cuda")
+    dy = torch.randn(rows, outputs, generator=gen, device="cuda").bfloat16()
+    _, kept = b.adasum_checkpoint_save(x, want_out=False)
+    ws = torch.empty(b.adasum_checkpoint_weight_grad_workspace_bytes(rows, features, outputs, "bf16"), dtype=torch.uint8,
+                     device="cuda")
+    dw = torch.zeros(outputs, features, dtype=out_type, device="cuda")
+    db = torch.zeros(outputs, dtype=out_type, device="cuda")
+    b.adasum_checkpoint_weight_grad_selftest(hand_over, kept, dy, dw, db, ws)
+    assert b.adasum_checkpoint_weight_grad_status(rows, features, outputs, "bf16", ws) == 7
+    assert torch.isnan(dw).all() and torch.isnan(db).all()
