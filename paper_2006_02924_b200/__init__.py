@@ -7,13 +7,14 @@ one gradient per GPU over a torch.distributed group (recursive vector halving).
 """
 
 _BINDING_NAMES = (
-    "adasum_reduce", "adasum_reduce_ex", "adasum_reduce_delta", "adasum_sharded_gram", "adasum_sharded_apply", "adasum_reduce_sharded",
-    "adasum_pair", "adasum_pair_noalloc", "adasum_workspace_bytes",
-    "adasum_plan_info", "adasum_status_string", "adasum_last_error", "adasum_shutdown",
+    "adasum_reduce", "adasum_reduce_ex", "adasum_reduce_delta", "adasum_reduce_scaled", "adasum_sharded_gram",
+    "adasum_sharded_apply", "adasum_reduce_sharded", "adasum_pair", "adasum_pair_noalloc", "adasum_workspace_bytes",
+    "adasum_device_status", "adasum_plan_info", "adasum_status_string", "adasum_last_error", "adasum_shutdown",
     "adasum_profile_enable", "adasum_profile_collect", "flags_radix", "AdasumError",
     "adasum_embedding_forward", "adasum_embedding_grad", "adasum_embedding_grad_workspace_bytes",
     "adasum_checkpoint_bytes", "adasum_checkpoint_save", "adasum_checkpoint_load", "adasum_checkpoint_act_grad",
     "adasum_checkpoint_weight_grad", "adasum_checkpoint_weight_grad_workspace_bytes",
+    "adasum_checkpoint_weight_grad_status", "adasum_checkpoint_weight_grad_selftest",
 )
 
 

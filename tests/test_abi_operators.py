@@ -200,3 +200,12 @@ def test_weight_grad_selftest_refusals(b):
     assert call(0) == call(7) == call(-1) == "ADASUM_ERR_ARG" and "hand-over" in b.adasum_last_error()
     assert call(1, kept=None) == "ADASUM_ERR_NULL"
     assert call(6, ws=None) == "ADASUM_ERR_WORKSPACE"
+
+
+def test_every_call_is_reached_through_the_package(b):
+    import paper_2006_02924_b200 as package
+
+    calls = [name for name in dir(b) if name.startswith("adasum_") and callable(getattr(b, name))]
+    assert "adasum_checkpoint_weight_grad_status" in calls and len(calls) > 25
+    for name in calls:
+        assert getattr(package, name) is getattr(b, name)
