@@ -487,17 +487,7 @@ adasum_status_t check_matrix(const char* name, const void* p, int64_t stride, in
     return ADASUM_OK;
 }
 
-// Calls f with a value of the run-time type, the constant of the run-time activation, or of a truth value.
-template <typename F>
-void with_type(adasum_dtype_t dtype, F&& f)
-{
-    if (dtype == ADASUM_F32)
-        f(float{});
-    else if (dtype == ADASUM_F16)
-        f(__half{});
-    else
-        f(__nv_bfloat16{});
-}
+// Calls f with the constant of the run-time activation, or of a truth value.
 template <int N>
 struct Constant { static constexpr int value = N; };
 template <typename F>

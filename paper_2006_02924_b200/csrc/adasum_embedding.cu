@@ -735,17 +735,6 @@ adasum_status_t check_tokens(const void* tokens, int32_t token_bytes, int64_t nu
     return ADASUM_OK;
 }
 
-template <typename F>
-void with_type(adasum_dtype_t dtype, F&& f)
-{
-    if (dtype == ADASUM_F32)
-        f(float{});
-    else if (dtype == ADASUM_F16)
-        f(__half{});
-    else
-        f(__nv_bfloat16{});
-}
-
 }  // namespace
 }  // namespace adasum
 

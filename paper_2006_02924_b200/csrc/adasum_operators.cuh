@@ -117,6 +117,18 @@ cudaError_t launch_after(void (*kernel)(Params...), dim3 grid, unsigned threads,
     return cudaLaunchKernelEx(&config, kernel, Params(args)...);
 }
 
+// Calls f with a value of the run-time type.
+template <typename F>
+void with_type(adasum_dtype_t dtype, F&& f)
+{
+    if (dtype == ADASUM_F32)
+        f(float{});
+    else if (dtype == ADASUM_F16)
+        f(__half{});
+    else
+        f(__nv_bfloat16{});
+}
+
 // ---- device ----------------------------------------------------------------------------------------
 
 __device__ __forceinline__ void divide_row(const RowDivider& d, uint64_t n, uint64_t& row, uint32_t& at)
