@@ -67,3 +67,21 @@ def test_a_group_kept_as_nan_has_no_gradient(b, name, dtype, pad):
     assert torch.equal(torch.isnan(got), bad)
     if name == "relu":
         assert torch.equal(got[~bad], torch.where(x > 0, dy, 0)[~bad])
+
+
+def test_fp32_tanh_gelu_slope_is_as_near_as_torch_arithmetic(b):
+    """Against 64 bits, the fp32 slope is no further off (in the norm) than the same formula in fp32 torch operations."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(21)
+    x = torch.randn(610, 1024, generator=gen, device="cuda")
+    _, kept = b.adasum_checkpoint_save(x, want_out=False)
+    at = b.adasum_checkpoint_load(kept, 610, 1024)
+
+    def slope(v):
+        k = (2 / torch.pi) ** 0.5
+        t = torch.tanh(k * (v + 0.044715 * v * v * v))
+        return 0.5 * (1 + t) + 0.5 * v * (1 - t * t) * k * (1 + 3 * 0.044715 * v * v)
+
+    want = slope(at.double())
+    got = b.adasum_checkpoint_act_grad(kept, torch.ones_like(x), "gelu_tanh")
+    assert (got.double() - want).norm() <= (slope(at).double() - want).norm()
