@@ -36,8 +36,9 @@ __device__ __forceinline__ int64_t token_row(const Id* tokens, int64_t t, int64_
 
 constexpr int kLookupRows = 4;             // tokens per thread
 
-// A copy with a product, bound by HBM and, for narrow outputs, by instruction issue: 32768 tokens in 30522 x 1024
-// fp32 rows to bf16 in 22 us (102 MB with each distinct row counted once: 4.6 TB/s).
+// A copy with a product: 32768 tokens in 30522 x 1024 fp32 rows to bf16 in 22 us (102 MB with each distinct row counted
+// once: 4.6 TB/s).  Bound by the loads' latency: the vectors wait in fp32 registers (56 a thread), which leaves 47 % of the
+// warps resident, and those stall for loads most of all; issue slots are 61 % used, the HBM less than half.
 // VEC: every row of the table and of the output starts on 16 bytes and dim is a multiple of 8.
 template <typename T, typename Id, bool VEC>
 __global__ void __launch_bounds__(kStripThreads)
@@ -289,9 +290,21 @@ embedding_sort_kernel(const Id* tokens, uint32_t n, uint32_t num_rows, int passe
 // Short lists: an item's place is the number of items that come before it.  Every block holds all keys in shared
 // memory; a warp counts for one item at a time.  n^2 comparisons, but spread over all multiprocessors and
 // without the radix sort's chain of passes: 4608 tokens of 30522 rows 5 us against 11 us, bound by instruction issue
-// (two per comparison).  6144 is where the radix sort, which zeros can be written beside, catches up.
+// (two per comparison).
+//
+// Up to one item per warp of a grid that covers the device (4736 on 148 multiprocessors); the second item costs 3 us at
+// once.  Whole calls, ranked against sorted, with 4736, 4800 and 6144 tokens (us): added to 30522 x 1024 23.6/24.7,
+// 26.3/24.4, 31.2/26.8; to 512 x 1024 22.7/25.1, 25.5/24.7, 24.6/22.0; written to 30522 x 64 19.5/18.3, 22.3/18.2, 25.6/18.7;
+// to 2 x 1024 16.6/14.7, 19.4/14.8, 21.5/15.2.  Where there are many zeros to write (after a ranking beside the sums,
+// otherwise beside the sort) ranking pays up to 6144: 30522 x 1024 33.8/39.8, 36.6/39.6, 41.4/41.7.
 constexpr int kRankThreads = 1024;
-constexpr int64_t kRankMost = 6144;
+constexpr int64_t kRankMost = 6144, kManyZeros = int64_t(32) << 20;
+
+bool ranked(int64_t num_tokens, int64_t zero_bytes, int sms)
+{
+    const int64_t one_each = (int64_t)sms * (kRankThreads / 32);
+    return num_tokens <= (zero_bytes >= kManyZeros || one_each > kRankMost ? kRankMost : one_each);
+}
 
 template <typename Id>
 __global__ void __launch_bounds__(kRankThreads)
@@ -655,9 +668,11 @@ __global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(const __gr
 
 // ---- host ------------------------------------------------------------------------------------------------
 
-// Entries per tile.
-// Measured with 8, 16, 32: 999 tokens (dim 203, fp32) 26, 28, 38 us, 16384 tokens on two rows 44, 36, 38 us, 200000 tokens
-// (dim 256) 237, 222, 234 us.
+// Entries per tile: short tiles spread a short list over more blocks, long ones leave fewer shares of long runs to be
+// joined.  Whole calls with 8 against 16 (us): into 1009 x 203 with 64 tokens 7.8/9.1, 999 11.6/13.9, 2047 12.2/16.7, 4096
+// 15.7/18.3, 16384 32.4/29.9; into 512 x 1024 with 999 10.4/11.8, 2047 14.2/13.6, 16384 37.3/32.6; into 30522 x 1024 with 999
+// 28.4/27.0, 2047 32.3/29.0, 16384 49.7/46.2.  The crossing moves from about 1000 tokens (wide rows) to 8000 (narrow ones);
+// 2048 lies between.  Up to 32 tokens, two tiles of 16 need no join.  (32: 38 us where 8 and 16 took 26 and 28, and 36.)
 constexpr int64_t kShortTilesBelow = 2048;
 int sum_tile(int64_t n) { return n > 2 * kMaxTile && n < kShortTilesBelow ? kMaxTile / 2 : kMaxTile; }
 int64_t sum_tiles(int64_t n) { return (n + sum_tile(n) - 1) / sum_tile(n); }
@@ -849,16 +864,17 @@ adasum_status_t adasum_embedding_grad(const void* grad_out, int64_t grad_out_str
         ADASUM_CUDA_CHECK(cudaMemsetAsync(grad_table, 0, (size_t)table_bytes, stream));
         return ADASUM_OK;
     }
+    const int64_t zero_bytes = accumulate ? 0 : table_bytes;
+    const bool rank = ranked(num_tokens, zero_bytes, sms);
     auto sort = [&](auto id) {
         using Id = decltype(id);
         const Id* ids = static_cast<const Id*>(tokens);
-        if (num_tokens <= kRankMost) {
+        if (rank) {
             const int64_t wanted = (num_tokens + kRankThreads / 32 - 1) / (kRankThreads / 32);
             embedding_rank_kernel<Id><<<(unsigned)(wanted < sms ? wanted : sms), kRankThreads,
                                         (size_t)((num_tokens + 127) / 128 * 128) * sizeof(uint32_t), stream>>>(
                 ids, (uint32_t)num_tokens, (uint32_t)num_rows, sorted, long_runs);
         } else {
-            const int64_t zero_bytes = accumulate ? 0 : table_bytes;
             const int64_t wanted = ((zero_bytes + kZeroBytes - 1) / kZeroBytes + kSortCluster - 1) / kSortCluster + 1;
             const int64_t clusters = resident_sort_clusters<Id>();
             embedding_sort_kernel<Id><<<(unsigned)((wanted < clusters ? wanted : clusters) * kSortCluster), kSortThreads, 0,
@@ -890,7 +906,7 @@ adasum_status_t adasum_embedding_grad(const void* grad_out, int64_t grad_out_str
     // about 64 KB of zeros per block
     const int64_t row_bytes = dim * operator_bytes(grad_dtype), fit = 65536 / row_bytes;
     a.zero_rows = (uint32_t)(fit < 1 ? 1 : fit < kZeroRows ? fit : kZeroRows);
-    const int64_t zero_blocks = accumulate || num_tokens > kRankMost ? 0 : (num_rows + a.zero_rows - 1) / a.zero_rows;
+    const int64_t zero_blocks = accumulate || !rank ? 0 : (num_rows + a.zero_rows - 1) / a.zero_rows;
     if (a.tiles + zero_blocks > 0x7fffffff)
         return fail(ADASUM_ERR_ARG, "%lld tokens and %lld rows are too many", (long long)num_tokens, (long long)num_rows);
     cudaError_t launch_error = cudaSuccess;

@@ -1009,8 +1009,10 @@ uint32_t launch_pairs(const WorkLayout& l, adasum_dtype_t dtype, bool bias)
         most = bias ? resident_pairs<__half, 1, true>() : resident_pairs<__half, 1, false>();
     else
         most = bias ? resident_pairs<__nv_bfloat16, 1, true>() : resident_pairs<__nv_bfloat16, 1, false>();
-    // Short sums are not cut: 16 steps take 5 us, leaving and joining a tile's parts as long, in one more launch
-    // (18 steps, 333 fp32 tokens of 1000 x 257: 12.6 + 4 us cut into three, 16 us whole).
+    // Short sums are not cut: leaving and joining a tile's parts takes one more launch.  Whole against cut (us), with 8,
+    // 16 and 24 steps: 16 tiles, bf16, 11.8/11.8, 15.1/16.1, 18.4/16.9; 8 tiles 13.4/13.5, 16.6/16.7, 20.0/17.5; one tile
+    // 11.8/11.8, 15.0/13.9, 18.2/14.2; fp32 gradients with 15 and 18 steps: 8 tiles 17.2/15.8, 18.6/16.6, 16 tiles 17.4/17.2,
+    // 18.7/20.4.  (Where the tiles nearly fill the device, whole would be better for longer: 64 tiles, 64 steps, 36/47.)
     if (l.tiles <= most && l.iterations <= 16)
         return l.tiles;
     return l.pairs < most ? l.pairs : most;

@@ -213,3 +213,21 @@ def test_refusals(b):
         b.adasum_embedding_grad(dy, ids)
     with pytest.raises(b.AdasumError, match="WORKSPACE"):
         b.adasum_embedding_grad(dy, ids, 5, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("n", [2047, 2048, 4736, 4737, 6144, 6145])
+@pytest.mark.parametrize("num_rows,dim", [(30522, 300), (997, 20)])
+def test_lists_around_a_change_of_method(b, n, num_rows, dim, accumulate):
+    """The same sums, whichever way the tokens were brought into order and however long the tiles are: small whole
+    numbers, so that every association gives the same."""
+    gen = _gen(31)
+    ids = _ids(gen, n, num_rows, 64, "uneven")
+    dy = torch.randint(-8, 9, (n, dim), generator=gen, device="cuda").float()
+    old = torch.randint(-8, 9, (num_rows, dim), generator=gen, device="cuda").float()
+    want = old.clone() if accumulate else torch.zeros_like(old)
+    inside = (ids >= 0) & (ids < num_rows)
+    want.index_add_(0, ids[inside], dy[inside] * 2)
+    workspace = torch.empty(b.adasum_embedding_grad_workspace_bytes(6145, num_rows, dim), dtype=torch.uint8, device="cuda")
+    got = b.adasum_embedding_grad(dy, ids, grad_table=old.clone(), scale=2.0, accumulate=accumulate, workspace=workspace)
+    assert torch.equal(got, want)
