@@ -440,7 +440,10 @@ _lib.adasum_checkpoint_weight_grad.argtypes = [_vp, _i64, _i64, _vp, _i64, _i64,
                                                ctypes.c_int, _i32, _vp, ctypes.c_size_t, _vp]
 
 
-# These calls sit in a training step's inner loop: their wrappers avoid what costs a microsecond each in Python
+# These calls are outside autograd, as the reduces are: results carry no graph, whatever the arguments require, and a
+# tensor that is written in place (out=x, grad_in=grad_out) is not marked as changed.
+#
+# They sit in a training step's inner loop: their wrappers avoid what costs a microsecond each in Python
 # (device objects, context managers, tensors built from keyword-laden factories).
 
 def _matrix(name: str, t, rows=None, cols=None):
