@@ -417,7 +417,8 @@ __device__ __forceinline__ uint32_t load_steps(const uint8_t* steps, int64_t gro
 // multiplications.  fp32 gradients: 350 us for the three products after 100 us (6.7 TB/s) that lay them out.
 //
 // T: 16-bit type of both operands.  PLANES: 1, or 3 for fp32 gradients, which arrive as three bf16 matrices
-// that add up to them; a step then is one plane of one block of tokens, planes fastest.
+// that add up to them; a step then is one plane of one block of tokens, planes fastest, the smallest first: what is added
+// while a sum is small is truncated at its size (64 tokens 3.9e-7 -> 0.6e-7 of the norm, 333 tokens 3.3e-7 -> 2.5e-7).
 // Warps 0 .. 7 sum, 8 .. 15 decode, 16 copies, 17 multiplies (first block only), 18 owns the tensor memory,
 // 19 loads step bytes.
 // Registers: 256 x 152 + 256 x 64 + 128 x 48 = 640 x 96.
@@ -700,7 +701,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                     if (!waiting)
                         break;
                     const uint32_t dst = stage0 + ring.stage * kStageBytes;
-                    const int t = (int)(step / PLANES) * kDepth, plane = (int)(step % PLANES);
+                    const int t = (int)(step / PLANES) * kDepth, plane = PLANES - 1 - (int)(step % PLANES);
                     if (elected()) {
                         expect_bytes(bar, bytes);
                         copy_box(dst, &grad_map, n, t, plane, bar);
