@@ -38,9 +38,7 @@
 // takes a part of a sum for a gradient.  Before a block ends its copies have landed, and the pair's
 // multiplications and their arrivals are done: a last commit says so, whatever happened before.  (Those two waits have
 // limits as well; copies and multiplications need microseconds, so one that ran out means that the device itself is stuck.)
-#include <cuda.h>
-
-#include "adasum_operators.cuh"
+#include "adasum_tensor.cuh"
 
 namespace adasum {
 namespace {
@@ -131,94 +129,12 @@ __device__ __forceinline__ void write_column(const WeightGradArgs& a, int64_t n,
 
 // ---- instructions --------------------------------------------------------------------------------------
 
-__device__ __forceinline__ uint32_t shared_address(const void* p)
-{
-    return static_cast<uint32_t>(__cvta_generic_to_shared(p));
-}
-__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
-}
-// Returns false if the barrier does not complete the phase within `cycles`.
-__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, long long cycles)
-{
-    long long began = 0;
-    for (uint32_t spin = 0;; ++spin) {
-        if (mbarrier_try_wait_parity(bar, parity))
-            return true;
-        if ((spin & 15) == 0) {                  // an attempt may itself pause for a while
-            const long long now = clock64();
-            if (spin == 0)
-                began = now;
-            else if (now - began > cycles)
-                return false;
-        }
-    }
-}
-// Arrives on the same barrier of the pair's first block.  Block scope is enough: what is handed over lies in the
-// arriving block's own shared (or tensor) memory, already visible to its tensor core by the proxy fence (or the
-// tensor-memory fence) before; cluster scope costs a memory barrier per arrival (349 against 259 us).
-__device__ __forceinline__ void arrive_at_first(uint32_t bar)
-{
-    asm volatile("{\n\t.reg .b32 remote;\n\tmapa.shared::cluster.u32 remote, %0, 0;\n\t"
-                 "mbarrier.arrive.shared::cluster.b64 _, [remote];\n\t}" ::"r"(bar)
-                 : "memory");
-}
-__device__ __forceinline__ void expect_bytes(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
-                 "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
-                 : "memory");
-}
-__device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
-                 "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar)
-                 : "memory");
-}
-__device__ __forceinline__ void cluster_barrier()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// Arrives on the barrier at this offset in both blocks once all multiplications issued so far are done.
-__device__ __forceinline__ void commit_to_both(uint32_t bar)
-{
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-                 "h"((uint16_t)3)
-                 : "memory");
-}
-// One lane of a converged warp.  (With a lane number instead, the compiler cannot see that one thread issues.)
-__device__ __forceinline__ bool elected()
-{
-    uint32_t yes;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
-    return yes != 0;
-}
-template <int REGS>
-__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS)); }
-template <int REGS>
-__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS)); }
-
 // Operand in shared memory with the summed index slow, 128-byte swizzle: rows of 64 features (outputs), one
 // row per token; eight rows 1024 bytes, the next 64 features one panel further.
 __device__ __forceinline__ uint64_t operand_descriptor(uint32_t address)
 {
     return (uint64_t)((address & 0x3ffffu) >> 4) | (uint64_t)(kPanelBytes >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 |
            (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
-
-__device__ __forceinline__ void load_sums(uint32_t address, uint32_t (&r)[16])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-                 : "r"(address)
-                 : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
 // ---- the codes of a step --------------------------------------------------------------------------------
@@ -380,19 +296,6 @@ __device__ __noinline__ void leave_nan(const WeightGradArgs& a, uint32_t begin, 
         }
     }
 }
-
-// A position in a ring of N stages and the parity of its current round.
-template <int N>
-struct Ring {
-    uint32_t stage = 0, phase = 0;
-    __device__ __forceinline__ void advance()
-    {
-        if (++stage == N) {
-            stage = 0;
-            phase ^= 1;
-        }
-    }
-};
 
 // Step bytes of one row (token) for the block's 128 features, zeros beyond the matrix.
 __device__ __forceinline__ uint32_t load_steps(const uint8_t* steps, int64_t groups, int64_t rows, int64_t row, int64_t group)
@@ -1017,22 +920,6 @@ uint32_t launch_pairs(const WorkLayout& l, adasum_dtype_t dtype, bool bias)
     if (l.tiles <= most && l.iterations <= 16)
         return l.tiles;
     return l.pairs < most ? l.pairs : most;
-}
-
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiled encode_tiled()
-{
-    static EncodeTiled cached = nullptr;
-    if (!cached) {
-        void* fn = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) == cudaSuccess &&
-            found == cudaDriverEntryPointSuccess)
-            cached = reinterpret_cast<EncodeTiled>(fn);
-    }
-    return cached;
 }
 
 // The codes of a checkpoint: [rows][width] bytes.
