@@ -532,6 +532,162 @@ adasum_status_t adasum_checkpoint_weight_grad_selftest(const void* checkpoint, i
                                                        void* workspace, size_t workspace_bytes, void* stream,
                                                        int32_t hand_over);
 
+/*
+ * ---- around the linear layers of a residual block ------------------------------------------------
+ *
+ * Dropout whose mask is computed and never stored, the joint between two blocks with its norms, gate and residual
+ * scale, and products in 8-bit floating point.  Together with the calls above they are a worker's forward and backward
+ * pass (the paper has no counterpart).  The same conventions hold; gradients of parameters are written into the
+ * worker's fused buffer in the same way (scale, accumulate).
+ *
+ * Dropout.  With t = round(65536 p) and q = t / 65536, an element of row r and column c is kept if its 16 random
+ * bits are at least t, and is then divided by 1 - q.  The bits come from Philox4x32-10 with the 64-bit key *seed and the
+ * counter (n, site), each 64 bits, low word first, n = r * ceil(features / 8) + c / 8: bits 16 (c % 2) .. + 15 of
+ * word (c % 8) / 2.  `seed` is read on the device when the kernel runs, so a captured graph draws new masks once the
+ * caller changes it (one seed per step and worker); `site` tells the dropouts of one step apart.  Forward and
+ * backward get the same mask from the same (seed, site).  A dropped element is 0 whatever it held (Inf and NaN too).
+ */
+
+/*
+ *     out = [residual +] dropout(x)
+ *
+ * Its gradient with respect to x is the same call on the gradient, without a residual.
+ *   x, residual, out   device, rows x features of `dtype`; residual may be NULL; out may be x or residual itself
+ *                      (same stride)
+ *   p                  0 .. 1; with t = 0 nothing is dropped and seed may be NULL
+ *   seed               device, one 64-bit word, 8-byte aligned
+ */
+adasum_status_t adasum_dropout(const void* x, int64_t x_stride, int64_t rows, int64_t features, adasum_dtype_t dtype,
+                               const void* residual, int64_t residual_stride, float p, const uint64_t* seed,
+                               uint64_t site, void* out, int64_t out_stride, void* stream);
+
+/*
+ * The joint between two blocks of a residual network:
+ *
+ *     n = post(x)                                                         norm after a block, or x itself
+ *     h = residual_scale * residual + branch_scale * gate * dropout(n)    the residual stream
+ *     y = pre(h)                                                          norm before the next block
+ *
+ * RMS norm: u = x rstd, rstd = (mean(x^2) + eps)^(-1/2); layer norm: u = (x - mean) rstd, rstd = (var + eps)^(-1/2) with the
+ * variance of all features; then u * weight + bias (NULL: 1 and 0).  Row r takes row r / rows_per_gate of the gate: one
+ * for all rows (a learned scale per channel), one per sequence, one per row.  Everything between the loads and the
+ * stored values is fp32; y is the norm of h before h is rounded.  At most ADASUM_NORM_MAX_FEATURES features.
+ */
+#define ADASUM_NORM_MAX_FEATURES 32768
+
+typedef enum {
+    ADASUM_NORM_NONE = 0,
+    ADASUM_NORM_RMS = 1,
+    ADASUM_NORM_LAYER = 2
+} adasum_norm_t;
+
+typedef struct {
+    int64_t rows, features;
+    adasum_dtype_t dtype;            /* of x, y and their gradients */
+    adasum_dtype_t stream_dtype;     /* of residual, h and their gradients: dtype or ADASUM_F32 */
+    adasum_dtype_t param_dtype;      /* of the norms' weights and biases */
+    adasum_dtype_t gate_dtype;
+    adasum_norm_t post_norm, pre_norm;
+    const void *post_weight, *post_bias, *pre_weight, *pre_bias;     /* `features` elements each, or NULL */
+    const void* gate;                /* ceil(rows / rows_per_gate) x features, rows gate_stride apart, or NULL */
+    int64_t gate_stride, rows_per_gate;
+    float eps;                       /* >= 0 */
+    float branch_scale, residual_scale;
+    float dropout;                   /* p; 0: none */
+    uint64_t site;
+    const uint64_t* seed;
+} adasum_residual_norm_t;
+
+/*
+ *   x            device, rows x features of dtype, or NULL: no branch (h = residual_scale * residual)
+ *   residual     device, rows x features of stream_dtype, or NULL: 0 (not both NULL)
+ *   h            device, of stream_dtype; may be the residual itself; may be NULL if there is a pre norm
+ *   y            device, of dtype; may be x itself; not written without a pre norm
+ *   stats        device, 4 x rows floats: means and rstds of post, means and rstds of pre, for the gradients (those
+ *                of a norm that the block does not have are not written); NULL: not kept
+ */
+adasum_status_t adasum_residual_norm(const adasum_residual_norm_t* block, const void* x, int64_t x_stride,
+                                     const void* residual, int64_t residual_stride, void* h, int64_t h_stride, void* y,
+                                     int64_t y_stride, float* stats, void* stream);
+
+/*
+ * Its gradients.  x, h and stats as the forward call took and left them; grad_y and grad_h are the gradients that come
+ * back through y and through the residual stream (either may be NULL: zero).  Any output may be NULL (not wanted);
+ * grad_x may be grad_y itself, grad_residual may be grad_h itself.  x is needed for a post norm or the gate's gradient only.
+ * Gradients of the vectors are summed over the rows in fp32 in a fixed order; those of the norms are multiplied
+ * by `scale`, the gate's by gate_scale; with accumulate != 0 they are added to what is there.  With rows == 0 the norms'
+ * are zeros.
+ *   grad_gate    ceil(rows / rows_per_gate) x features, contiguous
+ *   workspace    device, adasum_residual_norm_grad_workspace_bytes(block) bytes, 256-byte aligned; contents on entry are
+ *                ignored; may be NULL if no vector's gradient is wanted.  The size does not depend on the rows
+ */
+typedef struct {
+    const void *x, *h, *grad_y, *grad_h;
+    const float* stats;
+    int64_t x_stride, h_stride, grad_y_stride, grad_h_stride;
+    void *grad_x, *grad_residual;
+    int64_t grad_x_stride, grad_residual_stride;
+    void *grad_post_weight, *grad_post_bias, *grad_pre_weight, *grad_pre_bias;
+    void* grad_gate;
+    adasum_dtype_t grad_dtype;       /* of the norms' vectors' gradients */
+    adasum_dtype_t gate_grad_dtype;
+    float scale, gate_scale;
+    int32_t accumulate;
+} adasum_residual_norm_grads_t;
+
+size_t adasum_residual_norm_grad_workspace_bytes(const adasum_residual_norm_t* block);
+adasum_status_t adasum_residual_norm_grad(const adasum_residual_norm_t* block, const adasum_residual_norm_grads_t* grads,
+                                          void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Matrices in 8-bit floating point.  A packed matrix holds e4m3 codes (OCP: 4 exponent and 3 mantissa bits, largest value 448) and a
+ * power of two, the step, for every 128 neighbouring columns of a row (adasum_fp8_pack: activations and gradients)
+ * or for every 128 x 128 block (adasum_fp8_pack_weight).  The step is the smallest power of two, 2^-126 at least, by
+ * which the largest magnitude is at most 448; a code is value / step rounded to nearest, ties to even.  A
+ * block that holds an Inf or NaN is kept as NaN: step byte 255 and codes 0.
+ *
+ * Layout: with W = 128 * ceil(columns / 128), first rows x W codes, row by row, zeros beyond the matrix; then for every
+ * block of 128 rows and every 128 columns (columns fastest) 512 step bytes (exponent + 127) as the tensor core
+ * reads them: that of row r at 16 * (r % 32) + 4 * (r % 128 / 32), four times.  Those of rows beyond the matrix are
+ * unspecified in the first form and equal to the others in the second.  16-byte aligned.
+ */
+size_t adasum_fp8_bytes(int64_t rows, int64_t columns);
+adasum_status_t adasum_fp8_pack(const void* x, int64_t x_stride, int64_t rows, int64_t columns, adasum_dtype_t dtype,
+                                void* packed, void* stream);
+adasum_status_t adasum_fp8_pack_weight(const void* w, int64_t w_stride, int64_t rows, int64_t columns,
+                                       adasum_dtype_t dtype, void* packed, void* stream);
+
+/* The values of a packed matrix (either form), in `dtype`. */
+adasum_status_t adasum_fp8_unpack(const void* packed, int64_t rows, int64_t columns, void* out, int64_t out_stride,
+                                  adasum_dtype_t dtype, void* stream);
+
+/*
+ * A linear layer of packed matrices, and the gradient of its input:
+ *
+ *     y[r][n]  = sum_k x[r][k] w[n][k] + bias[n]          x: rows x features, adasum_fp8_pack
+ *     dx[r][k] = sum_n dy[r][n] w[n][k]                   dy: rows x outputs, adasum_fp8_pack
+ *
+ * w is outputs x features, packed once by adasum_fp8_pack_weight for both.  Products are exact, sums are fp32, with one rounding
+ * to the stored type.  (The weight's gradient is adasum_checkpoint_weight_grad's.)
+ *
+ *   bias          device, `outputs` elements of bias_dtype, or NULL
+ *   y, dx         device, rows x outputs (rows x features) of out_dtype, rows out_stride apart
+ *   workspace     device, adasum_fp8_linear_workspace_bytes(rows, features, outputs) bytes (both calls), 256-byte
+ *                 aligned; contents on entry are ignored.  One that is large enough for many rows does for fewer
+ *   limits        rows, features, outputs <= 2^31 - 256 (ADASUM_ERR_ARG)
+ *
+ * With nothing to sum y is the bias and dx is 0.  A product that the device did not finish (a bounded wait ran out)
+ * leaves NaN; adasum_fp8_linear_status tells, synchronising `stream`, for the last call on the workspace.
+ */
+size_t adasum_fp8_linear_workspace_bytes(int64_t rows, int64_t features, int64_t outputs);
+adasum_status_t adasum_fp8_linear(const void* x, const void* w, int64_t rows, int64_t features, int64_t outputs,
+                                  const void* bias, adasum_dtype_t bias_dtype, void* y, int64_t y_stride,
+                                  adasum_dtype_t out_dtype, void* workspace, size_t workspace_bytes, void* stream);
+adasum_status_t adasum_fp8_linear_grad(const void* dy, const void* w, int64_t rows, int64_t features, int64_t outputs,
+                                       void* dx, int64_t dx_stride, adasum_dtype_t out_dtype, void* workspace,
+                                       size_t workspace_bytes, void* stream);
+adasum_status_t adasum_fp8_linear_status(const void* workspace, void* stream);
+
 /* Static, human-readable name of a status code. */
 const char* adasum_status_string(adasum_status_t status);
 
@@ -565,6 +721,12 @@ const char* adasum_last_error(void);
 #define ADASUM_KERNEL_CHECKPOINT_LOAD 11
 #define ADASUM_KERNEL_ACT_GRAD 12
 #define ADASUM_KERNEL_WEIGHT_GRAD 13     /* level 0: gradients re-laid for the product, 1: the product, 2: sums joined */
+#define ADASUM_KERNEL_DROPOUT 14
+#define ADASUM_KERNEL_RESIDUAL_NORM 15
+#define ADASUM_KERNEL_RESIDUAL_NORM_GRAD 16  /* level 0: gradients, 1: vectors' sums joined */
+#define ADASUM_KERNEL_FP8_PACK 17
+#define ADASUM_KERNEL_FP8_UNPACK 18
+#define ADASUM_KERNEL_FP8_LINEAR 19      /* level 0: the product, 1: sums joined */
 
 typedef struct {
     int32_t kernel;

@@ -15,6 +15,9 @@ _BINDING_NAMES = (
     "adasum_checkpoint_bytes", "adasum_checkpoint_save", "adasum_checkpoint_load", "adasum_checkpoint_act_grad",
     "adasum_checkpoint_weight_grad", "adasum_checkpoint_weight_grad_workspace_bytes",
     "adasum_checkpoint_weight_grad_status", "adasum_checkpoint_weight_grad_selftest",
+    "adasum_dropout", "adasum_residual_norm", "adasum_residual_norm_grad", "adasum_residual_norm_grad_workspace_bytes",
+    "adasum_fp8_bytes", "adasum_fp8_pack", "adasum_fp8_pack_weight", "adasum_fp8_unpack", "adasum_fp8_linear",
+    "adasum_fp8_linear_grad", "adasum_fp8_linear_workspace_bytes", "adasum_fp8_linear_status",
 )
 
 

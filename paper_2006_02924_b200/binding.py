@@ -361,7 +361,8 @@ class _LaunchRecord(ctypes.Structure):
 
 KERNEL_NAMES = {0: "gram_partial", 1: "tree_weights", 2: "weighted_sum", 3: "convert", 4: "fused_small",
                 5: "wsum_gram", 6: "short_tensors", 7: "embedding", 8: "embedding_sort", 9: "embedding_sum",
-                10: "checkpoint_save", 11: "checkpoint_load", 12: "act_grad", 13: "weight_grad"}
+                10: "checkpoint_save", 11: "checkpoint_load", 12: "act_grad", 13: "weight_grad", 14: "dropout",
+                15: "residual_norm", 16: "residual_norm_grad", 17: "fp8_pack", 18: "fp8_unpack", 19: "fp8_linear"}
 
 _lib.adasum_profile_enable.restype = ctypes.c_int
 _lib.adasum_profile_enable.argtypes = [ctypes.c_int32]
@@ -732,3 +733,383 @@ def adasum_checkpoint_weight_grad_selftest(hand_over: str, checkpoint, grad_out,
         workspace.numel() * workspace.element_size(), _stream_handle(None), ADASUM_HAND_OVER[hand_over])
     if status != ADASUM_OK:
         raise AdasumError(status)
+
+
+# ---- around the linear layers of a residual block ----------------------------------------------------
+
+ADASUM_NORM = {"none": 0, "rms": 1, "layer": 2}
+ADASUM_NORM_MAX_FEATURES = 32768
+ADASUM_FP8_BLOCK = 128
+
+
+class _ResidualNorm(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("features", _i64), ("dtype", _i32), ("stream_dtype", _i32), ("param_dtype", _i32),
+                ("gate_dtype", _i32), ("post_norm", _i32), ("pre_norm", _i32), ("post_weight", _vp), ("post_bias", _vp),
+                ("pre_weight", _vp), ("pre_bias", _vp), ("gate", _vp), ("gate_stride", _i64), ("rows_per_gate", _i64),
+                ("eps", _f32), ("branch_scale", _f32), ("residual_scale", _f32), ("dropout", _f32),
+                ("site", ctypes.c_uint64), ("seed", _vp)]
+
+
+class _ResidualNormGrads(ctypes.Structure):
+    _fields_ = [("x", _vp), ("h", _vp), ("grad_y", _vp), ("grad_h", _vp), ("stats", _vp), ("x_stride", _i64),
+                ("h_stride", _i64), ("grad_y_stride", _i64), ("grad_h_stride", _i64), ("grad_x", _vp),
+                ("grad_residual", _vp), ("grad_x_stride", _i64), ("grad_residual_stride", _i64),
+                ("grad_post_weight", _vp), ("grad_post_bias", _vp), ("grad_pre_weight", _vp), ("grad_pre_bias", _vp),
+                ("grad_gate", _vp), ("grad_dtype", _i32), ("gate_grad_dtype", _i32), ("scale", _f32),
+                ("gate_scale", _f32), ("accumulate", _i32)]
+
+
+_u64 = ctypes.c_uint64
+_lib.adasum_dropout.restype = ctypes.c_int
+_lib.adasum_dropout.argtypes = [_vp, _i64, _i64, _i64, ctypes.c_int, _vp, _i64, _f32, _vp, _u64, _vp, _i64, _vp]
+_lib.adasum_residual_norm.restype = ctypes.c_int
+_lib.adasum_residual_norm.argtypes = [ctypes.POINTER(_ResidualNorm), _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp]
+_lib.adasum_residual_norm_grad_workspace_bytes.restype = ctypes.c_size_t
+_lib.adasum_residual_norm_grad_workspace_bytes.argtypes = [ctypes.POINTER(_ResidualNorm)]
+_lib.adasum_residual_norm_grad.restype = ctypes.c_int
+_lib.adasum_residual_norm_grad.argtypes = [ctypes.POINTER(_ResidualNorm), ctypes.POINTER(_ResidualNormGrads), _vp,
+                                           ctypes.c_size_t, _vp]
+_lib.adasum_fp8_bytes.restype = ctypes.c_size_t
+_lib.adasum_fp8_bytes.argtypes = [_i64, _i64]
+for _name in ("adasum_fp8_pack", "adasum_fp8_pack_weight"):
+    getattr(_lib, _name).restype = ctypes.c_int
+    getattr(_lib, _name).argtypes = [_vp, _i64, _i64, _i64, ctypes.c_int, _vp, _vp]
+_lib.adasum_fp8_unpack.restype = ctypes.c_int
+_lib.adasum_fp8_unpack.argtypes = [_vp, _i64, _i64, _vp, _i64, ctypes.c_int, _vp]
+_lib.adasum_fp8_linear_workspace_bytes.restype = ctypes.c_size_t
+_lib.adasum_fp8_linear_workspace_bytes.argtypes = [_i64, _i64, _i64]
+_lib.adasum_fp8_linear.restype = ctypes.c_int
+_lib.adasum_fp8_linear.argtypes = [_vp, _vp, _i64, _i64, _i64, _vp, ctypes.c_int, _vp, _i64, ctypes.c_int, _vp,
+                                   ctypes.c_size_t, _vp]
+_lib.adasum_fp8_linear_grad.restype = ctypes.c_int
+_lib.adasum_fp8_linear_grad.argtypes = [_vp, _vp, _i64, _i64, _i64, _vp, _i64, ctypes.c_int, _vp, ctypes.c_size_t, _vp]
+_lib.adasum_fp8_linear_status.restype = ctypes.c_int
+_lib.adasum_fp8_linear_status.argtypes = [_vp, _vp]
+
+
+def _seed(device: int, seed, p: float):
+    """Checks a dropout's seed; returns its address (None where nothing is dropped and no seed is given)."""
+    if seed is None:
+        if p > 0.0:
+            raise ValueError("dropout needs a seed: a CUDA tensor that holds one 64-bit integer")
+        return None
+    if not seed.is_cuda or seed.dtype not in (torch.int64, torch.uint64) or seed.numel() < 1:
+        raise TypeError("seed must be a CUDA tensor that holds one 64-bit integer")
+    _same_device(device, seed)
+    return seed.data_ptr()
+
+
+def adasum_dropout(x, p: float, seed, site: int = 0, residual=None, out=None, stream=None):
+    """``adasum_dropout`` of the C ABI: ``[residual +] dropout(x)``.  ``seed`` is a CUDA tensor with one 64-bit integer,
+    read when the kernel runs; ``site`` tells the dropouts of one step apart.  The gradient is the same call on
+    the gradient, without ``residual``.  ``out`` may be ``x`` or ``residual`` itself."""
+    stride = _matrix("x", x)
+    rows, features = x.shape
+    device = x.get_device()
+    residual_ptr, residual_stride = None, 0
+    if residual is not None:
+        residual_stride = _matrix("residual", residual, rows, features)
+        if residual.dtype != x.dtype:
+            raise TypeError("residual must have the type of x")
+        residual_ptr = residual.data_ptr()
+    if out is None:
+        out, out_stride = _allocate(x, stream, (rows, features), x.dtype), features
+    else:
+        out_stride = _matrix("out", out, rows, features)
+        if out.dtype != x.dtype:
+            raise TypeError("out must have the type of x")
+    _same_device(device, residual, out)
+    _operator_call(device, stream, _lib.adasum_dropout, x.data_ptr(), stride, rows, features, _operator_dtype(x.dtype),
+                   residual_ptr, residual_stride, p, _seed(device, seed, p), site, out.data_ptr(), out_stride)
+    return out
+
+
+def _vector(name: str, t, features: int, dtype, device: int):
+    """Checks a vector of a norm; returns its address."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must have the type of the norms' other vectors")
+    if t.numel() != features or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous and have {features} elements")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, not on cuda:{device}")
+    return t.data_ptr()
+
+
+def _residual_norm_block(rows, features, dtype, stream_dtype, device, post_norm, post_weight, post_bias, pre_norm,
+                         pre_weight, pre_bias, eps, gate, rows_per_gate, branch_scale, residual_scale, dropout, seed,
+                         site):
+    """The C description of a joint, and the rows of its gate."""
+    param = next((t.dtype for t in (post_weight, post_bias, pre_weight, pre_bias) if t is not None), torch.float32)
+    gate_ptr, gate_stride, gate_dtype, gate_rows = None, 0, 0, 0
+    if gate is not None:
+        if gate.dim() == 1:
+            gate = gate.view(1, -1)
+        gate_rows = gate.shape[0]
+        gate_stride = _matrix("gate", gate, None, features)
+        if rows_per_gate is None:
+            rows_per_gate = max(-(-rows // max(gate_rows, 1)), 1)
+        if rows_per_gate < 1 or (rows > 0 and gate_rows != -(-rows // rows_per_gate)):
+            raise ValueError(f"{rows} rows, {rows_per_gate} per row of the gate, need a gate of "
+                             f"{-(-rows // max(rows_per_gate, 1))} rows, not {gate_rows}")
+        _same_device(device, gate)
+        gate_ptr, gate_dtype = gate.data_ptr(), _operator_dtype(gate.dtype)
+    block = _ResidualNorm(rows, features, _operator_dtype(dtype), _operator_dtype(stream_dtype), _operator_dtype(param),
+                          gate_dtype, ADASUM_NORM[post_norm], ADASUM_NORM[pre_norm],
+                          _vector("post_weight", post_weight, features, param, device),
+                          _vector("post_bias", post_bias, features, param, device),
+                          _vector("pre_weight", pre_weight, features, param, device),
+                          _vector("pre_bias", pre_bias, features, param, device), gate_ptr, gate_stride,
+                          rows_per_gate or 0, eps, branch_scale, residual_scale, dropout, site,
+                          _seed(device, seed, dropout))
+    return block, gate_rows
+
+
+def adasum_residual_norm(x, residual, post_norm: str = "none", post_weight=None, post_bias=None, pre_norm: str = "rms",
+                         pre_weight=None, pre_bias=None, eps: float = 1e-5, gate=None, rows_per_gate=None,
+                         branch_scale: float = 1.0, residual_scale: float = 1.0, dropout: float = 0.0, seed=None,
+                         site: int = 0, h=None, y=None, stats=None, out_dtype=None, stream_dtype=None,
+                         want_h: bool = True, want_stats: bool = True, stream=None):
+    """``adasum_residual_norm`` of the C ABI: ``h = residual_scale * residual + branch_scale * gate *
+    dropout(post(x))`` and ``y = pre(h)``.  ``x`` or ``residual`` may be None.  ``gate`` is one row for all rows of ``x``
+    or one row per ``rows_per_gate``.  ``y`` is of ``x``'s type (``out_dtype`` without one), ``h`` of ``residual``'s
+    (``stream_dtype`` without one).  Returns ``(h, y, stats)``; ``h`` and ``stats`` are None if not wanted, ``y`` without
+    a ``pre_norm``.  ``h`` may be ``residual`` itself, ``y`` may be ``x`` itself."""
+    like = x if x is not None else residual
+    if like is None:
+        raise ValueError("x and residual are both missing")
+    rows, features = like.shape
+    device = like.get_device()
+    x_ptr, x_stride, residual_ptr, residual_stride = None, 0, None, 0
+    if x is not None:
+        x_stride = _matrix("x", x)
+        x_ptr = x.data_ptr()
+    if residual is not None:
+        residual_stride = _matrix("residual", residual, rows, features)
+        residual_ptr = residual.data_ptr()
+    dtype = x.dtype if x is not None else y.dtype if y is not None else out_dtype or residual.dtype
+    of_stream = residual.dtype if residual is not None else h.dtype if h is not None else stream_dtype or dtype
+    block, _ = _residual_norm_block(rows, features, dtype, of_stream, device, post_norm, post_weight, post_bias, pre_norm,
+                                    pre_weight, pre_bias, eps, gate, rows_per_gate, branch_scale, residual_scale, dropout,
+                                    seed, site)
+    h_stride = y_stride = features
+    if h is not None:
+        h_stride = _matrix("h", h, rows, features)
+        if h.dtype != of_stream:
+            raise TypeError("h must have the type of residual")
+    elif want_h:
+        h = _allocate(like, stream, (rows, features), of_stream)
+    if pre_norm == "none":
+        y = None
+    elif y is None:
+        y = _allocate(like, stream, (rows, features), dtype)
+    else:
+        y_stride = _matrix("y", y, rows, features)
+        if y.dtype != dtype:
+            raise TypeError("y must have the type of x")
+    if stats is not None:
+        if stats.dtype != torch.float32 or not stats.is_contiguous() or stats.numel() != 4 * rows:
+            raise ValueError(f"stats must be contiguous fp32 of 4 x {rows} elements")
+    elif want_stats:
+        stats = _allocate(like, stream, (4, rows), torch.float32)
+    _same_device(device, residual, h, y, stats)
+    _operator_call(device, stream, _lib.adasum_residual_norm, block, x_ptr, x_stride, residual_ptr, residual_stride,
+                   None if h is None else h.data_ptr(), h_stride, None if y is None else y.data_ptr(), y_stride,
+                   None if stats is None else stats.data_ptr())
+    return h, y, stats
+
+
+def adasum_residual_norm_grad_workspace_bytes(features: int, gate: bool = False) -> int:
+    """Bytes for any number of rows."""
+    block = _ResidualNorm()
+    block.features = int(features)
+    block.gate = 256 if gate else None       # only whether there is one matters
+    return int(_lib.adasum_residual_norm_grad_workspace_bytes(block))
+
+
+def adasum_residual_norm_grad(x, h, stats, grad_y, grad_h, post_norm: str = "none", post_weight=None, post_bias=None,
+                              pre_norm: str = "rms", pre_weight=None, pre_bias=None, eps: float = 1e-5, gate=None,
+                              rows_per_gate=None, branch_scale: float = 1.0, residual_scale: float = 1.0,
+                              dropout: float = 0.0, seed=None, site: int = 0, grad_x=None, grad_residual=None,
+                              want_x: bool = True, want_residual: bool = True, grad_post_weight=None,
+                              grad_post_bias=None, grad_pre_weight=None, grad_pre_bias=None, grad_gate=None,
+                              scale: float = 1.0, gate_scale: float = 1.0, accumulate: bool = False, out_dtype=None,
+                              workspace=None, stream=None):
+    """``adasum_residual_norm_grad`` of the C ABI, with the arguments of the forward call and what it left (``h``,
+    ``stats``).  ``grad_y`` and ``grad_h`` are the gradients of its results (None: zero).  Gradients of vectors are
+    written where they are given (``grad_gate``: contiguous, of the gate's size), multiplied by ``scale`` (``gate_scale``).
+    Returns ``(grad_x, grad_residual)``, allocated here unless given or not wanted.  ``x`` may be None where there is
+    neither a post norm nor a gate's gradient; ``out_dtype`` is then the type of ``grad_x`` unless ``grad_y`` has one."""
+    like = next((t for t in (grad_y, grad_h) if t is not None), None)
+    if like is None:
+        raise ValueError("grad_y and grad_h are both missing")
+    rows, features = like.shape
+    device = like.get_device()
+    if grad_y is not None and pre_norm == "none":
+        raise ValueError("grad_y without a pre_norm")
+    dtype = next((t.dtype for t in (x, grad_y, grad_x) if t is not None), out_dtype or like.dtype)
+    of_stream = next((t.dtype for t in (h, grad_h, grad_residual) if t is not None), dtype)
+
+    def place(name, t, wanted_dtype):
+        if t is None:
+            return None, 0
+        stride = _matrix(name, t, rows, features)
+        if t.dtype != wanted_dtype:
+            raise TypeError(f"{name} must be of {wanted_dtype}")
+        return t.data_ptr(), stride
+
+    block, gate_rows = _residual_norm_block(rows, features, dtype, of_stream, device, post_norm, post_weight, post_bias,
+                                            pre_norm, pre_weight, pre_bias, eps, gate, rows_per_gate, branch_scale,
+                                            residual_scale, dropout, seed, site)
+    if grad_x is None and want_x:
+        grad_x = _allocate(like, stream, (rows, features), dtype)
+    if grad_residual is None and want_residual:
+        grad_residual = _allocate(like, stream, (rows, features), of_stream)
+    x_ptr, x_stride = place("x", x, dtype)
+    h_ptr, h_stride = place("h", h, of_stream)
+    grad_y_ptr, grad_y_stride = place("grad_y", grad_y, dtype)
+    grad_h_ptr, grad_h_stride = place("grad_h", grad_h, of_stream)
+    grad_x_ptr, grad_x_stride = place("grad_x", grad_x, dtype)
+    grad_residual_ptr, grad_residual_stride = place("grad_residual", grad_residual, of_stream)
+    stats_ptr = None
+    if stats is not None:
+        if stats.dtype != torch.float32 or not stats.is_contiguous() or stats.numel() != 4 * rows:
+            raise ValueError(f"stats must be contiguous fp32 of 4 x {rows} elements")
+        stats_ptr = stats.data_ptr()
+    vectors = (grad_post_weight, grad_post_bias, grad_pre_weight, grad_pre_bias)
+    grad_dtype = next((t.dtype for t in vectors if t is not None), torch.float32)
+    gate_ptr, gate_code = None, 0
+    if grad_gate is not None:
+        if grad_gate.numel() != gate_rows * features or not grad_gate.is_contiguous():
+            raise ValueError(f"grad_gate must be contiguous and have {gate_rows} x {features} elements")
+        gate_ptr, gate_code = grad_gate.data_ptr(), _operator_dtype(grad_gate.dtype)
+        if rows == 0 and not accumulate:     # an empty sum
+            grad_gate.zero_()
+    workspace_ptr, workspace_bytes = None, 0
+    if grad_gate is not None or any(t is not None for t in vectors):
+        workspace = _operator_workspace(like, stream, workspace, _lib.adasum_residual_norm_grad_workspace_bytes(block))
+        workspace_ptr, workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        _same_device(device, workspace)
+    _same_device(device, x, h, stats, grad_y, grad_h, grad_x, grad_residual, grad_gate)
+    grads = _ResidualNormGrads(x_ptr, h_ptr, grad_y_ptr, grad_h_ptr, stats_ptr, x_stride, h_stride, grad_y_stride,
+                               grad_h_stride, grad_x_ptr, grad_residual_ptr, grad_x_stride, grad_residual_stride,
+                               _vector("grad_post_weight", grad_post_weight, features, grad_dtype, device),
+                               _vector("grad_post_bias", grad_post_bias, features, grad_dtype, device),
+                               _vector("grad_pre_weight", grad_pre_weight, features, grad_dtype, device),
+                               _vector("grad_pre_bias", grad_pre_bias, features, grad_dtype, device), gate_ptr,
+                               _operator_dtype(grad_dtype), gate_code, scale, gate_scale, accumulate)
+    _operator_call(device, stream, _lib.adasum_residual_norm_grad, block, grads, workspace_ptr, workspace_bytes)
+    return grad_x, grad_residual
+
+
+def adasum_fp8_bytes(rows: int, columns: int) -> int:
+    return int(_lib.adasum_fp8_bytes(int(rows), int(columns)))
+
+
+def _fp8_size(rows: int, columns: int) -> int:
+    blocks = -(-columns // ADASUM_FP8_BLOCK)
+    return blocks * (rows * ADASUM_FP8_BLOCK + -(-rows // ADASUM_FP8_BLOCK) * 512)
+
+
+def _packed(name: str, packed, rows: int, columns: int, device: int):
+    """Checks a packed matrix; returns its address."""
+    if packed.dtype != torch.uint8 or not packed.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous tensor of uint8")
+    need = _fp8_size(rows, columns)
+    if packed.numel() < need:
+        raise ValueError(f"{name} has {packed.numel()} bytes, {rows} x {columns} needs {need}")
+    if packed.get_device() != device:
+        raise ValueError(f"{name} is on {packed.device}, not on cuda:{device}")
+    return packed.data_ptr()
+
+
+def _fp8_pack(function, x, packed, stream):
+    stride = _matrix("x", x)
+    rows, columns = x.shape
+    device = x.get_device()
+    if packed is None:
+        packed = _allocate(x, stream, (_fp8_size(rows, columns),), torch.uint8)
+    _operator_call(device, stream, function, x.data_ptr(), stride, rows, columns, _operator_dtype(x.dtype),
+                   _packed("packed", packed, rows, columns, device))
+    return packed
+
+
+def adasum_fp8_pack(x, packed=None, stream=None):
+    """``adasum_fp8_pack`` of the C ABI: activations or gradients in 8 bits, a step for 128 columns of a row."""
+    return _fp8_pack(_lib.adasum_fp8_pack, x, packed, stream)
+
+
+def adasum_fp8_pack_weight(w, packed=None, stream=None):
+    """``adasum_fp8_pack_weight`` of the C ABI: a weight matrix ``[outputs, features]`` in 8 bits, a step for 128 x 128
+    values.  Both ``adasum_fp8_linear`` and ``adasum_fp8_linear_grad`` take it."""
+    return _fp8_pack(_lib.adasum_fp8_pack_weight, w, packed, stream)
+
+
+def adasum_fp8_unpack(packed, rows: int, columns: int, dtype=None, out=None, stream=None):
+    """``adasum_fp8_unpack`` of the C ABI: the values, in ``dtype`` (fp32 by default) or ``out``."""
+    if out is None:
+        if not packed.is_cuda:
+            raise TypeError("packed must be a CUDA tensor")
+        out, out_stride = _allocate(packed, stream, (rows, columns), dtype or torch.float32), columns
+    else:
+        out_stride = _matrix("out", out, rows, columns)
+    device = out.get_device()
+    _operator_call(device, stream, _lib.adasum_fp8_unpack, _packed("packed", packed, rows, columns, device), rows, columns,
+                   out.data_ptr(), out_stride, _operator_dtype(out.dtype))
+    return out
+
+
+def adasum_fp8_linear_workspace_bytes(rows: int, features: int, outputs: int) -> int:
+    return int(_lib.adasum_fp8_linear_workspace_bytes(int(rows), int(features), int(outputs)))
+
+
+def adasum_fp8_linear(x, w, rows: int, features: int, outputs: int, bias=None, out=None, out_dtype=None, workspace=None,
+                      stream=None):
+    """``adasum_fp8_linear`` of the C ABI: ``x w^T + bias`` of ``x`` (``adasum_fp8_pack`` of ``[rows, features]``) and ``w``
+    (``adasum_fp8_pack_weight`` of ``[outputs, features]``); bf16 unless ``out_dtype`` or ``out`` says otherwise."""
+    if not x.is_cuda:
+        raise TypeError("x must be a CUDA tensor")
+    device = x.get_device()
+    if out is None:
+        out, out_stride = _allocate(x, stream, (rows, outputs), out_dtype or torch.bfloat16), outputs
+    else:
+        out_stride = _matrix("out", out, rows, outputs)
+    bias_ptr, bias_code = None, 0
+    if bias is not None:
+        if not bias.is_contiguous() or bias.numel() != outputs:
+            raise ValueError(f"bias must be contiguous and have {outputs} elements")
+        bias_ptr, bias_code = bias.data_ptr(), _operator_dtype(bias.dtype)
+    workspace = _operator_workspace(x, stream, workspace, _lib.adasum_fp8_linear_workspace_bytes(rows, features, outputs))
+    _same_device(device, out, bias, workspace)
+    _operator_call(device, stream, _lib.adasum_fp8_linear, _packed("x", x, rows, features, device),
+                   _packed("w", w, outputs, features, device), rows, features, outputs, bias_ptr, bias_code, out.data_ptr(),
+                   out_stride, _operator_dtype(out.dtype), workspace.data_ptr(),
+                   workspace.numel() * workspace.element_size())
+    return out
+
+
+def adasum_fp8_linear_grad(grad_out, w, rows: int, features: int, outputs: int, out=None, out_dtype=None, workspace=None,
+                           stream=None):
+    """``adasum_fp8_linear_grad`` of the C ABI: ``grad_out w`` of ``grad_out`` (``adasum_fp8_pack`` of ``[rows, outputs]``)
+    and the forward call's ``w``."""
+    if not grad_out.is_cuda:
+        raise TypeError("grad_out must be a CUDA tensor")
+    device = grad_out.get_device()
+    if out is None:
+        out, out_stride = _allocate(grad_out, stream, (rows, features), out_dtype or torch.bfloat16), features
+    else:
+        out_stride = _matrix("out", out, rows, features)
+    workspace = _operator_workspace(grad_out, stream, workspace,
+                                    _lib.adasum_fp8_linear_workspace_bytes(rows, features, outputs))
+    _same_device(device, out, workspace)
+    _operator_call(device, stream, _lib.adasum_fp8_linear_grad, _packed("grad_out", grad_out, rows, outputs, device),
+                   _packed("w", w, outputs, features, device), rows, features, outputs, out.data_ptr(), out_stride,
+                   _operator_dtype(out.dtype), workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    return out
+
+
+def adasum_fp8_linear_status(workspace, stream=None) -> int:
+    """``adasum_fp8_linear_status`` of the C ABI: 0, or 7 (ADASUM_ERR_TIMEOUT) if a bounded wait of the last product on
+    ``workspace`` ran out.  Synchronises the stream."""
+    return int(_lib.adasum_fp8_linear_status(workspace.data_ptr(), _stream_handle(stream)))

@@ -331,17 +331,6 @@ adasum_status_t check_checkpoint(const void* checkpoint, int64_t rows, int64_t f
     return ADASUM_OK;
 }
 
-adasum_status_t check_matrix(const char* name, const void* p, int64_t stride, int64_t features, adasum_dtype_t dtype)
-{
-    if (!p)
-        return fail(ADASUM_ERR_NULL, "%s is NULL", name);
-    if (!aligned_to(p, operator_bytes(dtype)))
-        return fail(ADASUM_ERR_ARG, "%s is not aligned to its element size", name);
-    if (!stride_ok(stride, features))
-        return fail(ADASUM_ERR_ARG, "stride %lld of %s is shorter than a row or out of range", (long long)stride, name);
-    return ADASUM_OK;
-}
-
 // Calls f with the constant of the run-time activation, or of a truth value.
 template <int N>
 struct Constant { static constexpr int value = N; };

@@ -1,0 +1,245 @@
+// Matrices to 8-bit floating point and back.  One pass over a matrix each, bound by HBM traffic.
+#include "adasum_fp8.cuh"
+#include "adasum_vectors.cuh"
+
+namespace adasum {
+namespace {
+
+constexpr int kPackRows = 2;               // vectors per thread, in as many rows
+constexpr int kUnpackRows = 2;
+constexpr int kWeightThreads = 256;
+constexpr int kWeightRows = kFp8Block * kFp8Block / 8 / kWeightThreads;      // vectors per thread, in as many rows
+
+__device__ __forceinline__ uint2 codes_of(const Eight& x, uint32_t byte)
+{
+    const Pair inv = both(byte == 255u ? 0.0f : __uint_as_float((254u - byte) << 23));
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = values_of(x.p[i] * inv);
+        y[2 * i] = byte == 255u ? 0.0f : f.x;
+        y[2 * i + 1] = byte == 255u ? 0.0f : f.y;
+    }
+    return make_uint2(fp8_encode(y[0], y[1], y[2], y[3]), fp8_encode(y[4], y[5], y[6], y[7]));
+}
+
+// Sixteen neighbouring lanes hold the 128 columns of a block: the largest magnitude is four shuffles away.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kStripThreads)
+fp8_pack_kernel(const __grid_constant__ Strips s, const T* x, int64_t x_stride, uint8_t* codes, uint8_t* steps)
+{
+    const Place p = place_of<kPackRows>(s);
+    Raw<T> raw[kPackRows];
+#pragma unroll
+    for (int u = 0; u < kPackRows; ++u) {
+        const int64_t row = p.row0 + u * p.step;
+        raw[u] = load_vector<VEC>(x + row * x_stride + p.column, row < s.rows ? p.count : 0);
+    }
+#pragma unroll
+    for (int u = 0; u < kPackRows; ++u) {
+        const int64_t row = p.row0 + u * p.step;
+        uint32_t top = largest(raw[u]);
+#pragma unroll
+        for (int step = 1; step < 16; step *= 2)
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, step));
+        const uint32_t byte = fp8_step_byte(top);
+        if (p.inside && row < s.rows) {
+            *reinterpret_cast<uint2*>(codes + row * (int64_t)s.per_row * 8 + p.column) = codes_of(decode(raw[u]), byte);
+            if ((p.column & (kFp8Block - 1)) == 0)
+                *reinterpret_cast<uint32_t*>(steps + fp8_step_at(row, p.column / kFp8Block, s.per_row / 16)) = byte * 0x01010101u;
+        }
+    }
+}
+
+// One block of 128 x 128 per thread block; sixteen threads per row.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kWeightThreads)
+fp8_pack_weight_kernel(const T* w, int64_t w_stride, int64_t rows, int64_t columns, uint32_t column_blocks, uint8_t* codes,
+                       uint8_t* steps)
+{
+    __shared__ uint32_t warp_top[kWeightThreads / 32];
+    const uint32_t row_block = blockIdx.x / column_blocks, column_block = blockIdx.x - row_block * column_blocks;
+    const int64_t column = (int64_t)column_block * kFp8Block + (threadIdx.x & 15) * 8;
+    const int64_t row0 = (int64_t)row_block * kFp8Block + (threadIdx.x >> 4);
+    const int count = (int)max((int64_t)0, min((int64_t)8, columns - column));
+    Raw<T> raw[kWeightRows];
+    uint32_t top = 0;
+#pragma unroll
+    for (int u = 0; u < kWeightRows; ++u) {
+        const int64_t row = row0 + u * (kWeightThreads / 16);
+        raw[u] = load_vector<VEC>(w + row * w_stride + column, row < rows ? count : 0);
+    }
+#pragma unroll
+    for (int u = 0; u < kWeightRows; ++u)
+        top = max(top, largest(raw[u]));
+    top = __reduce_max_sync(0xffffffffu, top);
+    if ((threadIdx.x & 31) == 0)
+        warp_top[threadIdx.x >> 5] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kWeightThreads / 32; ++i)
+        top = max(top, warp_top[i]);
+    const uint32_t byte = fp8_step_byte(top);
+#pragma unroll
+    for (int u = 0; u < kWeightRows; ++u) {
+        const int64_t row = row0 + u * (kWeightThreads / 16);
+        if (row < rows)
+            *reinterpret_cast<uint2*>(codes + row * (int64_t)column_blocks * kFp8Block + column) = codes_of(decode(raw[u]), byte);
+    }
+    if (threadIdx.x < kFp8StepBytes / 4)
+        reinterpret_cast<uint32_t*>(steps + (int64_t)blockIdx.x * kFp8StepBytes)[threadIdx.x] = byte * 0x01010101u;
+}
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kStripThreads)
+fp8_unpack_kernel(const __grid_constant__ Strips s, const uint8_t* codes, const uint8_t* steps, int64_t width, T* out,
+                  int64_t out_stride)
+{
+    const Place p = place_of<kUnpackRows>(s);
+    if (p.count <= 0)
+        return;
+    uint2 packed[kUnpackRows];
+    uint32_t byte[kUnpackRows];
+#pragma unroll
+    for (int u = 0; u < kUnpackRows; ++u) {
+        const int64_t row = p.row0 + u * p.step;
+        if (row < s.rows) {
+            packed[u] = *reinterpret_cast<const uint2*>(codes + row * width + p.column);
+            byte[u] = steps[fp8_step_at(row, p.column / kFp8Block, width / kFp8Block)];
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kUnpackRows; ++u) {
+        const int64_t row = p.row0 + u * p.step;
+        if (row < s.rows) {
+            const float step = fp8_step_value(byte[u]);
+            float a[4], b[4];
+            fp8_decode(packed[u].x, a);
+            fp8_decode(packed[u].y, b);
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                y[i] = a[i] * step;
+                y[4 + i] = b[i] * step;
+            }
+            store_values<VEC>(out + row * out_stride + p.column, p.count, y);
+        }
+    }
+}
+
+// ---- host --------------------------------------------------------------------------------------------
+
+adasum_status_t check_packed(const void* packed, int64_t rows, int64_t columns, adasum_dtype_t dtype)
+{
+    if (!extent_ok(rows) || !extent_ok(columns))
+        return fail(ADASUM_ERR_ARG, "rows = %lld, columns = %lld out of range", (long long)rows, (long long)columns);
+    if (!operator_dtype(dtype))
+        return fail(ADASUM_ERR_DTYPE, "dtype %d is not fp32, fp16 or bf16", (int)dtype);
+    if (rows == 0 || columns == 0)
+        return ADASUM_OK;
+    if (!packed)
+        return fail(ADASUM_ERR_NULL, "packed is NULL");
+    if (!aligned_to(packed, 16))
+        return fail(ADASUM_ERR_ARG, "packed is not 16-byte aligned");
+    return ADASUM_OK;
+}
+
+adasum_status_t pack(const void* x, int64_t x_stride, int64_t rows, int64_t columns, adasum_dtype_t dtype, void* packed,
+                     bool weight, void* stream_ptr)
+{
+    clear_error();
+    adasum_status_t status = check_packed(packed, rows, columns, dtype);
+    if (status != ADASUM_OK || rows == 0 || columns == 0)
+        return status;
+    if ((status = check_matrix("the matrix", x, x_stride, columns, dtype)) != ADASUM_OK)
+        return status;
+    const int64_t eb = operator_bytes(dtype), width = fp8_width(columns);
+    if (spans_overlap(x, matrix_span(rows, columns, x_stride, eb), packed, fp8_bytes(rows, columns)))
+        return fail(ADASUM_ERR_ARG, "packed overlaps the matrix");
+    const bool vec = columns % 8 == 0 && rows_aligned(x, x_stride, eb);
+    uint8_t* codes = static_cast<uint8_t*>(packed);
+    uint8_t* steps = codes + rows * width;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+    Strips s;
+    unsigned blocks = 0;
+    if (weight) {
+        const int64_t n = fp8_blocks(rows) * fp8_blocks(columns);
+        if (n > 0x7fffffff)
+            return fail(ADASUM_ERR_ARG, "%lld x %lld is too large", (long long)rows, (long long)columns);
+        blocks = (unsigned)n;
+    } else if (!plan_strips(rows, columns, width / 8, kPackRows, &s, &blocks)) {
+        return fail(ADASUM_ERR_ARG, "%lld x %lld is too large", (long long)rows, (long long)columns);
+    }
+    profile_mark(stream, -1, 0, 0, true);
+    with_type(dtype, [&](auto t) {
+        using T = decltype(t);
+        if (weight) {
+            auto* kernel = vec ? fp8_pack_weight_kernel<T, true> : fp8_pack_weight_kernel<T, false>;
+            kernel<<<blocks, kWeightThreads, 0, stream>>>(static_cast<const T*>(x), x_stride, rows, columns,
+                                                          (uint32_t)fp8_blocks(columns), codes, steps);
+        } else {
+            auto* kernel = vec ? fp8_pack_kernel<T, true> : fp8_pack_kernel<T, false>;
+            kernel<<<blocks, kStripThreads, 0, stream>>>(s, static_cast<const T*>(x), x_stride, codes, steps);
+        }
+    });
+    ADASUM_CUDA_CHECK(cudaGetLastError());
+    profile_mark(stream, ADASUM_KERNEL_FP8_PACK, 0, 0, false);
+    return ADASUM_OK;
+}
+
+}  // namespace
+}  // namespace adasum
+
+extern "C" {
+
+size_t adasum_fp8_bytes(int64_t rows, int64_t columns)
+{
+    using namespace adasum;
+    if (!extent_ok(rows) || !extent_ok(columns))
+        return 0;
+    return fp8_bytes(rows, columns);
+}
+
+adasum_status_t adasum_fp8_pack(const void* x, int64_t x_stride, int64_t rows, int64_t columns, adasum_dtype_t dtype,
+                                void* packed, void* stream_ptr)
+{
+    return adasum::pack(x, x_stride, rows, columns, dtype, packed, false, stream_ptr);
+}
+
+adasum_status_t adasum_fp8_pack_weight(const void* w, int64_t w_stride, int64_t rows, int64_t columns,
+                                       adasum_dtype_t dtype, void* packed, void* stream_ptr)
+{
+    return adasum::pack(w, w_stride, rows, columns, dtype, packed, true, stream_ptr);
+}
+
+adasum_status_t adasum_fp8_unpack(const void* packed, int64_t rows, int64_t columns, void* out, int64_t out_stride,
+                                  adasum_dtype_t dtype, void* stream_ptr)
+{
+    using namespace adasum;
+    clear_error();
+    adasum_status_t status = check_packed(packed, rows, columns, dtype);
+    if (status != ADASUM_OK || rows == 0 || columns == 0)
+        return status;
+    if ((status = check_matrix("out", out, out_stride, columns, dtype)) != ADASUM_OK)
+        return status;
+    const int64_t eb = operator_bytes(dtype), width = fp8_width(columns);
+    if (spans_overlap(out, matrix_span(rows, columns, out_stride, eb), packed, fp8_bytes(rows, columns)))
+        return fail(ADASUM_ERR_ARG, "packed overlaps out");
+    Strips s;
+    unsigned blocks;
+    if (!plan_strips(rows, columns, (columns + 7) / 8, kUnpackRows, &s, &blocks))
+        return fail(ADASUM_ERR_ARG, "%lld x %lld is too large", (long long)rows, (long long)columns);
+    const uint8_t* codes = static_cast<const uint8_t*>(packed);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+    profile_mark(stream, -1, 0, 0, true);
+    with_type(dtype, [&](auto t) {
+        using T = decltype(t);
+        auto* kernel = columns % 8 == 0 && rows_aligned(out, out_stride, eb) ? fp8_unpack_kernel<T, true> : fp8_unpack_kernel<T, false>;
+        kernel<<<blocks, kStripThreads, 0, stream>>>(s, codes, codes + rows * width, width, static_cast<T*>(out), out_stride);
+    });
+    ADASUM_CUDA_CHECK(cudaGetLastError());
+    profile_mark(stream, ADASUM_KERNEL_FP8_UNPACK, 0, 0, false);
+    return ADASUM_OK;
+}
+
+}  // extern "C"

@@ -41,6 +41,17 @@ constexpr int64_t kMaxExtent = (int64_t(1) << 31) - 256;
 inline bool extent_ok(int64_t n) { return n >= 0 && n <= kMaxExtent; }
 inline bool stride_ok(int64_t stride, int64_t cols) { return stride >= cols && stride <= (int64_t(1) << 31); }
 
+inline adasum_status_t check_matrix(const char* name, const void* p, int64_t stride, int64_t features, adasum_dtype_t dtype)
+{
+    if (!p)
+        return fail(ADASUM_ERR_NULL, "%s is NULL", name);
+    if (!aligned_to(p, operator_bytes(dtype)))
+        return fail(ADASUM_ERR_ARG, "%s is not aligned to its element size", name);
+    if (!stride_ok(stride, features))
+        return fail(ADASUM_ERR_ARG, "stride %lld of %s is shorter than a row or out of range", (long long)stride, name);
+    return ADASUM_OK;
+}
+
 // Multiprocessors of the current device (0: unknown), looked up once per device.
 inline int device_sms()
 {

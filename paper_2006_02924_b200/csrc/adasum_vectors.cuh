@@ -114,16 +114,18 @@ __device__ __forceinline__ Eight decode(const Raw<T>& raw)
     }
     return x;
 }
-template <bool VEC, typename T>
-__device__ __forceinline__ void store_vector(T* p, int count, const Eight& x)
+__device__ __forceinline__ void values_of(const Eight& x, float (&y)[8])
 {
-    float y[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float2 f = values_of(x.p[i]);
         y[2 * i] = f.x;
         y[2 * i + 1] = f.y;
     }
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ void store_values(T* p, int count, const float (&y)[8])
+{
     if constexpr (VEC) {
         if (count > 0)
             store_vector_from_float<8>(p, TypeCode<T>::value, 0, y);
@@ -133,6 +135,13 @@ __device__ __forceinline__ void store_vector(T* p, int count, const Eight& x)
             if (i < count)
                 store_from_float(p, TypeCode<T>::value, i, y[i]);
     }
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ void store_vector(T* p, int count, const Eight& x)
+{
+    float y[8];
+    values_of(x, y);
+    store_values<VEC>(p, count, y);
 }
 
 // Bits of the largest magnitude as an fp32 number; NaN or Inf (exponent 255) if there is one.
