@@ -688,6 +688,16 @@ adasum_status_t adasum_fp8_linear_grad(const void* dy, const void* w, int64_t ro
                                        size_t workspace_bytes, void* stream);
 adasum_status_t adasum_fp8_linear_status(const void* workspace, void* stream);
 
+/*
+ * A self-test of the product's bounded waits, not a way to compute: adasum_fp8_linear without a bias, with one kind of
+ * hand-over (ADASUM_HAND_OVER_*, all but _ADDED) that never completes and with waits of a millisecond instead of a
+ * second.  The result is NaN and adasum_fp8_linear_status reports ADASUM_ERR_TIMEOUT, unless the sizes need no hand-over of
+ * that kind.  The next product on the workspace is not affected.
+ */
+adasum_status_t adasum_fp8_linear_selftest(const void* x, const void* w, int64_t rows, int64_t features, int64_t outputs,
+                                           void* y, int64_t y_stride, adasum_dtype_t out_dtype, void* workspace,
+                                           size_t workspace_bytes, void* stream, int32_t hand_over);
+
 /* Static, human-readable name of a status code. */
 const char* adasum_status_string(adasum_status_t status);
 

@@ -18,6 +18,7 @@ _BINDING_NAMES = (
     "adasum_dropout", "adasum_residual_norm", "adasum_residual_norm_grad", "adasum_residual_norm_grad_workspace_bytes",
     "adasum_fp8_bytes", "adasum_fp8_pack", "adasum_fp8_pack_weight", "adasum_fp8_unpack", "adasum_fp8_linear",
     "adasum_fp8_linear_grad", "adasum_fp8_linear_workspace_bytes", "adasum_fp8_linear_status",
+    "adasum_fp8_linear_selftest",
 )
 
 

@@ -1113,3 +1113,20 @@ def adasum_fp8_linear_status(workspace, stream=None) -> int:
     """``adasum_fp8_linear_status`` of the C ABI: 0, or 7 (ADASUM_ERR_TIMEOUT) if a bounded wait of the last product on
     ``workspace`` ran out.  Synchronises the stream."""
     return int(_lib.adasum_fp8_linear_status(workspace.data_ptr(), _stream_handle(stream)))
+
+
+_lib.adasum_fp8_linear_selftest.restype = ctypes.c_int
+_lib.adasum_fp8_linear_selftest.argtypes = [_vp, _vp, _i64, _i64, _i64, _vp, _i64, ctypes.c_int, _vp, ctypes.c_size_t, _vp,
+                                            _i32]
+
+
+def adasum_fp8_linear_selftest(hand_over: str, x, w, rows: int, features: int, outputs: int, out, workspace):
+    """``adasum_fp8_linear_selftest`` of the C ABI, on the current stream: the named kind of hand-over inside the product
+    never completes, so its bounded waits run out and are reported."""
+    device = out.get_device()
+    status = _lib.adasum_fp8_linear_selftest(
+        _packed("x", x, rows, features, device), _packed("w", w, outputs, features, device), rows, features, outputs,
+        out.data_ptr(), _matrix("out", out, rows, outputs), _operator_dtype(out.dtype), workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream_handle(None), ADASUM_HAND_OVER[hand_over])
+    if status != ADASUM_OK:
+        raise AdasumError(status)

@@ -2,72 +2,660 @@
 //
 //     y[r][n]  = sum_k x[r][k] w[n][k] + bias[n]
 //     dx[r][k] = sum_n dy[r][n] w[n][k]
+//
+// D[m][t] = sum over s of W[m][s] T[t][s] on the fifth-generation tensor cores, with the weights' outputs (features, for the
+// gradient) as rows m and the tokens as columns t, so that the lanes of a warp hold neighbouring elements of a row of the
+// result.  2 R N K operations on R K + N K bytes read and R N elements written: bound by the tensor cores from a few
+// hundred tokens on, by the weights' bytes (and the launch) below.
+//
+// The instruction multiplies e4m3 codes and applies a power of two per row and 32 products of either operand itself
+// (block scaling).  Steps cover 128 products here, so one step byte serves the four instructions of a step of depth 128.  The gradient
+// reads the same packed weights with the summed index as the slow one ("MN-major"): a step per 128 x 128 block is
+// the same for either direction, and nothing is transposed.
+//
+// A pair of blocks (a cluster of two) owns a tile of 256 rows m x TOKENS tokens.  Each block brings 128 rows of W and
+// half the tokens per step, and its tensor core multiplies its 128 rows with all tokens: with the operands halved per
+// block, shared memory and the L2 deliver half of what two separate blocks would need.
+//
+//   copies   one thread per block: bulk tensor copies of 128 x 128 codes of W and TOKENS / 2 x 128 of T, 128-byte swizzle,
+//            zeros beyond the matrices
+//   steps    one warp per block: the step bytes of its rows and of all tokens, loaded ahead, into shared memory in the
+//            form that the tensor core reads; it also says that the block's copies have landed
+//   D        one thread of the pair's first block copies the step bytes to tensor memory and issues the multiplications;
+//            eight warps per block add the sums from tensor memory into fp32 registers and store the result
+//
+// Sums are formed in tensor memory over kChain steps (1024 products) at most: the tensor core truncates where it adds, and over
+// thousands of products that adds up.  Tensor memory (512 columns) holds two such sums, so that the next is formed while
+// the previous one is read, and two sets of step bytes; that is why a tile has 240 tokens and not 256.
+//
+// Tiles are dealt to the pairs whole, unless that leaves too many pairs idle; then the steps of all tiles are cut into
+// equal runs, and a tile whose steps fall to several pairs is joined, in their order, by fp8_join_kernel.  The
+// association of every sum is fixed by the sizes and the number of pairs that fit the device.
+//
+// Every wait has a limit.  A thread whose wait runs out records it and goes on without waiting, but hands over and issues
+// nothing more, so the waits that depend on it run out in turn and the launch ends; the block leaves NaN for all its
+// shares of tiles, and adasum_fp8_linear_status reports it.  Before a block ends its copies have landed, and the
+// pair's multiplications and their arrivals are done.
 #include "adasum_fp8.cuh"
+#include "adasum_tensor.cuh"
 
 namespace adasum {
 namespace {
 
-constexpr int kTile = 64, kDepth = 32, kThreads = 256;
+constexpr int kHalf = 128;                       // rows of W that a block of the pair brings
+constexpr int kTileRows = 2 * kHalf;
+constexpr int kDepth = kFp8Block;                // products per step
+constexpr int kChain = 8;                        // steps that are summed in tensor memory
+constexpr int kWeightBytes = kHalf * kDepth;     // of a step and block
+constexpr int kScaleBytes = 3 * kFp8StepBytes;   // step bytes: the block's rows, 256 tokens
+constexpr int kSumWarps = 8, kCopyWarp = 8, kMultiplyWarp = 9, kMemoryWarp = 10, kStepWarp = 11;
+constexpr int kBlockThreads = 384;
+constexpr int kMaxPairs = 74;                    // 148 multiprocessors
 constexpr size_t kStatusBytes = 1024;
+constexpr int kStatusCount = 255;                // word that holds the number of blocks
+constexpr long long kWaitCycles = 2000000000;    // about a second (a real wait is microseconds): the clock counts pauses too
+constexpr long long kSelftestCycles = 2000000;   // about a millisecond
+constexpr int kLastWait = 4;                     // limits, for the last commit: other warps' waits may have to run out first
+
+template <int TOKENS>
+struct Shape {
+    static constexpr int kHalfTokens = TOKENS / 2;
+    static constexpr int kTokenBytes = kHalfTokens * kDepth;             // whole groups of 8 rows: 1024-byte aligned
+    static constexpr int kStageBytes = kWeightBytes + kTokenBytes;
+    static constexpr int kStages = TOKENS > 128 ? 6 : 8;
+    static constexpr size_t kSharedBytes = (size_t)kStages * (kStageBytes + kScaleBytes) + 1024;   // + room to align to 1024
+    // columns of tensor memory: a sum, step bytes (4 for the rows, 8 for the tokens), the other sum, step bytes
+    static constexpr int kSumColumns = 256, kScaleAt = 240;
+    static_assert(TOKENS <= kScaleAt && kHalfTokens % 8 == 0 && TOKENS % 16 == 0, "");
+};
 
 struct LinearArgs {
-    const uint8_t *a, *a_steps, *w, *w_steps;
-    int64_t rows, depth, wide;         // out: rows x wide, sums of `depth` products
-    int64_t a_width, w_width;
+    const uint8_t *token_steps, *weight_steps;
+    int64_t rows, wide;                // of the result
+    int64_t depth_blocks, weight_blocks;     // 128-column blocks of T and of the packed weights
+    int64_t weight_row_blocks;         // 128-row blocks of the packed weights
     const void* bias;
     int bias_dtype;
     void* out;
     int64_t out_stride;
     int out_dtype;
+    // units of chain_steps steps, tile after tile (tiles of the same tokens next to each other)
+    uint32_t tiles_k, tiles, iterations, chain_steps, chains, units;
+    bool whole;                        // no tile is cut: runs are whole tiles
+    int* status;                       // one word per block, and their number
+    long long wait_cycles;             // limit of a wait
+    int withheld;                      // hand-over that never completes (self-test), or ADASUM_HAND_OVER_NONE
+    float* slots;                      // [pair][first or last tile of its run][block][token][row of the block]
 };
 
-__device__ __forceinline__ float value_at(const uint8_t* codes, const uint8_t* steps, int64_t width, int64_t row, int64_t column)
+__host__ __device__ inline uint32_t run_begin(const LinearArgs& a, uint32_t pairs, uint32_t pair)
 {
-    const __half_raw h = __nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)codes[row * width + column], __NV_E4M3);
-    return __half2float(*reinterpret_cast<const __half*>(&h)) *
-           fp8_step_value(steps[fp8_step_at(row, column / kFp8Block, width / kFp8Block)]);
+    return a.whole ? first_unit(a.tiles, pairs, pair) * a.chains : first_unit(a.units, pairs, pair);
 }
 
-// GRAD: the weights are read with the summed index as rows.
-template <bool GRAD>
-__global__ void __launch_bounds__(kThreads) fp8_linear_kernel(const __grid_constant__ LinearArgs a)
+// ---- instructions ------------------------------------------------------------------------------------
+
+// Codes with the summed index fast: rows of 128 bytes, eight rows 1024 bytes, 128-byte swizzle.  The same words describe
+// codes with the summed index slow: 128 rows m side by side, eight products 1024 bytes further.
+__device__ __forceinline__ uint64_t codes_descriptor(uint32_t address)
 {
-    __shared__ float left[kDepth][kTile + 1], right[kDepth][kTile + 1];
-    const int64_t row0 = (int64_t)blockIdx.x * kTile, col0 = (int64_t)blockIdx.y * kTile;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float sum[4][4] = {};
-    for (int64_t k0 = 0; k0 < a.depth; k0 += kDepth) {
-        for (int i = threadIdx.x; i < kTile * kDepth; i += kThreads) {
-            const int64_t row = row0 + i / kDepth, k = k0 + i % kDepth;
-            left[i % kDepth][i / kDepth] = row < a.rows && k < a.depth ? value_at(a.a, a.a_steps, a.a_width, row, k) : 0.0f;
-            const int d = GRAD ? i / kTile : i % kDepth, c = GRAD ? i % kTile : i / kDepth;
-            const bool in = col0 + c < a.wide && k0 + d < a.depth;
-            right[d][c] = !in ? 0.0f : GRAD ? value_at(a.w, a.w_steps, a.w_width, k0 + d, col0 + c)
-                                            : value_at(a.w, a.w_steps, a.w_width, col0 + c, k0 + d);
+    return (uint64_t)((address & 0x3ffffu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
+           (uint64_t)2 << 61;
+}
+// Step bytes: 32 rows of 16 bytes, eight rows 128 bytes, no swizzle.
+__device__ __forceinline__ uint64_t steps_descriptor(uint32_t address)
+{
+    return (uint64_t)((address & 0x3ffffu) >> 4) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+}
+__device__ __forceinline__ void copy_steps(uint32_t tensor_address, uint64_t descriptor)
+{
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tensor_address), "l"(descriptor) : "memory");
+}
+__device__ __forceinline__ void multiply(uint32_t sum, uint64_t w, uint64_t t, uint32_t instruction, uint32_t w_steps,
+                                         uint32_t t_steps, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                 "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(sum),
+                 "l"(w), "l"(t), "r"(instruction), "r"(w_steps), "r"(t_steps), "r"(accumulate)
+                 : "memory");
+}
+__device__ __forceinline__ void load_eight_sums(uint32_t address, uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(address)
+                 : "memory");
+}
+
+// A thread's column of the result: one row m, consecutive tokens.
+template <typename TO, int COUNT>
+__device__ __forceinline__ void write_column(const LinearArgs& a, int64_t t, int64_t m, float bias, const float (&sum)[COUNT])
+{
+    TO* p = static_cast<TO*>(a.out) + t * a.out_stride + m;
+    const int count = (int)min((int64_t)COUNT, a.rows - t);
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i, p += a.out_stride)
+        if (i < count)
+            store_from_float(p, TypeCode<TO>::value, 0, sum[i] + bias);
+}
+
+// What a thread of the warps that sum leaves for its row and tokens where a wait of its block ran out: NaN, over whatever
+// it has left for any tile of the pair's run.
+template <int TOKENS>
+__device__ __noinline__ void leave_nan(const LinearArgs& a, uint32_t begin, uint32_t end, uint32_t pair, uint32_t rank,
+                                       uint32_t thread)
+{
+    constexpr int kHalfTokens = Shape<TOKENS>::kHalfTokens;
+    const float nan = __uint_as_float(0x7fc00000u);
+    const int row = 32 * ((thread >> 5) & 3) + (thread & 31), side = thread >> 7;
+    uint32_t chain_begin = 0;
+    bool fresh = true;
+    for (Cursor c(a, begin, end); !c.done(); c.advance(a)) {
+        if (fresh)
+            chain_begin = c.chain;
+        fresh = c.last_of_share(a);
+        if (!fresh)
+            continue;
+        const int64_t m = (int64_t)c.tile_k * kTileRows + rank * kHalf + row;
+        const int64_t t = (int64_t)c.tile_n * TOKENS + side * kHalfTokens;
+        if (chain_begin == 0 && c.chain + 1 == a.chains) {
+            for (int i = 0; i < kHalfTokens && m < a.wide && t + i < a.rows; ++i)
+                store_from_float(a.out, a.out_dtype, (t + i) * a.out_stride + m, nan);
+        } else {
+            float* dst = a.slots + ((int64_t)(2 * pair + (c.part == 0 ? 1 : 0)) * 2 + rank) * TOKENS * kHalf + side * kHalfTokens * kHalf + row;
+            for (int i = 0; i < kHalfTokens; ++i)
+                dst[i * kHalf] = nan;
         }
-        __syncthreads();
-        for (int k = 0; k < kDepth; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    sum[i][j] = fmaf(left[k][ty + 16 * i], right[k][tx + 16 * j], sum[i][j]);
-        __syncthreads();
     }
+}
+
+// ---- kernel ------------------------------------------------------------------------------------------
+//
+// GRAD: the weights' summed index is their row.
+template <int TOKENS, bool GRAD>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kBlockThreads, 1)
+fp8_linear_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap token_map,
+                  const __grid_constant__ CUtensorMap weight_map)
+{
+    using S = Shape<TOKENS>;
+    constexpr int kStages = S::kStages, kHalfTokens = S::kHalfTokens;
+    extern __shared__ __align__(1024) unsigned char dynamic_shared[];
+    // landed: this block's codes of a step are there; multiplied: the tensor cores are done with the step; ready (first
+    // block): both blocks' codes and step bytes are there.  formed: a sum in tensor memory is complete; taken (first
+    // block): it has been read by both blocks.  finished: so are all multiplications that were ever issued.  nowhere:
+    // what threads that gave up arrive on.
+    __shared__ __align__(8) unsigned long long landed[kStages], multiplied[kStages], ready[kStages], formed[2], taken[2], finished,
+        nowhere[kStages];
+    __shared__ uint32_t tensor_memory_slot;
+    __shared__ volatile uint32_t gave_up;        // some wait of this block ran out
+
+    start_next_kernel();             // the join; it waits for this kernel's end by itself
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const uint32_t unit_begin = run_begin(a, pairs, pair), unit_end = run_begin(a, pairs, pair + 1);
+    const uint32_t stage0 = (shared_address(dynamic_shared) + 1023u) & ~1023u;
+    const uint32_t scales0 = stage0 + kStages * S::kStageBytes;
+    const uint32_t landed0 = shared_address(landed), ready0 = shared_address(ready), multiplied0 = shared_address(multiplied);
+    const uint32_t formed0 = shared_address(formed), taken0 = shared_address(taken);
+    const uint32_t finished0 = shared_address(&finished), nowhere0 = shared_address(nowhere);
+
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        // a barrier that expects one arrival too many never completes a phase
+        auto init = [&](uint32_t bar, uint32_t count, int hand_over) { barrier_init(bar, count + (a.withheld == hand_over)); };
+        for (int s = 0; s < kStages; ++s) {
+            init(landed0 + 8 * s, 1, ADASUM_HAND_OVER_LANDED);
+            init(multiplied0 + 8 * s, 1, ADASUM_HAND_OVER_MULTIPLIED);
+            init(ready0 + 8 * s, 2, ADASUM_HAND_OVER_READY);
+            barrier_init(nowhere0 + 8 * s, 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            init(formed0 + 8 * s, 1, ADASUM_HAND_OVER_FORMED);
+            init(taken0 + 8 * s, 2 * kSumWarps, ADASUM_HAND_OVER_TAKEN);
+        }
+        barrier_init(finished0, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kMemoryWarp) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(
+            shared_address(&tensor_memory_slot)));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    if (warp == kCopyWarp && lane == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&token_map) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&weight_map) : "memory");
+    }
+    __syncthreads();
+    cluster_barrier();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tensor_memory = tensor_memory_slot;
+    wait_for_previous_kernel();      // the one that packed the tokens; nothing above reads or writes global memory
+    if (threadIdx.x == 0) {
+        a.status[blockIdx.x] = 0;
+        if (blockIdx.x == 0)
+            a.status[kStatusCount] = (int)gridDim.x;
+    }
+
+    // After a wait of this thread ran out it neither waits nor acts for its warp any more (arrives, multiplies, commits).
+    bool waiting = true;
+    uint32_t ready_at = ready0, taken_at = taken0;
+    auto wait_up_to = [&](uint32_t bar, uint32_t parity, long long cycles) {
+        if (waiting && !wait_phase(bar, parity, cycles)) {
+            waiting = false;
+            ready_at = taken_at = nowhere0;
+            gave_up = 1;
+            atomicExch(a.status + blockIdx.x, (int)ADASUM_DEVICE_TIMEOUT);
+        }
+    };
+    auto wait = [&](uint32_t bar, uint32_t parity) { wait_up_to(bar, parity, a.wait_cycles); };
+
+    if (warp < kSumWarps) {
+        // ---- sums: warp w reads tensor-memory lanes 32 (w % 4) .. + 31 (rows m), one half of the tokens
+        const int quarter = warp & 3, side = warp >> 2;
+        float sum[kHalfTokens];
+        uint32_t count = 0, chain_begin = 0;
+        bool fresh = true;                       // the next unit is the first of its tile's share
+        for (Cursor c(a, unit_begin, unit_end); !c.done(); c.advance(a), ++count) {
+            if (fresh) {
+                fresh = false;
+                chain_begin = c.chain;
+#pragma unroll
+                for (int i = 0; i < kHalfTokens; ++i)
+                    sum[i] = 0.0f;
+            }
+            wait(formed0 + 8 * (count & 1), (count >> 1) & 1);
+            __syncwarp();
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t source = tensor_memory + (count & 1) * S::kSumColumns + side * kHalfTokens + ((uint32_t)(32 * quarter) << 16);
+#pragma unroll
+            for (int g = 0; g < kHalfTokens / 8; ++g) {
+                uint32_t r[8];
+                load_eight_sums(source + 8 * g, r);
+                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    sum[8 * g + i] += __uint_as_float(r[i]);
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0)
+                arrive_at_first(taken_at + 8 * (count & 1));
+
+            if (!c.last_of_share(a))
+                continue;
+            fresh = true;
+            // ---- the pair's last unit of this tile: the result, or this pair's part of it
+            const int row = 32 * quarter + lane;
+            if (chain_begin == 0 && c.chain + 1 == a.chains) {
+                const int64_t m = (int64_t)c.tile_k * kTileRows + rank * kHalf + row;
+                const int64_t t = (int64_t)c.tile_n * TOKENS + side * kHalfTokens;
+                if (m < a.wide) {
+                    const float bias = a.bias ? load_as_float(a.bias, a.bias_dtype, m) : 0.0f;
+                    if (a.out_dtype == ADASUM_F32)
+                        write_column<float>(a, t, m, bias, sum);
+                    else if (a.out_dtype == ADASUM_F16)
+                        write_column<__half>(a, t, m, bias, sum);
+                    else
+                        write_column<__nv_bfloat16>(a, t, m, bias, sum);
+                }
+            } else {
+                float* dst = a.slots + ((int64_t)(2 * pair + (c.part == 0 ? 1 : 0)) * 2 + rank) * TOKENS * kHalf + side * kHalfTokens * kHalf + row;
+#pragma unroll
+                for (int i = 0; i < kHalfTokens; ++i)
+                    dst[i * kHalf] = sum[i];
+            }
+        }
+        if (gave_up != 0)
+            leave_nan<TOKENS>(a, unit_begin, unit_end, pair, rank, threadIdx.x);
+        // The last commit arrives in both blocks, and each waits for its own: in this warp, which has just seen the last sum.
+        if (warp == 0) {
+            waiting = true;
+            wait_up_to(finished0, 0, kLastWait * a.wait_cycles);
+        }
+    } else if (warp == kCopyWarp) {
+        // ---- copies of this block's rows of the weights, and of its half of the tokens
+        Ring<kStages> ring;
+        uint32_t issued = 0;
+        for (Cursor c(a, unit_begin, unit_end); !c.done() && waiting; c.advance(a)) {
+            const int m = (int)(c.tile_k * kTileRows + rank * kHalf), t = (int)(c.tile_n * TOKENS + rank * kHalfTokens);
+            const uint32_t end = c.first_step(a) + c.steps(a);
+            for (uint32_t step = c.first_step(a); step < end; ++step) {
+                const uint32_t bar = landed0 + 8 * ring.stage;
+                wait(multiplied0 + 8 * ring.stage, ring.phase ^ 1);
+                waiting = __all_sync(0xffffffffu, waiting);
+                if (!waiting)
+                    break;
+                const uint32_t dst = stage0 + ring.stage * S::kStageBytes;
+                const int s = (int)(step * kDepth);
+                if (elected()) {
+                    expect_bytes(bar, S::kStageBytes);
+                    copy_box(dst, &weight_map, GRAD ? m : s, GRAD ? s : m, bar);
+                    copy_box(dst + kWeightBytes, &token_map, s, t, bar);
+                }
+                __syncwarp();
+                ++issued;
+                ring.advance();
+            }
+        }
+        // nothing may still be on its way into shared memory when the block ends
+        waiting = true;
+        for (uint32_t back = min(issued, (uint32_t)kStages); back > 0; --back) {
+            const uint32_t step = issued - back;
+            wait(landed0 + 8 * (step % kStages), (step / kStages) & 1);
+        }
+    } else if (warp == kMultiplyWarp && rank == 0) {
+        // ---- multiplications: e4m3 codes, steps as powers of two, fp32 sums, 256 x TOKENS
+        constexpr uint32_t kInstruction = ((GRAD ? 1u : 0u) << 15) | ((uint32_t)(TOKENS >> 3) << 17) | (1u << 23) |
+                                          ((uint32_t)(kTileRows >> 4) << 24);
+        Ring<kStages> ring;
+        uint32_t count = 0, turn = 0;
+        for (Cursor c(a, unit_begin, unit_end); !c.done(); c.advance(a), ++count) {
+            const uint32_t target = tensor_memory + (count & 1) * S::kSumColumns;
+            wait(taken0 + 8 * (count & 1), ((count >> 1) & 1) ^ 1);
+            uint32_t accumulate = 0;
+            for (uint32_t steps = c.steps(a); steps > 0; --steps) {
+                wait(ready0 + 8 * ring.stage, ring.phase);
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t codes = stage0 + ring.stage * S::kStageBytes, scales = scales0 + ring.stage * kScaleBytes;
+                const uint64_t w = codes_descriptor(codes), t = codes_descriptor(codes + kWeightBytes), b = steps_descriptor(scales);
+                const uint32_t w_steps = tensor_memory + S::kScaleAt + (turn & 1) * S::kSumColumns, t_steps = w_steps + 4;
+                if (elected() && waiting) {
+                    copy_steps(w_steps, b);
+                    copy_steps(t_steps, b + (kFp8StepBytes >> 4));
+                    if (TOKENS > 128)
+                        copy_steps(t_steps + 4, b + 2 * (kFp8StepBytes >> 4));
+#pragma unroll
+                    for (int s = 0; s < kDepth / 32; ++s)
+                        // 32 products are 32 bytes further on, or 32 rows of 128 bytes (in units of 16)
+                        multiply(target, w + (GRAD ? 256 : 2) * s, t + 2 * s, kInstruction, w_steps, t_steps, s > 0 ? 1u : accumulate);
+                    commit_to_both(multiplied0 + 8 * ring.stage);
+                    if (steps == 1)
+                        commit_to_both(formed0 + 8 * (count & 1));
+                }
+                __syncwarp();
+                accumulate = 1;
+                ++turn;
+                ring.advance();
+            }
+        }
+        if (elected())
+            commit_to_both(finished0);
+        __syncwarp();
+    } else if (warp == kStepWarp) {
+        // ---- step bytes: a lane brings those of rows and tokens 32 j + lane, kBatch steps ahead of their use.  Rows beyond the
+        // matrices take 2^0: their codes are zeros or their results are not stored.
+        constexpr int kBatch = 4, kColumns = (TOKENS + 31) / 32;
+        constexpr uint32_t kOne = 0x7f7f7f7fu;
+        uint32_t words[kBatch][kColumns], weight_words[kBatch];
+        Ring<kStages> ring;
+        auto load = [&](const Cursor& c, uint32_t from) {
+            const int64_t first = (int64_t)c.first_step(a) + from;
+            const int64_t m_block = (int64_t)c.tile_k * 2 + rank;
+            const uint32_t left = c.steps(a) - from;
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                const int64_t s = first + j;
+                const int64_t block_row = GRAD ? s : m_block, block_column = GRAD ? m_block : s;
+                weight_words[j] = kOne;
+                if ((uint32_t)j < left && block_row < a.weight_row_blocks && block_column < a.weight_blocks)
+                    weight_words[j] = __ldg(reinterpret_cast<const uint32_t*>(
+                        a.weight_steps + (block_row * a.weight_blocks + block_column) * kFp8StepBytes));
+            }
+#pragma unroll
+            for (int i = 0; i < kColumns; ++i) {
+                const int64_t t = (int64_t)c.tile_n * TOKENS + 32 * i + lane;
+                const uint8_t* p = a.token_steps + fp8_step_at(t, first, a.depth_blocks);
+                const bool in = t < a.rows && 32 * i + lane < TOKENS;
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j)
+                    words[j][i] = in && (uint32_t)j < left ? __ldg(reinterpret_cast<const uint32_t*>(p + j * kFp8StepBytes)) : kOne;
+            }
+        };
+        Cursor c(a, unit_begin, unit_end);
+        uint32_t from = 0;               // first step of the batch within the unit
+        if (!c.done())
+            load(c, from);
+        while (!c.done()) {
+            uint32_t now[kBatch][8], weight_now[kBatch];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                weight_now[j] = weight_words[j];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    now[j][i] = i < kColumns ? words[j][i < kColumns ? i : 0] : kOne;
+            }
+            const int steps = (int)min((uint32_t)kBatch, c.steps(a) - from);
+            from += kBatch;
+            if (from >= c.steps(a)) {
+                from = 0;
+                c.advance(a);
+            }
+            if (!c.done())
+                load(c, from);
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                if (j < steps) {
+                    wait(landed0 + 8 * ring.stage, ring.phase);      // so the stage's last multiplications are done, too
+                    const uint32_t dst = scales0 + ring.stage * kScaleBytes + 16 * lane;
+                    store_shared_16B(dst, make_uint4(weight_now[j], weight_now[j], weight_now[j], weight_now[j]));
+                    store_shared_16B(dst + kFp8StepBytes, make_uint4(now[j][0], now[j][1], now[j][2], now[j][3]));
+                    if (kColumns > 4)
+                        store_shared_16B(dst + 2 * kFp8StepBytes, make_uint4(now[j][4], now[j][5], now[j][6], now[j][7]));
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0)
+                        arrive_at_first(ready_at + 8 * ring.stage);
+                    ring.advance();
+                }
+            }
+        }
+    }
+    __syncwarp();
+    // Neither block may end, nor free its tensor memory, while the other still multiplies or arrives here: both have
+    // waited for the last commit, the first block's copies of it included.
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncwarp();
+    cluster_barrier();
+    if (warp == kMemoryWarp)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tensor_memory) : "memory");
+}
+
+// Tiles whose units fell to several pairs: the pairs' parts added in order.  grid.x = tiles, grid.y = parts of a tile's
+// 2 x `tokens` rows of 128; one warp per row, four elements per lane.
+constexpr int kJoinThreads = 256;
+
+__global__ void __launch_bounds__(kJoinThreads)
+fp8_join_kernel(const __grid_constant__ LinearArgs a, uint32_t pairs, int tokens, bool vec)
+{
+    wait_for_previous_kernel();
+    const uint32_t tile = blockIdx.x;
+    const uint32_t first = pair_of_unit(a.units, pairs, tile * a.chains);
+    const uint32_t last = pair_of_unit(a.units, pairs, tile * a.chains + a.chains - 1);
+    if (first == last)
+        return;                      // written by the product itself
+    const int at = blockIdx.y * (kJoinThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (at >= 2 * tokens)
+        return;
+    const uint32_t tile_k = tile % a.tiles_k, tile_n = tile / a.tiles_k;
+    // only the first pair's run can have started in an earlier tile
+    const uint32_t first_slot = 2 * first + (tile == first_unit(a.units, pairs, first) / a.chains ? 0 : 1);
+    const int64_t slot_floats = (int64_t)2 * tokens * kHalf;
+    const float* source = a.slots + (int64_t)at * kHalf + 4 * lane;
+    float sum[4] = {};
+#pragma unroll 4
+    for (uint32_t pair = first; pair <= last; ++pair) {
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(source + (pair == first ? first_slot : 2 * pair) * slot_floats));
+        sum[0] += v.x;
+        sum[1] += v.y;
+        sum[2] += v.z;
+        sum[3] += v.w;
+    }
+    const int64_t t = (int64_t)tile_n * tokens + at % tokens;
+    const int64_t m = (int64_t)tile_k * kTileRows + at / tokens * kHalf + 4 * lane;
+    if (t >= a.rows || m >= a.wide)
+        return;
+    const int64_t e = t * a.out_stride + m;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
+        if (a.bias && m + i < a.wide)
+            sum[i] += load_as_float(a.bias, a.bias_dtype, m + i);
+    if (vec) {
+        store_vector_from_float<4>(a.out, a.out_dtype, e, sum);
+    } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t row = row0 + ty + 16 * i, column = col0 + tx + 16 * j;
-            if (row < a.rows && column < a.wide)
-                store_from_float(a.out, a.out_dtype, row * a.out_stride + column,
-                                 sum[i][j] + (a.bias ? load_as_float(a.bias, a.bias_dtype, column) : 0.0f));
-        }
+        for (int i = 0; i < 4; ++i)
+            if (m + i < a.wide)
+                store_from_float(a.out, a.out_dtype, e + i, sum[i]);
+    }
+}
+
+// Nothing to sum: the bias, or zeros.
+__global__ void __launch_bounds__(256) fp8_bias_kernel(const __grid_constant__ LinearArgs a, RowDivider divider, uint64_t elements)
+{
+    const uint64_t n = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (n == 0)
+        a.status[kStatusCount] = 0;
+    if (n >= elements)
+        return;
+    uint64_t row;
+    uint32_t column;
+    divide_row(divider, n, row, column);
+    store_from_float(a.out, a.out_dtype, (int64_t)row * a.out_stride + column,
+                     a.bias ? load_as_float(a.bias, a.bias_dtype, column) : 0.0f);
+}
+
+// ---- host --------------------------------------------------------------------------------------------
+
+struct Work {
+    int tokens;                // of a tile
+    uint32_t tiles_k, tiles, iterations, chain_steps, chains, units, pairs;
+    bool fits, whole;
+};
+
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to; }
+
+// Tokens of a tile.  The smaller tiles are for few tokens, and for counts that fill the largest badly: a step costs
+// shared memory 132, 96 and 80 cycles for 240, 128 and 64 tokens.
+int tile_tokens(int64_t rows)
+{
+    const int64_t cost[3] = {up(rows, 240) * 132, up(rows, 128) * 96, up(rows, 64) * 80};
+    return cost[2] <= cost[1] && cost[2] <= cost[0] ? 64 : cost[1] <= cost[0] ? 128 : 240;
+}
+
+// `most`: pairs that run at once.
+Work plan_work(int64_t rows, int64_t wide, int64_t depth, uint32_t most)
+{
+    Work w{};
+    w.tokens = tile_tokens(rows);
+    const int64_t tiles_k = up(wide, kTileRows), tiles_n = up(rows, w.tokens), iterations = up(depth, kDepth);
+    const int64_t limit = int64_t(1) << 31;
+    w.fits = tiles_k * tiles_n < limit && (iterations == 0 || tiles_k * tiles_n < limit / iterations);
+    if (!w.fits)
+        return w;
+    w.tiles_k = (uint32_t)tiles_k;
+    w.tiles = (uint32_t)(tiles_k * tiles_n);
+    w.iterations = (uint32_t)iterations;
+    // whole tiles, or equal runs of steps and a join of about 12 steps' time
+    const int64_t whole = up(w.tiles, most) * iterations, cut = up((int64_t)w.tiles * iterations, most) + 12;
+    w.whole = whole <= cut;
+    int64_t chain_steps = kChain;
+    if (!w.whole && (int64_t)w.tiles * up(iterations, kChain) < 2 * (int64_t)most) {
+        chain_steps = (int64_t)w.tiles * iterations / (2 * (int64_t)most);
+        chain_steps = chain_steps < 1 ? 1 : chain_steps;
+    }
+    w.chain_steps = (uint32_t)chain_steps;
+    w.chains = (uint32_t)up(iterations, chain_steps);
+    w.units = w.tiles * w.chains;
+    const uint32_t shares = w.whole ? w.tiles : w.units;
+    w.pairs = shares < most ? shares : most;
+    return w;
+}
+
+// An upper bound for any number of pairs, never falling as rows rise: partial sums of the largest tile that so few
+// rows take, for as many pairs as there are steps of the smallest.
+size_t linear_workspace(int64_t rows, int64_t wide, int64_t depth)
+{
+    if (rows == 0 || wide == 0 || depth == 0)
+        return kStatusBytes;
+    const int64_t tokens = rows <= 64 ? 64 : rows <= 128 ? 128 : 240;
+    const int64_t tiles = up(rows, 64) * up(wide, kTileRows);
+    const int64_t pairs = tiles >= kMaxPairs || tiles * up(depth, kDepth) >= kMaxPairs ? kMaxPairs : tiles * up(depth, kDepth);
+    return kStatusBytes + (size_t)(pairs * 2 * kTileRows * tokens) * sizeof(float);
+}
+
+template <int TOKENS, bool GRAD>
+cudaError_t prepare_kernel(uint32_t* pairs)
+{
+    static uint32_t cached[64] = {};
+    int device = 0;
+    cudaError_t err = cudaGetDevice(&device);
+    if (err != cudaSuccess)
+        return err;
+    if (device < 0 || device >= 64)
+        return cudaErrorInvalidDevice;
+    if (cached[device] == 0) {
+        auto* kernel = fp8_linear_kernel<TOKENS, GRAD>;
+        const size_t shared = Shape<TOKENS>::kSharedBytes;
+        if ((err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared)) != cudaSuccess)
+            return err;
+        cudaLaunchConfig_t config = {};
+        config.gridDim = dim3(2 * kMaxPairs);
+        config.blockDim = dim3(kBlockThreads);
+        config.dynamicSmemBytes = shared;
+        cudaLaunchAttribute attribute;
+        attribute.id = cudaLaunchAttributeClusterDimension;
+        attribute.val.clusterDim.x = 2;
+        attribute.val.clusterDim.y = attribute.val.clusterDim.z = 1;
+        config.attrs = &attribute;
+        config.numAttrs = 1;
+        int clusters = 0;
+        if ((err = cudaOccupancyMaxActiveClusters(&clusters, kernel, &config)) != cudaSuccess)
+            return err;
+        if (clusters < 1)
+            return cudaErrorLaunchOutOfResources;
+        cached[device] = clusters < kMaxPairs ? (uint32_t)clusters : kMaxPairs;
+    }
+    *pairs = cached[device];
+    return cudaSuccess;
+}
+
+// Calls f(constant of the tile's tokens, constant of the direction).
+template <int N>
+struct Number { static constexpr int value = N; };
+template <typename F>
+void with_shape(int tokens, bool grad, F&& f)
+{
+    auto with_tokens = [&](auto g) {
+        if (tokens == 64)
+            f(Number<64>{}, g);
+        else if (tokens == 128)
+            f(Number<128>{}, g);
+        else
+            f(Number<240>{}, g);
+    };
+    if (grad)
+        with_tokens(Number<1>{});
+    else
+        with_tokens(Number<0>{});
+}
+
+adasum_status_t describe_codes(CUtensorMap* map, const void* codes, int64_t width, int64_t rows, int box_rows)
+{
+    EncodeTiled encode = encode_tiled();
+    if (!encode)
+        return fail(ADASUM_ERR_CUDA, "the driver has no tensor map encoder");
+    const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)width};
+    const cuuint32_t box[2] = {128, (cuuint32_t)box_rows}, unit[2] = {1, 1};
+    const CUresult err = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(codes), dims, strides, box, unit,
+                                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return err == CUDA_SUCCESS ? ADASUM_OK : fail(ADASUM_ERR_CUDA, "tensor map of packed codes: error %d", (int)err);
 }
 
 adasum_status_t linear(const void* x, const void* w, int64_t rows, int64_t features, int64_t outputs, const void* bias,
                        adasum_dtype_t bias_dtype, void* out, int64_t out_stride, adasum_dtype_t out_dtype, void* workspace,
-                       size_t workspace_bytes, bool grad, void* stream_ptr)
+                       size_t workspace_bytes, bool grad, void* stream_ptr, int hand_over)
 {
     clear_error();
     if (!extent_ok(rows) || !extent_ok(features) || !extent_ok(outputs))
@@ -87,7 +675,9 @@ adasum_status_t linear(const void* x, const void* w, int64_t rows, int64_t featu
         return status;
     if (bias && !aligned_to(bias, operator_bytes(bias_dtype)))
         return fail(ADASUM_ERR_ARG, "bias is not aligned to its element size");
-    const size_t need = adasum_fp8_linear_workspace_bytes(rows, features, outputs);
+    if (!plan_work(rows, wide, depth, 1).fits)
+        return fail(ADASUM_ERR_ARG, "%lld x %lld x %lld is too large", (long long)rows, (long long)features, (long long)outputs);
+    const size_t need = linear_workspace(rows, wide, depth);
     if (!workspace || workspace_bytes < need)
         return fail(ADASUM_ERR_WORKSPACE, "workspace of %zu bytes, need %zu", workspace ? workspace_bytes : (size_t)0, need);
     if (!aligned_to(workspace, 256))
@@ -100,32 +690,68 @@ adasum_status_t linear(const void* x, const void* w, int64_t rows, int64_t featu
         spans_overlap(workspace, need, x, x_bytes) || spans_overlap(workspace, need, w, w_bytes) ||
         spans_overlap(workspace, need, bias, bias_bytes))
         return fail(ADASUM_ERR_ARG, "the output or the workspace overlaps an input or each other");
-    LinearArgs a;
+
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+    LinearArgs a{};
     a.rows = rows;
-    a.depth = depth;
     a.wide = wide;
-    a.a_width = fp8_width(depth);
-    a.w_width = fp8_width(features);
-    a.a = static_cast<const uint8_t*>(x);
-    a.a_steps = a.a + rows * a.a_width;
-    a.w = static_cast<const uint8_t*>(w);
-    a.w_steps = a.w + outputs * a.w_width;
     a.bias = bias;
     a.bias_dtype = (int)bias_dtype;
     a.out = out;
     a.out_stride = out_stride;
     a.out_dtype = (int)out_dtype;
-    cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+    a.status = static_cast<int*>(workspace);
+    if (depth == 0) {
+        const uint64_t elements = (uint64_t)rows * (uint64_t)wide, blocks = (elements + 255) / 256;
+        if (blocks > 0x7fffffffu)
+            return fail(ADASUM_ERR_ARG, "%lld x %lld is too large", (long long)rows, (long long)wide);
+        fp8_bias_kernel<<<(unsigned)blocks, 256, 0, stream>>>(a, row_divider(wide), elements);
+        ADASUM_CUDA_CHECK(cudaGetLastError());
+        return ADASUM_OK;
+    }
+    const int tokens = tile_tokens(rows);
+    uint32_t most = 0;
+    cudaError_t err = cudaSuccess;
+    with_shape(tokens, grad, [&](auto t, auto g) { err = prepare_kernel<decltype(t)::value, decltype(g)::value != 0>(&most); });
+    ADASUM_CUDA_CHECK(err);
+    const Work l = plan_work(rows, wide, depth, most);
+    const uint8_t* token_codes = static_cast<const uint8_t*>(x);
+    const uint8_t* weight_codes = static_cast<const uint8_t*>(w);
+    CUtensorMap token_map, weight_map;
+    status = describe_codes(&token_map, token_codes, fp8_width(depth), rows, tokens / 2);
+    if (status == ADASUM_OK)
+        status = describe_codes(&weight_map, weight_codes, fp8_width(features), outputs, kHalf);
+    if (status != ADASUM_OK)
+        return status;
+    a.token_steps = token_codes + rows * fp8_width(depth);
+    a.weight_steps = weight_codes + outputs * fp8_width(features);
+    a.depth_blocks = fp8_blocks(depth);
+    a.weight_blocks = fp8_blocks(features);
+    a.weight_row_blocks = fp8_blocks(outputs);
+    a.tiles_k = l.tiles_k;
+    a.tiles = l.tiles;
+    a.iterations = l.iterations;
+    a.chain_steps = l.chain_steps;
+    a.chains = l.chains;
+    a.units = l.units;
+    a.whole = l.whole;
+    a.wait_cycles = hand_over == ADASUM_HAND_OVER_NONE ? kWaitCycles : kSelftestCycles;
+    a.withheld = hand_over;
+    a.slots = reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes);
     profile_mark(stream, -1, 0, 0, true);
-    const dim3 grid((unsigned)((rows + kTile - 1) / kTile), (unsigned)((wide + kTile - 1) / kTile));
-    if (grid.y > 65535)
-        return fail(ADASUM_ERR_ARG, "too large");
-    if (grad)
-        fp8_linear_kernel<true><<<grid, kThreads, 0, stream>>>(a);
-    else
-        fp8_linear_kernel<false><<<grid, kThreads, 0, stream>>>(a);
-    ADASUM_CUDA_CHECK(cudaGetLastError());
+    with_shape(tokens, grad, [&](auto t, auto g) {
+        constexpr int TOKENS = decltype(t)::value;
+        err = launch_after(fp8_linear_kernel<TOKENS, decltype(g)::value != 0>, dim3(2 * l.pairs), kBlockThreads,
+                           Shape<TOKENS>::kSharedBytes, stream, a, token_map, weight_map);
+    });
+    ADASUM_CUDA_CHECK(err);
     profile_mark(stream, ADASUM_KERNEL_FP8_LINEAR, 0, 0, false);
+    if (!l.whole) {
+        const bool vec = aligned_to(out, 16) && out_stride % 4 == 0 && wide % 4 == 0;
+        ADASUM_CUDA_CHECK(launch_after(fp8_join_kernel, dim3(l.tiles, (unsigned)up(2 * tokens, kJoinThreads / 32)), kJoinThreads, 0,
+                                       stream, a, l.pairs, tokens, vec));
+        profile_mark(stream, ADASUM_KERNEL_FP8_LINEAR, 1, 0, false);
+    }
     return ADASUM_OK;
 }
 
@@ -139,7 +765,8 @@ size_t adasum_fp8_linear_workspace_bytes(int64_t rows, int64_t features, int64_t
     using namespace adasum;
     if (!extent_ok(rows) || !extent_ok(features) || !extent_ok(outputs))
         return 0;
-    return kStatusBytes;
+    const size_t forward = linear_workspace(rows, outputs, features), grad = linear_workspace(rows, features, outputs);
+    return forward > grad ? forward : grad;
 }
 
 adasum_status_t adasum_fp8_linear(const void* x, const void* w, int64_t rows, int64_t features, int64_t outputs,
@@ -147,7 +774,7 @@ adasum_status_t adasum_fp8_linear(const void* x, const void* w, int64_t rows, in
                                   adasum_dtype_t out_dtype, void* workspace, size_t workspace_bytes, void* stream_ptr)
 {
     return adasum::linear(x, w, rows, features, outputs, bias, bias_dtype, y, y_stride, out_dtype, workspace, workspace_bytes,
-                          false, stream_ptr);
+                          false, stream_ptr, ADASUM_HAND_OVER_NONE);
 }
 
 adasum_status_t adasum_fp8_linear_grad(const void* dy, const void* w, int64_t rows, int64_t features, int64_t outputs,
@@ -155,7 +782,19 @@ adasum_status_t adasum_fp8_linear_grad(const void* dy, const void* w, int64_t ro
                                        size_t workspace_bytes, void* stream_ptr)
 {
     return adasum::linear(dy, w, rows, features, outputs, nullptr, out_dtype, dx, dx_stride, out_dtype, workspace, workspace_bytes,
-                          true, stream_ptr);
+                          true, stream_ptr, ADASUM_HAND_OVER_NONE);
+}
+
+adasum_status_t adasum_fp8_linear_selftest(const void* x, const void* w, int64_t rows, int64_t features, int64_t outputs,
+                                           void* y, int64_t y_stride, adasum_dtype_t out_dtype, void* workspace,
+                                           size_t workspace_bytes, void* stream_ptr, int32_t hand_over)
+{
+    using namespace adasum;
+    clear_error();
+    if (hand_over < ADASUM_HAND_OVER_LANDED || hand_over > ADASUM_HAND_OVER_TAKEN || hand_over == ADASUM_HAND_OVER_ADDED)
+        return fail(ADASUM_ERR_ARG, "unknown hand-over %d", (int)hand_over);
+    return linear(x, w, rows, features, outputs, nullptr, out_dtype, y, y_stride, out_dtype, workspace, workspace_bytes, false,
+                  stream_ptr, hand_over);
 }
 
 adasum_status_t adasum_fp8_linear_status(const void* workspace, void* stream_ptr)
@@ -164,8 +803,13 @@ adasum_status_t adasum_fp8_linear_status(const void* workspace, void* stream_ptr
     clear_error();
     if (!workspace)
         return fail(ADASUM_ERR_NULL, "workspace is NULL");
+    int words[kStatusBytes / sizeof(int)] = {};
     cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+    ADASUM_CUDA_CHECK(cudaMemcpyAsync(words, workspace, kStatusBytes, cudaMemcpyDeviceToHost, stream));
     ADASUM_CUDA_CHECK(cudaStreamSynchronize(stream));
+    for (int i = 0; i < words[kStatusCount] && i < 2 * kMaxPairs; ++i)
+        if (words[i] == ADASUM_DEVICE_TIMEOUT)
+            return fail(ADASUM_ERR_TIMEOUT, "a bounded wait of block %d ran out", i);
     return ADASUM_OK;
 }
 

@@ -203,6 +203,17 @@ __device__ __forceinline__ void group_sum(Member& m, Exchange& e, float (&v)[N])
     m.parity ^= 1;
 }
 
+__device__ __forceinline__ bool in_range(float s) { return fabsf(s) < __uint_as_float(0x7f800000u); }
+// Has a sum of the group (of the warp's groups) left fp32's range, or is not a number?  The same answer for all its threads.
+__device__ __forceinline__ bool any_out_of_range(const Member& m, const float (&s)[kRows])
+{
+    bool out = false;
+#pragma unroll
+    for (int u = 0; u < kRows; ++u)
+        out |= !in_range(s[u]);
+    return m.deal.warps == 1 ? __any_sync(0xffffffffu, out) : out;
+}
+
 // Statistics of kRows rows; x becomes the normalised values.  Elements beyond the row are zeros and stay out.
 __device__ __forceinline__ void normalise(Member& m, Exchange& e, const NormArgs& a, int kind, int count, float (&x)[kRows][8],
                                           float (&mean)[kRows], float (&rstd)[kRows])
@@ -221,12 +232,27 @@ __device__ __forceinline__ void normalise(Member& m, Exchange& e, const NormArgs
         }
         group_sum(m, e, s);
 #pragma unroll
-        for (int u = 0; u < kRows; ++u) {
+        for (int u = 0; u < kRows; ++u)
             mean[u] = s[u] * a.inv_features;
+        if (any_out_of_range(m, s)) {            // such rows are divided before they are added
+            float t[kRows];
+#pragma unroll
+            for (int u = 0; u < kRows; ++u) {
+                t[u] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    t[u] = fmaf(x[u][i], a.inv_features, t[u]);
+            }
+            group_sum(m, e, t);
+#pragma unroll
+            for (int u = 0; u < kRows; ++u)
+                mean[u] = in_range(s[u]) ? mean[u] : t[u];
+        }
+#pragma unroll
+        for (int u = 0; u < kRows; ++u)
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 x[u][i] = i < count ? x[u][i] - mean[u] : 0.0f;
-        }
     }
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
@@ -237,12 +263,28 @@ __device__ __forceinline__ void normalise(Member& m, Exchange& e, const NormArgs
     }
     group_sum(m, e, s);
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
+    for (int u = 0; u < kRows; ++u)
         rstd[u] = reciprocal_root(fmaf(s[u], a.inv_features, a.eps));
+    if (any_out_of_range(m, s)) {                // such rows: of the values times 2^-96
+        const float down = __uint_as_float((127u - 96u) << 23);
+        float t[kRows];
+#pragma unroll
+        for (int u = 0; u < kRows; ++u) {
+            t[u] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                t[u] = fmaf(x[u][i] * down, x[u][i] * down, t[u]);
+        }
+        group_sum(m, e, t);
+#pragma unroll
+        for (int u = 0; u < kRows; ++u)
+            rstd[u] = in_range(s[u]) ? rstd[u] : down * reciprocal_root(fmaf(t[u], a.inv_features, a.eps * down * down));
+    }
+#pragma unroll
+    for (int u = 0; u < kRows; ++u)
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             x[u][i] *= rstd[u];
-    }
 }
 
 __device__ __forceinline__ void affine(const Vector& weight, const Vector& bias, int64_t column, int count, float (&x)[kRows][8])

@@ -86,16 +86,6 @@ struct WeightGradArgs {
     float* bias_slots;       // [pair + tile][256 outputs]: the pairs' shares of the tiles' parts of the bias gradient
 };
 
-__host__ __device__ inline uint32_t first_unit(uint32_t units, uint32_t pairs, uint32_t pair)
-{
-    return (uint32_t)((uint64_t)pair * units / pairs);
-}
-// The pair whose run holds a unit: the largest p with floor(p units / pairs) <= unit.
-__host__ __device__ inline uint32_t pair_of_unit(uint32_t units, uint32_t pairs, uint32_t unit)
-{
-    return (uint32_t)((((uint64_t)unit + 1) * pairs - 1) / units);
-}
-
 __device__ __forceinline__ void write_gradient(const WeightGradArgs& a, void* dst, int64_t e, float sum)
 {
     float y = sum * a.scale;
@@ -196,68 +186,6 @@ struct Decoder<__half> {
     {
         const uint32_t biased = packed ^ 0x80808080u;
         return make_uint2(pair(biased, 0x4140), pair(biased, 0x4342));
-    }
-};
-
-// Where a role stands in its pair's run of units [begin, end).
-//
-// A run is the end of one tile, some whole tiles and the beginning of another.  They are walked in the order
-// beginning, end, whole tiles: all runs are equally long, so at any time the pairs stand at one of two tokens
-// (the beginnings at s, all others at the same distance from it, modulo the tokens), read the same rows of both
-// matrices at the same time and find them in the L2's nearer half.
-struct Cursor {
-    uint32_t unit, stop, chain, tile_k, tile_n, part;
-    uint32_t begin, end;
-    __device__ __forceinline__ Cursor(const WeightGradArgs& a, uint32_t b, uint32_t e) : part(0), begin(b), end(e)
-    {
-        unit = max(b, e / a.chains * a.chains);          // the beginning of the last tile, if it is cut off
-        stop = e;
-        if (e / a.chains == b / a.chains)
-            unit = stop;                                 // a run inside one tile is an "end" throughout
-        enter(a);
-    }
-    __device__ __forceinline__ void enter(const WeightGradArgs& a)
-    {
-        while (unit == stop && part < 3) {
-            ++part;
-            const uint32_t first_whole =
-                end / a.chains == begin / a.chains ? end : (begin + a.chains - 1) / a.chains * a.chains;
-            if (part == 1) {
-                unit = begin;
-                stop = min(end, first_whole);
-            } else if (part == 2) {
-                unit = min(end, first_whole);
-                stop = max(unit, end / a.chains * a.chains);
-            }
-        }
-        const uint32_t tile = unit / a.chains;
-        chain = unit - tile * a.chains;
-        tile_n = tile / a.tiles_k;
-        tile_k = tile - tile_n * a.tiles_k;
-    }
-    __device__ __forceinline__ bool done() const { return part == 3; }
-    // Is this the last unit of the pair's share of the tile?
-    __device__ __forceinline__ bool last_of_share(const WeightGradArgs& a) const
-    {
-        return unit + 1 == stop || chain + 1 == a.chains;
-    }
-    __device__ __forceinline__ uint32_t first_step(const WeightGradArgs& a) const { return chain * a.chain_steps; }
-    __device__ __forceinline__ uint32_t steps(const WeightGradArgs& a) const
-    {
-        return min(a.chain_steps, a.iterations - chain * a.chain_steps);
-    }
-    __device__ __forceinline__ void advance(const WeightGradArgs& a)
-    {
-        ++unit;
-        if (unit == stop) {
-            enter(a);
-        } else if (++chain == a.chains) {
-            chain = 0;
-            if (++tile_k == a.tiles_k) {
-                tile_k = 0;
-                ++tile_n;
-            }
-        }
     }
 };
 

@@ -281,9 +281,10 @@ def test_captured_beside_an_eager_graph_and_on_two_streams(b):
         want.append((h, y, stats, _grads(b, c, h, stats)))
     leaf = cases[0].x.float().requires_grad_()               # an eager graph of the same data lives on
     alive = (leaf * 2).sum()
-    streams, graphs, got = [torch.cuda.Stream() for _ in cases], [], []
+    streams, graphs, got, workspaces = [torch.cuda.Stream() for _ in cases], [], [], []
     for c, s in zip(cases, streams):
         ws = torch.empty(b.adasum_residual_norm_grad_workspace_bytes(520, gate=True), dtype=torch.uint8, device="cuda")
+        workspaces.append(ws)                                # they live as long as the graphs
         torch.cuda.synchronize()
         g = torch.cuda.CUDAGraph()
         with torch.cuda.graph(g, stream=s):
