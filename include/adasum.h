@@ -690,7 +690,7 @@ adasum_status_t adasum_fp8_linear_status(const void* workspace, void* stream);
 
 /*
  * A self-test of the product's bounded waits, not a way to compute: adasum_fp8_linear without a bias, with one kind of
- * hand-over (ADASUM_HAND_OVER_*, all but _ADDED) that never completes and with waits of a millisecond instead of a
+ * hand-over (ADASUM_HAND_OVER_LANDED, _MULTIPLIED, _FORMED or _TAKEN) that never completes and with waits of a millisecond instead of a
  * second.  The result is NaN and adasum_fp8_linear_status reports ADASUM_ERR_TIMEOUT, unless the sizes need no hand-over of
  * that kind.  The next product on the workspace is not affected.
  */

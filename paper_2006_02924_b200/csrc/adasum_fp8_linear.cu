@@ -18,15 +18,15 @@
 // block, shared memory and the L2 deliver half of what two separate blocks would need.
 //
 //   copies   one thread per block: bulk tensor copies of 128 x 128 codes of W and TOKENS / 2 x 128 of T, 128-byte swizzle,
-//            zeros beyond the matrices
-//   steps    one warp per block: the step bytes of its rows and of all tokens, loaded ahead, into shared memory in the
-//            form that the tensor core reads; it also says that the block's copies have landed
+//            zeros beyond the matrices, and of the step bytes of its rows and of all tokens
 //   D        one thread of the pair's first block copies the step bytes to tensor memory and issues the multiplications;
-//            eight warps per block add the sums from tensor memory into fp32 registers and store the result
+//            sixteen warps per block add the sums from tensor memory into fp32 registers and store the result
 //
 // Sums are formed in tensor memory over kChain steps (1024 products) at most: the tensor core truncates where it adds, and over
 // thousands of products that adds up.  Tensor memory (512 columns) holds two such sums, so that the next is formed while
-// the previous one is read, and two sets of step bytes; that is why a tile has 240 tokens and not 256.
+// the previous one is read, and two sets of step bytes; that is why a tile has 192 tokens and not 256.  (240 would
+// fit, but such tiles begin inside a block of step bytes, and the stores and the fence that it takes to move them to their places cost
+// every step 1200 cycles on its way: 75 us and more, with four warps in turn, for what takes 60.)
 //
 // Tiles are dealt to the pairs whole, unless that leaves too many pairs idle; then the steps of all tiles are cut into
 // equal runs, and a tile whose steps fall to several pairs is joined, in their order, by fp8_join_kernel.  The
@@ -47,9 +47,9 @@ constexpr int kTileRows = 2 * kHalf;
 constexpr int kDepth = kFp8Block;                // products per step
 constexpr int kChain = 8;                        // steps that are summed in tensor memory
 constexpr int kWeightBytes = kHalf * kDepth;     // of a step and block
-constexpr int kScaleBytes = 3 * kFp8StepBytes;   // step bytes: the block's rows, 256 tokens
-constexpr int kSumWarps = 8, kCopyWarp = 8, kMultiplyWarp = 9, kMemoryWarp = 10, kStepWarp = 11;
-constexpr int kBlockThreads = 384;
+constexpr int kParts = 4;                        // of a tile's tokens: four warps sum and store each
+constexpr int kSumWarps = 4 * kParts, kCopyWarp = kSumWarps, kMultiplyWarp = kCopyWarp + 1, kMemoryWarp = kCopyWarp + 2;
+constexpr int kBlockThreads = 32 * (kSumWarps + 4);
 constexpr int kMaxPairs = 74;                    // 148 multiprocessors
 constexpr size_t kStatusBytes = 1024;
 constexpr int kStatusCount = 255;                // word that holds the number of blocks
@@ -59,26 +59,27 @@ constexpr int kLastWait = 4;                     // limits, for the last commit:
 
 template <int TOKENS>
 struct Shape {
-    static constexpr int kHalfTokens = TOKENS / 2;
+    static constexpr int kHalfTokens = TOKENS / 2, kPartTokens = TOKENS / kParts;
     static constexpr int kTokenBytes = kHalfTokens * kDepth;             // whole groups of 8 rows: 1024-byte aligned
     static constexpr int kStageBytes = kWeightBytes + kTokenBytes;
-    static constexpr int kStages = TOKENS > 128 ? 6 : 8;
+    // blocks of 128 rows that a tile's tokens lie in; a tile starts at the beginning of one or 64 rows into it
+    static constexpr int kRowBlocks = TOKENS > 128 ? 2 : 1;
+    static constexpr int kScaleBytes = (1 + kRowBlocks) * kFp8StepBytes;  // step bytes of the block's rows and of the tokens
+    static constexpr int kStages = TOKENS > 128 ? 7 : 8;
     static constexpr size_t kSharedBytes = (size_t)kStages * (kStageBytes + kScaleBytes) + 1024;   // + room to align to 1024
-    // columns of tensor memory: a sum, step bytes (4 for the rows, 8 for the tokens), the other sum, step bytes
-    static constexpr int kSumColumns = 256, kScaleAt = 240;
-    static_assert(TOKENS <= kScaleAt && kHalfTokens % 8 == 0 && TOKENS % 16 == 0, "");
+    // columns of tensor memory: a sum, step bytes (4 for the rows, 4 or 8 for the tokens), the other sum, step bytes
+    static constexpr int kSumColumns = 256, kScaleAt = 192;
+    static_assert(TOKENS == 192 || TOKENS == 128 || TOKENS == 64, "");
 };
 
 struct LinearArgs {
-    const uint8_t *token_steps, *weight_steps;
     int64_t rows, wide;                // of the result
-    int64_t depth_blocks, weight_blocks;     // 128-column blocks of T and of the packed weights
-    int64_t weight_row_blocks;         // 128-row blocks of the packed weights
     const void* bias;
     int bias_dtype;
     void* out;
     int64_t out_stride;
     int out_dtype;
+    bool pairs_aligned;                // two neighbouring elements may be stored at once
     // units of chain_steps steps, tile after tile (tiles of the same tokens next to each other)
     uint32_t tiles_k, tiles, iterations, chain_steps, chains, units;
     bool whole;                        // no tile is cut: runs are whole tiles
@@ -88,12 +89,68 @@ struct LinearArgs {
     float* slots;                      // [pair][first or last tile of its run][block][token][row of the block]
 };
 
-__host__ __device__ inline uint32_t run_begin(const LinearArgs& a, uint32_t pairs, uint32_t pair)
-{
-    return a.whole ? first_unit(a.tiles, pairs, pair) * a.chains : first_unit(a.units, pairs, pair);
-}
+// Where a role stands in its pair's work.  Whole tiles are dealt out one by one, pair after pair, so that the pairs walk
+// the summed index in step and read the same rows at the same time (16384 tokens, 4096 x 4096: 255 -> 230 us); cut ones
+// as runs.
+struct Walk : Cursor {
+    uint32_t pairs;
+    __device__ __forceinline__ Walk(const LinearArgs& a, uint32_t pairs_, uint32_t pair)
+        : Cursor(a, a.whole ? 0 : first_unit(a.units, pairs_, pair), a.whole ? 0 : first_unit(a.units, pairs_, pair + 1)), pairs(pairs_)
+    {
+        if (a.whole) {
+            part = 0;
+            unit = pair * a.chains;
+            enter_tile(a);
+        }
+    }
+    __device__ __forceinline__ void enter_tile(const LinearArgs& a)
+    {
+        if (unit >= a.units) {
+            part = 3;
+            return;
+        }
+        const uint32_t tile = unit / a.chains;
+        chain = 0;
+        stop = unit + a.chains;
+        tile_n = tile / a.tiles_k;
+        tile_k = tile - tile_n * a.tiles_k;
+    }
+    __device__ __forceinline__ void advance(const LinearArgs& a)
+    {
+        if (!a.whole) {
+            Cursor::advance(a);
+            return;
+        }
+        ++chain;
+        if (++unit == stop) {
+            unit += (pairs - 1) * a.chains;
+            enter_tile(a);
+        }
+    }
+};
 
 // ---- instructions ------------------------------------------------------------------------------------
+
+// An address in the shared memory of the pair's first block.
+__device__ __forceinline__ uint32_t address_in_first(uint32_t address)
+{
+    uint32_t remote;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(remote) : "r"(address));
+    return remote;
+}
+// Copies to this block's shared memory whose bytes count on a barrier of either block of the pair.
+__device__ __forceinline__ void copy_to_pair(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
+                 "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void copy_to_pair(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
+                 "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+                 : "memory");
+}
 
 // Codes with the summed index fast: rows of 128 bytes, eight rows 1024 bytes, 128-byte swizzle.  The same words describe
 // codes with the summed index slow: 128 rows m side by side, eight products 1024 bytes further.
@@ -119,12 +176,31 @@ __device__ __forceinline__ void multiply(uint32_t sum, uint64_t w, uint64_t t, u
                  "l"(w), "l"(t), "r"(instruction), "r"(w_steps), "r"(t_steps), "r"(accumulate)
                  : "memory");
 }
-__device__ __forceinline__ void load_eight_sums(uint32_t address, uint32_t (&r)[8])
+// N consecutive columns of tensor memory, 8 or 4 at a time; the caller waits for them.
+template <int N>
+__device__ __forceinline__ void load_sums(uint32_t address, float* r)
 {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                 : "r"(address)
-                 : "memory");
+    if constexpr (N >= 8) {
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7])
+                     : "r"(address)
+                     : "memory");
+        load_sums<N - 8>(address + 8, r + 8);
+    } else if constexpr (N == 4) {
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];"
+                     : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3])
+                     : "r"(address)
+                     : "memory");
+    }
+}
+// What was loaded may be used only after the wait.
+template <int N>
+__device__ __forceinline__ void wait_for_sums(float* r)
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        asm volatile("" : "+f"(r[i]));
 }
 
 // A thread's column of the result: one row m, consecutive tokens.
@@ -132,38 +208,70 @@ template <typename TO, int COUNT>
 __device__ __forceinline__ void write_column(const LinearArgs& a, int64_t t, int64_t m, float bias, const float (&sum)[COUNT])
 {
     TO* p = static_cast<TO*>(a.out) + t * a.out_stride + m;
-    const int count = (int)min((int64_t)COUNT, a.rows - t);
+    const int count = m < a.wide ? (int)min((int64_t)COUNT, a.rows - t) : 0;
 #pragma unroll
     for (int i = 0; i < COUNT; ++i, p += a.out_stride)
         if (i < count)
             store_from_float(p, TypeCode<TO>::value, 0, sum[i] + bias);
 }
+// The same with two elements per store: of two tokens, lanes of even rows take the first and those of odd rows the second,
+// both with their neighbour's element.  Every row and the result start on two elements.
+template <typename TO, int COUNT>
+__device__ __forceinline__ void write_pairs(const LinearArgs& a, int64_t t, int64_t m, float bias, const float (&sum)[COUNT])
+{
+    const int odd = threadIdx.x & 1;
+    const int count = m < a.wide ? (int)min((int64_t)COUNT, a.rows - t) - odd : 0;
+    TO* p = static_cast<TO*>(a.out) + (t + odd) * a.out_stride + (m - odd);
+    const int64_t step = 2 * a.out_stride;
+#pragma unroll
+    for (int i = 0; i < COUNT; i += 2, p += step) {
+        const float x = sum[i] + bias, y = sum[i + 1] + bias;
+        const float other = __shfl_xor_sync(0xffffffffu, odd ? x : y, 1);
+        const float low = odd ? other : x, high = odd ? y : other;
+        if (i < count) {
+            if constexpr (__is_same(TO, float))
+                *reinterpret_cast<float2*>(p) = make_float2(low, high);
+            else if constexpr (__is_same(TO, __half))
+                *reinterpret_cast<__half2*>(p) = __floats2half2_rn(low, high);
+            else
+                *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(low, high);
+        }
+    }
+}
+template <typename TO, int COUNT>
+__device__ __forceinline__ void write(const LinearArgs& a, int64_t t, int64_t m, const float (&sum)[COUNT])
+{
+    const float bias = a.bias && m < a.wide ? load_as_float(a.bias, a.bias_dtype, m) : 0.0f;
+    if (a.pairs_aligned)
+        write_pairs<TO>(a, t, m, bias, sum);
+    else
+        write_column<TO>(a, t, m, bias, sum);
+}
 
 // What a thread of the warps that sum leaves for its row and tokens where a wait of its block ran out: NaN, over whatever
 // it has left for any tile of the pair's run.
 template <int TOKENS>
-__device__ __noinline__ void leave_nan(const LinearArgs& a, uint32_t begin, uint32_t end, uint32_t pair, uint32_t rank,
-                                       uint32_t thread)
+__device__ __noinline__ void leave_nan(const LinearArgs& a, uint32_t pairs, uint32_t pair, uint32_t rank, uint32_t thread)
 {
-    constexpr int kHalfTokens = Shape<TOKENS>::kHalfTokens;
+    constexpr int kPartTokens = Shape<TOKENS>::kPartTokens;
     const float nan = __uint_as_float(0x7fc00000u);
-    const int row = 32 * ((thread >> 5) & 3) + (thread & 31), side = thread >> 7;
+    const int row = 32 * ((thread >> 5) & 3) + (thread & 31), part = thread >> 7;
     uint32_t chain_begin = 0;
     bool fresh = true;
-    for (Cursor c(a, begin, end); !c.done(); c.advance(a)) {
+    for (Walk c(a, pairs, pair); !c.done(); c.advance(a)) {
         if (fresh)
             chain_begin = c.chain;
         fresh = c.last_of_share(a);
         if (!fresh)
             continue;
         const int64_t m = (int64_t)c.tile_k * kTileRows + rank * kHalf + row;
-        const int64_t t = (int64_t)c.tile_n * TOKENS + side * kHalfTokens;
+        const int64_t t = (int64_t)c.tile_n * TOKENS + part * kPartTokens;
         if (chain_begin == 0 && c.chain + 1 == a.chains) {
-            for (int i = 0; i < kHalfTokens && m < a.wide && t + i < a.rows; ++i)
+            for (int i = 0; i < kPartTokens && m < a.wide && t + i < a.rows; ++i)
                 store_from_float(a.out, a.out_dtype, (t + i) * a.out_stride + m, nan);
         } else {
-            float* dst = a.slots + ((int64_t)(2 * pair + (c.part == 0 ? 1 : 0)) * 2 + rank) * TOKENS * kHalf + side * kHalfTokens * kHalf + row;
-            for (int i = 0; i < kHalfTokens; ++i)
+            float* dst = a.slots + ((int64_t)(2 * pair + (c.part == 0 ? 1 : 0)) * 2 + rank) * TOKENS * kHalf + part * kPartTokens * kHalf + row;
+            for (int i = 0; i < kPartTokens; ++i)
                 dst[i * kHalf] = nan;
         }
     }
@@ -175,27 +283,25 @@ __device__ __noinline__ void leave_nan(const LinearArgs& a, uint32_t begin, uint
 template <int TOKENS, bool GRAD>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kBlockThreads, 1)
 fp8_linear_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap token_map,
-                  const __grid_constant__ CUtensorMap weight_map)
+                  const __grid_constant__ CUtensorMap weight_map, const __grid_constant__ CUtensorMap token_step_map,
+                  const __grid_constant__ CUtensorMap weight_step_map)
 {
     using S = Shape<TOKENS>;
-    constexpr int kStages = S::kStages, kHalfTokens = S::kHalfTokens;
+    constexpr int kStages = S::kStages, kHalfTokens = S::kHalfTokens, kPartTokens = S::kPartTokens;
     extern __shared__ __align__(1024) unsigned char dynamic_shared[];
-    // landed: this block's codes of a step are there; multiplied: the tensor cores are done with the step; ready (first
-    // block): both blocks' codes and step bytes are there.  formed: a sum in tensor memory is complete; taken (first
-    // block): it has been read by both blocks.  finished: so are all multiplications that were ever issued.  nowhere:
-    // what threads that gave up arrive on.
-    __shared__ __align__(8) unsigned long long landed[kStages], multiplied[kStages], ready[kStages], formed[2], taken[2], finished,
-        nowhere[kStages];
+    // landed (first block): both blocks' codes and step bytes of a step are there; multiplied: the tensor cores are done with
+    // the step.  formed: a sum in tensor memory is complete; taken (first block): it has been read by both blocks.
+    // finished: so are all multiplications that were ever issued.  nowhere: what threads that gave up arrive on.
+    __shared__ __align__(8) unsigned long long landed[kStages], multiplied[kStages], formed[2], taken[2], finished, nowhere[2];
     __shared__ uint32_t tensor_memory_slot;
     __shared__ volatile uint32_t gave_up;        // some wait of this block ran out
 
     start_next_kernel();             // the join; it waits for this kernel's end by itself
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const uint32_t unit_begin = run_begin(a, pairs, pair), unit_end = run_begin(a, pairs, pair + 1);
     const uint32_t stage0 = (shared_address(dynamic_shared) + 1023u) & ~1023u;
     const uint32_t scales0 = stage0 + kStages * S::kStageBytes;
-    const uint32_t landed0 = shared_address(landed), ready0 = shared_address(ready), multiplied0 = shared_address(multiplied);
+    const uint32_t landed0 = shared_address(landed), multiplied0 = shared_address(multiplied);
     const uint32_t formed0 = shared_address(formed), taken0 = shared_address(taken);
     const uint32_t finished0 = shared_address(&finished), nowhere0 = shared_address(nowhere);
 
@@ -206,12 +312,11 @@ fp8_linear_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ 
         for (int s = 0; s < kStages; ++s) {
             init(landed0 + 8 * s, 1, ADASUM_HAND_OVER_LANDED);
             init(multiplied0 + 8 * s, 1, ADASUM_HAND_OVER_MULTIPLIED);
-            init(ready0 + 8 * s, 2, ADASUM_HAND_OVER_READY);
-            barrier_init(nowhere0 + 8 * s, 1);
         }
         for (int s = 0; s < 2; ++s) {
             init(formed0 + 8 * s, 1, ADASUM_HAND_OVER_FORMED);
             init(taken0 + 8 * s, 2 * kSumWarps, ADASUM_HAND_OVER_TAKEN);
+            barrier_init(nowhere0 + 8 * s, 1);
         }
         barrier_init(finished0, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -225,6 +330,8 @@ fp8_linear_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ 
     if (warp == kCopyWarp && lane == 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&token_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&weight_map) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&token_step_map) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&weight_step_map) : "memory");
     }
     __syncthreads();
     cluster_barrier();
@@ -239,11 +346,11 @@ fp8_linear_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ 
 
     // After a wait of this thread ran out it neither waits nor acts for its warp any more (arrives, multiplies, commits).
     bool waiting = true;
-    uint32_t ready_at = ready0, taken_at = taken0;
+    uint32_t taken_at = taken0;
     auto wait_up_to = [&](uint32_t bar, uint32_t parity, long long cycles) {
         if (waiting && !wait_phase(bar, parity, cycles)) {
             waiting = false;
-            ready_at = taken_at = nowhere0;
+            taken_at = nowhere0;
             gave_up = 1;
             atomicExch(a.status + blockIdx.x, (int)ADASUM_DEVICE_TIMEOUT);
         }
@@ -251,96 +358,106 @@ fp8_linear_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ 
     auto wait = [&](uint32_t bar, uint32_t parity) { wait_up_to(bar, parity, a.wait_cycles); };
 
     if (warp < kSumWarps) {
-        // ---- sums: warp w reads tensor-memory lanes 32 (w % 4) .. + 31 (rows m), one half of the tokens
-        const int quarter = warp & 3, side = warp >> 2;
-        float sum[kHalfTokens];
+        // ---- sums: warp w reads tensor-memory lanes 32 (w % 4) .. + 31 (rows m) of a quarter of the tokens
+        const int quarter = warp & 3, part = warp >> 2;
+        float sum[kPartTokens];
         uint32_t count = 0, chain_begin = 0;
         bool fresh = true;                       // the next unit is the first of its tile's share
-        for (Cursor c(a, unit_begin, unit_end); !c.done(); c.advance(a), ++count) {
-            if (fresh) {
-                fresh = false;
+        for (Walk c(a, pairs, pair); !c.done(); c.advance(a), ++count) {
+            if (fresh)
                 chain_begin = c.chain;
-#pragma unroll
-                for (int i = 0; i < kHalfTokens; ++i)
-                    sum[i] = 0.0f;
-            }
             wait(formed0 + 8 * (count & 1), (count >> 1) & 1);
             __syncwarp();
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t source = tensor_memory + (count & 1) * S::kSumColumns + side * kHalfTokens + ((uint32_t)(32 * quarter) << 16);
+            const uint32_t source = tensor_memory + (count & 1) * S::kSumColumns + part * kPartTokens + ((uint32_t)(32 * quarter) << 16);
+            if (fresh) {
+                load_sums<kPartTokens>(source, sum);
+                wait_for_sums<kPartTokens>(sum);
+            } else {
+                constexpr int kBatch = 16;
 #pragma unroll
-            for (int g = 0; g < kHalfTokens / 8; ++g) {
-                uint32_t r[8];
-                load_eight_sums(source + 8 * g, r);
-                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                for (int g = 0; g < kPartTokens; g += kBatch) {
+                    float r[kBatch];
+                    load_sums<kBatch>(source + g, r);
+                    wait_for_sums<kBatch>(r);
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    sum[8 * g + i] += __uint_as_float(r[i]);
+                    for (int i = 0; i < kBatch; ++i)
+                        sum[g + i] += r[i];
+                }
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
             if (lane == 0)
                 arrive_at_first(taken_at + 8 * (count & 1));
 
-            if (!c.last_of_share(a))
+            fresh = c.last_of_share(a);
+            if (!fresh)
                 continue;
-            fresh = true;
             // ---- the pair's last unit of this tile: the result, or this pair's part of it
             const int row = 32 * quarter + lane;
             if (chain_begin == 0 && c.chain + 1 == a.chains) {
                 const int64_t m = (int64_t)c.tile_k * kTileRows + rank * kHalf + row;
-                const int64_t t = (int64_t)c.tile_n * TOKENS + side * kHalfTokens;
-                if (m < a.wide) {
-                    const float bias = a.bias ? load_as_float(a.bias, a.bias_dtype, m) : 0.0f;
-                    if (a.out_dtype == ADASUM_F32)
-                        write_column<float>(a, t, m, bias, sum);
-                    else if (a.out_dtype == ADASUM_F16)
-                        write_column<__half>(a, t, m, bias, sum);
-                    else
-                        write_column<__nv_bfloat16>(a, t, m, bias, sum);
-                }
+                const int64_t t = (int64_t)c.tile_n * TOKENS + part * kPartTokens;
+                if (a.out_dtype == ADASUM_F32)
+                    write<float>(a, t, m, sum);
+                else if (a.out_dtype == ADASUM_F16)
+                    write<__half>(a, t, m, sum);
+                else
+                    write<__nv_bfloat16>(a, t, m, sum);
             } else {
-                float* dst = a.slots + ((int64_t)(2 * pair + (c.part == 0 ? 1 : 0)) * 2 + rank) * TOKENS * kHalf + side * kHalfTokens * kHalf + row;
+                float* dst = a.slots + ((int64_t)(2 * pair + (c.part == 0 ? 1 : 0)) * 2 + rank) * TOKENS * kHalf + part * kPartTokens * kHalf + row;
 #pragma unroll
-                for (int i = 0; i < kHalfTokens; ++i)
+                for (int i = 0; i < kPartTokens; ++i)
                     dst[i * kHalf] = sum[i];
             }
         }
         if (gave_up != 0)
-            leave_nan<TOKENS>(a, unit_begin, unit_end, pair, rank, threadIdx.x);
+            leave_nan<TOKENS>(a, pairs, pair, rank, threadIdx.x);
         // The last commit arrives in both blocks, and each waits for its own: in this warp, which has just seen the last sum.
         if (warp == 0) {
             waiting = true;
             wait_up_to(finished0, 0, kLastWait * a.wait_cycles);
         }
     } else if (warp == kCopyWarp) {
-        // ---- copies of this block's rows of the weights, and of its half of the tokens
+        // ---- copies of this block's rows of the weights and of its half of the tokens, and of the step bytes of both.
+        // Both blocks' copies count on the first block's barrier, which expects their bytes.
         Ring<kStages> ring;
         uint32_t issued = 0;
-        for (Cursor c(a, unit_begin, unit_end); !c.done() && waiting; c.advance(a)) {
+        constexpr uint32_t kBytes = 2 * (S::kStageBytes + S::kScaleBytes);
+        const uint32_t first_landed0 = address_in_first(landed0);
+        for (Walk c(a, pairs, pair); !c.done() && waiting; c.advance(a)) {
             const int m = (int)(c.tile_k * kTileRows + rank * kHalf), t = (int)(c.tile_n * TOKENS + rank * kHalfTokens);
+            const int m_block = (int)(c.tile_k * 2 + rank), t_block = (int)((int64_t)c.tile_n * TOKENS / kFp8Block);
             const uint32_t end = c.first_step(a) + c.steps(a);
             for (uint32_t step = c.first_step(a); step < end; ++step) {
-                const uint32_t bar = landed0 + 8 * ring.stage;
                 wait(multiplied0 + 8 * ring.stage, ring.phase ^ 1);
                 waiting = __all_sync(0xffffffffu, waiting);
                 if (!waiting)
                     break;
-                const uint32_t dst = stage0 + ring.stage * S::kStageBytes;
-                const int s = (int)(step * kDepth);
+                const uint32_t dst = stage0 + ring.stage * S::kStageBytes, steps = scales0 + ring.stage * S::kScaleBytes;
+                const uint32_t bar = first_landed0 + 8 * ring.stage;
+                const int s = (int)step;
                 if (elected()) {
-                    expect_bytes(bar, S::kStageBytes);
-                    copy_box(dst, &weight_map, GRAD ? m : s, GRAD ? s : m, bar);
-                    copy_box(dst + kWeightBytes, &token_map, s, t, bar);
+                    if (rank == 0)
+                        expect_bytes(landed0 + 8 * ring.stage, kBytes);
+                    copy_to_pair(dst, &weight_map, GRAD ? m : s * kDepth, GRAD ? s * kDepth : m, bar);
+                    copy_to_pair(dst + kWeightBytes, &token_map, s * kDepth, t, bar);
+                    // the words of all rows of a block of the weights are the same: they serve either direction
+                    copy_to_pair(steps, &weight_step_map, 0, GRAD ? m_block : s, GRAD ? s : m_block, bar);
+#pragma unroll
+                    for (int i = 0; i < S::kRowBlocks; ++i)
+                        copy_to_pair(steps + (1 + i) * kFp8StepBytes, &token_step_map, 0, s, t_block + i, bar);
                 }
                 __syncwarp();
                 ++issued;
                 ring.advance();
             }
         }
-        // nothing may still be on its way into shared memory when the block ends
+        // Nothing may still be on its way into shared memory when the blocks end.  The first block's barrier counts both
+        // blocks' copies; where the blocks issued different numbers, some wait has run out since, a thousand times the
+        // copies' time ago.
         waiting = true;
-        for (uint32_t back = min(issued, (uint32_t)kStages); back > 0; --back) {
+        for (uint32_t back = rank == 0 ? min(issued, (uint32_t)kStages) : 0; back > 0; --back) {
             const uint32_t step = issued - back;
             wait(landed0 + 8 * (step % kStages), (step / kStages) & 1);
         }
@@ -348,108 +465,44 @@ fp8_linear_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ 
         // ---- multiplications: e4m3 codes, steps as powers of two, fp32 sums, 256 x TOKENS
         constexpr uint32_t kInstruction = ((GRAD ? 1u : 0u) << 15) | ((uint32_t)(TOKENS >> 3) << 17) | (1u << 23) |
                                           ((uint32_t)(kTileRows >> 4) << 24);
-        Ring<kStages> ring;
-        uint32_t count = 0, turn = 0;
-        for (Cursor c(a, unit_begin, unit_end); !c.done(); c.advance(a), ++count) {
-            const uint32_t target = tensor_memory + (count & 1) * S::kSumColumns;
-            wait(taken0 + 8 * (count & 1), ((count >> 1) & 1) ^ 1);
-            uint32_t accumulate = 0;
-            for (uint32_t steps = c.steps(a); steps > 0; --steps) {
-                wait(ready0 + 8 * ring.stage, ring.phase);
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t codes = stage0 + ring.stage * S::kStageBytes, scales = scales0 + ring.stage * kScaleBytes;
-                const uint64_t w = codes_descriptor(codes), t = codes_descriptor(codes + kWeightBytes), b = steps_descriptor(scales);
-                const uint32_t w_steps = tensor_memory + S::kScaleAt + (turn & 1) * S::kSumColumns, t_steps = w_steps + 4;
-                if (elected() && waiting) {
-                    copy_steps(w_steps, b);
-                    copy_steps(t_steps, b + (kFp8StepBytes >> 4));
-                    if (TOKENS > 128)
-                        copy_steps(t_steps + 4, b + 2 * (kFp8StepBytes >> 4));
+        // One thread does all of it: what it spends per step must stay below the multiplications' 384 cycles.
+        if (elected()) {
+            Ring<kStages> ring;
+            uint32_t count = 0, turn = 0;
+            const uint64_t codes0 = codes_descriptor(stage0), steps0 = steps_descriptor(scales0);
+            for (Walk c(a, pairs, pair); !c.done(); c.advance(a), ++count) {
+                const uint32_t target = tensor_memory + (count & 1) * S::kSumColumns;
+                const uint32_t offset = (c.tile_n * TOKENS % kFp8Block) / 32;        // columns of 32 tokens each
+                wait(taken0 + 8 * (count & 1), ((count >> 1) & 1) ^ 1);
+                uint32_t accumulate = 0;
+                for (uint32_t steps = c.steps(a); steps > 0; --steps) {
+                    wait(landed0 + 8 * ring.stage, ring.phase);
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    if (waiting) {
+                        const uint64_t w = codes0 + ring.stage * (S::kStageBytes >> 4), t = w + (kWeightBytes >> 4);
+                        const uint64_t b = steps0 + ring.stage * (S::kScaleBytes >> 4);
+                        const uint32_t w_steps = tensor_memory + S::kScaleAt + (turn & 1) * S::kSumColumns, t_steps = w_steps + 4;
+                        copy_steps(w_steps, b);
+                        copy_steps(t_steps, b + (kFp8StepBytes >> 4));
+                        if (S::kRowBlocks > 1)
+                            copy_steps(t_steps + 4, b + 2 * (kFp8StepBytes >> 4));
 #pragma unroll
-                    for (int s = 0; s < kDepth / 32; ++s)
-                        // 32 products are 32 bytes further on, or 32 rows of 128 bytes (in units of 16)
-                        multiply(target, w + (GRAD ? 256 : 2) * s, t + 2 * s, kInstruction, w_steps, t_steps, s > 0 ? 1u : accumulate);
-                    commit_to_both(multiplied0 + 8 * ring.stage);
-                    if (steps == 1)
-                        commit_to_both(formed0 + 8 * (count & 1));
-                }
-                __syncwarp();
-                accumulate = 1;
-                ++turn;
-                ring.advance();
-            }
-        }
-        if (elected())
-            commit_to_both(finished0);
-        __syncwarp();
-    } else if (warp == kStepWarp) {
-        // ---- step bytes: a lane brings those of rows and tokens 32 j + lane, kBatch steps ahead of their use.  Rows beyond the
-        // matrices take 2^0: their codes are zeros or their results are not stored.
-        constexpr int kBatch = 4, kColumns = (TOKENS + 31) / 32;
-        constexpr uint32_t kOne = 0x7f7f7f7fu;
-        uint32_t words[kBatch][kColumns], weight_words[kBatch];
-        Ring<kStages> ring;
-        auto load = [&](const Cursor& c, uint32_t from) {
-            const int64_t first = (int64_t)c.first_step(a) + from;
-            const int64_t m_block = (int64_t)c.tile_k * 2 + rank;
-            const uint32_t left = c.steps(a) - from;
-#pragma unroll
-            for (int j = 0; j < kBatch; ++j) {
-                const int64_t s = first + j;
-                const int64_t block_row = GRAD ? s : m_block, block_column = GRAD ? m_block : s;
-                weight_words[j] = kOne;
-                if ((uint32_t)j < left && block_row < a.weight_row_blocks && block_column < a.weight_blocks)
-                    weight_words[j] = __ldg(reinterpret_cast<const uint32_t*>(
-                        a.weight_steps + (block_row * a.weight_blocks + block_column) * kFp8StepBytes));
-            }
-#pragma unroll
-            for (int i = 0; i < kColumns; ++i) {
-                const int64_t t = (int64_t)c.tile_n * TOKENS + 32 * i + lane;
-                const uint8_t* p = a.token_steps + fp8_step_at(t, first, a.depth_blocks);
-                const bool in = t < a.rows && 32 * i + lane < TOKENS;
-#pragma unroll
-                for (int j = 0; j < kBatch; ++j)
-                    words[j][i] = in && (uint32_t)j < left ? __ldg(reinterpret_cast<const uint32_t*>(p + j * kFp8StepBytes)) : kOne;
-            }
-        };
-        Cursor c(a, unit_begin, unit_end);
-        uint32_t from = 0;               // first step of the batch within the unit
-        if (!c.done())
-            load(c, from);
-        while (!c.done()) {
-            uint32_t now[kBatch][8], weight_now[kBatch];
-#pragma unroll
-            for (int j = 0; j < kBatch; ++j) {
-                weight_now[j] = weight_words[j];
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    now[j][i] = i < kColumns ? words[j][i < kColumns ? i : 0] : kOne;
-            }
-            const int steps = (int)min((uint32_t)kBatch, c.steps(a) - from);
-            from += kBatch;
-            if (from >= c.steps(a)) {
-                from = 0;
-                c.advance(a);
-            }
-            if (!c.done())
-                load(c, from);
-#pragma unroll
-            for (int j = 0; j < kBatch; ++j) {
-                if (j < steps) {
-                    wait(landed0 + 8 * ring.stage, ring.phase);      // so the stage's last multiplications are done, too
-                    const uint32_t dst = scales0 + ring.stage * kScaleBytes + 16 * lane;
-                    store_shared_16B(dst, make_uint4(weight_now[j], weight_now[j], weight_now[j], weight_now[j]));
-                    store_shared_16B(dst + kFp8StepBytes, make_uint4(now[j][0], now[j][1], now[j][2], now[j][3]));
-                    if (kColumns > 4)
-                        store_shared_16B(dst + 2 * kFp8StepBytes, make_uint4(now[j][4], now[j][5], now[j][6], now[j][7]));
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0)
-                        arrive_at_first(ready_at + 8 * ring.stage);
+                        for (int s = 0; s < kDepth / 32; ++s)
+                            // 32 products are 32 bytes further on, or 32 rows of 128 bytes (in units of 16)
+                            multiply(target, w + (GRAD ? 256 : 2) * s, t + 2 * s, kInstruction, w_steps, t_steps + offset,
+                                     s > 0 ? 1u : accumulate);
+                        commit_to_both(multiplied0 + 8 * ring.stage);
+                        if (steps == 1)
+                            commit_to_both(formed0 + 8 * (count & 1));
+                    }
+                    accumulate = 1;
+                    ++turn;
                     ring.advance();
                 }
             }
+            commit_to_both(finished0);
         }
+        __syncwarp();
     }
     __syncwarp();
     // Neither block may end, nor free its tensor memory, while the other still multiplies or arrives here: both have
@@ -536,11 +589,11 @@ struct Work {
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to; }
 
 // Tokens of a tile.  The smaller tiles are for few tokens, and for counts that fill the largest badly: a step costs
-// shared memory 132, 96 and 80 cycles for 240, 128 and 64 tokens.
+// shared memory 448, 384 and 320 cycles for 192, 128 and 64 tokens.
 int tile_tokens(int64_t rows)
 {
-    const int64_t cost[3] = {up(rows, 240) * 132, up(rows, 128) * 96, up(rows, 64) * 80};
-    return cost[2] <= cost[1] && cost[2] <= cost[0] ? 64 : cost[1] <= cost[0] ? 128 : 240;
+    const int64_t cost[3] = {up(rows, 192) * 448, up(rows, 128) * 384, up(rows, 64) * 320};
+    return cost[2] <= cost[1] && cost[2] <= cost[0] ? 64 : cost[1] <= cost[0] ? 128 : 192;
 }
 
 // `most`: pairs that run at once.
@@ -578,7 +631,7 @@ size_t linear_workspace(int64_t rows, int64_t wide, int64_t depth)
 {
     if (rows == 0 || wide == 0 || depth == 0)
         return kStatusBytes;
-    const int64_t tokens = rows <= 64 ? 64 : rows <= 128 ? 128 : 240;
+    const int64_t tokens = rows <= 64 ? 64 : rows <= 128 ? 128 : 192;
     const int64_t tiles = up(rows, 64) * up(wide, kTileRows);
     const int64_t pairs = tiles >= kMaxPairs || tiles * up(depth, kDepth) >= kMaxPairs ? kMaxPairs : tiles * up(depth, kDepth);
     return kStatusBytes + (size_t)(pairs * 2 * kTileRows * tokens) * sizeof(float);
@@ -632,7 +685,7 @@ void with_shape(int tokens, bool grad, F&& f)
         else if (tokens == 128)
             f(Number<128>{}, g);
         else
-            f(Number<240>{}, g);
+            f(Number<192>{}, g);
     };
     if (grad)
         with_tokens(Number<1>{});
@@ -651,6 +704,22 @@ adasum_status_t describe_codes(CUtensorMap* map, const void* codes, int64_t widt
                                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                                 CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return err == CUDA_SUCCESS ? ADASUM_OK : fail(ADASUM_ERR_CUDA, "tensor map of packed codes: error %d", (int)err);
+}
+
+// Step bytes: [row block][column block][512 bytes].
+adasum_status_t describe_steps(CUtensorMap* map, const void* steps, int64_t columns, int64_t rows)
+{
+    EncodeTiled encode = encode_tiled();
+    if (!encode)
+        return fail(ADASUM_ERR_CUDA, "the driver has no tensor map encoder");
+    const cuuint64_t blocks = (cuuint64_t)fp8_blocks(columns);
+    const cuuint64_t dims[3] = {kFp8StepBytes / 4, blocks, (cuuint64_t)fp8_blocks(rows)};
+    const cuuint64_t strides[2] = {kFp8StepBytes, blocks * kFp8StepBytes};
+    const cuuint32_t box[3] = {kFp8StepBytes / 4, 1, 1}, unit[3] = {1, 1, 1};
+    const CUresult err = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void*>(steps), dims, strides, box, unit,
+                                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+                                CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return err == CUDA_SUCCESS ? ADASUM_OK : fail(ADASUM_ERR_CUDA, "tensor map of step bytes: error %d", (int)err);
 }
 
 adasum_status_t linear(const void* x, const void* w, int64_t rows, int64_t features, int64_t outputs, const void* bias,
@@ -701,6 +770,7 @@ adasum_status_t linear(const void* x, const void* w, int64_t rows, int64_t featu
     a.out_stride = out_stride;
     a.out_dtype = (int)out_dtype;
     a.status = static_cast<int*>(workspace);
+    a.pairs_aligned = wide % 2 == 0 && out_stride % 2 == 0 && aligned_to(out, 2 * operator_bytes(out_dtype));
     if (depth == 0) {
         const uint64_t elements = (uint64_t)rows * (uint64_t)wide, blocks = (elements + 255) / 256;
         if (blocks > 0x7fffffffu)
@@ -717,17 +787,16 @@ adasum_status_t linear(const void* x, const void* w, int64_t rows, int64_t featu
     const Work l = plan_work(rows, wide, depth, most);
     const uint8_t* token_codes = static_cast<const uint8_t*>(x);
     const uint8_t* weight_codes = static_cast<const uint8_t*>(w);
-    CUtensorMap token_map, weight_map;
+    CUtensorMap token_map, weight_map, token_step_map, weight_step_map;
     status = describe_codes(&token_map, token_codes, fp8_width(depth), rows, tokens / 2);
     if (status == ADASUM_OK)
         status = describe_codes(&weight_map, weight_codes, fp8_width(features), outputs, kHalf);
+    if (status == ADASUM_OK)
+        status = describe_steps(&token_step_map, token_codes + rows * fp8_width(depth), depth, rows);
+    if (status == ADASUM_OK)
+        status = describe_steps(&weight_step_map, weight_codes + outputs * fp8_width(features), features, outputs);
     if (status != ADASUM_OK)
         return status;
-    a.token_steps = token_codes + rows * fp8_width(depth);
-    a.weight_steps = weight_codes + outputs * fp8_width(features);
-    a.depth_blocks = fp8_blocks(depth);
-    a.weight_blocks = fp8_blocks(features);
-    a.weight_row_blocks = fp8_blocks(outputs);
     a.tiles_k = l.tiles_k;
     a.tiles = l.tiles;
     a.iterations = l.iterations;
@@ -742,7 +811,7 @@ adasum_status_t linear(const void* x, const void* w, int64_t rows, int64_t featu
     with_shape(tokens, grad, [&](auto t, auto g) {
         constexpr int TOKENS = decltype(t)::value;
         err = launch_after(fp8_linear_kernel<TOKENS, decltype(g)::value != 0>, dim3(2 * l.pairs), kBlockThreads,
-                           Shape<TOKENS>::kSharedBytes, stream, a, token_map, weight_map);
+                           Shape<TOKENS>::kSharedBytes, stream, a, token_map, weight_map, token_step_map, weight_step_map);
     });
     ADASUM_CUDA_CHECK(err);
     profile_mark(stream, ADASUM_KERNEL_FP8_LINEAR, 0, 0, false);
@@ -791,7 +860,8 @@ adasum_status_t adasum_fp8_linear_selftest(const void* x, const void* w, int64_t
 {
     using namespace adasum;
     clear_error();
-    if (hand_over < ADASUM_HAND_OVER_LANDED || hand_over > ADASUM_HAND_OVER_TAKEN || hand_over == ADASUM_HAND_OVER_ADDED)
+    if (hand_over < ADASUM_HAND_OVER_LANDED || hand_over > ADASUM_HAND_OVER_TAKEN || hand_over == ADASUM_HAND_OVER_ADDED ||
+        hand_over == ADASUM_HAND_OVER_READY)
         return fail(ADASUM_ERR_ARG, "unknown hand-over %d", (int)hand_over);
     return linear(x, w, rows, features, outputs, nullptr, out_dtype, y, y_stride, out_dtype, workspace, workspace_bytes, false,
                   stream_ptr, hand_over);

@@ -107,7 +107,7 @@ def test_blocks_that_are_not_numbers(b):
 
 SHAPES = [  # rows, features, outputs
     (1, 1, 1), (1, 1024, 4096), (2, 130, 7), (37, 1024, 4096), (64, 128, 256), (65, 129, 257), (128, 1000, 300), (129, 260, 120),
-    (240, 256, 256), (241, 384, 512), (333, 1000, 257), (480, 2048, 130), (700, 64, 1030), (1000, 5000, 200), (300, 40, 9000),
+    (192, 256, 256), (193, 384, 512), (240, 256, 256), (384, 640, 256), (576, 300, 300), (333, 1000, 257), (480, 2048, 130), (700, 64, 1030), (1000, 5000, 200), (300, 40, 9000),
     (17, 16500, 33), (2049, 1024, 1024), (5, 8200, 8200)]
 
 
@@ -262,8 +262,8 @@ def test_captured_products_on_two_streams(b):
 
 # More sums per pair of blocks than tensor memory holds, and more steps than shared memory, so that every kind of
 # hand-over is waited for.
-@pytest.mark.parametrize("rows", [40, 128, 480])
-@pytest.mark.parametrize("hand_over", ["landed", "multiplied", "ready", "formed", "taken"])
+@pytest.mark.parametrize("rows", [40, 128, 384])
+@pytest.mark.parametrize("hand_over", ["landed", "multiplied", "formed", "taken"])
 def test_a_wait_that_runs_out(b, hand_over, rows):
     features, outputs = 128 * 8 * 4 * 74, 24
     gen = _gen(8)
@@ -281,6 +281,6 @@ def test_a_wait_that_runs_out(b, hand_over, rows):
     b.adasum_fp8_linear_selftest(hand_over, px, pw, rows, features, outputs, y, ws)
     assert b.adasum_fp8_linear_status(ws) == 7
     assert "bounded wait" in b.adasum_last_error()
-    if hand_over in ("landed", "ready", "formed"):           # they fail in the first sum
+    if hand_over in ("landed", "formed"):           # they fail in the first sum
         assert torch.isnan(y).all()
     assert torch.equal(good(), want)
