@@ -69,13 +69,21 @@ __device__ __forceinline__ void random_words(const Dropout& d, uint64_t seed, co
     }
 }
 
-// x of a vector with its dropped elements replaced by zero (whatever they hold) and the others scaled.
+// x of a vector with its dropped elements replaced by zero (whatever they hold) and the others scaled.  16 bits are
+// compared as the upper half of a word; what the lower half holds makes no difference.
 __device__ __forceinline__ void drop(const Dropout& d, const uint32_t (&word)[4], float (&x)[8])
 {
+    const uint32_t limit = d.threshold << 16;
+    if (d.threshold >= 65536u) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            x[i] = 0.0f;
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const uint32_t bits = i & 1 ? word[i / 2] >> 16 : word[i / 2] & 0xffffu;
-        x[i] = bits >= d.threshold ? x[i] * d.factor : 0.0f;
+        const uint32_t bits = i & 1 ? word[i / 2] : word[i / 2] << 16;
+        x[i] = bits >= limit ? x[i] * d.factor : 0.0f;
     }
 }
 
