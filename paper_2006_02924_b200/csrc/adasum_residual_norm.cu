@@ -9,7 +9,7 @@ template <typename T, typename R, bool WHOLE, bool FULL, int V>
 __global__ void __maxnreg__(V == 1 ? 64 : 80)
 residual_norm_kernel(const __grid_constant__ NormArgs a)
 {
-    constexpr int ROWS = V == 1 ? 2 : 1;
+    constexpr int ROWS = WHOLE ? 1 : 2;
     extern __shared__ __align__(16) unsigned char rows_shared[];
     __shared__ Exchange exchange;
     Member m(a.deal);
@@ -20,7 +20,7 @@ residual_norm_kernel(const __grid_constant__ NormArgs a)
         count[v] = m.count(v, a.features);
     Staged staged = stage_vectors(a, m, rows_shared, ROWS, V);
     const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(rows_shared)) + a.rows_at + threadIdx.x * 16;
-    const uint32_t stage_bytes = a.turn_pieces * blockDim.x * 16;
+    const uint32_t apart = blockDim.x * 16, stage_bytes = a.turn_pieces * apart;
     auto first_row = [&](uint32_t round) { return ((int64_t)round * a.deal.groups + m.group) * ROWS; };
     auto bring = [&](uint32_t round, uint32_t stage) {
         if (round < a.deal.rounds) {
@@ -29,16 +29,10 @@ residual_norm_kernel(const __grid_constant__ NormArgs a)
             for (int u = 0; u < ROWS; ++u) {
                 const int64_t row = first_row(round) + u;
                 const bool valid = row < a.rows;
-                if (a.x) {
-#pragma unroll
-                    for (int v = 0; v < V; ++v)
-                        fetch<T>(slot, a.x, row * a.x_stride + m.column(v), valid && count[v] > 0);
-                }
-                if (a.residual) {
-#pragma unroll
-                    for (int v = 0; v < V; ++v)
-                        fetch<R>(slot, a.residual, row * a.residual_stride + m.column(v), valid && count[v] > 0);
-                }
+                if (a.x)
+                    fetch_row<T>(slot, apart, a.x, row * a.x_stride + m.column(0), m.members, valid, count);
+                if (a.residual)
+                    fetch_row<R>(slot, apart, a.residual, row * a.residual_stride + m.column(0), m.members, valid, count);
             }
         }
         close_turn();
@@ -50,7 +44,7 @@ residual_norm_kernel(const __grid_constant__ NormArgs a)
     uint64_t seed = 0;
     if (a.drop.seed)
         seed = __ldg(reinterpret_cast<const unsigned long long*>(a.drop.seed));
-    const uint32_t r_piece = a.x ? V * sizeof(T) / 2 : 0;      // place of the residual among the thread's pieces of a row
+    const uint32_t r_piece = a.x ? V * (uint32_t)(sizeof(T) / 2) * apart : 0;      // place of the residual among the thread's pieces of a row
     uint32_t stage = 0;
     for (uint32_t round = 0; round < a.deal.rounds; ++round) {
         int64_t row[ROWS];
@@ -64,8 +58,7 @@ residual_norm_kernel(const __grid_constant__ NormArgs a)
         auto row_of = [&](auto t, const void* base, int64_t stride, uint32_t piece, int u, int v) {
             using E = decltype(t);
             if constexpr (WHOLE) {
-                uint32_t at = slot + (piece + v * (uint32_t)(sizeof(E) / 2) + u * a.turn_pieces / ROWS) * (blockDim.x * 16);
-                return decode(fetched<E>(at));
+                return decode(fetched<E>(slot + piece + v * (uint32_t)(sizeof(E) / 2) * apart + u * (stage_bytes / ROWS), apart));
             } else {
                 return decode(load_vector<false>(static_cast<const E*>(base) + row[u] * stride + m.column(v), row[u] < a.rows ? count[v] : 0));
             }
@@ -246,10 +239,12 @@ adasum_status_t adasum_residual_norm(const adasum_residual_norm_t* b, const void
         a.post_weight = a.post_bias = Vector{};
     if (!pre)
         a.pre_weight = a.pre_bias = Vector{};
-    const bool four = vec && features > 128;   // four vectors per thread, where that leaves a row eight threads or more
+    // several vectors per thread, where that leaves a row four threads or more: what is spent per thread and row falls; two beside
+    // a norm after the block, so that wide rows leave room for a turn ahead
+    const bool four = vec && features > 128;
     unsigned blocks;
-    const int per_processor = four ? plan_blocks(&a, vec, 4, (int)((x ? tb / 2 : 0) + (residual ? rb / 2 : 0)), 768, {512, 256})
-                                   : plan_blocks(&a, vec, 1, (int)((x ? tb / 2 : 0) + (residual ? rb / 2 : 0)), 1024, {512, 256});
+    const int per_processor = four ? plan_blocks(&a, vec, full ? 2 : 4, 1, (int)((x ? tb / 2 : 0) + (residual ? rb / 2 : 0)), 768, {512, 256})
+                                   : plan_blocks(&a, vec, 1, vec ? 1 : 2, (int)((x ? tb / 2 : 0) + (residual ? rb / 2 : 0)), 1024, {512, 256});
     if (per_processor == 0)
         return fail(ADASUM_ERR_ARG, "%lld features are too many", (long long)features);
     plan_units(rows, rows, false, (int64_t)per_processor * sms, &a.deal, &blocks);
@@ -261,7 +256,7 @@ adasum_status_t adasum_residual_norm(const adasum_residual_norm_t* b, const void
         using T = decltype(t);
         using R = decltype(r);
         auto* kernel = !vec   ? residual_norm_kernel<T, R, false, true, 1>
-                       : four ? full ? residual_norm_kernel<T, R, true, true, 4> : residual_norm_kernel<T, R, true, false, 4>
+                       : four ? full ? residual_norm_kernel<T, R, true, true, 2> : residual_norm_kernel<T, R, true, false, 4>
                               : residual_norm_kernel<T, R, true, true, 1>;
         err = launch_rows(kernel, blocks, a, shared, stream);
     });

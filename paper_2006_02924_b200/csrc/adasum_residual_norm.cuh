@@ -224,10 +224,13 @@ __device__ __forceinline__ void group_sum(Member& m, Exchange& e, float (&v)[N])
 {
     const Deal& d = m.deal;
     if (d.warps == 1) {
-        for (int step = d.lanes >> 1; step > 0; step >>= 1) {
 #pragma unroll
-            for (int n = 0; n < N; ++n)
-                v[n] += __shfl_xor_sync(0xffffffffu, v[n], step);
+        for (int step = 16; step > 0; step >>= 1) {
+            if (step < d.lanes) {
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+                    v[n] += __shfl_xor_sync(0xffffffffu, v[n], step);
+            }
         }
         return;
     }
@@ -290,26 +293,30 @@ __device__ __forceinline__ void group_sum(Member& m, Exchange& e, float (&v)[N])
 //
 // Shared memory holds [stage][vector of the turn][thread] pieces of 16 bytes.
 
-// Eight elements to this thread's pieces; zeros without an access where not `valid`.
-template <typename T>
-__device__ __forceinline__ void fetch(uint32_t& slot, const void* base, int64_t at, bool valid)
+// A row's vectors to this thread's pieces, `apart` bytes between pieces; zeros without an access where there is nothing.
+template <typename T, int V>
+__device__ __forceinline__ void fetch_row(uint32_t& slot, uint32_t apart, const void* base, int64_t at, int members, bool valid,
+                                          const int (&count)[V])
 {
-    const char* p = reinterpret_cast<const char*>(static_cast<const T*>(base) + (valid ? at : 0));
+    const char* p = reinterpret_cast<const char*>(static_cast<const T*>(base) + at);
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) {
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(slot), "l"(p + 16 * i), "r"(valid ? 16 : 0) : "memory");
-        slot += blockDim.x * 16;
+    for (int v = 0; v < V; ++v) {
+        const int bytes = valid && count[v] > 0 ? 16 : 0;
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(T) / 2); ++i) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(slot), "l"(p + 16 * i), "r"(bytes) : "memory");
+            slot += apart;
+        }
+        p += members * (int)(8 * sizeof(T));
     }
 }
 template <typename T>
-__device__ __forceinline__ Raw<T> fetched(uint32_t& slot)
+__device__ __forceinline__ Raw<T> fetched(uint32_t slot, uint32_t apart)
 {
     Raw<T> raw;
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) {
-        raw.w[i] = load_shared_16B(slot);
-        slot += blockDim.x * 16;
-    }
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i)
+        raw.w[i] = load_shared_16B(slot + i * apart);
     return raw;
 }
 __device__ __forceinline__ void close_turn() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -595,11 +602,11 @@ __device__ __forceinline__ void drop_vectors(const NormArgs& a, const Member& m,
 // ---- host --------------------------------------------------------------------------------------------
 
 // How a launch deals its rows out: `per_thread` vectors per thread, blocks of at most `most_threads`.
-inline void plan_groups(int64_t features, int per_thread, int most_threads, Deal* d)
+inline void plan_groups(int64_t features, int per_thread, int rows_at_once, int most_threads, Deal* d)
 {
     const int64_t vectors = (features + 7) / 8;
     d->per_thread = per_thread;
-    d->rows_at_once = per_thread == 1 ? 2 : 1;
+    d->rows_at_once = rows_at_once;
     d->cluster = (int)((vectors + (int64_t)per_thread * most_threads - 1) / ((int64_t)per_thread * most_threads));
     d->block_vectors = (int)((vectors + d->cluster - 1) / d->cluster);
     const int threads = (d->block_vectors + per_thread - 1) / per_thread;
@@ -622,13 +629,13 @@ constexpr size_t kSharedBeside = sizeof(Exchange) + 1024;        // of a block, 
 // Blocks of `threads` at most, turns on their way (two or three) and blocks per multiprocessor, of two sizes of blocks the one
 // with which more warps are resident: large blocks share the vectors, small ones fill a multiprocessor better.
 // `threads_resident`: as many as their registers allow.  Returns blocks per multiprocessor.
-inline int plan_blocks(NormArgs* a, bool whole, int per_thread, int pieces_per_vector, int threads_resident, const int (&threads)[2])
+inline int plan_blocks(NormArgs* a, bool whole, int per_thread, int rows_at_once, int pieces_per_vector, int threads_resident, const int (&threads)[2])
 {
     Deal best{};
     int best_threads = 0, best_blocks = 0;
     for (int most_threads : threads) {
         Deal d{};
-        plan_groups(a->features, per_thread, most_threads, &d);
+        plan_groups(a->features, per_thread, rows_at_once, most_threads, &d);
         if (d.cluster > kMaxCluster)
             continue;
         a->deal = d;
@@ -646,7 +653,7 @@ inline int plan_blocks(NormArgs* a, bool whole, int per_thread, int pieces_per_v
         d.stages = stages < 1 ? 1 : stages > 3 ? 3 : (int)stages;
         // without a second turn on its way a block is worth half
         const int worth = blocks * threads_of(d) * (turn > 0 && d.stages == 1 ? 1 : 2);
-        if (worth > best_threads) {
+        if (worth > best_threads || (worth == best_threads && d.stages > best.stages)) {
             best_threads = worth;
             best_blocks = blocks;
             best = d;

@@ -108,10 +108,10 @@ struct Turn {
 
 // WHOLE: 16-byte aligned rows of whole vectors.  FULL: a norm after the block or a gate.
 template <typename T, typename R, bool WHOLE, bool FULL, int V>
-__global__ void __maxnreg__(128)
+__global__ void __maxnreg__(FULL ? 128 : 80)
 residual_norm_grad_kernel(const __grid_constant__ NormArgs a)
 {
-    constexpr int ROWS = V == 1 ? 2 : 1;
+    constexpr int ROWS = WHOLE ? 1 : 2;
     extern __shared__ __align__(16) unsigned char rows_shared[];
     __shared__ Exchange exchange;
     float* columns = reinterpret_cast<float*>(rows_shared + a.rows_at);      // after the rows
@@ -126,11 +126,11 @@ residual_norm_grad_kernel(const __grid_constant__ NormArgs a)
     const bool with_x = FULL && a.x;
     Staged staged = stage_vectors(a, m, rows_shared, ROWS, V);
     const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(rows_shared)) + a.rows_at + threadIdx.x * 16;
-    const uint32_t stage_bytes = a.turn_pieces * blockDim.x * 16;
+    const uint32_t apart = blockDim.x * 16, stage_bytes = a.turn_pieces * apart;
     const uint32_t turns = a.deal.rounds * a.deal.steps;
     // places of a row's vectors among the thread's pieces
-    const uint32_t h_piece = V * sizeof(T) / 2, d_piece = pre ? V * (sizeof(T) + sizeof(R)) / 2 : 0;
-    const uint32_t x_piece = d_piece + (a.grad_h ? V * sizeof(R) / 2 : 0);
+    const uint32_t t_bytes = V * (uint32_t)(sizeof(T) / 2) * apart, r_bytes = V * (uint32_t)(sizeof(R) / 2) * apart;
+    const uint32_t h_piece = t_bytes, d_piece = pre ? t_bytes + r_bytes : 0, x_piece = d_piece + (a.grad_h ? r_bytes : 0);
     Turn now(a.deal, m.group, a.rows), ahead(a.deal, m.group, a.rows);
     auto bring = [&](uint32_t turn, uint32_t stage) {
         if (turn < turns) {
@@ -139,19 +139,14 @@ residual_norm_grad_kernel(const __grid_constant__ NormArgs a)
             for (int r = 0; r < ROWS; ++r) {
                 const int64_t row = ahead.row + r;
                 const bool valid = row < ahead.end;
-                auto fetch_row = [&](auto t, const void* base, int64_t stride) {
-#pragma unroll
-                    for (int v = 0; v < V; ++v)
-                        fetch<decltype(t)>(slot, base, row * stride + m.column(v), valid && count[v] > 0);
-                };
                 if (pre) {
-                    fetch_row(T{}, a.grad_y, a.grad_y_stride);
-                    fetch_row(R{}, a.h, a.h_stride);
+                    fetch_row<T>(slot, apart, a.grad_y, row * a.grad_y_stride + m.column(0), m.members, valid, count);
+                    fetch_row<R>(slot, apart, a.h, row * a.h_stride + m.column(0), m.members, valid, count);
                 }
                 if (a.grad_h)
-                    fetch_row(R{}, a.grad_h, a.grad_h_stride);
+                    fetch_row<R>(slot, apart, a.grad_h, row * a.grad_h_stride + m.column(0), m.members, valid, count);
                 if (with_x)
-                    fetch_row(T{}, a.x, a.x_stride);
+                    fetch_row<T>(slot, apart, a.x, row * a.x_stride + m.column(0), m.members, valid, count);
             }
             ahead.advance(a.deal, a.rows);
         }
@@ -206,8 +201,7 @@ residual_norm_grad_kernel(const __grid_constant__ NormArgs a)
         auto row_of = [&](auto t, const void* base, int64_t stride, uint32_t piece, int r, int v) {
             using E = decltype(t);
             if constexpr (WHOLE) {
-                uint32_t at = slot + (piece + v * (uint32_t)(sizeof(E) / 2) + r * a.turn_pieces / ROWS) * (blockDim.x * 16);
-                return decode(fetched<E>(at));
+                return decode(fetched<E>(slot + piece + v * (uint32_t)(sizeof(E) / 2) * apart + r * (stage_bytes / ROWS), apart));
             } else {
                 return decode(load_vector<false>(static_cast<const E*>(base) + row[r] * stride + m.column(v), valid[r] ? count[v] : 0));
             }
@@ -442,7 +436,7 @@ size_t norm_workspace(const adasum_residual_norm_t& b, bool by_unit)
     if (by_unit) {
         // pieces of a gate row: fewer than groups / gates + 1, so fewer than twice the groups in all where cut
         Deal d{};
-        plan_groups(b.features, 1, 512, &d);       // as many groups as in any form
+        plan_groups(b.features, 1, 1, 512, &d);       // as many groups as in any form
         total += 2 * (size_t)kMaxBlocks * (size_t)(d.groups_per_block > 64 ? d.groups_per_block : 64) * (size_t)columns * 4;
     }
     return (total + 255) / 256 * 256;
@@ -590,7 +584,7 @@ adasum_status_t adasum_residual_norm_grad(const adasum_residual_norm_t* b, const
                      (!g->grad_residual || rows_aligned(g->grad_residual, g->grad_residual_stride, rb));
     // several vectors per thread, as many as their sums leave registers for, where a row then has eight threads or more
     const bool full = post || (branch && b->gate);
-    const int per_thread = !vec || features <= 128 ? 1 : full ? 2 : 4;
+    const int per_thread = !vec || features <= 128 || full ? 1 : 2;
     if (!full)
         a.x = nullptr;                     // without a norm or a gate its values make no difference
     if (!post)
@@ -599,8 +593,8 @@ adasum_status_t adasum_residual_norm_grad(const adasum_residual_norm_t* b, const
         a.pre_weight = Vector{};
     a.pre_bias = Vector{};                 // gradients do not depend on it
     unsigned blocks;
-    const int per_processor = plan_blocks(&a, vec, per_thread, (int)((pre ? (tb + rb) / 2 : 0) + (g->grad_h ? rb / 2 : 0) + (a.x ? tb / 2 : 0)),
-                                          512, {512, 256});
+    const int per_processor = plan_blocks(&a, vec, per_thread, vec ? 1 : 2, (int)((pre ? (tb + rb) / 2 : 0) + (g->grad_h ? rb / 2 : 0) + (a.x ? tb / 2 : 0)),
+                                          full || per_thread == 1 ? 512 : 768, {512, 256});
     if (per_processor == 0)
         return fail(ADASUM_ERR_ARG, "%lld features are too many", (long long)features);
     plan_units(rows, b->gate ? b->rows_per_gate : rows, by_unit, (int64_t)per_processor * sms, &a.deal, &blocks);
@@ -622,8 +616,7 @@ adasum_status_t adasum_residual_norm_grad(const adasum_residual_norm_t* b, const
         const size_t threads = (size_t)threads_of(a.deal), sums = wanted > 0 ? threads * per_thread * 32 : 0;
         const size_t rows_bytes = vec ? (size_t)a.deal.stages * a.turn_pieces * threads * 16 : 0;
         auto* kernel = !vec               ? residual_norm_grad_kernel<T, R, false, true, 1>
-                       : per_thread == 4 ? residual_norm_grad_kernel<T, R, true, false, 4>
-                       : per_thread == 2 ? residual_norm_grad_kernel<T, R, true, true, 2>
+                       : per_thread == 2 ? residual_norm_grad_kernel<T, R, true, false, 2>
                                          : residual_norm_grad_kernel<T, R, true, true, 1>;
         err = launch_rows(kernel, blocks, a, a.rows_at + (rows_bytes > sums ? rows_bytes : sums), stream);
     });
