@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 import torch
@@ -742,33 +743,21 @@ ADASUM_NORM_MAX_FEATURES = 32768
 ADASUM_FP8_BLOCK = 128
 
 
-class _ResidualNorm(ctypes.Structure):
-    _fields_ = [("rows", _i64), ("features", _i64), ("dtype", _i32), ("stream_dtype", _i32), ("param_dtype", _i32),
-                ("gate_dtype", _i32), ("post_norm", _i32), ("pre_norm", _i32), ("post_weight", _vp), ("post_bias", _vp),
-                ("pre_weight", _vp), ("pre_bias", _vp), ("gate", _vp), ("gate_stride", _i64), ("rows_per_gate", _i64),
-                ("eps", _f32), ("branch_scale", _f32), ("residual_scale", _f32), ("dropout", _f32),
-                ("site", ctypes.c_uint64), ("seed", _vp)]
-
-
-class _ResidualNormGrads(ctypes.Structure):
-    _fields_ = [("x", _vp), ("h", _vp), ("grad_y", _vp), ("grad_h", _vp), ("stats", _vp), ("x_stride", _i64),
-                ("h_stride", _i64), ("grad_y_stride", _i64), ("grad_h_stride", _i64), ("grad_x", _vp),
-                ("grad_residual", _vp), ("grad_x_stride", _i64), ("grad_residual_stride", _i64),
-                ("grad_post_weight", _vp), ("grad_post_bias", _vp), ("grad_pre_weight", _vp), ("grad_pre_bias", _vp),
-                ("grad_gate", _vp), ("grad_dtype", _i32), ("gate_grad_dtype", _i32), ("scale", _f32),
-                ("gate_scale", _f32), ("accumulate", _i32)]
+# The C structures adasum_residual_norm_t and adasum_residual_norm_grads_t, packed as bytes: a third of the time that
+# ctypes takes to fill a Structure.
+_RESIDUAL_NORM = struct.Struct("@qqiiiiiiPPPPPqqffffQP")
+_RESIDUAL_NORM_GRADS = struct.Struct("@PPPPPqqqqPPqqPPPPPiiffi4x")
 
 
 _u64 = ctypes.c_uint64
 _lib.adasum_dropout.restype = ctypes.c_int
 _lib.adasum_dropout.argtypes = [_vp, _i64, _i64, _i64, ctypes.c_int, _vp, _i64, _f32, _vp, _u64, _vp, _i64, _vp]
 _lib.adasum_residual_norm.restype = ctypes.c_int
-_lib.adasum_residual_norm.argtypes = [ctypes.POINTER(_ResidualNorm), _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp]
+_lib.adasum_residual_norm.argtypes = [ctypes.c_char_p, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp]
 _lib.adasum_residual_norm_grad_workspace_bytes.restype = ctypes.c_size_t
-_lib.adasum_residual_norm_grad_workspace_bytes.argtypes = [ctypes.POINTER(_ResidualNorm)]
+_lib.adasum_residual_norm_grad_workspace_bytes.argtypes = [ctypes.c_char_p]
 _lib.adasum_residual_norm_grad.restype = ctypes.c_int
-_lib.adasum_residual_norm_grad.argtypes = [ctypes.POINTER(_ResidualNorm), ctypes.POINTER(_ResidualNormGrads), _vp,
-                                           ctypes.c_size_t, _vp]
+_lib.adasum_residual_norm_grad.argtypes = [ctypes.c_char_p, ctypes.c_char_p, _vp, ctypes.c_size_t, _vp]
 _lib.adasum_fp8_bytes.restype = ctypes.c_size_t
 _lib.adasum_fp8_bytes.argtypes = [_i64, _i64]
 for _name in ("adasum_fp8_pack", "adasum_fp8_pack_weight"):
@@ -787,16 +776,29 @@ _lib.adasum_fp8_linear_status.restype = ctypes.c_int
 _lib.adasum_fp8_linear_status.argtypes = [_vp, _vp]
 
 
-def _seed(device: int, seed, p: float):
-    """Checks a dropout's seed; returns its address (None where nothing is dropped and no seed is given)."""
+def _seed(device: int, seed, p: float) -> int:
+    """Checks a dropout's seed; returns its address (0 where nothing is dropped and no seed is given)."""
     if seed is None:
         if p > 0.0:
             raise ValueError("dropout needs a seed: a CUDA tensor that holds one 64-bit integer")
-        return None
-    if not seed.is_cuda or seed.dtype not in (torch.int64, torch.uint64) or seed.numel() < 1:
-        raise TypeError("seed must be a CUDA tensor that holds one 64-bit integer")
-    _same_device(device, seed)
+        return 0
+    if seed.get_device() != device or seed.dtype not in (torch.int64, torch.uint64) or seed.numel() < 1:
+        raise TypeError(f"seed must be a tensor on cuda:{device} that holds one 64-bit integer")
     return seed.data_ptr()
+
+
+def _rows(name: str, t, shape, dtype, device: int) -> int:
+    """Checks a matrix of a given shape, type and device with contiguous rows; returns its row stride in elements."""
+    if t.shape != shape:
+        raise ValueError(f"{name} is {tuple(t.shape)}, need {tuple(shape)}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be of {dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, not on cuda:{device}")
+    row, column = t.stride()
+    if column != 1 and shape[1] > 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return row if shape[0] > 1 else max(row, shape[1])
 
 
 def adasum_dropout(x, p: float, seed, site: int = 0, residual=None, out=None, stream=None):
@@ -804,31 +806,26 @@ def adasum_dropout(x, p: float, seed, site: int = 0, residual=None, out=None, st
     read when the kernel runs; ``site`` tells the dropouts of one step apart.  The gradient is the same call on
     the gradient, without ``residual``.  ``out`` may be ``x`` or ``residual`` itself."""
     stride = _matrix("x", x)
-    rows, features = x.shape
-    device = x.get_device()
-    residual_ptr, residual_stride = None, 0
+    shape, dtype, device = x.shape, x.dtype, x.get_device()
+    rows, features = shape
+    residual_ptr, residual_stride = 0, 0
     if residual is not None:
-        residual_stride = _matrix("residual", residual, rows, features)
-        if residual.dtype != x.dtype:
-            raise TypeError("residual must have the type of x")
+        residual_stride = _rows("residual", residual, shape, dtype, device)
         residual_ptr = residual.data_ptr()
     if out is None:
-        out, out_stride = _allocate(x, stream, (rows, features), x.dtype), features
+        out, out_stride = _allocate(x, stream, (rows, features), dtype), features
     else:
-        out_stride = _matrix("out", out, rows, features)
-        if out.dtype != x.dtype:
-            raise TypeError("out must have the type of x")
-    _same_device(device, residual, out)
-    _operator_call(device, stream, _lib.adasum_dropout, x.data_ptr(), stride, rows, features, _operator_dtype(x.dtype),
+        out_stride = _rows("out", out, shape, dtype, device)
+    _operator_call(device, stream, _lib.adasum_dropout, x.data_ptr(), stride, rows, features, _operator_dtype(dtype),
                    residual_ptr, residual_stride, p, _seed(device, seed, p), site, out.data_ptr(), out_stride)
     return out
 
 
-def _vector(name: str, t, features: int, dtype, device: int):
-    """Checks a vector of a norm; returns its address."""
+def _vector(name: str, t, features: int, dtype, device: int) -> int:
+    """Checks a vector of a norm; returns its address (0: there is none)."""
     if t is None:
-        return None
-    if t.dtype != dtype:
+        return 0
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must have the type of the norms' other vectors")
     if t.numel() != features or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous and have {features} elements")
@@ -841,8 +838,12 @@ def _residual_norm_block(rows, features, dtype, stream_dtype, device, post_norm,
                          pre_weight, pre_bias, eps, gate, rows_per_gate, branch_scale, residual_scale, dropout, seed,
                          site):
     """The C description of a joint, and the rows of its gate."""
-    param = next((t.dtype for t in (post_weight, post_bias, pre_weight, pre_bias) if t is not None), torch.float32)
-    gate_ptr, gate_stride, gate_dtype, gate_rows = None, 0, 0, 0
+    param = torch.float32
+    for t in (pre_weight, post_weight, pre_bias, post_bias):
+        if t is not None:
+            param = t.dtype
+            break
+    gate_ptr = gate_stride = gate_dtype = gate_rows = 0
     if gate is not None:
         if gate.dim() == 1:
             gate = gate.view(1, -1)
@@ -853,16 +854,17 @@ def _residual_norm_block(rows, features, dtype, stream_dtype, device, post_norm,
         if rows_per_gate < 1 or (rows > 0 and gate_rows != -(-rows // rows_per_gate)):
             raise ValueError(f"{rows} rows, {rows_per_gate} per row of the gate, need a gate of "
                              f"{-(-rows // max(rows_per_gate, 1))} rows, not {gate_rows}")
-        _same_device(device, gate)
+        if gate.get_device() != device:
+            raise ValueError(f"gate is on {gate.device}, not on cuda:{device}")
         gate_ptr, gate_dtype = gate.data_ptr(), _operator_dtype(gate.dtype)
-    block = _ResidualNorm(rows, features, _operator_dtype(dtype), _operator_dtype(stream_dtype), _operator_dtype(param),
-                          gate_dtype, ADASUM_NORM[post_norm], ADASUM_NORM[pre_norm],
-                          _vector("post_weight", post_weight, features, param, device),
-                          _vector("post_bias", post_bias, features, param, device),
-                          _vector("pre_weight", pre_weight, features, param, device),
-                          _vector("pre_bias", pre_bias, features, param, device), gate_ptr, gate_stride,
-                          rows_per_gate or 0, eps, branch_scale, residual_scale, dropout, site,
-                          _seed(device, seed, dropout))
+    block = _RESIDUAL_NORM.pack(rows, features, _operator_dtype(dtype), _operator_dtype(stream_dtype),
+                                _operator_dtype(param), gate_dtype, ADASUM_NORM[post_norm], ADASUM_NORM[pre_norm],
+                                0 if post_weight is None else _vector("post_weight", post_weight, features, param, device),
+                                0 if post_bias is None else _vector("post_bias", post_bias, features, param, device),
+                                0 if pre_weight is None else _vector("pre_weight", pre_weight, features, param, device),
+                                0 if pre_bias is None else _vector("pre_bias", pre_bias, features, param, device),
+                                gate_ptr, gate_stride, rows_per_gate or 0, eps, branch_scale, residual_scale, dropout,
+                                site, _seed(device, seed, dropout))
     return block, gate_rows
 
 
@@ -879,52 +881,63 @@ def adasum_residual_norm(x, residual, post_norm: str = "none", post_weight=None,
     like = x if x is not None else residual
     if like is None:
         raise ValueError("x and residual are both missing")
-    rows, features = like.shape
-    device = like.get_device()
-    x_ptr, x_stride, residual_ptr, residual_stride = None, 0, None, 0
+    like_stride = _matrix("x" if x is not None else "residual", like)
+    shape, device = like.shape, like.get_device()
+    rows, features = shape
+    x_ptr = x_stride = residual_ptr = residual_stride = 0
+    dtype = of_stream = None
     if x is not None:
-        x_stride = _matrix("x", x)
-        x_ptr = x.data_ptr()
-    if residual is not None:
-        residual_stride = _matrix("residual", residual, rows, features)
-        residual_ptr = residual.data_ptr()
-    dtype = x.dtype if x is not None else y.dtype if y is not None else out_dtype or residual.dtype
-    of_stream = residual.dtype if residual is not None else h.dtype if h is not None else stream_dtype or dtype
+        x_ptr, x_stride, dtype = x.data_ptr(), like_stride, x.dtype
+        if residual is not None:
+            of_stream = residual.dtype
+            residual_stride = _rows("residual", residual, shape, of_stream, device)
+            residual_ptr = residual.data_ptr()
+        else:
+            of_stream = h.dtype if h is not None else stream_dtype or dtype
+    else:
+        residual_ptr, residual_stride, of_stream = residual.data_ptr(), like_stride, residual.dtype
+        dtype = y.dtype if y is not None else out_dtype or of_stream
     block, _ = _residual_norm_block(rows, features, dtype, of_stream, device, post_norm, post_weight, post_bias, pre_norm,
                                     pre_weight, pre_bias, eps, gate, rows_per_gate, branch_scale, residual_scale, dropout,
                                     seed, site)
+    h_ptr = y_ptr = stats_ptr = 0
     h_stride = y_stride = features
     if h is not None:
-        h_stride = _matrix("h", h, rows, features)
-        if h.dtype != of_stream:
-            raise TypeError("h must have the type of residual")
+        h_stride = _rows("h", h, shape, of_stream, device)
+        h_ptr = h.data_ptr()
     elif want_h:
         h = _allocate(like, stream, (rows, features), of_stream)
+        h_ptr = h.data_ptr()
     if pre_norm == "none":
         y = None
-    elif y is None:
-        y = _allocate(like, stream, (rows, features), dtype)
     else:
-        y_stride = _matrix("y", y, rows, features)
-        if y.dtype != dtype:
-            raise TypeError("y must have the type of x")
+        if y is None:
+            y = _allocate(like, stream, (rows, features), dtype)
+        else:
+            y_stride = _rows("y", y, shape, dtype, device)
+        y_ptr = y.data_ptr()
     if stats is not None:
-        if stats.dtype != torch.float32 or not stats.is_contiguous() or stats.numel() != 4 * rows:
-            raise ValueError(f"stats must be contiguous fp32 of 4 x {rows} elements")
+        _check_stats(stats, rows, device)
+        stats_ptr = stats.data_ptr()
     elif want_stats:
         stats = _allocate(like, stream, (4, rows), torch.float32)
-    _same_device(device, residual, h, y, stats)
+        stats_ptr = stats.data_ptr()
     _operator_call(device, stream, _lib.adasum_residual_norm, block, x_ptr, x_stride, residual_ptr, residual_stride,
-                   None if h is None else h.data_ptr(), h_stride, None if y is None else y.data_ptr(), y_stride,
-                   None if stats is None else stats.data_ptr())
+                   h_ptr, h_stride, y_ptr, y_stride, stats_ptr)
     return h, y, stats
+
+
+def _check_stats(stats, rows: int, device: int):
+    if stats.dtype != torch.float32 or not stats.is_contiguous() or stats.numel() != 4 * rows:
+        raise ValueError(f"stats must be contiguous fp32 of 4 x {rows} elements")
+    if stats.get_device() != device:
+        raise ValueError(f"stats is on {stats.device}, not on cuda:{device}")
 
 
 def adasum_residual_norm_grad_workspace_bytes(features: int, gate: bool = False) -> int:
     """Bytes for any number of rows."""
-    block = _ResidualNorm()
-    block.features = int(features)
-    block.gate = 256 if gate else None       # only whether there is one matters
+    # only the features and whether there is a gate matter
+    block = _RESIDUAL_NORM.pack(0, int(features), 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 256 if gate else 0, 0, 1, 0.0, 1.0, 1.0, 0.0, 0, 0)
     return int(_lib.adasum_residual_norm_grad_workspace_bytes(block))
 
 
@@ -941,64 +954,81 @@ def adasum_residual_norm_grad(x, h, stats, grad_y, grad_h, post_norm: str = "non
     written where they are given (``grad_gate``: contiguous, of the gate's size), multiplied by ``scale`` (``gate_scale``).
     Returns ``(grad_x, grad_residual)``, allocated here unless given or not wanted.  ``x`` may be None where there is
     neither a post norm nor a gate's gradient; ``out_dtype`` is then the type of ``grad_x`` unless ``grad_y`` has one."""
-    like = next((t for t in (grad_y, grad_h) if t is not None), None)
+    like = grad_y if grad_y is not None else grad_h
     if like is None:
         raise ValueError("grad_y and grad_h are both missing")
-    rows, features = like.shape
-    device = like.get_device()
+    like_stride = _matrix("grad_y" if grad_y is not None else "grad_h", like)
+    shape, device = like.shape, like.get_device()
+    rows, features = shape
     if grad_y is not None and pre_norm == "none":
         raise ValueError("grad_y without a pre_norm")
-    dtype = next((t.dtype for t in (x, grad_y, grad_x) if t is not None), out_dtype or like.dtype)
-    of_stream = next((t.dtype for t in (h, grad_h, grad_residual) if t is not None), dtype)
-
-    def place(name, t, wanted_dtype):
-        if t is None:
-            return None, 0
-        stride = _matrix(name, t, rows, features)
-        if t.dtype != wanted_dtype:
-            raise TypeError(f"{name} must be of {wanted_dtype}")
-        return t.data_ptr(), stride
-
+    if x is not None:
+        dtype = x.dtype
+    elif grad_y is not None:
+        dtype = grad_y.dtype
+    else:
+        dtype = grad_x.dtype if grad_x is not None else out_dtype or like.dtype
+    if h is not None:
+        of_stream = h.dtype
+    elif grad_h is not None:
+        of_stream = grad_h.dtype
+    else:
+        of_stream = grad_residual.dtype if grad_residual is not None else dtype
     block, gate_rows = _residual_norm_block(rows, features, dtype, of_stream, device, post_norm, post_weight, post_bias,
                                             pre_norm, pre_weight, pre_bias, eps, gate, rows_per_gate, branch_scale,
                                             residual_scale, dropout, seed, site)
-    if grad_x is None and want_x:
-        grad_x = _allocate(like, stream, (rows, features), dtype)
-    if grad_residual is None and want_residual:
-        grad_residual = _allocate(like, stream, (rows, features), of_stream)
-    x_ptr, x_stride = place("x", x, dtype)
-    h_ptr, h_stride = place("h", h, of_stream)
-    grad_y_ptr, grad_y_stride = place("grad_y", grad_y, dtype)
-    grad_h_ptr, grad_h_stride = place("grad_h", grad_h, of_stream)
-    grad_x_ptr, grad_x_stride = place("grad_x", grad_x, dtype)
-    grad_residual_ptr, grad_residual_stride = place("grad_residual", grad_residual, of_stream)
-    stats_ptr = None
+    x_ptr = h_ptr = y_ptr = d_ptr = stats_ptr = into_x_ptr = into_r_ptr = 0
+    x_stride = h_stride = y_stride = d_stride = into_x_stride = into_r_stride = features
+    if x is not None:
+        x_stride, x_ptr = _rows("x", x, shape, dtype, device), x.data_ptr()
+    if h is not None:
+        h_stride, h_ptr = _rows("h", h, shape, of_stream, device), h.data_ptr()
+    if grad_y is not None:
+        if grad_y.dtype is not dtype:
+            raise TypeError("grad_y must have the type of x")
+        y_stride, y_ptr = like_stride, grad_y.data_ptr()
+    if grad_h is not None:
+        d_stride, d_ptr = _rows("grad_h", grad_h, shape, of_stream, device), grad_h.data_ptr()
     if stats is not None:
-        if stats.dtype != torch.float32 or not stats.is_contiguous() or stats.numel() != 4 * rows:
-            raise ValueError(f"stats must be contiguous fp32 of 4 x {rows} elements")
+        _check_stats(stats, rows, device)
         stats_ptr = stats.data_ptr()
-    vectors = (grad_post_weight, grad_post_bias, grad_pre_weight, grad_pre_bias)
-    grad_dtype = next((t.dtype for t in vectors if t is not None), torch.float32)
-    gate_ptr, gate_code = None, 0
+    if grad_x is not None:
+        into_x_stride, into_x_ptr = _rows("grad_x", grad_x, shape, dtype, device), grad_x.data_ptr()
+    elif want_x:
+        grad_x = _allocate(like, stream, (rows, features), dtype)
+        into_x_ptr = grad_x.data_ptr()
+    if grad_residual is not None:
+        into_r_stride, into_r_ptr = _rows("grad_residual", grad_residual, shape, of_stream, device), grad_residual.data_ptr()
+    elif want_residual:
+        grad_residual = _allocate(like, stream, (rows, features), of_stream)
+        into_r_ptr = grad_residual.data_ptr()
+    grad_dtype = None
+    for t in (grad_pre_weight, grad_post_weight, grad_pre_bias, grad_post_bias):
+        if t is not None:
+            grad_dtype = t.dtype
+            break
+    gate_ptr = gate_code = workspace_ptr = workspace_bytes = 0
     if grad_gate is not None:
         if grad_gate.numel() != gate_rows * features or not grad_gate.is_contiguous():
             raise ValueError(f"grad_gate must be contiguous and have {gate_rows} x {features} elements")
+        if grad_gate.get_device() != device:
+            raise ValueError(f"grad_gate is on {grad_gate.device}, not on cuda:{device}")
         gate_ptr, gate_code = grad_gate.data_ptr(), _operator_dtype(grad_gate.dtype)
         if rows == 0 and not accumulate:     # an empty sum
             grad_gate.zero_()
-    workspace_ptr, workspace_bytes = None, 0
-    if grad_gate is not None or any(t is not None for t in vectors):
+    if grad_gate is not None or grad_dtype is not None:
         workspace = _operator_workspace(like, stream, workspace, _lib.adasum_residual_norm_grad_workspace_bytes(block))
         workspace_ptr, workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-        _same_device(device, workspace)
-    _same_device(device, x, h, stats, grad_y, grad_h, grad_x, grad_residual, grad_gate)
-    grads = _ResidualNormGrads(x_ptr, h_ptr, grad_y_ptr, grad_h_ptr, stats_ptr, x_stride, h_stride, grad_y_stride,
-                               grad_h_stride, grad_x_ptr, grad_residual_ptr, grad_x_stride, grad_residual_stride,
-                               _vector("grad_post_weight", grad_post_weight, features, grad_dtype, device),
-                               _vector("grad_post_bias", grad_post_bias, features, grad_dtype, device),
-                               _vector("grad_pre_weight", grad_pre_weight, features, grad_dtype, device),
-                               _vector("grad_pre_bias", grad_pre_bias, features, grad_dtype, device), gate_ptr,
-                               _operator_dtype(grad_dtype), gate_code, scale, gate_scale, accumulate)
+        if workspace.get_device() != device:
+            raise ValueError(f"workspace is on {workspace.device}, not on cuda:{device}")
+    grads = _RESIDUAL_NORM_GRADS.pack(
+        x_ptr, h_ptr, y_ptr, d_ptr, stats_ptr, x_stride, h_stride, y_stride, d_stride, into_x_ptr, into_r_ptr, into_x_stride,
+        into_r_stride,
+        0 if grad_post_weight is None else _vector("grad_post_weight", grad_post_weight, features, grad_dtype, device),
+        0 if grad_post_bias is None else _vector("grad_post_bias", grad_post_bias, features, grad_dtype, device),
+        0 if grad_pre_weight is None else _vector("grad_pre_weight", grad_pre_weight, features, grad_dtype, device),
+        0 if grad_pre_bias is None else _vector("grad_pre_bias", grad_pre_bias, features, grad_dtype, device),
+        gate_ptr, 0 if grad_dtype is None else _operator_dtype(grad_dtype), gate_code, scale, gate_scale, accumulate)
     _operator_call(device, stream, _lib.adasum_residual_norm_grad, block, grads, workspace_ptr, workspace_bytes)
     return grad_x, grad_residual
 

@@ -7,7 +7,8 @@
 namespace adasum {
 namespace {
 
-constexpr int kDropRows = 2;               // vectors per thread, in as many rows
+// Vectors per thread, in as many rows.  16384 x 4096 bf16 with 1, 2, 4: 71, 57, 55 us (fp32: 78, 79, 79).
+constexpr int kDropRows = 4;
 
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kStripThreads)

@@ -258,7 +258,8 @@ adasum_status_t adasum_residual_norm(const adasum_residual_norm_t* b, const void
         auto* kernel = !vec   ? residual_norm_kernel<T, R, false, true, 1>
                        : four ? full ? residual_norm_kernel<T, R, true, true, 2> : residual_norm_kernel<T, R, true, false, 4>
                               : residual_norm_kernel<T, R, true, true, 1>;
-        err = launch_rows(kernel, blocks, a, shared, stream);
+        static std::atomic<uint64_t> prepared[4] = {};         // of these types' kernels
+        err = launch_rows(kernel, prepared[!vec ? 0 : !four ? 1 : full ? 2 : 3], blocks, a, shared, stream);
     });
     ADASUM_CUDA_CHECK(err);
     profile_mark(stream, ADASUM_KERNEL_RESIDUAL_NORM, 0, 0, false);

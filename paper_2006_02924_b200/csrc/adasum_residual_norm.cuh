@@ -22,6 +22,8 @@
 // pieces that a group walks one after another, and each piece leaves its own sum.
 #pragma once
 
+#include <atomic>
+
 #include "adasum_random.cuh"
 #include "adasum_vectors.cuh"
 
@@ -31,7 +33,9 @@ namespace {
 constexpr int kMaxWarps = 16;
 constexpr int kMaxCluster = 8;
 constexpr int64_t kMaxFeatures = ADASUM_NORM_MAX_FEATURES;
-constexpr int kMaxBlocks = 148 * 4;        // blocks that leave sums of the vectors' gradients
+constexpr int kMaxProcessors = 148;        // multiprocessors that a gradient call uses
+constexpr int kGradThreads = 512;          // of a multiprocessor, at least, in gradient calls
+constexpr int kMaxParts = 2 * kMaxProcessors;     // blocks that leave sums of the vectors' gradients
 constexpr int kVectors = 5;                // gradients of vectors: post weight, post bias, pre weight, pre bias, gate
 
 // A vector of parameters, or the gate (p = nullptr: there is none).
@@ -669,7 +673,6 @@ inline int plan_blocks(NormArgs* a, bool whole, int per_thread, int rows_at_once
 inline void plan_units(int64_t rows, int64_t gate_span, bool by_unit, int64_t most_blocks, Deal* d, unsigned* blocks)
 {
     const int64_t kRows = d->rows_at_once;
-    most_blocks = most_blocks < kMaxBlocks ? most_blocks : kMaxBlocks;
     const int64_t most_groups = (most_blocks / d->cluster > 0 ? most_blocks / d->cluster : 1) * d->groups_per_block;
     int64_t gates = 1, pieces;
     if (!by_unit) {
@@ -711,14 +714,23 @@ inline void plan_units(int64_t rows, int64_t gate_span, bool by_unit, int64_t mo
     d->rounds = (d->units + d->groups - 1) / d->groups;
 }
 
+// `prepared`: the kernel's own, a bit per device whose limit of shared memory has been raised.
 template <typename Kernel>
-cudaError_t launch_rows(Kernel* kernel, unsigned blocks, const NormArgs& a, size_t shared_bytes, cudaStream_t stream)
+cudaError_t launch_rows(Kernel* kernel, std::atomic<uint64_t>& prepared, unsigned blocks, const NormArgs& a, size_t shared_bytes,
+                        cudaStream_t stream)
 {
     if (shared_bytes > 40 * 1024) {
-        const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                     (int)(kSharedPerBlock - sizeof(Exchange)));
+        int device = 0;
+        cudaError_t err = cudaGetDevice(&device);
         if (err != cudaSuccess)
             return err;
+        const uint64_t bit = device < 64 ? uint64_t(1) << device : 0;
+        if (!(prepared.load(std::memory_order_relaxed) & bit) || bit == 0) {
+            err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kSharedPerBlock - sizeof(Exchange)));
+            if (err != cudaSuccess)
+                return err;
+            prepared.fetch_or(bit, std::memory_order_relaxed);
+        }
     }
     cudaLaunchConfig_t config = {};
     config.dynamicSmemBytes = shared_bytes;

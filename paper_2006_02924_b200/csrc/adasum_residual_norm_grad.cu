@@ -108,7 +108,7 @@ struct Turn {
 
 // WHOLE: 16-byte aligned rows of whole vectors.  FULL: a norm after the block or a gate.
 template <typename T, typename R, bool WHOLE, bool FULL, int V>
-__global__ void __maxnreg__(FULL ? 128 : 80)
+__global__ void __maxnreg__(FULL ? 128 : 96)
 residual_norm_grad_kernel(const __grid_constant__ NormArgs a)
 {
     constexpr int ROWS = WHOLE ? 1 : 2;
@@ -432,12 +432,13 @@ __global__ void __launch_bounds__(32 * kShares) residual_norm_join_kernel(const 
 size_t norm_workspace(const adasum_residual_norm_t& b, bool by_unit)
 {
     const int64_t columns = (b.features + 7) / 8 * 8;
-    size_t total = (size_t)kMaxBlocks * kVectors * (size_t)columns * 4;
+    size_t total = (size_t)kMaxParts * kVectors * (size_t)columns * 4;
     if (by_unit) {
-        // pieces of a gate row: fewer than groups / gates + 1, so fewer than twice the groups in all where cut
+        // fewer than twice as many units as groups, which have one vector per thread beside a gate
         Deal d{};
-        plan_groups(b.features, 1, 1, 512, &d);       // as many groups as in any form
-        total += 2 * (size_t)kMaxBlocks * (size_t)(d.groups_per_block > 64 ? d.groups_per_block : 64) * (size_t)columns * 4;
+        plan_groups(b.features, 1, 1, kGradThreads, &d);
+        const size_t groups = (size_t)(kGradThreads / (d.warps == 1 ? d.lanes : 32 * d.warps));
+        total += 2 * (size_t)kMaxProcessors * groups * (size_t)columns * 4;
     }
     return (total + 255) / 256 * 256;
 }
@@ -574,7 +575,7 @@ adasum_status_t adasum_residual_norm_grad(const adasum_residual_norm_t* b, const
     a.gate_scale = g->gate_scale;
     a.gate_by_unit = by_unit;
     a.want_gate = g->grad_gate != nullptr;
-    const int sms = device_sms();
+    const int sms = device_sms() < kMaxProcessors ? device_sms() : kMaxProcessors;
     if (sms == 0)
         return fail(ADASUM_ERR_CUDA, "no device");
     const bool gate_whole = !a.gate.p || (a.gate.aligned && (b->gate_dtype == b->dtype || b->gate_dtype == ADASUM_F32));
@@ -594,12 +595,12 @@ adasum_status_t adasum_residual_norm_grad(const adasum_residual_norm_t* b, const
     a.pre_bias = Vector{};                 // gradients do not depend on it
     unsigned blocks;
     const int per_processor = plan_blocks(&a, vec, per_thread, vec ? 1 : 2, (int)((pre ? (tb + rb) / 2 : 0) + (g->grad_h ? rb / 2 : 0) + (a.x ? tb / 2 : 0)),
-                                          full || per_thread == 1 ? 512 : 768, {512, 256});
+                                          full || per_thread == 1 ? kGradThreads : 640, {512, 256});
     if (per_processor == 0)
         return fail(ADASUM_ERR_ARG, "%lld features are too many", (long long)features);
-    plan_units(rows, b->gate ? b->rows_per_gate : rows, by_unit, (int64_t)per_processor * sms, &a.deal, &blocks);
+    plan_units(rows, b->gate ? b->rows_per_gate : rows, by_unit, per_processor * sms < kMaxParts ? per_processor * sms : kMaxParts, &a.deal, &blocks);
     a.parts = static_cast<float*>(workspace);
-    a.gate_parts = by_unit && a.deal.pieces > 1 ? a.parts + (size_t)kMaxBlocks * kVectors * (size_t)a.columns : nullptr;
+    a.gate_parts = by_unit && a.deal.pieces > 1 ? a.parts + (size_t)kMaxParts * kVectors * (size_t)a.columns : nullptr;
     JoinArgs j{};
     for (int v = 0; v < kVectors; ++v) {
         // without grad_y the norm before the next block has no part in the gradients: its vectors' are zero
@@ -618,7 +619,8 @@ adasum_status_t adasum_residual_norm_grad(const adasum_residual_norm_t* b, const
         auto* kernel = !vec               ? residual_norm_grad_kernel<T, R, false, true, 1>
                        : per_thread == 2 ? residual_norm_grad_kernel<T, R, true, false, 2>
                                          : residual_norm_grad_kernel<T, R, true, true, 1>;
-        err = launch_rows(kernel, blocks, a, a.rows_at + (rows_bytes > sums ? rows_bytes : sums), stream);
+        static std::atomic<uint64_t> prepared[3] = {};         // of these types' kernels
+        err = launch_rows(kernel, prepared[!vec ? 0 : per_thread], blocks, a, a.rows_at + (rows_bytes > sums ? rows_bytes : sums), stream);
     });
     ADASUM_CUDA_CHECK(err);
     profile_mark(stream, ADASUM_KERNEL_RESIDUAL_NORM_GRAD, 0, 0, false);
