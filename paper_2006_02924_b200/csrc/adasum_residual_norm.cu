@@ -65,12 +65,12 @@ residual_norm_kernel(const __grid_constant__ NormArgs a)
         };
         if constexpr (WHOLE)
             wait_for_turn(a.deal.stages);
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                h[u][v] = a.x ? row_of(T{}, a.x, a.x_stride, 0, u, v) : Eight{};
         if constexpr (FULL) {
-#pragma unroll
-            for (int u = 0; u < ROWS; ++u)
-#pragma unroll
-                for (int v = 0; v < V; ++v)
-                    h[u][v] = a.x ? row_of(T{}, a.x, a.x_stride, 0, u, v) : Eight{};
             if (a.post != ADASUM_NORM_NONE) {
                 normalise<WHOLE>(m, exchange, a, a.post, count, h, mean, rstd);
                 if (a.stats && m.leads()) {
@@ -93,6 +93,8 @@ residual_norm_kernel(const __grid_constant__ NormArgs a)
                 hold_gate<ROWS, V>(a, m, row, valid, staged);
             }
         }
+        if (a.drop.seed && a.x)
+            drop_vectors(a, m, seed, row, h);
         const Pair branch = both(a.branch_scale), stream = both(a.residual_scale);
 #pragma unroll
         for (int u = 0; u < ROWS; ++u) {
@@ -100,14 +102,6 @@ residual_norm_kernel(const __grid_constant__ NormArgs a)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 if (a.x) {
-                    if constexpr (!FULL)
-                        h[u][v] = row_of(T{}, a.x, a.x_stride, 0, u, v);
-                    if (a.drop.seed) {
-                        const uint64_t number[1] = {(uint64_t)row[u] * (uint32_t)(a.columns / 8) + (uint32_t)m.vector_number(v)};
-                        uint32_t word[1][4];
-                        random_words(a.drop, seed, number, word);
-                        drop(a.drop, word[0], h[u][v]);
-                    }
                     if constexpr (FULL) {
                         if (a.gate.p && valid && count[v] > 0) {
                             Eight g;

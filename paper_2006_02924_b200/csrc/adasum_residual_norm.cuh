@@ -586,20 +586,22 @@ __device__ __forceinline__ void hold_gate(const NormArgs& a, const Member& m, co
     }
 }
 
+// The masks of two vectors at a time, which share the generator's round keys.
 template <int ROWS, int V>
 __device__ __forceinline__ void drop_vectors(const NormArgs& a, const Member& m, uint64_t seed, const int64_t (&row)[ROWS], Eight (&x)[ROWS][V])
 {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        uint64_t number[ROWS];
-        uint32_t word[ROWS][4];
+    for (int j = 0; j < ROWS * V; j += 2) {
+        constexpr int kPair = ROWS * V > 1 ? 2 : 1;
+        uint64_t number[kPair];
+        uint32_t word[kPair][4];
 #pragma unroll
-        for (int u = 0; u < ROWS; ++u)
-            number[u] = (uint64_t)row[u] * (uint32_t)(a.columns / 8) + (uint32_t)m.vector_number(v);
+        for (int i = 0; i < kPair; ++i)
+            number[i] = (uint64_t)row[(j + i) / V] * (uint32_t)(a.columns / 8) + (uint32_t)m.vector_number((j + i) % V);
         random_words(a.drop, seed, number, word);
 #pragma unroll
-        for (int u = 0; u < ROWS; ++u)
-            drop(a.drop, word[u], x[u][v]);
+        for (int i = 0; i < kPair; ++i)
+            drop(a.drop, word[i], x[(j + i) / V][(j + i) % V]);
     }
 }
 
