@@ -4,7 +4,7 @@
 namespace adasum {
 namespace {
 
-// Normalised values of a row from its kept statistics; zeros beyond the row.
+// Normalised values of a row from its kept statistics.  Vectors beyond the row meet gradients of zero only.
 template <bool WHOLE>
 __device__ __forceinline__ Eight kept_normalised(const Eight& x, float mean, float rstd, int count)
 {
@@ -13,15 +13,13 @@ __device__ __forceinline__ Eight kept_normalised(const Eight& x, float mean, flo
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         u.p[i] = (x.p[i] + off) * by;
-    if (count <= 0)
-        u = Eight{};
     cut_off<WHOLE>(u, count);
     return u;
 }
 
 // v, the gradients of the normalised values u, to the gradients of the norm's input; zeros beyond the row.  u(r, i)
-// gives the normalised values, twice, so that they need not be kept.
-template <bool WHOLE, int ROWS, int V, typename U>
+// gives the normalised values, twice, so that they need not be kept.  CLEAR: zeros beyond the row, for sums to come.
+template <bool WHOLE, bool CLEAR, int ROWS, int V, typename U>
 __device__ __forceinline__ void norm_back(Member& m, Exchange& e, const NormArgs& a, int kind, const int (&count)[V], U&& u,
                                           const float (&rstd)[ROWS], Eight (&v)[ROWS][V])
 {
@@ -68,7 +66,7 @@ __device__ __forceinline__ void norm_back(Member& m, Exchange& e, const NormArgs
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 v[r][j].p[i] = fma2(n.p[i], down, v[r][j].p[i] + off) * by;
-            if (count[j] <= 0)
+            if (CLEAR && count[j] <= 0)
                 v[r][j] = Eight{};
             cut_off<WHOLE>(v[r][j], count[j]);
         }
@@ -227,7 +225,7 @@ residual_norm_grad_kernel(const __grid_constant__ NormArgs a)
                     }
                 }
             affine(staged.pre_weight, nullptr, m, d);
-            norm_back<WHOLE>(m, exchange, a, a.pre, count, u, rstd, d);
+            norm_back<WHOLE, FULL>(m, exchange, a, a.pre, count, u, rstd, d);
         }
 #pragma unroll
         for (int r = 0; r < ROWS; ++r)
@@ -243,16 +241,19 @@ residual_norm_grad_kernel(const __grid_constant__ NormArgs a)
                 }
                 if (a.grad_residual && valid[r] && count[v] > 0) {
                     Eight back = d[r][v];
-                    scale(back, a.residual_scale);
+                    if (a.residual_scale != 1.0f)
+                        scale(back, a.residual_scale);
                     store_vector<WHOLE>(static_cast<R*>(a.grad_residual) + row[r] * a.grad_residual_stride + m.column(v), count[v], back);
                 }
             }
         if (a.branch) {
+            if (a.branch_scale != 1.0f) {
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r)
+                for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-                for (int v = 0; v < V; ++v)
-                    scale(d[r][v], a.branch_scale);
+                    for (int v = 0; v < V; ++v)
+                        scale(d[r][v], a.branch_scale);
+            }
             if constexpr (FULL) {
                 auto u = [&](int r, int v) {
                     return kept_normalised<WHOLE>(row_of(T{}, a.x, a.x_stride, x_piece, r, v), post_mean[r], post_rstd[r],
@@ -312,7 +313,7 @@ residual_norm_grad_kernel(const __grid_constant__ NormArgs a)
                             }
                         }
                     affine(staged.post_weight, nullptr, m, d);
-                    norm_back<WHOLE>(m, exchange, a, a.post, count, u, post_rstd, d);
+                    norm_back<WHOLE, false>(m, exchange, a, a.post, count, u, post_rstd, d);
                 }
             } else {
                 if (a.drop.seed)
