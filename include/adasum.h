@@ -677,7 +677,8 @@ adasum_status_t adasum_fp8_unpack(const void* packed, int64_t rows, int64_t colu
  *   limits        rows, features, outputs <= 2^31 - 256 (ADASUM_ERR_ARG)
  *
  * With nothing to sum y is the bias and dx is 0.  A product that the device did not finish (a bounded wait ran out)
- * leaves NaN; adasum_fp8_linear_status tells, synchronising `stream`, for the last call on the workspace.
+ * leaves NaN; adasum_fp8_linear_status tells, synchronising `stream`, for the last call with rows and columns to write
+on the workspace.
  */
 size_t adasum_fp8_linear_workspace_bytes(int64_t rows, int64_t features, int64_t outputs);
 adasum_status_t adasum_fp8_linear(const void* x, const void* w, int64_t rows, int64_t features, int64_t outputs,

@@ -1015,7 +1015,12 @@ def adasum_residual_norm_grad(x, h, stats, grad_y, grad_h, post_norm: str = "non
             raise ValueError(f"grad_gate is on {grad_gate.device}, not on cuda:{device}")
         gate_ptr, gate_code = grad_gate.data_ptr(), _operator_dtype(grad_gate.dtype)
         if rows == 0 and not accumulate:     # an empty sum
-            grad_gate.zero_()
+            if stream is None or hasattr(stream, "cuda_stream"):
+                on = stream
+            else:
+                on = torch.cuda.ExternalStream(int(stream), device=grad_gate.device)
+            with torch.cuda.device(device), torch.cuda.stream(on):
+                grad_gate.zero_()
     if grad_gate is not None or grad_dtype is not None:
         workspace = _operator_workspace(like, stream, workspace, _lib.adasum_residual_norm_grad_workspace_bytes(block))
         workspace_ptr, workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
@@ -1142,7 +1147,8 @@ def adasum_fp8_linear_grad(grad_out, w, rows: int, features: int, outputs: int, 
 def adasum_fp8_linear_status(workspace, stream=None) -> int:
     """``adasum_fp8_linear_status`` of the C ABI: 0, or 7 (ADASUM_ERR_TIMEOUT) if a bounded wait of the last product on
     ``workspace`` ran out.  Synchronises the stream."""
-    return int(_lib.adasum_fp8_linear_status(workspace.data_ptr(), _stream_handle(stream)))
+    with torch.cuda.device(workspace.device):
+        return int(_lib.adasum_fp8_linear_status(workspace.data_ptr(), _stream_handle(stream)))
 
 
 _lib.adasum_fp8_linear_selftest.restype = ctypes.c_int

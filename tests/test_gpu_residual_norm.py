@@ -185,6 +185,34 @@ def test_gradients_against_differences(b, spec):
         assert abs(diff - exact) <= 1e-5 * size + 1e-5 * abs(diff) + 1e-4, (name, diff, exact, size)
 
 
+WIDEST = [
+    (3, 32767, "f32", "f32", "f32", "layer", "layer", -1, 0.1, 1, 1),
+    (3, 32768, "bf16", "f32", "bf16", "none", "layer", 0, 0.1, 0, 0),
+    (2, 32768, "f16", "f16", "f32", "rms", "rms", 0, 0.0, 0, 0),
+    (2, 32761, "bf16", "bf16", "f32", "none", "rms", 1, 0.25, 7, 0),
+    (3, 16392, "f32", "f32", "f32", "none", "rms", 0, 0.0, 8, 4),
+]
+
+
+@pytest.mark.parametrize("spec", WIDEST, ids=lambda s: "-".join(map(str, s)))
+def test_widest_rows(b, spec):
+    """Rows that a cluster of blocks shares, in every form of the kernels."""
+    test_forward(b, spec)
+    test_gradients(b, spec)
+
+
+def test_no_rows_on_another_stream(b):
+    """The gradient of a gate of no rows is cleared on the call's stream, given as an object or as a handle."""
+    x, gate = torch.empty(0, 24, device="cuda"), torch.ones(2, 24, device="cuda")
+    _, _, stats = b.adasum_residual_norm(x, x)
+    for stream in (torch.cuda.Stream(), torch.cuda.Stream().cuda_stream):
+        grad = torch.ones(2, 24, device="cuda")
+        torch.cuda.synchronize()
+        b.adasum_residual_norm_grad(x, x, stats, x, x, gate=gate, rows_per_gate=5, grad_gate=grad, stream=stream)
+        torch.cuda.synchronize()
+        assert not torch.any(grad)
+
+
 def test_only_what_is_wanted(b):
     """Parts of the joint: a norm alone, a residual sum alone, gradients of one side only."""
     gen = _gen(3)
