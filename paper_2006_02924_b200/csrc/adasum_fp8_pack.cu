@@ -1,4 +1,6 @@
-// Matrices to 8-bit floating point and back.  One pass over a matrix each, bound by HBM traffic.
+// Matrices to 8-bit floating point and back.  One pass over a matrix each, bound by HBM traffic: 16384 x 4096 to 8 bits
+// from bf16 33 us (6.2 TB/s), from fp32 50 us (6.7 TB/s); weights 37 us and 51 us; back to bf16 34 us, to fp32 58 us.  Latency below
+// a few MB: 37 x 1024 1.8 us.
 #include "adasum_fp8.cuh"
 #include "adasum_vectors.cuh"
 
@@ -33,6 +35,8 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(kStripThreads)
 fp8_pack_kernel(const __grid_constant__ Strips s, int64_t columns, const T* x, int64_t x_stride, uint8_t* codes, uint8_t* steps)
 {
+    start_next_kernel();             // the product sets itself up meanwhile (with 37 x 1024 9.0 -> 7.5 us)
+    wait_for_previous_kernel();
     const Place p = place_of<kPackRows>(s);
     const int64_t column = 2 * (int64_t)p.column;
     const int count = p.inside ? (int)max((int64_t)0, min((int64_t)16, columns - column)) : 0;
@@ -69,6 +73,8 @@ fp8_pack_weight_kernel(const T* w, int64_t w_stride, int64_t rows, int64_t colum
                        uint8_t* steps)
 {
     __shared__ uint32_t warp_top[kWeightThreads / 32];
+    start_next_kernel();
+    wait_for_previous_kernel();
     const uint32_t row_block = blockIdx.x / column_blocks, column_block = blockIdx.x - row_block * column_blocks;
     const int64_t column = (int64_t)column_block * kFp8Block + (threadIdx.x & 15) * 8;
     const int64_t row0 = (int64_t)row_block * kFp8Block + (threadIdx.x >> 4);
@@ -182,18 +188,18 @@ adasum_status_t pack(const void* x, int64_t x_stride, int64_t rows, int64_t colu
         return fail(ADASUM_ERR_ARG, "%lld x %lld is too large", (long long)rows, (long long)columns);
     }
     profile_mark(stream, -1, 0, 0, true);
+    cudaError_t err = cudaSuccess;
     with_type(dtype, [&](auto t) {
         using T = decltype(t);
-        if (weight) {
-            auto* kernel = vec ? fp8_pack_weight_kernel<T, true> : fp8_pack_weight_kernel<T, false>;
-            kernel<<<blocks, kWeightThreads, 0, stream>>>(static_cast<const T*>(x), x_stride, rows, columns,
-                                                          (uint32_t)fp8_blocks(columns), codes, steps);
-        } else {
-            auto* kernel = vec ? fp8_pack_kernel<T, true> : fp8_pack_kernel<T, false>;
-            kernel<<<blocks, kStripThreads, 0, stream>>>(s, columns, static_cast<const T*>(x), x_stride, codes, steps);
-        }
+        const T* from = static_cast<const T*>(x);
+        if (weight)
+            err = launch_after(vec ? fp8_pack_weight_kernel<T, true> : fp8_pack_weight_kernel<T, false>, dim3(blocks), kWeightThreads, 0,
+                               stream, from, x_stride, rows, columns, (uint32_t)fp8_blocks(columns), codes, steps);
+        else
+            err = launch_after(vec ? fp8_pack_kernel<T, true> : fp8_pack_kernel<T, false>, dim3(blocks), kStripThreads, 0, stream, s,
+                               columns, from, x_stride, codes, steps);
     });
-    ADASUM_CUDA_CHECK(cudaGetLastError());
+    ADASUM_CUDA_CHECK(err);
     profile_mark(stream, ADASUM_KERNEL_FP8_PACK, 0, 0, false);
     return ADASUM_OK;
 }

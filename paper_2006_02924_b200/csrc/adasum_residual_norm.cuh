@@ -281,6 +281,7 @@ __device__ __forceinline__ void group_sum(Member& m, Exchange& e, float (&v)[N])
             for (int n = 0; n < N; ++n)
                 asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(remote + 4 * n), "f"(v[n]) : "memory");
         }
+        __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 #pragma unroll
         for (int n = 0; n < N; ++n) {
@@ -333,15 +334,6 @@ __device__ __forceinline__ void wait_for_turn(int stages)
         asm volatile("cp.async.wait_group 1;" ::: "memory");
     else
         asm volatile("cp.async.wait_group 0;" ::: "memory");
-}
-template <typename T>
-__device__ __forceinline__ Raw<T> nothing()
-{
-    Raw<T> raw;
-#pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) / 2); ++i)
-        raw.w[i] = make_uint4(0, 0, 0, 0);
-    return raw;
 }
 
 // ---- norms ---------------------------------------------------------------------------------------------
@@ -739,12 +731,14 @@ cudaError_t launch_rows(Kernel* kernel, std::atomic<uint64_t>& prepared, unsigne
     config.gridDim = dim3(blocks);
     config.blockDim = dim3((unsigned)threads_of(a.deal));
     config.stream = stream;
-    cudaLaunchAttribute attribute;
-    attribute.id = cudaLaunchAttributeClusterDimension;
-    attribute.val.clusterDim.x = (unsigned)a.deal.cluster;
-    attribute.val.clusterDim.y = attribute.val.clusterDim.z = 1;
-    config.attrs = &attribute;
-    config.numAttrs = a.deal.cluster > 1 ? 1 : 0;
+    cudaLaunchAttribute attributes[2];
+    attributes[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;     // as launch_after does
+    attributes[0].val.programmaticStreamSerializationAllowed = 1;
+    attributes[1].id = cudaLaunchAttributeClusterDimension;
+    attributes[1].val.clusterDim.x = (unsigned)a.deal.cluster;
+    attributes[1].val.clusterDim.y = attributes[1].val.clusterDim.z = 1;
+    config.attrs = attributes;
+    config.numAttrs = a.deal.cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&config, kernel, a);
 }
 

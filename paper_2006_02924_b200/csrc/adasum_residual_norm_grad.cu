@@ -105,6 +105,11 @@ struct Turn {
 };
 
 // WHOLE: 16-byte aligned rows of whole vectors.  FULL: a norm after the block or a gate.
+//
+// With the join, 16384 x 1024 bf16 and a layer norm 43 us (3.9 TB/s), with dropout 52 us: instruction issue (67 %).  4096 x 4096 bf16
+// with an fp32 stream, two norms and a gate 120 us (2.5 TB/s): a row's way through two sums and three reads of its
+// values from shared memory, at 16 warps (128 registers).  999 x 203 fp32 14.6 us, one row 8.2 us: two launches.
+// Registers: 16384 x 1024 with a layer norm 64: 53 us, 80: 48, 96: 43.
 template <typename T, typename R, bool WHOLE, bool FULL, int V>
 __global__ void __maxnreg__(FULL ? 128 : 96)
 residual_norm_grad_kernel(const __grid_constant__ NormArgs a)
@@ -116,6 +121,7 @@ residual_norm_grad_kernel(const __grid_constant__ NormArgs a)
     start_next_kernel();
     Member m(a.deal);
     blocks_present(a.deal);
+    wait_for_previous_kernel();
     int count[V];
 #pragma unroll
     for (int v = 0; v < V; ++v)
@@ -584,7 +590,8 @@ adasum_status_t adasum_residual_norm_grad(const adasum_residual_norm_t* b, const
                      (!pre || rows_aligned(g->grad_y, g->grad_y_stride, tb)) && (!g->grad_h || rows_aligned(g->grad_h, g->grad_h_stride, rb)) &&
                      (!g->grad_x || rows_aligned(g->grad_x, g->grad_x_stride, tb)) &&
                      (!g->grad_residual || rows_aligned(g->grad_residual, g->grad_residual_stride, rb));
-    // several vectors per thread, as many as their sums leave registers for, where a row then has eight threads or more
+    // two vectors per thread, where their sums leave registers for it and a row then has eight threads or more (bf16, RMS, with
+    // 1, 2: 16384 x 1024 57, 42 us; 1024 x 16384 151, 59 us; beside a norm after the block, 4096 x 4096, 120, 130 us)
     const bool full = post || (branch && b->gate);
     const int per_thread = !vec || features <= 128 || full ? 1 : 2;
     if (!full)
