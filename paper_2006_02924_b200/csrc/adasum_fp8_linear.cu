@@ -26,7 +26,13 @@
 // thousands of products that adds up.  Tensor memory (512 columns) holds two such sums, so that the next is formed while
 // the previous one is read, and two sets of step bytes; that is why a tile has 192 tokens and not 256.  (240 would
 // fit, but such tiles begin inside a block of step bytes, and the stores and the fence that it takes to move them to their places cost
-// every step 1200 cycles on its way: 75 us and more, with four warps in turn, for what takes 60.)
+// every step 1200 cycles on its way: with four warps in turn 71 to 83 us for 16384 tokens, 1024 to 4096, and 243 to 280 for 4096 to
+// 4096, against 73 and 254.)  Small products take tiles of 128 or 64 tokens, so that more pairs have one (plan_tiles).
+//
+// What bounds it: with all pairs at work, shared memory (each tensor core reads its rows and all tokens of a step, 448 cycles
+// for 384 of multiplications) and the power limit: 16384 tokens in bf16, 1024 to 4096 73 us (1.87 PFLOP/s), its gradient 66 us (2.07),
+// 4096 to 4096 254 us (2.16); a product of 8192 x 8192 x 8192 470 to 530 us (2.1 to 2.3).  The tensor cores' counter stands at 48
+// to 58 %.  Small products are bound by start and latency: 1024 to 4096, 1 to 64 tokens 5.7 us, 512 tokens 7.2, 2048 tokens 13.8.
 //
 // Tiles are dealt to the pairs whole, unless that leaves too many pairs idle; then the steps of all tiles are cut into
 // equal runs, and a tile whose steps fall to several pairs is joined, in their order, by fp8_join_kernel.  The
@@ -36,6 +42,8 @@
 // nothing more, so the waits that depend on it run out in turn and the launch ends; the block leaves NaN for all its
 // shares of tiles, and adasum_fp8_linear_status reports it.  Before a block ends its copies have landed, and the
 // pair's multiplications and their arrivals are done.
+#include <atomic>
+
 #include "adasum_fp8.cuh"
 #include "adasum_tensor.cuh"
 
@@ -51,7 +59,7 @@ constexpr int kWeightBytes = kHalf * kDepth;     // of a step and block
 constexpr int kParts = 4;                        // of a tile's tokens: four warps sum and store each
 constexpr int kSumWarps = 4 * kParts, kCopyWarp = kSumWarps, kMultiplyWarp = kCopyWarp + 1, kMemoryWarp = kCopyWarp + 2;
 constexpr int kBlockThreads = 32 * (kSumWarps + 4);
-constexpr uint32_t kBand = 8;
+constexpr uint32_t kBand = 8;                     // tiles of rows that are dealt out next to each other
 constexpr int kMaxPairs = 74;                    // 148 multiprocessors
 constexpr size_t kStatusBytes = 1024;
 constexpr int kStatusCount = 255;                // word that holds the number of blocks
@@ -92,8 +100,8 @@ struct LinearArgs {
 };
 
 // Where a role stands in its pair's work.  Whole tiles are dealt out one by one, pair after pair, so that the pairs walk
-// the summed index in step and read the same rows at the same time (16384 tokens, 4096 x 4096: 255 -> 230 us); cut ones
-// as runs.
+// the summed index in step and read the same rows at the same time; cut ones as runs (4608 tokens, 4096 to 4096: whole tiles 73 us,
+// runs and the join 86).
 struct Walk : Cursor {
     uint32_t pairs;
     __device__ __forceinline__ Walk(const LinearArgs& a, uint32_t pairs_, uint32_t pair)
@@ -111,7 +119,8 @@ struct Walk : Cursor {
             part = 3;
             return;
         }
-        // in bands of kBand tiles of rows, so that the tiles at hand share both operands
+        // in bands of kBand tiles of rows, so that the tiles at hand share both operands (16384 tokens, 4096 to 4096: row after
+        // row 266 us, in bands 254)
         const uint32_t tile = unit / a.chains, tiles_n = a.tiles / a.tiles_k;
         const uint32_t band = tile / (kBand * tiles_n), first = band * kBand, width = min(kBand, a.tiles_k - first);
         const uint32_t rest = tile - first * tiles_n;
@@ -234,7 +243,7 @@ __device__ __forceinline__ void write_pairs(const LinearArgs& a, int64_t t, int6
         const float other = __shfl_xor_sync(0xffffffffu, odd ? x : y, 1);
         const float low = odd ? other : x, high = odd ? y : other;
         if (i < count) {
-            // the result does not stay in the L2 in place of the operands (16384 tokens, 4096 x 4096: 249 -> 239 us)
+            // the result does not stay in the L2 in place of the operands (16384 tokens, 1024 to 4096: 75.7 -> 73.2 us)
             if constexpr (__is_same(TO, float))
                 __stcs(reinterpret_cast<float2*>(p), make_float2(low, high));
             else if constexpr (__is_same(TO, __half))
@@ -521,7 +530,8 @@ fp8_linear_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ 
 }
 
 // Tiles whose units fell to several pairs: the pairs' parts added in order.  grid.x = tiles, grid.y = parts of a tile's
-// 2 x `tokens` rows of 128; one warp per row, four elements per lane.
+// 2 x `tokens` rows of 128; one warp per row, four elements per lane.  Latency: 3 to 4 us (64 tokens, 4096 to 1024: 32 parts, 8.8 us
+// with the product) to 9 (512 tokens, 8192 to 1024: 12 MB of parts from the L2).
 constexpr int kJoinThreads = 256;
 
 __global__ void __launch_bounds__(kJoinThreads)
@@ -590,46 +600,59 @@ struct Work {
     int tokens;                // of a tile
     uint32_t tiles_k, tiles, iterations, chain_steps, chains, units, pairs;
     bool fits, whole;
+    int64_t cost;              // cycles, about
 };
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to; }
 
-// Tokens of a tile.  The smaller tiles are for few tokens, and for counts that fill the largest badly: a step costs
-// shared memory 448, 384 and 320 cycles for 192, 128 and 64 tokens.
-int tile_tokens(int64_t rows)
-{
-    const int64_t cost[3] = {up(rows, 192) * 448, up(rows, 128) * 384, up(rows, 64) * 320};
-    return cost[2] <= cost[1] && cost[2] <= cost[0] ? 64 : cost[1] <= cost[0] ? 128 : 192;
-}
-
-// `most`: pairs that run at once.
-Work plan_work(int64_t rows, int64_t wide, int64_t depth, uint32_t most)
+// Tiles of `tokens` tokens.  `most`: pairs that run at once.  A step costs shared memory (of 64 tokens: the loads from the
+// L2) about 448, 360 and 320 cycles for 192, 128 and 64 tokens.  Tiles are dealt out whole, or cut into equal runs of steps whose
+// parts a second kernel joins, whichever comes to less.  The join costs a launch, the parts' way through the L2 and, where
+// the product leaves it no idle multiprocessors to be brought in early, another microsecond.  Measured on 60 products of 1 to
+// 4608 tokens, the choice is the best of the six in 53 and 4 % off at worst (8192 to 1024, 512 tokens: 64 whole 19.4 us, cut
+// 18.3, 128 whole 20.1, cut 16.8, 192 whole 23.3, cut 19.4; 2048 tokens: 35.8, 39.1, 21.1, 27.8, 24.7, 28.6).
+Work plan_tiles(int tokens, int64_t rows, int64_t wide, int64_t depth, int64_t most)
 {
     Work w{};
-    w.tokens = tile_tokens(rows);
-    const int64_t tiles_k = up(wide, kTileRows), tiles_n = up(rows, w.tokens), iterations = up(depth, kDepth);
+    w.tokens = tokens;
+    const int64_t tiles_k = up(wide, kTileRows), tiles = tiles_k * up(rows, tokens), iterations = up(depth, kDepth);
     const int64_t limit = int64_t(1) << 31;
-    w.fits = tiles_k * tiles_n < limit && (iterations == 0 || tiles_k * tiles_n < limit / iterations);
+    w.fits = tiles < limit && tiles < limit / iterations;
     if (!w.fits)
         return w;
-    w.tiles_k = (uint32_t)tiles_k;
-    w.tiles = (uint32_t)(tiles_k * tiles_n);
-    w.iterations = (uint32_t)iterations;
-    // whole tiles, or equal runs of steps and a join of about 28 steps' time (1024 tokens, 4096 to 1024: 32 steps or 11,
-    // 16 us or 17 + 8)
-    const int64_t whole = up(w.tiles, most) * iterations, cut = up((int64_t)w.tiles * iterations, most) + 28;
-    w.whole = whole <= cut;
-    int64_t chain_steps = kChain;
-    if (!w.whole && (int64_t)w.tiles * up(iterations, kChain) < 2 * (int64_t)most) {
-        chain_steps = (int64_t)w.tiles * iterations / (2 * (int64_t)most);
-        chain_steps = chain_steps < kShortChain ? kShortChain : chain_steps;
+    int64_t cut_steps = kChain;
+    if (tiles * up(iterations, kChain) < 2 * most) {
+        cut_steps = tiles * iterations / (2 * most);
+        cut_steps = cut_steps < kShortChain ? kShortChain : cut_steps;
     }
-    w.chain_steps = (uint32_t)chain_steps;
-    w.chains = (uint32_t)up(iterations, chain_steps);
+    const int64_t cut_units = tiles * up(iterations, cut_steps), cut_pairs = cut_units < most ? cut_units : most;
+    const int64_t run = up(cut_units, cut_pairs) * cut_steps, share = up(tiles * iterations, cut_pairs);
+    const int64_t parts = cut_pairs + (tiles < cut_pairs ? tiles : cut_pairs);
+    const int64_t step = tokens == 192 ? 448 : tokens == 128 ? 360 : 320;
+    const int64_t whole = up(tiles, most) * iterations * step;
+    const int64_t cut = (run < share ? run : share) * step + 4200 + parts * tokens * 2 / 3 + (2 * cut_pairs > most ? 2500 : 0);
+    w.whole = whole <= cut;
+    w.cost = w.whole ? whole : cut;
+    w.tiles_k = (uint32_t)tiles_k;
+    w.tiles = (uint32_t)tiles;
+    w.iterations = (uint32_t)iterations;
+    w.chain_steps = (uint32_t)(w.whole ? kChain : cut_steps);
+    w.chains = (uint32_t)up(iterations, w.chain_steps);
     w.units = w.tiles * w.chains;
-    const uint32_t shares = w.whole ? w.tiles : w.units;
-    w.pairs = shares < most ? shares : most;
+    w.pairs = (uint32_t)(!w.whole ? cut_pairs : tiles < most ? tiles : most);
     return w;
+}
+
+// Tokens of a tile, or 0 if there are too many tiles.  More than the rows fill never cost less.
+int tile_tokens(int64_t rows, int64_t wide, int64_t depth)
+{
+    Work best{};
+    for (int tokens : {64, 128, 192}) {
+        const Work w = plan_tiles(tokens, rows, wide, depth, kMaxPairs);
+        if (w.fits && (!best.fits || w.cost < best.cost))
+            best = w;
+    }
+    return best.tokens;
 }
 
 // An upper bound for any number of pairs, never falling as rows rise: partial sums of the largest tile that so few
@@ -647,14 +670,15 @@ size_t linear_workspace(int64_t rows, int64_t wide, int64_t depth)
 template <int TOKENS, bool GRAD>
 cudaError_t prepare_kernel(uint32_t* pairs)
 {
-    static uint32_t cached[64] = {};
+    static std::atomic<uint32_t> cached[64] = {};
     int device = 0;
     cudaError_t err = cudaGetDevice(&device);
     if (err != cudaSuccess)
         return err;
     if (device < 0 || device >= 64)
         return cudaErrorInvalidDevice;
-    if (cached[device] == 0) {
+    *pairs = cached[device].load(std::memory_order_relaxed);
+    if (*pairs == 0) {
         auto* kernel = fp8_linear_kernel<TOKENS, GRAD>;
         const size_t shared = Shape<TOKENS>::kSharedBytes;
         if ((err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared)) != cudaSuccess)
@@ -674,9 +698,9 @@ cudaError_t prepare_kernel(uint32_t* pairs)
             return err;
         if (clusters < 1)
             return cudaErrorLaunchOutOfResources;
-        cached[device] = clusters < kMaxPairs ? (uint32_t)clusters : kMaxPairs;
+        *pairs = clusters < kMaxPairs ? (uint32_t)clusters : kMaxPairs;
+        cached[device].store(*pairs, std::memory_order_relaxed);
     }
-    *pairs = cached[device];
     return cudaSuccess;
 }
 
@@ -751,7 +775,8 @@ adasum_status_t linear(const void* x, const void* w, int64_t rows, int64_t featu
         return status;
     if (bias && !aligned_to(bias, operator_bytes(bias_dtype)))
         return fail(ADASUM_ERR_ARG, "bias is not aligned to its element size");
-    if (!plan_work(rows, wide, depth, 1).fits)
+    const int tokens = depth > 0 ? tile_tokens(rows, wide, depth) : 64;
+    if (tokens == 0)
         return fail(ADASUM_ERR_ARG, "%lld x %lld x %lld is too large", (long long)rows, (long long)features, (long long)outputs);
     const size_t need = linear_workspace(rows, wide, depth);
     if (!workspace || workspace_bytes < need)
@@ -786,12 +811,11 @@ adasum_status_t linear(const void* x, const void* w, int64_t rows, int64_t featu
         ADASUM_CUDA_CHECK(cudaGetLastError());
         return ADASUM_OK;
     }
-    const int tokens = tile_tokens(rows);
     uint32_t most = 0;
     cudaError_t err = cudaSuccess;
     with_shape(tokens, grad, [&](auto t, auto g) { err = prepare_kernel<decltype(t)::value, decltype(g)::value != 0>(&most); });
     ADASUM_CUDA_CHECK(err);
-    const Work l = plan_work(rows, wide, depth, most);
+    const Work l = plan_tiles(tokens, rows, wide, depth, most);
     const uint8_t* token_codes = static_cast<const uint8_t*>(x);
     const uint8_t* weight_codes = static_cast<const uint8_t*>(w);
     CUtensorMap token_map, weight_map, token_step_map, weight_step_map;
