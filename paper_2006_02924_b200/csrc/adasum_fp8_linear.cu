@@ -30,13 +30,16 @@
 // 4096, against 73 and 254.)  Small products take tiles of 128 or 64 tokens, so that more pairs have one (plan_tiles).
 //
 // What bounds it: with all pairs at work, shared memory (each tensor core reads its rows and all tokens of a step, 448 cycles
-// for 384 of multiplications) and the power limit: 16384 tokens in bf16, 1024 to 4096 73 us (1.87 PFLOP/s), its gradient 66 us (2.07),
-// 4096 to 4096 254 us (2.16); a product of 8192 x 8192 x 8192 470 to 530 us (2.1 to 2.3).  The tensor cores' counter stands at 48
+// for 384 of multiplications) and the power limit: 16384 tokens in bf16, 1024 to 4096 67 us (2.05 PFLOP/s), its gradient 66 us (2.07),
+// 4096 to 4096 250 us (2.2); a product of 8192 x 8192 x 8192 470 to 530 us (2.1 to 2.3).  The tensor cores' counter stands at 48
 // to 58 %.  Small products are bound by start and latency: 1024 to 4096, 1 to 64 tokens 5.7 us, 512 tokens 7.2, 2048 tokens 13.8.
 //
 // Tiles are dealt to the pairs whole, unless that leaves too many pairs idle; then the steps of all tiles are cut into
 // equal runs, and a tile whose steps fall to several pairs is joined, in their order, by fp8_join_kernel.  The
 // association of every sum is fixed by the sizes and the number of pairs that fit the device.
+//
+// Where a tile has eight steps at most and a pair several tiles of the same rows, the weights' codes stay in shared memory
+// and only tokens move: less than half the bytes from the L2 (16384 tokens, 1024 to 4096: 73 -> 67 us).
 //
 // Every wait has a limit.  A thread whose wait runs out records it and goes on without waiting, but hands over and issues
 // nothing more, so the waits that depend on it run out in turn and the launch ends; the block leaves NaN for all its
@@ -54,6 +57,7 @@ constexpr int kHalf = 128;                       // rows of W that a block of th
 constexpr int kTileRows = 2 * kHalf;
 constexpr int kDepth = kFp8Block;                // products per step
 constexpr int kChain = 8;                        // steps that are summed in tensor memory
+constexpr int kStaySteps = 8;                     // of a tile whose weights may stay
 constexpr int kShortChain = 4;                   // at least, where few tiles are cut: shorter runs save less than their parts cost to join
 constexpr int kWeightBytes = kHalf * kDepth;     // of a step and block
 constexpr int kParts = 4;                        // of a tile's tokens: four warps sum and store each
@@ -67,19 +71,24 @@ constexpr long long kWaitCycles = 2000000000;    // about a second (a real wait 
 constexpr long long kSelftestCycles = 2000000;   // about a millisecond
 constexpr int kLastWait = 4;                     // limits, for the last commit: other warps' waits may have to run out first
 
-template <int TOKENS>
+// Shared memory: the stages' codes, then the stages' step bytes.  A step's weights are part of its stage, or (STAY) have places
+// of their own in front of the stages' codes and step bytes, one per step of a tile.
+template <int TOKENS, bool STAY>
 struct Shape {
     static constexpr int kHalfTokens = TOKENS / 2, kPartTokens = TOKENS / kParts;
     static constexpr int kTokenBytes = kHalfTokens * kDepth;             // whole groups of 8 rows: 1024-byte aligned
-    static constexpr int kStageBytes = kWeightBytes + kTokenBytes;
+    static constexpr int kStageBytes = (STAY ? 0 : kWeightBytes) + kTokenBytes;
     // blocks of 128 rows that a tile's tokens lie in; a tile starts at the beginning of one or 64 rows into it
     static constexpr int kRowBlocks = TOKENS > 128 ? 2 : 1;
-    static constexpr int kScaleBytes = (1 + kRowBlocks) * kFp8StepBytes;  // step bytes of the block's rows and of the tokens
+    static constexpr int kScaleBytes = ((STAY ? 0 : 1) + kRowBlocks) * kFp8StepBytes;     // step bytes of the block's rows and of the tokens
     static constexpr int kStages = TOKENS > 128 ? 7 : 8;
-    static constexpr size_t kSharedBytes = (size_t)kStages * (kStageBytes + kScaleBytes) + 1024;   // + room to align to 1024
+    static constexpr int kStayBytes = STAY ? kStaySteps * kWeightBytes : 0, kStayScaleBytes = STAY ? kStaySteps * kFp8StepBytes : 0;
+    static constexpr size_t kSharedBytes =
+        (size_t)kStages * (kStageBytes + kScaleBytes) + kStayBytes + kStayScaleBytes + 1024;      // + room to align to 1024
     // columns of tensor memory: a sum, step bytes (4 for the rows, 4 or 8 for the tokens), the other sum, step bytes
     static constexpr int kSumColumns = 256, kScaleAt = 192;
     static_assert(TOKENS == 192 || TOKENS == 128 || TOKENS == 64, "");
+    static_assert(kSharedBytes <= 227 * 1024 - 512, "");
 };
 
 struct LinearArgs {
@@ -93,6 +102,7 @@ struct LinearArgs {
     // units of chain_steps steps, tile after tile (tiles of the same tokens next to each other)
     uint32_t tiles_k, tiles, iterations, chain_steps, chains, units;
     bool whole;                        // no tile is cut: runs are whole tiles
+    bool stay;                         // pairs take neighbouring tiles of the same rows, whose weights stay
     int* status;                       // one word per block, and their number
     long long wait_cycles;             // limit of a wait
     int withheld;                      // hand-over that never completes (self-test), or ADASUM_HAND_OVER_NONE
@@ -101,31 +111,37 @@ struct LinearArgs {
 
 // Where a role stands in its pair's work.  Whole tiles are dealt out one by one, pair after pair, so that the pairs walk
 // the summed index in step and read the same rows at the same time; cut ones as runs (4608 tokens, 4096 to 4096: whole tiles 73 us,
-// runs and the join 86).
+// runs and the join 86); tiles whose weights stay as runs too, tokens fastest.
 struct Walk : Cursor {
-    uint32_t pairs;
+    uint32_t pairs, until;
     __device__ __forceinline__ Walk(const LinearArgs& a, uint32_t pairs_, uint32_t pair)
         : Cursor(a, a.whole ? 0 : first_unit(a.units, pairs_, pair), a.whole ? 0 : first_unit(a.units, pairs_, pair + 1)), pairs(pairs_)
     {
         if (a.whole) {
             part = 0;
-            unit = pair * a.chains;
+            unit = a.stay ? first_unit(a.tiles, pairs, pair) * a.chains : pair * a.chains;
+            until = a.stay ? first_unit(a.tiles, pairs, pair + 1) * a.chains : a.units;
             enter_tile(a);
         }
     }
     __device__ __forceinline__ void enter_tile(const LinearArgs& a)
     {
-        if (unit >= a.units) {
+        if (unit >= until) {
             part = 3;
+            return;
+        }
+        chain = 0;
+        stop = unit + a.chains;
+        const uint32_t tile = unit / a.chains, tiles_n = a.tiles / a.tiles_k;
+        if (a.stay) {
+            tile_k = tile / tiles_n;
+            tile_n = tile - tile_k * tiles_n;
             return;
         }
         // in bands of kBand tiles of rows, so that the tiles at hand share both operands (16384 tokens, 4096 to 4096: row after
         // row 266 us, in bands 254)
-        const uint32_t tile = unit / a.chains, tiles_n = a.tiles / a.tiles_k;
         const uint32_t band = tile / (kBand * tiles_n), first = band * kBand, width = min(kBand, a.tiles_k - first);
         const uint32_t rest = tile - first * tiles_n;
-        chain = 0;
-        stop = unit + a.chains;
         tile_n = rest / width;
         tile_k = first + rest - tile_n * width;
     }
@@ -137,7 +153,8 @@ struct Walk : Cursor {
         }
         ++chain;
         if (++unit == stop) {
-            unit += (pairs - 1) * a.chains;
+            if (!a.stay)
+                unit += (pairs - 1) * a.chains;
             enter_tile(a);
         }
     }
@@ -268,7 +285,7 @@ __device__ __forceinline__ void write(const LinearArgs& a, int64_t t, int64_t m,
 template <int TOKENS>
 __device__ __noinline__ void leave_nan(const LinearArgs& a, uint32_t pairs, uint32_t pair, uint32_t rank, uint32_t thread)
 {
-    constexpr int kPartTokens = Shape<TOKENS>::kPartTokens;
+    constexpr int kPartTokens = Shape<TOKENS, false>::kPartTokens;
     const float nan = __uint_as_float(0x7fc00000u);
     const int row = 32 * ((thread >> 5) & 3) + (thread & 31), part = thread >> 7;
     uint32_t chain_begin = 0;
@@ -294,14 +311,14 @@ __device__ __noinline__ void leave_nan(const LinearArgs& a, uint32_t pairs, uint
 
 // ---- kernel ------------------------------------------------------------------------------------------
 //
-// GRAD: the weights' summed index is their row.
-template <int TOKENS, bool GRAD>
+// GRAD: the weights' summed index is their row.  STAY: the weights of a tile stay for the pair's next tile of the same rows.
+template <int TOKENS, bool GRAD, bool STAY>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kBlockThreads, 1)
 fp8_linear_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap token_map,
                   const __grid_constant__ CUtensorMap weight_map, const __grid_constant__ CUtensorMap token_step_map,
                   const __grid_constant__ CUtensorMap weight_step_map)
 {
-    using S = Shape<TOKENS>;
+    using S = Shape<TOKENS, STAY>;
     constexpr int kStages = S::kStages, kHalfTokens = S::kHalfTokens, kPartTokens = S::kPartTokens;
     extern __shared__ __align__(1024) unsigned char dynamic_shared[];
     // landed (first block): both blocks' codes and step bytes of a step are there; multiplied: the tensor cores are done with
@@ -314,8 +331,8 @@ fp8_linear_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ 
     start_next_kernel();             // the join; it waits for this kernel's end by itself
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const uint32_t stage0 = (shared_address(dynamic_shared) + 1023u) & ~1023u;
-    const uint32_t scales0 = stage0 + kStages * S::kStageBytes;
+    const uint32_t stay0 = (shared_address(dynamic_shared) + 1023u) & ~1023u, stage0 = stay0 + S::kStayBytes;
+    const uint32_t stay_scales0 = stage0 + kStages * S::kStageBytes, scales0 = stay_scales0 + S::kStayScaleBytes;
     const uint32_t landed0 = shared_address(landed), multiplied0 = shared_address(multiplied);
     const uint32_t formed0 = shared_address(formed), taken0 = shared_address(taken);
     const uint32_t finished0 = shared_address(&finished), nowhere0 = shared_address(nowhere);
@@ -438,30 +455,42 @@ fp8_linear_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ 
         // Both blocks' copies count on the first block's barrier, which expects their bytes.
         Ring<kStages> ring;
         uint32_t issued = 0;
-        constexpr uint32_t kBytes = 2 * (S::kStageBytes + S::kScaleBytes);
+        constexpr uint32_t kBytes = 2 * (S::kStageBytes + S::kScaleBytes), kStayingBytes = 2 * (kWeightBytes + kFp8StepBytes);
+        uint32_t held = ~0u;                     // STAY: rows whose weights are there
         const uint32_t first_landed0 = address_in_first(landed0);
         for (Walk c(a, pairs, pair); !c.done() && waiting; c.advance(a)) {
             const int m = (int)(c.tile_k * kTileRows + rank * kHalf), t = (int)(c.tile_n * TOKENS + rank * kHalfTokens);
             const int m_block = (int)(c.tile_k * 2 + rank), t_block = (int)((int64_t)c.tile_n * TOKENS / kFp8Block);
             const uint32_t end = c.first_step(a) + c.steps(a);
+            const bool bring = !STAY || c.tile_k != held;
+            held = c.tile_k;
             for (uint32_t step = c.first_step(a); step < end; ++step) {
                 wait(multiplied0 + 8 * ring.stage, ring.phase ^ 1);
+                // the last tile's step of the same place, which the stage's turn does not cover where tiles are short
+                if (STAY && bring && a.iterations < (uint32_t)kStages && issued >= a.iterations) {
+                    const uint32_t last = issued - a.iterations;
+                    wait(multiplied0 + 8 * (last % kStages), (last / kStages) & 1);
+                }
                 waiting = __all_sync(0xffffffffu, waiting);
                 if (!waiting)
                     break;
                 const uint32_t dst = stage0 + ring.stage * S::kStageBytes, steps = scales0 + ring.stage * S::kScaleBytes;
+                const uint32_t w_dst = STAY ? stay0 + step * kWeightBytes : dst, w_steps = STAY ? stay_scales0 + step * kFp8StepBytes : steps;
+                const uint32_t t_dst = STAY ? dst : dst + kWeightBytes, t_steps = STAY ? steps : steps + kFp8StepBytes;
                 const uint32_t bar = first_landed0 + 8 * ring.stage;
                 const int s = (int)step;
                 if (elected()) {
                     if (rank == 0)
-                        expect_bytes(landed0 + 8 * ring.stage, kBytes);
-                    copy_to_pair(dst, &weight_map, GRAD ? m : s * kDepth, GRAD ? s * kDepth : m, bar);
-                    copy_to_pair(dst + kWeightBytes, &token_map, s * kDepth, t, bar);
-                    // the words of all rows of a block of the weights are the same: they serve either direction
-                    copy_to_pair(steps, &weight_step_map, 0, GRAD ? m_block : s, GRAD ? s : m_block, bar);
+                        expect_bytes(landed0 + 8 * ring.stage, STAY && bring ? kBytes + kStayingBytes : kBytes);
+                    if (bring) {
+                        copy_to_pair(w_dst, &weight_map, GRAD ? m : s * kDepth, GRAD ? s * kDepth : m, bar);
+                        // the words of all rows of a block of the weights are the same: they serve either direction
+                        copy_to_pair(w_steps, &weight_step_map, 0, GRAD ? m_block : s, GRAD ? s : m_block, bar);
+                    }
+                    copy_to_pair(t_dst, &token_map, s * kDepth, t, bar);
 #pragma unroll
                     for (int i = 0; i < S::kRowBlocks; ++i)
-                        copy_to_pair(steps + (1 + i) * kFp8StepBytes, &token_step_map, 0, s, t_block + i, bar);
+                        copy_to_pair(t_steps + i * kFp8StepBytes, &token_step_map, 0, s, t_block + i, bar);
                 }
                 __syncwarp();
                 ++issued;
@@ -485,22 +514,25 @@ fp8_linear_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ 
             Ring<kStages> ring;
             uint32_t count = 0, turn = 0;
             const uint64_t codes0 = codes_descriptor(stage0), steps0 = steps_descriptor(scales0);
+            const uint64_t stay_codes0 = codes_descriptor(stay0), stay_steps0 = steps_descriptor(stay_scales0);
             for (Walk c(a, pairs, pair); !c.done(); c.advance(a), ++count) {
                 const uint32_t target = tensor_memory + (count & 1) * S::kSumColumns;
                 const uint32_t offset = (c.tile_n * TOKENS % kFp8Block) / 32;        // columns of 32 tokens each
                 wait(taken0 + 8 * (count & 1), ((count >> 1) & 1) ^ 1);
-                uint32_t accumulate = 0;
+                uint32_t accumulate = 0, place = 0;
                 for (uint32_t steps = c.steps(a); steps > 0; --steps) {
                     wait(landed0 + 8 * ring.stage, ring.phase);
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     if (waiting) {
-                        const uint64_t w = codes0 + ring.stage * (S::kStageBytes >> 4), t = w + (kWeightBytes >> 4);
-                        const uint64_t b = steps0 + ring.stage * (S::kScaleBytes >> 4);
+                        const uint64_t stage = codes0 + ring.stage * (S::kStageBytes >> 4), stage_steps = steps0 + ring.stage * (S::kScaleBytes >> 4);
+                        const uint64_t w = STAY ? stay_codes0 + place * (kWeightBytes >> 4) : stage;
+                        const uint64_t t = STAY ? stage : stage + (kWeightBytes >> 4);
+                        const uint64_t b = STAY ? stage_steps : stage_steps + (kFp8StepBytes >> 4);
                         const uint32_t w_steps = tensor_memory + S::kScaleAt + (turn & 1) * S::kSumColumns, t_steps = w_steps + 4;
-                        copy_steps(w_steps, b);
-                        copy_steps(t_steps, b + (kFp8StepBytes >> 4));
+                        copy_steps(w_steps, STAY ? stay_steps0 + place * (kFp8StepBytes >> 4) : stage_steps);
+                        copy_steps(t_steps, b);
                         if (S::kRowBlocks > 1)
-                            copy_steps(t_steps + 4, b + 2 * (kFp8StepBytes >> 4));
+                            copy_steps(t_steps + 4, b + (kFp8StepBytes >> 4));
 #pragma unroll
                         for (int s = 0; s < kDepth / 32; ++s)
                             // 32 products are 32 bytes further on, or 32 rows of 128 bytes (in units of 16)
@@ -511,6 +543,7 @@ fp8_linear_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ 
                             commit_to_both(formed0 + 8 * (count & 1));
                     }
                     accumulate = 1;
+                    ++place;
                     ++turn;
                     ring.advance();
                 }
@@ -599,7 +632,7 @@ __global__ void __launch_bounds__(256) fp8_bias_kernel(const __grid_constant__ L
 struct Work {
     int tokens;                // of a tile
     uint32_t tiles_k, tiles, iterations, chain_steps, chains, units, pairs;
-    bool fits, whole;
+    bool fits, whole, stay;
     int64_t cost;              // cycles, about
 };
 
@@ -640,6 +673,9 @@ Work plan_tiles(int tokens, int64_t rows, int64_t wide, int64_t depth, int64_t m
     w.chains = (uint32_t)up(iterations, w.chain_steps);
     w.units = w.tiles * w.chains;
     w.pairs = (uint32_t)(!w.whole ? cut_pairs : tiles < most ? tiles : most);
+    // Weights of a few steps stay in shared memory while a pair walks the tokens, where it has tiles enough of the same rows
+    // (16384 tokens, 1024 to 4096: 73 us brought anew for each tile, 67 kept).
+    w.stay = tokens == 192 && w.whole && iterations <= kStaySteps && tiles >= 2 * most && up(rows, tokens) >= 4;
     return w;
 }
 
@@ -667,7 +703,7 @@ size_t linear_workspace(int64_t rows, int64_t wide, int64_t depth)
     return kStatusBytes + (size_t)(pairs * 2 * kTileRows * tokens) * sizeof(float);
 }
 
-template <int TOKENS, bool GRAD>
+template <int TOKENS, bool GRAD, bool STAY>
 cudaError_t prepare_kernel(uint32_t* pairs)
 {
     static std::atomic<uint32_t> cached[64] = {};
@@ -679,8 +715,8 @@ cudaError_t prepare_kernel(uint32_t* pairs)
         return cudaErrorInvalidDevice;
     *pairs = cached[device].load(std::memory_order_relaxed);
     if (*pairs == 0) {
-        auto* kernel = fp8_linear_kernel<TOKENS, GRAD>;
-        const size_t shared = Shape<TOKENS>::kSharedBytes;
+        auto* kernel = fp8_linear_kernel<TOKENS, GRAD, STAY>;
+        const size_t shared = Shape<TOKENS, STAY>::kSharedBytes;
         if ((err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared)) != cudaSuccess)
             return err;
         cudaLaunchConfig_t config = {};
@@ -704,19 +740,21 @@ cudaError_t prepare_kernel(uint32_t* pairs)
     return cudaSuccess;
 }
 
-// Calls f(constant of the tile's tokens, constant of the direction).
+// Calls f(constant of the tile's tokens, constant of the direction, constant: the weights stay).
 template <int N>
 struct Number { static constexpr int value = N; };
 template <typename F>
-void with_shape(int tokens, bool grad, F&& f)
+void with_shape(const Work& w, bool grad, F&& f)
 {
     auto with_tokens = [&](auto g) {
-        if (tokens == 64)
-            f(Number<64>{}, g);
-        else if (tokens == 128)
-            f(Number<128>{}, g);
+        if (w.tokens == 64)
+            f(Number<64>{}, g, Number<0>{});
+        else if (w.tokens == 128)
+            f(Number<128>{}, g, Number<0>{});
+        else if (w.stay)
+            f(Number<192>{}, g, Number<1>{});
         else
-            f(Number<192>{}, g);
+            f(Number<192>{}, g, Number<0>{});
     };
     if (grad)
         with_tokens(Number<1>{});
@@ -813,9 +851,17 @@ adasum_status_t linear(const void* x, const void* w, int64_t rows, int64_t featu
     }
     uint32_t most = 0;
     cudaError_t err = cudaSuccess;
-    with_shape(tokens, grad, [&](auto t, auto g) { err = prepare_kernel<decltype(t)::value, decltype(g)::value != 0>(&most); });
+    Work l = plan_tiles(tokens, rows, wide, depth, kMaxPairs);
+    auto prepare = [&](auto t, auto g, auto s) {
+        err = prepare_kernel<decltype(t)::value, decltype(g)::value != 0, decltype(s)::value != 0>(&most);
+    };
+    with_shape(l, grad, prepare);
     ADASUM_CUDA_CHECK(err);
-    const Work l = plan_tiles(tokens, rows, wide, depth, most);
+    if (most != kMaxPairs) {
+        l = plan_tiles(tokens, rows, wide, depth, most);
+        with_shape(l, grad, prepare);
+        ADASUM_CUDA_CHECK(err);
+    }
     const uint8_t* token_codes = static_cast<const uint8_t*>(x);
     const uint8_t* weight_codes = static_cast<const uint8_t*>(w);
     CUtensorMap token_map, weight_map, token_step_map, weight_step_map;
@@ -835,14 +881,16 @@ adasum_status_t linear(const void* x, const void* w, int64_t rows, int64_t featu
     a.chains = l.chains;
     a.units = l.units;
     a.whole = l.whole;
+    a.stay = l.stay;
     a.wait_cycles = hand_over == ADASUM_HAND_OVER_NONE ? kWaitCycles : kSelftestCycles;
     a.withheld = hand_over;
     a.slots = reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes);
     profile_mark(stream, -1, 0, 0, true);
-    with_shape(tokens, grad, [&](auto t, auto g) {
+    with_shape(l, grad, [&](auto t, auto g, auto s) {
         constexpr int TOKENS = decltype(t)::value;
-        err = launch_after(fp8_linear_kernel<TOKENS, decltype(g)::value != 0>, dim3(2 * l.pairs), kBlockThreads,
-                           Shape<TOKENS>::kSharedBytes, stream, a, token_map, weight_map, token_step_map, weight_step_map);
+        constexpr bool STAY = decltype(s)::value != 0;
+        err = launch_after(fp8_linear_kernel<TOKENS, decltype(g)::value != 0, STAY>, dim3(2 * l.pairs), kBlockThreads,
+                           Shape<TOKENS, STAY>::kSharedBytes, stream, a, token_map, weight_map, token_step_map, weight_step_map);
     });
     ADASUM_CUDA_CHECK(err);
     profile_mark(stream, ADASUM_KERNEL_FP8_LINEAR, 0, 0, false);
