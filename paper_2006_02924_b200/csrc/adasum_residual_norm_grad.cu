@@ -88,6 +88,11 @@ struct Turn {
     __device__ __forceinline__ Turn(const Deal& d, uint32_t group, int64_t rows) : step(0), unit(group) { enter(d, rows); }
     __device__ __forceinline__ void enter(const Deal& d, int64_t rows)
     {
+        if (d.units <= d.pieces) {               // one gate row: nothing to divide
+            row = (int64_t)unit * d.unit_rows;
+            end = unit < d.units ? min(rows, row + d.unit_rows) : row;
+            return;
+        }
         const uint32_t of = unit / d.pieces, piece = unit - of * d.pieces;
         const int64_t span_end = min(rows, (int64_t)(of + 1) * d.gate_rows_span);
         row = (int64_t)of * d.gate_rows_span + (int64_t)piece * d.unit_rows;
@@ -106,9 +111,9 @@ struct Turn {
 
 // WHOLE: 16-byte aligned rows of whole vectors.  FULL: a norm after the block or a gate.
 //
-// With the join, 16384 x 1024 bf16 and a layer norm 43 us (3.9 TB/s), with dropout 52 us: instruction issue (67 %).  4096 x 4096 bf16
-// with an fp32 stream, two norms and a gate 120 us (2.5 TB/s): a row's way through two sums and three reads of its
-// values from shared memory, at 16 warps (128 registers).  999 x 203 fp32 14.6 us, one row 8.2 us: two launches.
+// With the join, 16384 x 1024 bf16 and an RMS norm 41 us (4.1 TB/s), a layer norm with dropout 50 us: instruction issue (67 %).
+// 4096 x 4096 bf16 with an fp32 stream, two norms and a gate 115 us (2.6 TB/s): a row's way through two sums and three reads of its
+// values from shared memory, at 16 warps (128 registers).  999 x 203 fp32 14.5 us, one row 7.9 us: two launches.
 // Registers: 16384 x 1024 with a layer norm 64: 53 us, 80: 48, 96: 43.
 template <typename T, typename R, bool WHOLE, bool FULL, int V>
 __global__ void __maxnreg__(FULL ? 128 : 96)
@@ -384,8 +389,9 @@ residual_norm_grad_kernel(const __grid_constant__ NormArgs a)
     }
 }
 
-// The parts of every sum added in order: grid.y = the vectors that are wanted, then the gate's rows.  32 columns x 32
-// shares of the parts per block: loads in flight are what it needs (256 threads, 296 parts: 10 us).
+// The parts of every sum added in order: grid.y = the vectors that are wanted, then the gate's rows.  128 columns x 32
+// shares of the parts per block, four columns per thread: loads in flight are what it needs (4096 x 4096 with 8 gates: a column
+// per thread 11 us after the gradients, four 6 us).
 struct JoinArgs {
     const float* parts;
     const float* gate_parts;
@@ -400,36 +406,43 @@ struct JoinArgs {
     bool accumulate;
     void* grad_gate;
 };
-constexpr int kShares = 32;
+constexpr int kShares = 32, kJoinColumns = 128;
 __global__ void __launch_bounds__(32 * kShares) residual_norm_join_kernel(const __grid_constant__ JoinArgs a)
 {
-    __shared__ float share[kShares][32];
+    __shared__ float4 share[kShares][32];
     wait_for_previous_kernel();
     const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
-    const int64_t column = (int64_t)blockIdx.x * 32 + lane;
+    const int64_t column = (int64_t)blockIdx.x * kJoinColumns + 4 * lane;
     const bool gate = (int)blockIdx.y >= a.vectors;
     const uint32_t gate_row = blockIdx.y - a.vectors;
     const int v = gate ? 0 : a.which[blockIdx.y];
     const uint32_t n = gate ? a.pieces : a.parts_count;
     const int64_t apart = gate ? a.columns : kVectors * a.columns;
     const float* p = gate ? a.gate_parts + (int64_t)gate_row * a.pieces * a.columns : a.parts + v * a.columns;
-    float total = 0.0f;
-    if (column < a.features) {
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (column < a.columns) {
 #pragma unroll 8
-        for (uint32_t i = slice; i < n; i += kShares)
-            total += __ldcg(p + i * apart + column);
+        for (uint32_t i = slice; i < n; i += kShares) {
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(p + i * apart + column));
+            sum.x += x.x;
+            sum.y += x.y;
+            sum.z += x.z;
+            sum.w += x.w;
+        }
     }
-    share[slice][lane] = total;
+    share[slice][lane] = sum;
     __syncthreads();
-    if (slice == 0 && column < a.features) {
-        total = 0.0f;
+    const int64_t at = (int64_t)blockIdx.x * kJoinColumns + threadIdx.x;
+    if (threadIdx.x < kJoinColumns && at < a.features) {
+        const float* part = reinterpret_cast<const float*>(share) + threadIdx.x;
+        float total = 0.0f;
 #pragma unroll
         for (int i = 0; i < kShares; ++i)
-            total += share[i][lane];
+            total += part[i * kJoinColumns];
         if (gate)
-            write_sum(a.grad_gate, a.gate_dtype, (int64_t)gate_row * a.features + column, total, a.gate_scale, a.accumulate);
+            write_sum(a.grad_gate, a.gate_dtype, (int64_t)gate_row * a.features + at, total, a.gate_scale, a.accumulate);
         else
-            write_sum(a.grad[v], v == 4 ? a.gate_dtype : a.dtype, column, total, v == 4 ? a.gate_scale : a.scale, a.accumulate);
+            write_sum(a.grad[v], v == 4 ? a.gate_dtype : a.dtype, at, total, v == 4 ? a.gate_scale : a.scale, a.accumulate);
     }
 }
 
@@ -646,7 +659,7 @@ adasum_status_t adasum_residual_norm_grad(const adasum_residual_norm_t* b, const
         j.gate_scale = g->gate_scale;
         j.accumulate = a.accumulate;
         j.grad_gate = g->grad_gate;
-        ADASUM_CUDA_CHECK(launch_after(residual_norm_join_kernel, dim3((unsigned)((features + 31) / 32), (unsigned)joined), 32 * kShares, 0,
+        ADASUM_CUDA_CHECK(launch_after(residual_norm_join_kernel, dim3((unsigned)((features + kJoinColumns - 1) / kJoinColumns), (unsigned)joined), 32 * kShares, 0,
                                        stream, j));
         profile_mark(stream, ADASUM_KERNEL_RESIDUAL_NORM_GRAD, 1, 0, false);
     }
