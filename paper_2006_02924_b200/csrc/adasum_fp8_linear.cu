@@ -38,7 +38,7 @@
 // equal runs, and a tile whose steps fall to several pairs is joined, in their order, by fp8_join_kernel.  The
 // association of every sum is fixed by the sizes and the number of pairs that fit the device.
 //
-// Where a tile has eight steps at most and a pair several tiles of the same rows, the weights' codes stay in shared memory
+// Where a tile has five to eight steps and a pair several tiles of the same rows, the weights' codes stay in shared memory
 // and only tokens move: less than half the bytes from the L2 (16384 tokens, 1024 to 4096: 73 -> 67 us).
 //
 // Every wait has a limit.  A thread whose wait runs out records it and goes on without waiting, but hands over and issues
@@ -102,7 +102,6 @@ struct LinearArgs {
     // units of chain_steps steps, tile after tile (tiles of the same tokens next to each other)
     uint32_t tiles_k, tiles, iterations, chain_steps, chains, units;
     bool whole;                        // no tile is cut: runs are whole tiles
-    bool stay;                         // pairs take neighbouring tiles of the same rows, whose weights stay
     int* status;                       // one word per block, and their number
     long long wait_cycles;             // limit of a wait
     int withheld;                      // hand-over that never completes (self-test), or ADASUM_HAND_OVER_NONE
@@ -112,6 +111,7 @@ struct LinearArgs {
 // Where a role stands in its pair's work.  Whole tiles are dealt out one by one, pair after pair, so that the pairs walk
 // the summed index in step and read the same rows at the same time; cut ones as runs (4608 tokens, 4096 to 4096: whole tiles 73 us,
 // runs and the join 86); tiles whose weights stay as runs too, tokens fastest.
+template <bool STAY>
 struct Walk : Cursor {
     uint32_t pairs, until;
     __device__ __forceinline__ Walk(const LinearArgs& a, uint32_t pairs_, uint32_t pair)
@@ -119,8 +119,13 @@ struct Walk : Cursor {
     {
         if (a.whole) {
             part = 0;
-            unit = a.stay ? first_unit(a.tiles, pairs, pair) * a.chains : pair * a.chains;
-            until = a.stay ? first_unit(a.tiles, pairs, pair + 1) * a.chains : a.units;
+            if constexpr (STAY) {
+                unit = first_unit(a.tiles, pairs, pair) * a.chains;
+                until = first_unit(a.tiles, pairs, pair + 1) * a.chains;
+            } else {
+                unit = pair * a.chains;
+                until = a.units;
+            }
             enter_tile(a);
         }
     }
@@ -133,7 +138,7 @@ struct Walk : Cursor {
         chain = 0;
         stop = unit + a.chains;
         const uint32_t tile = unit / a.chains, tiles_n = a.tiles / a.tiles_k;
-        if (a.stay) {
+        if constexpr (STAY) {
             tile_k = tile / tiles_n;
             tile_n = tile - tile_k * tiles_n;
             return;
@@ -153,7 +158,7 @@ struct Walk : Cursor {
         }
         ++chain;
         if (++unit == stop) {
-            if (!a.stay)
+            if (!STAY)
                 unit += (pairs - 1) * a.chains;
             enter_tile(a);
         }
@@ -282,7 +287,7 @@ __device__ __forceinline__ void write(const LinearArgs& a, int64_t t, int64_t m,
 
 // What a thread of the warps that sum leaves for its row and tokens where a wait of its block ran out: NaN, over whatever
 // it has left for any tile of the pair's run.
-template <int TOKENS>
+template <int TOKENS, bool STAY>
 __device__ __noinline__ void leave_nan(const LinearArgs& a, uint32_t pairs, uint32_t pair, uint32_t rank, uint32_t thread)
 {
     constexpr int kPartTokens = Shape<TOKENS, false>::kPartTokens;
@@ -290,7 +295,7 @@ __device__ __noinline__ void leave_nan(const LinearArgs& a, uint32_t pairs, uint
     const int row = 32 * ((thread >> 5) & 3) + (thread & 31), part = thread >> 7;
     uint32_t chain_begin = 0;
     bool fresh = true;
-    for (Walk c(a, pairs, pair); !c.done(); c.advance(a)) {
+    for (Walk<STAY> c(a, pairs, pair); !c.done(); c.advance(a)) {
         if (fresh)
             chain_begin = c.chain;
         fresh = c.last_of_share(a);
@@ -395,7 +400,7 @@ fp8_linear_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ 
         float sum[kPartTokens];
         uint32_t count = 0, chain_begin = 0;
         bool fresh = true;                       // the next unit is the first of its tile's share
-        for (Walk c(a, pairs, pair); !c.done(); c.advance(a), ++count) {
+        for (Walk<STAY> c(a, pairs, pair); !c.done(); c.advance(a), ++count) {
             if (fresh)
                 chain_begin = c.chain;
             wait(formed0 + 8 * (count & 1), (count >> 1) & 1);
@@ -444,7 +449,7 @@ fp8_linear_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ 
             }
         }
         if (gave_up != 0)
-            leave_nan<TOKENS>(a, pairs, pair, rank, threadIdx.x);
+            leave_nan<TOKENS, STAY>(a, pairs, pair, rank, threadIdx.x);
         // The last commit arrives in both blocks, and each waits for its own: in this warp, which has just seen the last sum.
         if (warp == 0) {
             waiting = true;
@@ -458,7 +463,7 @@ fp8_linear_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ 
         constexpr uint32_t kBytes = 2 * (S::kStageBytes + S::kScaleBytes), kStayingBytes = 2 * (kWeightBytes + kFp8StepBytes);
         uint32_t held = ~0u;                     // STAY: rows whose weights are there
         const uint32_t first_landed0 = address_in_first(landed0);
-        for (Walk c(a, pairs, pair); !c.done() && waiting; c.advance(a)) {
+        for (Walk<STAY> c(a, pairs, pair); !c.done() && waiting; c.advance(a)) {
             const int m = (int)(c.tile_k * kTileRows + rank * kHalf), t = (int)(c.tile_n * TOKENS + rank * kHalfTokens);
             const int m_block = (int)(c.tile_k * 2 + rank), t_block = (int)((int64_t)c.tile_n * TOKENS / kFp8Block);
             const uint32_t end = c.first_step(a) + c.steps(a);
@@ -515,7 +520,7 @@ fp8_linear_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ 
             uint32_t count = 0, turn = 0;
             const uint64_t codes0 = codes_descriptor(stage0), steps0 = steps_descriptor(scales0);
             const uint64_t stay_codes0 = codes_descriptor(stay0), stay_steps0 = steps_descriptor(stay_scales0);
-            for (Walk c(a, pairs, pair); !c.done(); c.advance(a), ++count) {
+            for (Walk<STAY> c(a, pairs, pair); !c.done(); c.advance(a), ++count) {
                 const uint32_t target = tensor_memory + (count & 1) * S::kSumColumns;
                 const uint32_t offset = (c.tile_n * TOKENS % kFp8Block) / 32;        // columns of 32 tokens each
                 wait(taken0 + 8 * (count & 1), ((count >> 1) & 1) ^ 1);
@@ -673,9 +678,10 @@ Work plan_tiles(int tokens, int64_t rows, int64_t wide, int64_t depth, int64_t m
     w.chains = (uint32_t)up(iterations, w.chain_steps);
     w.units = w.tiles * w.chains;
     w.pairs = (uint32_t)(!w.whole ? cut_pairs : tiles < most ? tiles : most);
-    // Weights of a few steps stay in shared memory while a pair walks the tokens, where it has tiles enough of the same rows
-    // (16384 tokens, 1024 to 4096: 73 us brought anew for each tile, 67 kept).
-    w.stay = tokens == 192 && w.whole && iterations <= kStaySteps && tiles >= 2 * most && up(rows, tokens) >= 4;
+    // Weights of five to eight steps stay in shared memory while a pair walks the tokens, where it has tiles enough of the same
+    // rows (1024 to 4096, brought anew for each tile or kept: 2048 tokens 14.0, 14.5 us, 4608 23.5, 22.9, 8192 39.1, 36.3, 16384 74.3, 68.6;
+    // with four steps, 512 to 2048, 16384 tokens: 35.7, 38.0: what it takes to store the result).
+    w.stay = tokens == 192 && w.whole && iterations > kStaySteps / 2 && iterations <= kStaySteps && tiles >= 4 * most;
     return w;
 }
 
@@ -881,7 +887,6 @@ adasum_status_t linear(const void* x, const void* w, int64_t rows, int64_t featu
     a.chains = l.chains;
     a.units = l.units;
     a.whole = l.whole;
-    a.stay = l.stay;
     a.wait_cycles = hand_over == ADASUM_HAND_OVER_NONE ? kWaitCycles : kSelftestCycles;
     a.withheld = hand_over;
     a.slots = reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes);
