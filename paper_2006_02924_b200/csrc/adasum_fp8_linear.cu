@@ -31,7 +31,7 @@
 //
 // What bounds it: with all pairs at work, shared memory (each tensor core reads its rows and all tokens of a step, 448 cycles
 // for 384 of multiplications) and the power limit: 16384 tokens in bf16, 1024 to 4096 67 us (2.05 PFLOP/s), its gradient 66 us (2.07),
-// 4096 to 4096 250 us (2.2); a product of 8192 x 8192 x 8192 470 to 530 us (2.1 to 2.3).  The tensor cores' counter stands at 48
+// 4096 to 4096 250 us (2.2); a product of 8192 x 8192 x 8192 470 to 530 us (2.1 to 2.3).  The tensor cores' counter stands at 51
 // to 58 %.  Small products are bound by start and latency: 1024 to 4096, 1 to 64 tokens 5.7 us, 512 tokens 7.2, 2048 tokens 13.8.
 //
 // Tiles are dealt to the pairs whole, unless that leaves too many pairs idle; then the steps of all tiles are cut into

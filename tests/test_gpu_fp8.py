@@ -319,3 +319,33 @@ def test_a_wait_that_runs_out_where_weights_stay(b, hand_over):
         assert torch.isnan(y).all()
     b.adasum_fp8_linear(px, pw, rows, features, outputs, out=y, workspace=ws)
     assert b.adasum_fp8_linear_status(ws) == 0 and torch.equal(y, want)
+
+
+def test_calls_from_two_threads(b):
+    """Threads with streams and workspaces of their own, whose calls overlap on the host and on the GPU."""
+    from concurrent.futures import ThreadPoolExecutor
+
+    jobs = []
+    for seed, (rows, features, outputs) in enumerate([(300, 1024, 1000), (3700, 700, 4096), (70, 2000, 640), (1000, 1024, 4096)]):
+        gen = _gen(seed)
+        px, pw = b.adasum_fp8_pack(_matrix(gen, rows, features, "bf16")), b.adasum_fp8_pack_weight(_matrix(gen, outputs, features, "f32"))
+        want = b.adasum_fp8_linear(px, pw, rows, features, outputs)
+        norm = b.adasum_residual_norm(None, want, pre_norm="layer")[1]
+        jobs.append((px, pw, rows, features, outputs, want, norm))
+    torch.cuda.synchronize()
+
+    def work(order):
+        stream = torch.cuda.Stream()
+        same = []
+        with torch.cuda.stream(stream):
+            for _ in range(10):
+                for i in order:
+                    px, pw, rows, features, outputs, want, norm = jobs[i]
+                    y = b.adasum_fp8_linear(px, pw, rows, features, outputs)
+                    z = b.adasum_residual_norm(None, y, pre_norm="layer")[1]
+                    same += [(y == want).all(), (z == norm).all()]
+        stream.synchronize()
+        return all(bool(s) for s in same)
+
+    with ThreadPoolExecutor(2) as pool:
+        assert all(pool.map(work, [(0, 1, 2, 3), (3, 1, 0, 2)]))
