@@ -34,7 +34,7 @@ dropout_kernel(const __grid_constant__ Strips s, const __grid_constant__ Dropout
     }
     uint32_t word[kDropRows][4];
     if (d.seed)
-        random_words(d, __ldg(reinterpret_cast<const unsigned long long*>(d.seed)), vector, word);
+        random_words(d, *d.seed, vector, word);
 #pragma unroll
     for (int u = 0; u < kDropRows; ++u) {
         const int64_t row = p.row0 + u * p.step;

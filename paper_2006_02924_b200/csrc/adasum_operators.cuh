@@ -149,7 +149,9 @@ __device__ __forceinline__ void divide_row(const RowDivider& d, uint64_t n, uint
 }
 
 // Until the previous kernel of the stream has ended and its writes are visible.  The first thing that every
-// thread of a kernel launched by launch_after does: then "ended" also covers the kernels before that one.
+// thread of a kernel launched by launch_after does: then "ended" also covers the kernels before that one.  Such a kernel
+// reads global memory by coherent loads only: the non-coherent ones (__ldg) ask for memory that nobody writes in the
+// kernel's whole life, and the previous kernel may write while this one waits.
 __device__ __forceinline__ void wait_for_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 // From here on the stream's next kernel may be brought in.
 __device__ __forceinline__ void start_next_kernel() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }

@@ -49,7 +49,7 @@ residual_norm_kernel(const __grid_constant__ NormArgs a)
     }
     uint64_t seed = 0;
     if (a.drop.seed)
-        seed = __ldg(reinterpret_cast<const unsigned long long*>(a.drop.seed));
+        seed = *a.drop.seed;
     const uint32_t r_piece = a.x ? V * (uint32_t)(sizeof(T) / 2) * apart : 0;      // place of the residual among the thread's pieces of a row
     uint32_t stage = 0;
     for (uint32_t round = 0; round < a.deal.rounds; ++round) {

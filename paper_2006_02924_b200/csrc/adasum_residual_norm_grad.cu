@@ -169,11 +169,11 @@ residual_norm_grad_kernel(const __grid_constant__ NormArgs a)
             const bool valid = t.row + r < t.end;
             const float* p = a.stats + t.row + r;
             if constexpr (FULL) {
-                next_stats[r][0] = valid && a.post == ADASUM_NORM_LAYER ? __ldg(p) : 0.0f;
-                next_stats[r][1] = post ? valid ? __ldg(p + a.rows) : 0.0f : 1.0f;
+                next_stats[r][0] = valid && a.post == ADASUM_NORM_LAYER ? *p : 0.0f;
+                next_stats[r][1] = post ? valid ? p[a.rows] : 0.0f : 1.0f;
             }
-            next_stats[r][2] = valid && pre && a.pre == ADASUM_NORM_LAYER ? __ldg(p + 2 * a.rows) : 0.0f;
-            next_stats[r][3] = valid && pre ? __ldg(p + 3 * a.rows) : 0.0f;
+            next_stats[r][2] = valid && pre && a.pre == ADASUM_NORM_LAYER ? p[2 * a.rows] : 0.0f;
+            next_stats[r][3] = valid && pre ? p[3 * a.rows] : 0.0f;
         }
     };
     // sums of the vectors' gradients: pre weight, pre bias, then post weight, post bias, gate
@@ -184,7 +184,7 @@ residual_norm_grad_kernel(const __grid_constant__ NormArgs a)
     }
     uint64_t seed = 0;
     if (a.drop.seed)
-        seed = __ldg(reinterpret_cast<const unsigned long long*>(a.drop.seed));
+        seed = *a.drop.seed;
     load_stats(now);
     uint32_t stage = 0;
     for (uint32_t turn = 0; turn < turns; ++turn) {

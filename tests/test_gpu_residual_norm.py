@@ -352,3 +352,32 @@ def test_no_rows(b):
     empty = torch.empty(4, 0, device="cuda")
     h, y, _ = b.adasum_residual_norm(empty, empty)
     assert h.shape == (4, 0) and y.shape == (4, 0)
+
+
+@pytest.mark.parametrize("rows,features", [(600, 512), (37, 203), (2000, 64), (20, 8192)])
+def test_calls_in_a_row_on_one_stream_read_the_last_statistics(b, rows, features):
+    """Forward and gradient calls in turn, each brought in while the last one ends, over one buffer of statistics and with
+    other inputs each time: the same bits as calls that wait for one another."""
+    gen = _gen(11)
+    xs = [_matrix(gen, rows, features, "bf16", size=2.0**i, mean=0.5 * i) for i in range(4)]
+    residual, dy, dh = (_matrix(gen, rows, features, "bf16") for _ in range(3))
+    seeds = [_seed(5), _seed(6), _seed(7)]
+    stats, h, y = torch.empty(4, rows, device="cuda"), torch.empty_like(residual), torch.empty_like(residual)
+
+    def run(times, wait):
+        out = [torch.empty(2, rows, features, dtype=torch.bfloat16, device="cuda") for _ in range(times)]
+        torch.cuda.synchronize()
+        for i, (dx, dr) in enumerate(out):
+            call = dict(post_norm="layer", pre_norm="layer", dropout=0.25, seed=seeds[i % 3], site=i)
+            b.adasum_residual_norm(xs[i % 4], residual, h=h, y=y, stats=stats, **call)
+            if wait:
+                torch.cuda.synchronize()
+            b.adasum_residual_norm_grad(xs[i % 4], h, stats, dy, dh, grad_x=dx, grad_residual=dr, **call)
+            if wait:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        return out
+
+    want = run(60, True)
+    for _ in range(3):
+        assert all(torch.equal(x, y) for x, y in zip(run(60, False), want))
