@@ -786,10 +786,8 @@ inline adasum_status_t check_block(const adasum_residual_norm_t* b)
     return ADASUM_OK;
 }
 
-inline int64_t gate_rows_of(const adasum_residual_norm_t& b)
-{
-    return b.rows > 0 ? (b.rows + b.rows_per_gate - 1) / b.rows_per_gate : 0;
-}
+// rows_per_gate may be anything up to the type's end.
+inline int64_t gate_rows_of(const adasum_residual_norm_t& b) { return b.rows > 0 ? (b.rows - 1) / b.rows_per_gate + 1 : 0; }
 
 inline adasum_status_t describe(const adasum_residual_norm_t& b, bool has_x, NormArgs* a)
 {

@@ -192,3 +192,18 @@ def test_reference_rounding_to_eight_bits():
     assert np.array_equal(codes[:, 0], np.arange(127)) and np.all(steps == 127)
     codes, _ = ref.fp8_pack(np.stack(((values[1:] + values[:-1]) / 2, np.full(126, 448.0)), axis=1))
     assert np.all(codes[:, 0] % 2 == 0)
+
+
+@pytest.mark.parametrize("per_gate", [7, 1 << 31, (1 << 63) - 6, (1 << 63) - 1])
+def test_a_gate_for_more_rows_than_there_are(b, per_gate):
+    """A gate whose row serves any number of rows is one row: it and its gradient are checked for overlaps as such."""
+    gate = dict(gate=P, per_gate=per_gate)
+    forward = b.raw().adasum_residual_norm
+    for h in (P, P - 80, P + 79 - 79 % 16):
+        code = forward(_block(b, **gate), A, 40, B, 40, h, 40, D, 40, W, None)
+        assert b.adasum_status_string(code) == "ADASUM_ERR_ARG"
+    E, F, G = 0x70000000, 0x80000000, 0x90000000
+    for into in (F, G, A, W, P):
+        grads = b._RESIDUAL_NORM_GRADS.pack(A, B, C, D, E, 40, 40, 40, 40, F, G, 40, 40, 0, 0, 0, 0, into, F32, F32, 1.0, 1.0, 0)
+        code = b.raw().adasum_residual_norm_grad(_block(b, **gate), grads, W, BIG, None)
+        assert b.adasum_status_string(code) == "ADASUM_ERR_ARG"
