@@ -571,7 +571,9 @@ adasum_status_t adasum_dropout(const void* x, int64_t x_stride, int64_t rows, in
  * RMS norm: u = x rstd, rstd = (mean(x^2) + eps)^(-1/2); layer norm: u = (x - mean) rstd, rstd = (var + eps)^(-1/2) with the
  * variance of all features; then u * weight + bias (NULL: 1 and 0).  Row r takes row r / rows_per_gate of the gate: one
  * for all rows (a learned scale per channel), one per sequence, one per row.  Everything between the loads and the
- * stored values is fp32; y is the norm of h before h is rounded.  At most ADASUM_NORM_MAX_FEATURES features.
+ * stored values is fp32; y is the norm of h before h is rounded.  Rows whose sum of squares leaves fp32's range at either end
+(the lower one matters without eps, or next to none) are scaled by a power of two for it; an rstd that itself is too large
+for fp32 is kept as Inf, and the gradients of such a row are not finite.  At most ADASUM_NORM_MAX_FEATURES features.
  */
 #define ADASUM_NORM_MAX_FEATURES 32768
 

@@ -68,6 +68,7 @@ struct NormArgs {
     int64_t rows;
     int features, post, pre;
     float inv_features, eps, branch_scale, residual_scale;
+    float least_squares;       // a row whose sum of squares is smaller is scaled up first; 0: eps makes that needless
     Vector post_weight, post_bias, pre_weight, pre_bias, gate;
     int64_t gate_stride;
     RowDivider rows_per_gate;
@@ -339,16 +340,13 @@ __device__ __forceinline__ void wait_for_turn(int stages)
 // ---- norms ---------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ bool in_range(float s) { return fabsf(s) < __uint_as_float(0x7f800000u); }
-// Has a sum of the group (of the warp's groups) left fp32's range, or is not a number?  The same answer for all its threads.
-template <int ROWS>
-__device__ __forceinline__ bool any_out_of_range(const Member& m, const float (&s)[ROWS])
-{
-    bool out = false;
-#pragma unroll
-    for (int u = 0; u < ROWS; ++u)
-        out |= !in_range(s[u]);
-    return m.deal.warps == 1 ? __any_sync(0xffffffffu, out) : out;
-}
+// Does something hold for a thread of the group (of the warp's groups)?  `some` is the same for all threads of a group; so is the answer.
+__device__ __forceinline__ bool any_of(const Member& m, bool some) { return m.deal.warps == 1 ? __any_sync(0xffffffffu, some) : some; }
+
+// Powers of two that bring a row's squares back into fp32's range, and the least sum of squares that is taken as it is: of
+// 2^-100, squares below fp32's normal values (2^-150 off each, 2^15 at most) take 2^-35 away.  Smaller sums make no difference
+// beside an eps of 2^-66 or more.
+constexpr float kRowDown = 0x1p-96f, kRowUp = 0x1p96f, kLeastSquares = 0x1p-100f, kEpsAbove = 0x1p-66f;
 
 // Statistics of ROWS rows; x becomes the normalised values.  count: the elements of the thread's vectors.
 template <bool WHOLE, int ROWS, int V>
@@ -371,7 +369,11 @@ __device__ __forceinline__ void normalise(Member& m, Exchange& e, const NormArgs
 #pragma unroll
         for (int u = 0; u < ROWS; ++u)
             mean[u] = s[u] * a.inv_features;
-        if (any_out_of_range(m, s)) {            // such rows are divided before they are added
+        bool outside = false;
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u)
+            outside |= !in_range(s[u]);
+        if (any_of(m, outside)) {                // such rows are divided before they are added
             float t[ROWS];
 #pragma unroll
             for (int u = 0; u < ROWS; ++u) {
@@ -408,32 +410,45 @@ __device__ __forceinline__ void normalise(Member& m, Exchange& e, const NormArgs
             s[u] += count[v] > 0 ? dot_of(x[u][v], x[u][v]) : 0.0f;
     }
     group_sum(m, e, s);
+    float factor[ROWS];                          // of the values
+    bool outside = false;
 #pragma unroll
-    for (int u = 0; u < ROWS; ++u)
-        rstd[u] = reciprocal_root(fmaf(s[u], a.inv_features, a.eps));
-    if (any_out_of_range(m, s)) {                // such rows: of the values times 2^-96
-        const float down = __uint_as_float((127u - 96u) << 23);
+    for (int u = 0; u < ROWS; ++u) {
+        factor[u] = rstd[u] = reciprocal_root(fmaf(s[u], a.inv_features, a.eps));
+        outside |= !(s[u] >= a.least_squares && in_range(s[u]));
+    }
+    if (any_of(m, outside)) {                    // such rows: of the values times 2^-96 or 2^96
         float t[ROWS];
 #pragma unroll
         for (int u = 0; u < ROWS; ++u) {
+            const float by = s[u] < a.least_squares ? kRowUp : kRowDown;
             t[u] = 0.0f;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 Eight y = x[u][v];
-                scale(y, down);
+                scale(y, by);
                 t[u] += count[v] > 0 ? dot_of(y, y) : 0.0f;
             }
         }
         group_sum(m, e, t);
 #pragma unroll
-        for (int u = 0; u < ROWS; ++u)
-            rstd[u] = in_range(s[u]) ? rstd[u] : down * reciprocal_root(fmaf(t[u], a.inv_features, a.eps * down * down));
+        for (int u = 0; u < ROWS; ++u) {
+            if (s[u] < a.least_squares) {        // rstd may leave fp32's range, the normalised values do not
+                factor[u] = reciprocal_root(fmaf(t[u], a.inv_features, a.eps * kRowUp * kRowUp));
+                rstd[u] = kRowUp * factor[u];
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    scale(x[u][v], kRowUp);
+            } else if (!in_range(s[u])) {
+                factor[u] = rstd[u] = kRowDown * reciprocal_root(fmaf(t[u], a.inv_features, a.eps * kRowDown * kRowDown));
+            }
+        }
     }
 #pragma unroll
     for (int u = 0; u < ROWS; ++u)
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            scale(x[u][v], rstd[u]);
+            scale(x[u][v], factor[u]);
 }
 
 // The norms' vectors of the block's columns, and every thread's columns of the gate's rows, in shared memory.
@@ -798,6 +813,7 @@ inline adasum_status_t describe(const adasum_residual_norm_t& b, bool has_x, Nor
     a->pre = b.pre_norm;
     a->inv_features = 1.0f / (float)b.features;
     a->eps = b.eps;
+    a->least_squares = b.eps < kEpsAbove ? kLeastSquares : 0.0f;
     a->branch_scale = b.branch_scale;
     a->residual_scale = b.residual_scale;
     a->post_weight = vector_of(b.post_weight, b.param_dtype);

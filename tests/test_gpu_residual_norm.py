@@ -381,3 +381,82 @@ def test_calls_in_a_row_on_one_stream_read_the_last_statistics(b, rows, features
     want = run(60, True)
     for _ in range(3):
         assert all(torch.equal(x, y) for x, y in zip(run(60, False), want))
+
+
+# rows, features, dtype: a few lanes, whole vectors, short ones, several warps, a cluster of blocks
+ENDS = [(9, 24, "f32"), (50, 1000, "f32"), (33, 203, "f32"), (5, 4096, "bf16"), (3, 20001, "f32"), (2, 32768, "bf16")]
+
+
+def _check_norm_alone(b, x, kind, eps, dtype, what):
+    eps = float(np.float32(eps))
+    none, y, stats = b.adasum_residual_norm(None, x, pre_norm=kind, eps=eps, want_h=False)
+    want, bound, mean, dmean, rstd, drstd = ref.norm(to64(x), 0 * to64(x), kind, eps)
+    _close(y, (want, bound), dtype, f"{what} y")
+    if kind == "layer":
+        # a rounding below fp32's normal values is off by half their step, 2^-150, once in the mean and once in its sum
+        assert_close(to64(stats[2]), mean, 1.1 * dmean + 2 * ref.U * np.abs(mean) + 2.0**-149, f"{what} mean")
+    assert_close(to64(stats[3]), rstd, 1.1 * drstd + 2 * ref.U * rstd, f"{what} rstd")
+    return stats
+
+
+@pytest.mark.parametrize("shape", ENDS, ids=lambda s: "-".join(map(str, s)))
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("size", [1e-15, 1e-18, 1e-20, 1e-22, 1e-25, 1e-36, 1e18, 1e22, 1e36])
+def test_rows_whose_squares_leave_the_range(b, size, kind, shape):
+    """Without eps, and with one that fp32 holds as a subnormal: sums of squares that are too small or too large for fp32,
+    and (1e36, layer) sums of the values that are too large, give what the formula gives, and so do the gradients."""
+    rows, features, dtype = shape
+    gen = _gen(12)
+    x = (_matrix(gen, rows, features, "f32", mean=3.0 if size > 1 else 0.3).double() * size).to(TORCH[dtype])
+    for eps in (0.0, 1e-40):
+        stats = _check_norm_alone(b, x, kind, eps, dtype, f"eps {eps}")
+    dy = _matrix(gen, rows, features, dtype)
+    _, dr = b.adasum_residual_norm_grad(None, x, stats, dy, None, pre_norm=kind, want_x=False)
+    o = dict(post_norm="none", pre_norm=kind, pre_weight=1.0, pre_bias=0.0, gate=None, branch_scale=1.0, residual_scale=1.0)
+    _close(dr, ref.joint_grad(None, to64(x), to64(stats), to64(dy), None, o, None)["residual"], dtype, "gradient")
+
+
+@pytest.mark.parametrize("shape", ENDS, ids=lambda s: "-".join(map(str, s)))
+def test_rows_of_all_sizes_side_by_side(b, shape):
+    """Rows of one warp or block that need no other scale, a larger and a smaller one; a row of zeros without eps is no
+    number; one of the smallest subnormals, whose rstd fp32 cannot hold, still has its normalised values."""
+    _, features, dtype = shape
+    gen = _gen(13)
+    sizes = torch.tensor([1.0, 1e-25, 1e25, 1e-22, 0.0, 1e-3, 1e-36, 1e30, 1.0], dtype=torch.float64, device="cuda")
+    x = (_matrix(gen, 9, features, "f32").double() * sizes[:, None]).to(TORCH[dtype])
+    some = sizes != 0
+    for kind in ("rms", "layer"):
+        none, y, stats = b.adasum_residual_norm(None, x, pre_norm=kind, eps=0.0, want_h=False)
+        assert torch.isnan(y[~some]).all()
+        want, bound, *_ = ref.norm(to64(x[some]), 0 * to64(x[some]), kind, 0.0)
+        _close(y[some], (want, bound), dtype, kind)
+    steps = torch.randint(1, 100, (9, features), generator=gen, device="cuda").double()
+    x = (steps * (2.0**-149 if dtype == "f32" else 2.0**-133)).to(TORCH[dtype])
+    none, y, stats = b.adasum_residual_norm(None, x, eps=0.0, want_h=False)
+    want, bound, *_ = ref.norm(to64(x), 0 * to64(x), "rms", 0.0)
+    _close(y, (want, bound), dtype, "subnormal")
+
+
+@pytest.mark.parametrize("eps", [2.0**-68, 2.0**-66, 2.0**-64, 1e-12])
+def test_small_rows_beside_eps(b, eps):
+    """Rows from far above eps to far below it."""
+    gen = _gen(14)
+    for size in (2.0**-20, 2.0**-33, 2.0**-45, 2.0**-52, 2.0**-60, 2.0**-80):
+        x = _matrix(gen, 20, 1000, "f32", mean=0.3) * size
+        for kind in ("rms", "layer"):
+            _check_norm_alone(b, x, kind, eps, "f32", f"{size} {kind}")
+
+
+@pytest.mark.parametrize("features", [24, 203, 1024, 4096])
+def test_small_branches_behind_a_norm(b, features):
+    """The norm after the block has the same range as the one before the next."""
+    gen = _gen(15)
+    for size in (1e-25, 1e-36, 1e25):
+        x, r = _matrix(gen, 17, features, "f32", mean=0.3) * size, _matrix(gen, 17, features, "f32")
+        for post in ("rms", "layer"):
+            h, y, stats = b.adasum_residual_norm(x, r, post_norm=post, pre_norm="rms", eps=0.0)
+            o = dict(post_norm=post, post_weight=1.0, post_bias=0.0, pre_norm="rms", pre_weight=1.0, pre_bias=0.0, eps=0.0, gate=None,
+                     rows_per_gate=None, branch_scale=1.0, residual_scale=1.0)
+            want = ref.joint(to64(x), to64(r), o, (np.ones((17, features), bool), 1.0))
+            _close(h, want["h"], "f32", f"{size} {post} h")
+            _close(y, want["y"], "f32", f"{size} {post} y")
