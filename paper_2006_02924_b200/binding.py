@@ -118,8 +118,9 @@ def adasum_device_status(total_elems: int, num_tensors: int, n_workers: int, dty
                          stream=None) -> int:
     """``adasum_device_status`` of the C ABI: 0, or 7 (ADASUM_ERR_TIMEOUT) if a bounded device-side
     wait of the last reduce on ``workspace`` ran out.  Synchronises the stream."""
-    return int(_lib.adasum_device_status(int(total_elems), int(num_tensors), int(n_workers), _dtype_code(dtype),
-                                         int(flags), workspace.data_ptr(), _stream_handle(stream)))
+    with torch.cuda.device(workspace.device):
+        return int(_lib.adasum_device_status(int(total_elems), int(num_tensors), int(n_workers), _dtype_code(dtype),
+                                             int(flags), workspace.data_ptr(), _stream_handle(stream)))
 
 
 def _dtype_code(dtype) -> int:
@@ -712,8 +713,9 @@ _lib.adasum_checkpoint_weight_grad_status.argtypes = [_i64, _i64, _i64, ctypes.c
 def adasum_checkpoint_weight_grad_status(rows: int, features: int, outputs: int, dtype, workspace, stream=None) -> int:
     """``adasum_checkpoint_weight_grad_status`` of the C ABI: 0, or 7 (ADASUM_ERR_TIMEOUT) if a bounded wait of
     the last weight gradient on ``workspace`` ran out.  Synchronises the stream."""
-    return int(_lib.adasum_checkpoint_weight_grad_status(int(rows), int(features), int(outputs), _dtype_code(dtype),
-                                                         workspace.data_ptr(), _stream_handle(stream)))
+    with torch.cuda.device(workspace.device):
+        return int(_lib.adasum_checkpoint_weight_grad_status(int(rows), int(features), int(outputs), _dtype_code(dtype),
+                                                             workspace.data_ptr(), _stream_handle(stream)))
 
 
 ADASUM_HAND_OVER = {"landed": 1, "multiplied": 2, "added": 3, "ready": 4, "formed": 5, "taken": 6}
@@ -723,15 +725,19 @@ _lib.adasum_checkpoint_weight_grad_selftest.argtypes = _lib.adasum_checkpoint_we
 
 
 def adasum_checkpoint_weight_grad_selftest(hand_over: str, checkpoint, grad_out, grad_weight, grad_bias, workspace):
-    """``adasum_checkpoint_weight_grad_selftest`` of the C ABI, on the current stream: the named kind of hand-over
-    inside the product never completes, so its bounded waits run out and are reported."""
+    """``adasum_checkpoint_weight_grad_selftest`` of the C ABI, on the current stream of the tensors' device: the named kind
+    of hand-over inside the product never completes, so its bounded waits run out and are reported."""
+    stride = _matrix("grad_out", grad_out)
     rows, outputs = grad_out.shape
     features = grad_weight.shape[1]
-    status = _lib.adasum_checkpoint_weight_grad_selftest(
-        _checkpoint(grad_out.get_device(), checkpoint, rows, features), rows, features, grad_out.data_ptr(),
-        _matrix("grad_out", grad_out), outputs, _operator_dtype(grad_out.dtype), 1.0, grad_weight.data_ptr(),
-        None if grad_bias is None else grad_bias.data_ptr(), _operator_dtype(grad_weight.dtype), 0, workspace.data_ptr(),
-        workspace.numel() * workspace.element_size(), _stream_handle(None), ADASUM_HAND_OVER[hand_over])
+    device = grad_out.get_device()
+    _same_device(device, grad_weight, grad_bias, workspace)
+    with torch.cuda.device(device):
+        status = _lib.adasum_checkpoint_weight_grad_selftest(
+            _checkpoint(device, checkpoint, rows, features), rows, features, grad_out.data_ptr(), stride, outputs,
+            _operator_dtype(grad_out.dtype), 1.0, grad_weight.data_ptr(), None if grad_bias is None else grad_bias.data_ptr(),
+            _operator_dtype(grad_weight.dtype), 0, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+            _stream_handle(None), ADASUM_HAND_OVER[hand_over])
     if status != ADASUM_OK:
         raise AdasumError(status)
 
@@ -1157,12 +1163,15 @@ _lib.adasum_fp8_linear_selftest.argtypes = [_vp, _vp, _i64, _i64, _i64, _vp, _i6
 
 
 def adasum_fp8_linear_selftest(hand_over: str, x, w, rows: int, features: int, outputs: int, out, workspace):
-    """``adasum_fp8_linear_selftest`` of the C ABI, on the current stream: the named kind of hand-over inside the product
-    never completes, so its bounded waits run out and are reported."""
+    """``adasum_fp8_linear_selftest`` of the C ABI, on the current stream of the tensors' device: the named kind of
+    hand-over inside the product never completes, so its bounded waits run out and are reported."""
+    stride = _matrix("out", out, rows, outputs)
     device = out.get_device()
-    status = _lib.adasum_fp8_linear_selftest(
-        _packed("x", x, rows, features, device), _packed("w", w, outputs, features, device), rows, features, outputs,
-        out.data_ptr(), _matrix("out", out, rows, outputs), _operator_dtype(out.dtype), workspace.data_ptr(),
-        workspace.numel() * workspace.element_size(), _stream_handle(None), ADASUM_HAND_OVER[hand_over])
+    _same_device(device, workspace)
+    with torch.cuda.device(device):
+        status = _lib.adasum_fp8_linear_selftest(
+            _packed("x", x, rows, features, device), _packed("w", w, outputs, features, device), rows, features, outputs,
+            out.data_ptr(), stride, _operator_dtype(out.dtype), workspace.data_ptr(),
+            workspace.numel() * workspace.element_size(), _stream_handle(None), ADASUM_HAND_OVER[hand_over])
     if status != ADASUM_OK:
         raise AdasumError(status)

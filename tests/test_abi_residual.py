@@ -207,3 +207,77 @@ def test_a_gate_for_more_rows_than_there_are(b, per_gate):
         grads = b._RESIDUAL_NORM_GRADS.pack(A, B, C, D, E, 40, 40, 40, 40, F, G, 40, 40, 0, 0, 0, 0, into, F32, F32, 1.0, 1.0, 0)
         code = b.raw().adasum_residual_norm_grad(_block(b, **gate), grads, W, BIG, None)
         assert b.adasum_status_string(code) == "ADASUM_ERR_ARG"
+
+
+class _OnDevice:
+    """Stands in for a contiguous tensor of a GPU that this machine need not have."""
+    is_cuda = True
+
+    def __init__(self, device, shape, dtype=torch.float32):
+        self.device, self.shape, self.dtype = torch.device("cuda", device), torch.Size(shape), dtype
+
+    def get_device(self):
+        return self.device.index
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return self.shape.numel()
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def stride(self):
+        return tuple(torch.Size(self.shape[i + 1:]).numel() for i in range(len(self.shape)))
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 0x10000000
+
+
+@pytest.fixture
+def current(monkeypatch):
+    """The current device as torch.cuda.device makes it, without a GPU; the handle of its current stream tells it."""
+    now = [0]
+
+    class Guard:
+        def __init__(self, device):
+            self.index = device.index if isinstance(device, torch.device) else device
+
+        def __enter__(self):
+            self.before, now[0] = now[0], self.index
+
+        def __exit__(self, *_):
+            now[0] = self.before
+
+    monkeypatch.setattr(torch.cuda, "device", Guard)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *_: type("Stream", (), {"cuda_stream": 1000 + now[0]}))
+    return now
+
+
+def test_status_and_self_test_calls_run_on_their_tensors_device(b, monkeypatch, current):
+    """With GPU 0 current and everything on GPU 1, the library is called with GPU 1 current, on its current stream."""
+    seen = []
+
+    def library(*args):
+        seen.append((current[0], [a for a in args if a in (1000, 1001)]))
+        return 0
+
+    for name in ("adasum_device_status", "adasum_checkpoint_weight_grad_status", "adasum_checkpoint_weight_grad_selftest",
+                 "adasum_fp8_linear_status", "adasum_fp8_linear_selftest"):
+        monkeypatch.setattr(b._lib, name, library)
+    ws, u8 = _OnDevice(1, (1 << 20,), torch.uint8), torch.uint8
+    assert b.adasum_device_status(100, 1, 2, "f32", ws) == 0
+    assert b.adasum_checkpoint_weight_grad_status(4, 40, 24, "f32", ws) == 0
+    b.adasum_checkpoint_weight_grad_selftest("landed", _OnDevice(1, (4 * 66,), u8), _OnDevice(1, (4, 24)), _OnDevice(1, (24, 40)), None, ws)
+    assert b.adasum_fp8_linear_status(ws) == 0
+    x8, w8 = _OnDevice(1, (b._fp8_size(4, 40),), u8), _OnDevice(1, (b._fp8_size(24, 40),), u8)
+    b.adasum_fp8_linear_selftest("landed", x8, w8, 4, 40, 24, _OnDevice(1, (4, 24)), ws)
+    assert seen == [(1, [1001])] * 5 and current[0] == 0
+    with pytest.raises(ValueError):
+        b.adasum_fp8_linear_selftest("landed", x8, w8, 4, 40, 24, _OnDevice(1, (4, 24)), _OnDevice(0, (1 << 20,), u8))
+    with pytest.raises(ValueError):
+        b.adasum_checkpoint_weight_grad_selftest("landed", _OnDevice(1, (4 * 66,), u8), _OnDevice(1, (4, 24)), _OnDevice(0, (24, 40)), None, ws)
