@@ -349,3 +349,22 @@ def test_calls_from_two_threads(b):
 
     with ThreadPoolExecutor(2) as pool:
         assert all(pool.map(work, [(0, 1, 2, 3), (3, 1, 0, 2)]))
+
+
+# Every pair of blocks has more steps than shared memory has stages and more than two sums, so no kind of hand-over that never
+# completes lets a pair finish: (rows, features, outputs) of tiles of 64, 128 and 192 tokens that are cut, and of whole ones
+# whose weights stay.
+@pytest.mark.parametrize("rows,features,outputs", [(40, 128 * 8 * 4 * 74, 24), (128, 128 * 8 * 4 * 74, 24), (384, 128 * 8 * 4 * 74, 24),
+                                                   (3700, 700, 4096)])
+@pytest.mark.parametrize("hand_over", ["landed", "multiplied", "formed", "taken"])
+def test_nothing_of_an_unfinished_product_is_left(b, hand_over, rows, features, outputs):
+    """NaN everywhere, whatever the result and the workspace held."""
+    gen = _gen(10)
+    px, pw = b.adasum_fp8_pack(_matrix(gen, rows, features, "bf16")), b.adasum_fp8_pack_weight(_matrix(gen, outputs, features, "bf16"))
+    ws = torch.empty(b.adasum_fp8_linear_workspace_bytes(rows, features, outputs), dtype=torch.uint8, device="cuda")
+    for dtype in (torch.float32, torch.bfloat16):
+        y = torch.full((rows, outputs), 123.0, dtype=dtype, device="cuda")
+        b.adasum_fp8_linear(px, pw, rows, features, outputs, out=torch.empty_like(y), workspace=ws)    # sums of a finished one
+        b.adasum_fp8_linear_selftest(hand_over, px, pw, rows, features, outputs, y, ws)
+        assert b.adasum_fp8_linear_status(ws) == 7
+        assert torch.isnan(y).all()
