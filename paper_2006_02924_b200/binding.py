@@ -1153,6 +1153,9 @@ def adasum_fp8_linear_grad(grad_out, w, rows: int, features: int, outputs: int, 
 def adasum_fp8_linear_status(workspace, stream=None) -> int:
     """``adasum_fp8_linear_status`` of the C ABI: 0, or 7 (ADASUM_ERR_TIMEOUT) if a bounded wait of the last product on
     ``workspace`` ran out.  Synchronises the stream."""
+    need, given = _lib.adasum_fp8_linear_workspace_bytes(0, 0, 0), workspace.numel() * workspace.element_size()
+    if given < need:
+        raise ValueError(f"workspace has {given} bytes, that of the smallest product {need}")
     with torch.cuda.device(workspace.device):
         return int(_lib.adasum_fp8_linear_status(workspace.data_ptr(), _stream_handle(stream)))
 

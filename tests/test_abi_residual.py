@@ -281,3 +281,14 @@ def test_status_and_self_test_calls_run_on_their_tensors_device(b, monkeypatch, 
         b.adasum_fp8_linear_selftest("landed", x8, w8, 4, 40, 24, _OnDevice(1, (4, 24)), _OnDevice(0, (1 << 20,), u8))
     with pytest.raises(ValueError):
         b.adasum_checkpoint_weight_grad_selftest("landed", _OnDevice(1, (4 * 66,), u8), _OnDevice(1, (4, 24)), _OnDevice(0, (24, 40)), None, ws)
+
+
+def test_status_of_what_is_no_workspace(b, monkeypatch, current):
+    """The library reads the words of all blocks: a buffer that has no room for them is refused."""
+    monkeypatch.setattr(b._lib, "adasum_fp8_linear_status", lambda *_: 0)
+    smallest = b.adasum_fp8_linear_workspace_bytes(1, 0, 1)
+    assert b.adasum_fp8_linear_status(_OnDevice(1, (smallest,), torch.uint8)) == 0
+    assert b.adasum_fp8_linear_status(_OnDevice(1, (smallest // 4,), torch.int32)) == 0
+    for size in (0, 256, smallest - 1):
+        with pytest.raises(ValueError):
+            b.adasum_fp8_linear_status(_OnDevice(1, (size,), torch.uint8))
