@@ -5,6 +5,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -649,7 +650,7 @@ bool small_input_plan(const LevelPlan& plan, int64_t total, int32_t num_tensors,
 // Blocks of fused_small_kernel that the current device keeps resident (0: no cooperative launch).
 int resident_small_blocks()
 {
-    static int cached[64] = {};
+    static std::atomic<int> cached[64] = {};
     int device = 0;
     if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= 64)
         return 0;
@@ -661,7 +662,8 @@ int resident_small_blocks()
         else
             cached[device] = sms * kSmallBlocksPerSm;
     }
-    return cached[device] > 0 ? cached[device] : 0;
+    const int blocks = cached[device];
+    return blocks > 0 ? blocks : 0;
 }
 
 int launches_of(const LevelPlan& plan, int n_workers, uint32_t flags, int64_t total, int32_t num_tensors,

@@ -690,7 +690,7 @@ int64_t most_sum_tiles(int64_t n)
 template <typename Id>
 int resident_sort_clusters()
 {
-    static int cached[64] = {};
+    static std::atomic<int> cached[64] = {};
     int device = 0;
     if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= 64)
         return 2;

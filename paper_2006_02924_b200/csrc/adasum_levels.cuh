@@ -3,6 +3,8 @@
 // unit per element type, which instantiates the entry points declared in adasum_internal.h.
 #pragma once
 
+#include <atomic>
+
 #include "adasum_internal.h"
 
 namespace adasum {
@@ -11,7 +13,7 @@ namespace adasum {
 
 // Opt a kernel in to `bytes` of dynamic shared memory, once per device.
 template <typename Kernel>
-cudaError_t allow_dynamic_smem(Kernel kernel, size_t bytes, bool (&configured)[64])
+cudaError_t allow_dynamic_smem(Kernel kernel, size_t bytes, std::atomic<bool> (&configured)[64])
 {
     int device = 0;
     cudaError_t err = cudaGetDevice(&device);
@@ -37,7 +39,7 @@ cudaError_t launch_gram_variant(GramKind kind, const OperandTable& ops, int oper
         // every group complete: the tcgen05 kernel (64 x 64 accumulator in tensor memory)
         if (kind == GRAM_MMA && tc_status != nullptr && operands == groups_here * 64) {
             auto kernel = gram_partial_tc64_kernel<T>;
-            static bool configured[64] = {};
+            static std::atomic<bool> configured[64] = {};
             cudaError_t err = allow_dynamic_smem(kernel, kTcSmemBytes, configured);
             if (err != cudaSuccess)
                 return err;
@@ -52,7 +54,7 @@ cudaError_t launch_gram_variant(GramKind kind, const OperandTable& ops, int oper
             if constexpr (R <= 32 || sizeof(T) == 2) {
                 constexpr size_t smem = mma_smem_bytes<T, R, DELTA>();
                 auto kernel = gram_partial_mma_kernel<T, R, VEC, DELTA>;
-                static bool configured[64] = {};
+                static std::atomic<bool> configured[64] = {};
                 cudaError_t err = allow_dynamic_smem(kernel, smem, configured);
                 if (err != cudaSuccess)
                     return err;

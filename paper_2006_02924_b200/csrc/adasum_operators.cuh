@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "adasum_internal.h"
 
 namespace adasum {
@@ -55,7 +57,7 @@ inline adasum_status_t check_matrix(const char* name, const void* p, int64_t str
 // Multiprocessors of the current device (0: unknown), looked up once per device.
 inline int device_sms()
 {
-    static int cached[64] = {};
+    static std::atomic<int> cached[64] = {};
     int device = 0;
     if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= 64)
         return 0;

@@ -197,7 +197,7 @@ using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, 
                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 inline EncodeTiled encode_tiled()
 {
-    static EncodeTiled cached = nullptr;
+    static std::atomic<EncodeTiled> cached{nullptr};
     if (!cached) {
         void* fn = nullptr;
         cudaDriverEntryPointQueryResult found;

@@ -806,7 +806,7 @@ WorkLayout work_layout(int64_t rows, int64_t features, int64_t outputs, adasum_d
 template <typename T, int PLANES, bool BIAS>
 uint32_t resident_pairs()
 {
-    static uint32_t cached[64] = {};
+    static std::atomic<uint32_t> cached[64] = {};
     int device = 0;
     if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= 64)
         return 0;

@@ -57,3 +57,11 @@ def test_kernels_that_start_early_read_what_is_written_meanwhile_coherently(name
                                   "adasum_fp8.cuh", "adasum_tensor.cuh"])
 def test_what_those_kernels_share_reads_coherently(file):
     assert not re.findall(r"__ldg\b|ld\.global\.nc", _code(os.path.join(CSRC, file)))
+
+
+@pytest.mark.parametrize("path", SOURCES, ids=os.path.basename)
+def test_what_calls_keep_for_one_another_is_atomic(path):
+    """Threads may make their first calls at once: a function's static that is written is an atomic.  (Namespaces hold
+    mutable objects behind a mutex.)"""
+    statics = re.findall(r"^[ \t]+static\s+(?!constexpr\b|const\b|inline\b|__)([^;={(]*[\w\]])\s*[;={]", _code(path), flags=re.M)
+    assert not [s for s in statics if not s.startswith("std::atomic<")]
