@@ -669,8 +669,9 @@ adasum_status_t adasum_fp8_unpack(const void* packed, int64_t rows, int64_t colu
  *     y[r][n]  = sum_k x[r][k] w[n][k] + bias[n]          x: rows x features, adasum_fp8_pack
  *     dx[r][k] = sum_n dy[r][n] w[n][k]                   dy: rows x outputs, adasum_fp8_pack
  *
- * w is outputs x features, packed once by adasum_fp8_pack_weight for both.  Products are exact, sums are fp32, with one rounding
- * to the stored type.  (The weight's gradient is adasum_checkpoint_weight_grad's.)
+ * w is outputs x features, packed once by adasum_fp8_pack_weight for both.  Products are exact.  Up to 1024 of them are summed in
+ * tensor memory, where every addition truncates to fp32; those sums are added in fp32, and the result is rounded once to the
+ * stored type.  (The weight's gradient is adasum_checkpoint_weight_grad's.)
  *
  *   bias          device, `outputs` elements of bias_dtype, or NULL
  *   y, dx         device, rows x outputs (rows x features) of out_dtype, rows out_stride apart
@@ -680,7 +681,7 @@ adasum_status_t adasum_fp8_unpack(const void* packed, int64_t rows, int64_t colu
  *
  * With nothing to sum y is the bias and dx is 0.  A product that the device did not finish (a bounded wait ran out)
  * leaves NaN; adasum_fp8_linear_status tells, synchronising `stream`, for the last call with rows and columns to write
-on the workspace.
+ * on the workspace.
  */
 size_t adasum_fp8_linear_workspace_bytes(int64_t rows, int64_t features, int64_t outputs);
 adasum_status_t adasum_fp8_linear(const void* x, const void* w, int64_t rows, int64_t features, int64_t outputs,

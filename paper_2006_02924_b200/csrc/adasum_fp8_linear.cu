@@ -29,8 +29,8 @@
 // every step 1200 cycles on its way: with four warps in turn 71 to 83 us for 16384 tokens, 1024 to 4096, and 243 to 280 for 4096 to
 // 4096, against 73 and 254.)  Small products take tiles of 128 or 64 tokens, so that more pairs have one (plan_tiles).
 //
-// What bounds it: with all pairs at work, shared memory (each tensor core reads its rows and all tokens of a step, 448 cycles
-// for 384 of multiplications) and the power limit: 16384 tokens in bf16, 1024 to 4096 67 us (2.05 PFLOP/s), its gradient 66 us (2.07),
+// What bounds it: with all pairs at work, in part shared memory (each tensor core reads its rows and all tokens of a step, 448
+// cycles for 384 of multiplications) and the power limit; tiles of 192 tokens also spill 72 to 80 bytes a thread: 16384 tokens in bf16, 1024 to 4096 67 us (2.05 PFLOP/s), its gradient 66 us (2.07),
 // 4096 to 4096 250 us (2.2); a product of 8192 x 8192 x 8192 470 to 530 us (2.1 to 2.3).  The tensor cores' counter stands at 51
 // to 58 %.  Small products are bound by start and latency: 1024 to 4096, 1 to 64 tokens 5.7 us, 512 tokens 7.2, 2048 tokens 13.8.
 //

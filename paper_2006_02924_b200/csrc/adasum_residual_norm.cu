@@ -6,9 +6,9 @@ namespace {
 
 // WHOLE: 16-byte aligned rows of whole vectors.  FULL: a norm after the block or a gate.
 //
-// 16384 x 1024 bf16: RMS norm 25 us (5.3 TB/s), layer norm 28 us, with dropout 36 us (the generator, 55 % of the issue slots);
-// 4096 x 4096 bf16 with an fp32 stream, two RMS norms and a gate 63 us (3.2 TB/s: a row's way through two sums, at half the
-// warps); one row 4.4 us.
+// 16384 x 1024 bf16: RMS norm 25 us (5.3 TB/s), layer norm 28 us, with dropout 36 us (the generator 8; 55 % of the issue slots at
+// 16 warps per multiprocessor: latency); 4096 x 4096 bf16 with an fp32 stream, two RMS norms and a gate 62 us (3.2 TB/s: a row's
+// way through two sums, at half the warps); one row 4.0 us.
 template <typename T, typename R, bool WHOLE, bool FULL, int V>
 __global__ void __maxnreg__(V == 1 ? 64 : 80)
 residual_norm_kernel(const __grid_constant__ NormArgs a)

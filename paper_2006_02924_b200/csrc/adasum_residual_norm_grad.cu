@@ -111,7 +111,8 @@ struct Turn {
 
 // WHOLE: 16-byte aligned rows of whole vectors.  FULL: a norm after the block or a gate.
 //
-// With the join, 16384 x 1024 bf16 and an RMS norm 41 us (4.1 TB/s), a layer norm with dropout 50 us: instruction issue (67 %).
+// With the join, 16384 x 1024 bf16 and an RMS norm 41 us (4.1 TB/s), a layer norm with dropout 50 us: latency at 16 warps per
+// multiprocessor, 65 % of the issue slots.
 // 4096 x 4096 bf16 with an fp32 stream, two norms and a gate 115 us (2.6 TB/s): a row's way through two sums and three reads of its
 // values from shared memory, at 16 warps (128 registers).  999 x 203 fp32 14.5 us, one row 7.9 us: two launches.
 // Registers: 16384 x 1024 with a layer norm 64: 53 us, 80: 48, 96: 43.
