@@ -460,3 +460,25 @@ def test_small_branches_behind_a_norm(b, features):
             want = ref.joint(to64(x), to64(r), o, (np.ones((17, features), bool), 1.0))
             _close(h, want["h"], "f32", f"{size} {post} h")
             _close(y, want["y"], "f32", f"{size} {post} y")
+
+
+def test_offsets_beyond_32_bits(b):
+    """Rows past element 2^31 of every matrix: the same bits as calls on those rows alone."""
+    rows, features, tail = (1 << 21) + 2000, 1024, 3000
+    x = torch.empty(rows, features, dtype=torch.bfloat16, device="cuda").normal_(generator=_gen(16))
+    weight, gates = torch.rand(features, device="cuda") + 0.5, torch.rand(-(-rows // 1000), features, device="cuda")
+    call = dict(post_norm="rms", post_weight=weight, pre_norm="layer", pre_weight=weight, eps=EPS)
+    h, y, stats = b.adasum_residual_norm(x, x, gate=gates, rows_per_gate=1000, **call)
+    first = rows - tail - rows % 1000                        # a gate row's first
+    part, gate = x[first:], gates[first // 1000:].contiguous()
+    h2, y2, stats2 = b.adasum_residual_norm(part, part, gate=gate, rows_per_gate=1000, **call)
+    assert torch.equal(h[first:], h2) and torch.equal(y[first:], y2) and torch.equal(stats[:, first:], stats2)
+    grad_gate, grad_gate2 = torch.empty_like(gates), torch.empty_like(gate)
+    dx, dr = b.adasum_residual_norm_grad(x, h, stats, y, x, gate=gates, rows_per_gate=1000, grad_gate=grad_gate, **call)
+    dx2, dr2 = b.adasum_residual_norm_grad(part, h2, stats2, y2, part, gate=gate, rows_per_gate=1000, grad_gate=grad_gate2, **call)
+    assert torch.equal(dx[first:], dx2) and torch.equal(dr[first:], dr2)
+    # a gate row's sum is cut in other places: twice 1000 terms with a rounding each and a few for the parts.  A term is the
+    # gradient of h (that of the residual before its rounding to bf16, 2^-8) times the branch behind its norm
+    n = part.double() * stats2[1].double()[:, None] * weight.double()
+    size = torch.stack([t.sum(0) for t in (dr2.double() * n).abs().split(1000)]) * (1 + 2.0**-7)
+    assert ((grad_gate[first // 1000:].double() - grad_gate2.double()).abs() <= 2 * 1010 * ref.U * size).all()
